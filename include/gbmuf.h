@@ -317,6 +317,151 @@ gbmuf_status gbmuf_peer_sync_round(gbmuf_peer* h, uint64_t round, const uint8_t*
 gbmuf_status gbmuf_peer_device_status(gbmuf_peer* h, void* stream, int32_t* out);
 gbmuf_status gbmuf_peer_destroy(gbmuf_peer* h);
 
+/* ---- a worker's local step on a model: linear layers, loss, gradient clipping ---------------------
+ * What produces the gradients that gbmuf_local_adagrad takes.  The paper's language models are
+ * stacks of matrix products with a softmax over the vocabulary on top, trained with the norm of
+ * a group of gradients clipped (Section 3.2); these calls are those pieces, on caller-owned device
+ * memory of any stream.
+ *
+ * Conventions of this section (the ones at the top hold too)
+ *   - Matrices are row-major with a row stride in elements (ld >= columns).  Pointers need only the
+ *     alignment of their element type, strides have no rule: a weight matrix may be a component
+ *     inside a replica's row of theta, a gradient one inside a row of the optimiser's buffer.
+ *     (16-byte aligned pointers and strides that are multiples of 16 bytes are read in place;
+ *     others are first copied into the workspace.)
+ *   - `dtype` is the type of activations, weights, biases and their gradients with respect to
+ *     activations.  Products are summed in fp32 (fp32 operands as three bf16 parts each, whose
+ *     six leading products carry at least the 24 bits of an fp32 product; an fp32 operand that is
+ *     infinite gives NaN where the plain product would give an infinity), epilogues are computed
+ *     in fp32 from the unrounded sum, and every output is rounded once, to nearest even.
+ *   - Outputs may not overlap inputs or each other, except where a call says so.
+ *   - A zero in rows, n_in or n_out is allowed: an empty sum is 0.
+ *   - workspace: device memory of at least the bytes that the _workspace call of the same arguments
+ *     gives (256-byte aligned; may be NULL when that is 0), not shared by calls that can overlap.
+ *   - Calls only launch kernels and may be recorded into a stream capture.
+ *   - Device-side waits are bounded as everywhere in this library; gbmuf_ops_device_status reads
+ *     and clears the word that records one that expired (GBMUF_ERR_TIMEOUT), or a target outside
+ *     the vocabulary (GBMUF_ERR_INVALID_ARG). */
+typedef struct gbmuf_ops gbmuf_ops; /* one per device: status word, device properties; any streams */
+
+/* h = act(z) element by element: identity, max(z, 0), z Phi(z) (Phi the normal distribution
+ * function), z sigmoid(z), tanh(z), sigmoid(z). */
+typedef enum { GBMUF_ACT_NONE = 0, GBMUF_ACT_RELU = 1, GBMUF_ACT_GELU = 2, GBMUF_ACT_SILU = 3,
+               GBMUF_ACT_TANH = 4, GBMUF_ACT_SIGMOID = 5 } gbmuf_activation;
+
+gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out);
+gbmuf_status gbmuf_ops_device_status(gbmuf_ops* ops, void* stream, int32_t* out);
+/* Waits for nothing: the caller has synchronised with the calls that used `ops`. */
+gbmuf_status gbmuf_ops_destroy(gbmuf_ops* ops);
+
+/* y = act(x w^T + bias) + residual, and z = x w^T + bias.
+ * x [rows][n_in], w [n_out][n_in], bias [n_out] or NULL, residual [rows][n_out] or NULL,
+ * y [rows][n_out], z [rows][n_out] or NULL (what the gradient of act needs). */
+typedef struct {
+  int64_t rows, n_in, n_out;
+  const void *x, *w, *bias, *residual;
+  void *y, *z;
+  int64_t ld_x, ld_w, ld_residual, ld_y, ld_z;
+  int32_t dtype, activation;
+  void* workspace;
+  int64_t workspace_bytes;
+} gbmuf_linear_forward_args;
+gbmuf_status gbmuf_linear_forward_workspace(gbmuf_ops* ops, const gbmuf_linear_forward_args* a, int64_t* bytes);
+gbmuf_status gbmuf_linear_forward(gbmuf_ops* ops, const gbmuf_linear_forward_args* a, void* stream);
+
+/* dx = dz w + residual (the gradient that reaches x, plus what reaches it along a residual branch)
+ * and dz_prev = dx * act'(z_prev) (what reaches the layer below through its activation).
+ * dz [rows][n_out], w [n_out][n_in], residual [rows][n_in] or NULL, z_prev [rows][n_in] (NULL only
+ * without dz_prev), dx [rows][n_in] or NULL, dz_prev [rows][n_in] or NULL; one of the two is given.
+ * max(z, 0) has slope 0 at z = 0. */
+typedef struct {
+  int64_t rows, n_in, n_out;
+  const void *dz, *w, *residual, *z_prev;
+  void *dx, *dz_prev;
+  int64_t ld_dz, ld_w, ld_residual, ld_z_prev, ld_dx, ld_dz_prev;
+  int32_t dtype, activation;
+  void* workspace;
+  int64_t workspace_bytes;
+} gbmuf_linear_backward_input_args;
+gbmuf_status gbmuf_linear_backward_input_workspace(gbmuf_ops* ops, const gbmuf_linear_backward_input_args* a,
+                                                   int64_t* bytes);
+gbmuf_status gbmuf_linear_backward_input(gbmuf_ops* ops, const gbmuf_linear_backward_input_args* a,
+                                         void* stream);
+
+/* dw = dz^T x and dbias = sum over the rows of dz; with accumulate != 0 both are added to what dw
+ * and dbias hold (several micro-batches, a matrix used twice).
+ * dz [rows][n_out], x [rows][n_in] of dtype; dw [n_out][n_in] or NULL, dbias [n_out] or NULL of
+ * grad_dtype.  The sums do not depend on timing: two calls give the same bits. */
+typedef struct {
+  int64_t rows, n_in, n_out;
+  const void *dz, *x;
+  void *dw, *dbias;
+  int64_t ld_dz, ld_x, ld_dw;
+  int32_t dtype, grad_dtype, accumulate, reserved;
+  void* workspace;
+  int64_t workspace_bytes;
+} gbmuf_linear_backward_weight_args;
+gbmuf_status gbmuf_linear_backward_weight_workspace(gbmuf_ops* ops, const gbmuf_linear_backward_weight_args* a,
+                                                    int64_t* bytes);
+gbmuf_status gbmuf_linear_backward_weight(gbmuf_ops* ops, const gbmuf_linear_backward_weight_args* a,
+                                          void* stream);
+
+/* dz = dy * act'(z), for an activation that no further linear layer follows.  [rows][cols] each;
+ * dz may be dy (same ld). */
+gbmuf_status gbmuf_activation_backward(gbmuf_ops* ops, int64_t rows, int64_t cols, int32_t dtype,
+                                       int32_t activation, const void* dy, int64_t ld_dy, const void* z,
+                                       int64_t ld_z, void* dz, int64_t ld_dz, void* stream);
+
+/* Cross-entropy of a softmax over `vocab` logits per row against one target word, and its gradient.
+ * For row i with target t: lse_i = log sum_v exp(logits_iv), loss_i = s_i (lse_i - logits_it),
+ * dlogits_iv = s_i (exp(logits_iv - lse_i) - [v = t]), s_i = scale * row_weight_i.
+ * logits [rows][vocab] of dtype; targets: device int64 [rows]; row_weight: device fp32 [rows] or
+ * NULL (1); loss, lse: device fp32 [rows] or NULL; dlogits: [rows][vocab] of dtype or NULL, may be
+ * logits itself (same ld).  A row whose target is ignore_index, or whose s_i is 0, has loss 0 and
+ * a zero gradient (whatever its logits hold).  A logit of -inf is a word that cannot occur; a row of nothing else
+ * has lse -inf, loss +inf and a zero gradient.  A row with a NaN or a +inf gives NaN throughout.
+ * A target outside 0 .. vocab-1 gives loss NaN and a zero gradient, and GBMUF_ERR_INVALID_ARG in
+ * the status word.  vocab = 0 is refused unless rows = 0. */
+typedef struct {
+  int64_t rows, vocab;
+  const void* logits;
+  const int64_t* targets;
+  const float* row_weight;
+  float *loss, *lse;
+  void* dlogits;
+  int64_t ld_logits, ld_dlogits, ignore_index;
+  int32_t dtype;
+  float scale;
+} gbmuf_cross_entropy_args;
+gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args* a, void* stream);
+
+/* The norm of all gradients of a group (a worker), over any number of tensors, and clipping.
+ * A tensor is [rows][cols] with row stride ld_grad, fp32 or bf16; out (or NULL: it only counts in
+ * the norm) has row stride ld_out and is fp32 or of the gradient's own type, and may be the
+ * gradient itself (same stride and type).  Groups are 0 .. groups-1.
+ * gbmuf_clip_create and gbmuf_clip_set_tensors read the host table before they return; the device
+ * memory it names must stay valid while the handle is used with it.  set_tensors waits for the
+ * work that this handle has enqueued.  Work of one handle is kept on one stream at a time.
+ *   gbmuf_clip_norms: norms[g] = sqrt(sum of squares over the tensors of group g), squares and sums
+ *     in double in a fixed order; 0 for a group without elements.  norms: device fp32 [groups].
+ *   gbmuf_clip_scale: the norms, and out = grad * (max_norm / max(norm_g, max_norm)); max_norm <= 0
+ *     copies without clipping.  A group whose norm is not finite has its outputs filled with zeros,
+ *     so that the worker's step leaves theta and the accumulator as they are; its norm tells.
+ * Both may be recorded into a stream capture. */
+typedef struct gbmuf_clip gbmuf_clip;
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t rows, cols, ld_grad, ld_out;
+  int32_t dtype, out_dtype, group, reserved;
+} gbmuf_grad_tensor;
+gbmuf_status gbmuf_clip_create(int32_t device, int32_t groups, int64_t count,
+                               const gbmuf_grad_tensor* tensors_host, gbmuf_clip** out);
+gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_grad_tensor* tensors_host);
+gbmuf_status gbmuf_clip_norms(gbmuf_clip* h, float* norms_device, void* stream);
+gbmuf_status gbmuf_clip_scale(gbmuf_clip* h, float max_norm, float* norms_device, void* stream);
+gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h);
+
 /* Sentence about the last error on this context ("" if none); valid until the next call on it.
  * With ctx == NULL: the last error of a failed gbmuf_create on this thread. */
 const char* gbmuf_last_error(const gbmuf_ctx* ctx);

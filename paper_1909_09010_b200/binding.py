@@ -26,7 +26,14 @@ EXPORTS = ["gbmuf_create", "gbmuf_set_partition", "gbmuf_init", "gbmuf_local_per
            "gbmuf_sync_round_noalloc", "gbmuf_sync_round_host", "gbmuf_host_create",
            "gbmuf_host_sync_round", "gbmuf_host_destroy", "gbmuf_local_adagrad",
            "gbmuf_selftest_wait_timeout", "gbmuf_selftest_divide", "gbmuf_peer_create", "gbmuf_peer_set_partition",
-           "gbmuf_peer_sync_round", "gbmuf_peer_device_status", "gbmuf_peer_destroy"]
+           "gbmuf_peer_sync_round", "gbmuf_peer_device_status", "gbmuf_peer_destroy",
+           "gbmuf_ops_create", "gbmuf_ops_device_status", "gbmuf_ops_destroy",
+           "gbmuf_linear_forward_workspace", "gbmuf_linear_forward",
+           "gbmuf_linear_backward_input_workspace", "gbmuf_linear_backward_input",
+           "gbmuf_linear_backward_weight_workspace", "gbmuf_linear_backward_weight",
+           "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_clip_create",
+           "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_destroy"]
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 
 
 class Config(ctypes.Structure):
@@ -36,6 +43,42 @@ class Config(ctypes.Structure):
                 ("zeta", ctypes.c_float), ("mode", ctypes.c_int32), ("theta_dtype", ctypes.c_int32),
                 ("seed", ctypes.c_uint64), ("device", ctypes.c_int32), ("comp_base", ctypes.c_int32),
                 ("elem_base", ctypes.c_int64)]
+
+
+def _fields(spec: str):
+    """ctypes fields from "type name name, type name ..." (i: int32, l: int64, f: float, p: pointer)."""
+    types = {"i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float, "p": ctypes.c_void_p}
+    return [(name, types[part.split()[0]]) for part in spec.split(",") for name in part.split()[1:]]
+
+
+class LinearForwardArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_linear_forward_args``."""
+    _fields_ = _fields("l rows n_in n_out, p x w bias residual y z, l ld_x ld_w ld_residual ld_y ld_z, "
+                       "i dtype activation, p workspace, l workspace_bytes")
+
+
+class LinearBackwardInputArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_linear_backward_input_args``."""
+    _fields_ = _fields("l rows n_in n_out, p dz w residual z_prev dx dz_prev, "
+                       "l ld_dz ld_w ld_residual ld_z_prev ld_dx ld_dz_prev, i dtype activation, "
+                       "p workspace, l workspace_bytes")
+
+
+class LinearBackwardWeightArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_linear_backward_weight_args``."""
+    _fields_ = _fields("l rows n_in n_out, p dz x dw dbias, l ld_dz ld_x ld_dw, "
+                       "i dtype grad_dtype accumulate reserved, p workspace, l workspace_bytes")
+
+
+class CrossEntropyArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_cross_entropy_args``."""
+    _fields_ = _fields("l rows vocab, p logits targets row_weight loss lse dlogits, "
+                       "l ld_logits ld_dlogits ignore_index, i dtype, f scale")
+
+
+class GradTensor(ctypes.Structure):
+    """Mirror of ``gbmuf_grad_tensor``."""
+    _fields_ = _fields("p grad out, l rows cols ld_grad ld_out, i dtype out_dtype group reserved")
 
 
 class GbmufError(RuntimeError):
@@ -85,6 +128,19 @@ def lib() -> ctypes.CDLL:
     L.gbmuf_peer_sync_round.argtypes = [vp, u64, vp, i32, vp]
     L.gbmuf_peer_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     L.gbmuf_peer_destroy.argtypes = [vp]
+    L.gbmuf_ops_create.argtypes = [i32, ctypes.POINTER(vp)]
+    L.gbmuf_ops_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
+    L.gbmuf_ops_destroy.argtypes = [vp]
+    for name in ("forward", "backward_input", "backward_weight"):
+        getattr(L, "gbmuf_linear_" + name).argtypes = [vp, vp, vp]
+        getattr(L, "gbmuf_linear_" + name + "_workspace").argtypes = [vp, vp, vp]
+    L.gbmuf_activation_backward.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
+    L.gbmuf_cross_entropy.argtypes = [vp, vp, vp]
+    L.gbmuf_clip_create.argtypes = [i32, i32, i64, vp, ctypes.POINTER(vp)]
+    L.gbmuf_clip_set_tensors.argtypes = [vp, i64, vp]
+    L.gbmuf_clip_norms.argtypes = [vp, vp, vp]
+    L.gbmuf_clip_scale.argtypes = [vp, f32, vp, vp]
+    L.gbmuf_clip_destroy.argtypes = [vp]
     L.gbmuf_last_error.argtypes = [vp]
     L.gbmuf_last_error.restype = ctypes.c_char_p
     L.gbmuf_destroy.argtypes = [vp]
@@ -355,6 +411,359 @@ class Gbmuf:
             if word != GBMUF_OK:
                 raise GbmufError(word, "a device-side wait expired in an earlier call on this context "
                                        "and was never read; its results were unspecified")
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+# ------------------------------------------------------------------------------------------------
+# The operators of a worker's local step
+# ------------------------------------------------------------------------------------------------
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise TypeError(f"tensors are float32 or bfloat16, not {t.dtype}")
+
+
+def _matrix(name, t, rows, cols, like):
+    """(address, row stride) of a matrix of the given shape, type and device; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}][{cols}], not {list(t.shape)}")
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    ld, step = t.stride()
+    if step != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"{name} must have its columns next to one another")
+    return t.data_ptr(), (ld if rows > 1 and cols > 0 else cols)
+
+
+def _vector(name, t, n, dtype, device):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be [{n}], not {list(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class LocalOps:
+    """``gbmuf_ops_*``: linear layers with their gradients and the loss, on one device.  Tensors are
+    torch tensors on it; results that are not handed in are allocated by torch on its current
+    stream, and so is the workspace of a call that needs one.  ``stream`` (default: the current one
+    of the device) is where the call runs; tensors used on another stream than their own are the
+    caller's to guard, as for any torch operation."""
+
+    def __init__(self, device=0):
+        import torch
+        self._torch = torch
+        self._L = lib()
+        self._h = ctypes.c_void_p()
+        self.device = device
+        st = self._L.gbmuf_ops_create(device, ctypes.byref(self._h))
+        if st != GBMUF_OK:
+            raise GbmufError(st, self._L.gbmuf_last_error(None).decode())
+
+    def _check(self, st):
+        if st != GBMUF_OK:
+            raise GbmufError(st, self._L.gbmuf_last_error(None).decode())
+
+    def _on(self, stream):
+        if stream is None:
+            return self._torch.cuda.current_stream(self.device).cuda_stream
+        return getattr(stream, "cuda_stream", stream)
+
+    def _own(self, t, name):
+        if t.device.type != "cuda" or t.device.index != self.device:
+            raise ValueError(f"{name} is on {t.device}, not on cuda:{self.device}")
+
+    def _linear(self, name, args, like, stream):
+        """Asks for the workspace, allocates it, runs the call."""
+        ref = ctypes.byref(args)
+        need = ctypes.c_int64()
+        self._check(getattr(self._L, name + "_workspace")(self._h, ref, ctypes.byref(need)))
+        work = None
+        if need.value:
+            torch = self._torch
+            work = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+            if stream is not None:
+                work.record_stream(stream if hasattr(stream, "cuda_stream")
+                                   else torch.cuda.ExternalStream(stream, device=like.device))
+            args.workspace, args.workspace_bytes = work.data_ptr(), need.value
+        self._check(getattr(self._L, name)(self._h, ref, self._on(stream)))
+
+    def linear_forward(self, x, w, bias=None, residual=None, activation="none", keep_z=False, out=None,
+                       z_out=None, stream=None):
+        """``gbmuf_linear_forward``: y = act(x w^T + bias) + residual; with ``keep_z`` (or ``z_out``)
+        returns (y, z), z = x w^T + bias.  x [rows][n_in], w [n_out][n_in]."""
+        if x.dim() != 2 or w.dim() != 2:
+            raise ValueError("x and w must be matrices")
+        (rows, n_in), n_out = x.shape, w.shape[0]
+        self._own(x, "x")
+        y = out if out is not None else x.new_empty((rows, n_out))
+        z = z_out if z_out is not None else (x.new_empty((rows, n_out)) if keep_z else None)
+        px, lx = _matrix("x", x, rows, n_in, x)
+        pw, lw = _matrix("w", w, n_out, n_in, x)
+        pr, lr = _matrix("residual", residual, rows, n_out, x)
+        py, ly = _matrix("out", y, rows, n_out, x)
+        pz, lz = _matrix("z_out", z, rows, n_out, x)
+        pb = _vector("bias", bias, n_out, x.dtype, x.device)
+        args = LinearForwardArgs(rows, n_in, n_out, px, pw, pb, pr, py, pz, lx, lw, lr, ly, lz,
+                                 _dtype_code(x), ACTIVATIONS[activation], None, 0)
+        self._linear("gbmuf_linear_forward", args, x, stream)
+        return y if z is None else (y, z)
+
+    def linear_backward_input(self, dz, w, residual=None, z_prev=None, activation="none", want_dx=None,
+                              dx_out=None, dz_out=None, stream=None):
+        """``gbmuf_linear_backward_input``: dx = dz w + residual, and with ``z_prev`` also
+        dz_prev = dx * act'(z_prev).  Returns dx without ``z_prev``; dz_prev with it, or
+        (dx, dz_prev) if ``want_dx`` or ``dx_out``."""
+        if dz.dim() != 2 or w.dim() != 2:
+            raise ValueError("dz and w must be matrices")
+        (rows, n_out), n_in = dz.shape, w.shape[1]
+        self._own(dz, "dz")
+        dx, dp = dx_out, dz_out
+        if dx is None and (want_dx or z_prev is None):
+            dx = dz.new_empty((rows, n_in))
+        if dp is None and z_prev is not None:
+            dp = dz.new_empty((rows, n_in))
+        if z_prev is None and dp is not None:
+            raise ValueError("dz_out needs z_prev")
+        pd, ldd = _matrix("dz", dz, rows, n_out, dz)
+        pw, lw = _matrix("w", w, n_out, n_in, dz)
+        pr, lr = _matrix("residual", residual, rows, n_in, dz)
+        pz, lz = _matrix("z_prev", z_prev, rows, n_in, dz)
+        px, lx = _matrix("dx_out", dx, rows, n_in, dz)
+        pp, lp = _matrix("dz_out", dp, rows, n_in, dz)
+        args = LinearBackwardInputArgs(rows, n_in, n_out, pd, pw, pr, pz, px, pp, ldd, lw, lr, lz, lx, lp,
+                                       _dtype_code(dz), ACTIVATIONS[activation], None, 0)
+        self._linear("gbmuf_linear_backward_input", args, dz, stream)
+        return dx if dp is None else (dp if dx is None else (dx, dp))
+
+    def linear_backward_weight(self, dz, x, grad_dtype=None, want_bias=True, dw_out=None, dbias_out=None,
+                               accumulate=False, stream=None):
+        """``gbmuf_linear_backward_weight``: dw = dz^T x and dbias = sum over the rows of dz, in
+        ``grad_dtype`` (default: the operands' type); with ``accumulate`` added to ``dw_out`` and
+        ``dbias_out``.  Returns dw, or (dw, dbias) if ``want_bias`` or ``dbias_out``."""
+        if dz.dim() != 2 or x.dim() != 2:
+            raise ValueError("dz and x must be matrices")
+        (rows, n_out), n_in = dz.shape, x.shape[1]
+        self._own(dz, "dz")
+        if dw_out is not None:
+            if grad_dtype is not None and dw_out.dtype is not grad_dtype:
+                raise TypeError(f"dw_out must be {grad_dtype}, not {dw_out.dtype}")
+            grad_dtype = dw_out.dtype
+        elif grad_dtype is None:
+            grad_dtype = dz.dtype
+        if accumulate and (dw_out is None or (want_bias and dbias_out is None)):
+            raise ValueError("accumulate adds to dw_out and dbias_out: hand them in")
+        dw = dw_out if dw_out is not None else dz.new_empty((n_out, n_in), dtype=grad_dtype)
+        db = dbias_out if dbias_out is not None else (
+            dz.new_empty((n_out,), dtype=grad_dtype) if want_bias else None)
+        pd, ldd = _matrix("dz", dz, rows, n_out, dz)
+        px, lx = _matrix("x", x, rows, n_in, dz)
+        if dw.device != dz.device:
+            raise ValueError(f"dw_out is on {dw.device}, not on {dz.device}")
+        pw, lw = _matrix("dw_out", dw, n_out, n_in, dw)
+        pb = _vector("dbias_out", db, n_out, grad_dtype, dz.device)
+        args = LinearBackwardWeightArgs(rows, n_in, n_out, pd, px, pw, pb, ldd, lx, lw, _dtype_code(dz),
+                                        _dtype_code(dw), 1 if accumulate else 0, 0, None, 0)
+        self._linear("gbmuf_linear_backward_weight", args, dz, stream)
+        return dw if db is None else (dw, db)
+
+    def activation_backward(self, dy, z, activation, out=None, stream=None):
+        """``gbmuf_activation_backward``: dy * act'(z); ``out`` may be dy."""
+        if dy.dim() != 2:
+            raise ValueError("dy must be a matrix")
+        rows, cols = dy.shape
+        self._own(dy, "dy")
+        dz = out if out is not None else dy.new_empty((rows, cols))
+        py, ly = _matrix("dy", dy, rows, cols, dy)
+        pz, lz = _matrix("z", z, rows, cols, dy)
+        po, lo = _matrix("out", dz, rows, cols, dy)
+        self._check(self._L.gbmuf_activation_backward(self._h, rows, cols, _dtype_code(dy),
+                                                      ACTIVATIONS[activation], py, ly, pz, lz, po, lo,
+                                                      self._on(stream)))
+        return dz
+
+    def cross_entropy(self, logits, targets, ignore_index=-100, row_weight=None, scale=1.0,
+                      want_grad=True, dlogits_out=None, stream=None):
+        """``gbmuf_cross_entropy``: (loss, lse, dlogits), or (loss, lse) without ``want_grad``.  loss
+        and lse are float32 [rows]; ``dlogits_out`` may be the logits."""
+        torch = self._torch
+        if logits.dim() != 2:
+            raise ValueError("logits must be a matrix")
+        rows, vocab = logits.shape
+        self._own(logits, "logits")
+        both = torch.empty((2, rows), dtype=torch.float32, device=logits.device)
+        d = dlogits_out
+        if d is None and want_grad:
+            d = logits.new_empty((rows, vocab))
+        pl, ll = _matrix("logits", logits, rows, vocab, logits)
+        pd, ldd = _matrix("dlogits_out", d, rows, vocab, logits)
+        pt = _vector("targets", targets, rows, torch.int64, logits.device)
+        pw = _vector("row_weight", row_weight, rows, torch.float32, logits.device)
+        at = both.data_ptr()
+        args = CrossEntropyArgs(rows, vocab, pl, pt, pw, at, at + 4 * rows, pd, ll, ldd, ignore_index,
+                                _dtype_code(logits), scale)
+        self._check(self._L.gbmuf_cross_entropy(self._h, ctypes.byref(args), self._on(stream)))
+        loss, lse = both[0], both[1]
+        return (loss, lse) if d is None else (loss, lse, d)
+
+    def device_status(self, stream=None) -> int:
+        """Waits for the stream; reads and clears the status word."""
+        v = ctypes.c_int32(-1)
+        self._check(self._L.gbmuf_ops_device_status(self._h, self._on(stream), ctypes.byref(v)))
+        return v.value
+
+    def destroy(self):
+        if self._h:
+            self._L.gbmuf_ops_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+_local_ops = {}
+
+
+def local_ops(device=None) -> LocalOps:
+    """The process's :class:`LocalOps` of a device (default: the current one)."""
+    if device is None:
+        import torch
+        device = torch.cuda.current_device()
+    ops = _local_ops.get(device)
+    if ops is None:
+        ops = _local_ops[device] = LocalOps(device)
+    return ops
+
+
+def _rows_cols(name, t):
+    """A tensor as rows of elements that follow one another: (rows, cols, row stride)."""
+    dims = [(n, s) for n, s in zip(t.shape, t.stride()) if n != 1]
+    if t.numel() == 0 or not dims:
+        return 1, t.numel(), max(1, t.numel())
+    cols, inner = 1, 1
+    while dims and dims[-1][1] == inner:
+        cols *= dims[-1][0]
+        inner = cols
+        dims.pop()
+    rows, ld = 1, cols
+    if dims:
+        rows, ld = dims[-1]
+        dims.pop()
+        while dims and dims[-1][1] == ld * rows:
+            rows *= dims.pop()[0]
+    if dims or ld < cols:
+        raise ValueError(f"{name} must be rows of elements that follow one another, with one stride")
+    return rows, cols, ld
+
+
+class GradClip:
+    """``gbmuf_clip_*``: the gradient norm of each group (a worker) over a list of tensors, and the
+    clipped copies.  entries: (gradient, out or None, group); gradient float32 or bfloat16, out of
+    the same shape in float32 or the gradient's type (or the gradient itself)."""
+
+    def __init__(self, entries, groups=1, device=None):
+        import torch
+        self._torch = torch
+        self._L = lib()
+        self._h = ctypes.c_void_p()
+        entries = list(entries)
+        if device is None:
+            device = entries[0][0].device.index if entries else torch.cuda.current_device()
+        self.device, self.groups = device, groups
+        arr = self._table(entries)
+        st = self._L.gbmuf_clip_create(device, groups, len(entries), arr, ctypes.byref(self._h))
+        self._check(st)
+        self._keep = entries
+
+    def _check(self, st):
+        if st != GBMUF_OK:
+            raise GbmufError(st, self._L.gbmuf_last_error(None).decode())
+
+    def _table(self, entries):
+        arr = (GradTensor * len(entries))()
+        for i, (g, out, group) in enumerate(entries):
+            for name, t in (("gradient", g), ("out", out)):
+                if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+                    raise ValueError(f"{name} {i} is on {t.device}, not on cuda:{self.device}")
+            if out is not None and out.shape != g.shape:
+                raise ValueError(f"out {i} must have its gradient's shape")
+            # dimensions in the order of memory, the same for both (a transposed pair is fine)
+            order = sorted(range(g.dim()), key=lambda d: -g.stride(d))
+            g = g.permute(order)
+            rows, cols, ld = _rows_cols(f"gradient {i}", g)
+            ld_out = 0
+            if out is not None:
+                out = out.permute(order)
+                r2, c2, ld_out = _rows_cols(f"out {i}", out)
+                if (r2, c2) != (rows, cols):       # one of the two is whole: cut it like the other
+                    if r2 * c2 != rows * cols or 1 not in (r2, rows):
+                        raise ValueError(f"out {i} and its gradient have rows of different lengths")
+                    if r2 == 1:
+                        ld_out = cols
+                    else:
+                        rows, cols, ld = r2, c2, c2
+            arr[i] = GradTensor(g.data_ptr(), None if out is None else out.data_ptr(), rows, cols, ld,
+                                ld_out, _dtype_code(g), 0 if out is None else _dtype_code(out), group, 0)
+        return arr
+
+    def set_tensors(self, entries):
+        """New tensors (and groups) for the same number of groups; waits for this handle's work."""
+        entries = list(entries)
+        self._check(self._L.gbmuf_clip_set_tensors(self._h, len(entries), self._table(entries)))
+        self._keep = entries
+
+    def _norms(self, out):
+        if out is None:
+            return self._torch.empty(self.groups, dtype=self._torch.float32, device=f"cuda:{self.device}")
+        if out.dtype is not self._torch.float32 or out.dim() != 1 or out.shape[0] != self.groups \
+                or out.device.type != "cuda" or out.device.index != self.device \
+                or (self.groups > 1 and out.stride(0) != 1):
+            raise ValueError(f"norms_out must be contiguous float32 [{self.groups}] on cuda:{self.device}")
+        return out
+
+    def norms(self, norms_out=None, stream=None):
+        """``gbmuf_clip_norms``: float32 [groups]."""
+        norms = self._norms(norms_out)
+        self._check(self._L.gbmuf_clip_norms(self._h, norms.data_ptr(), self._on(stream)))
+        return norms
+
+    def clip(self, max_norm, norms_out=None, stream=None):
+        """``gbmuf_clip_scale``: writes every entry's out; returns the norms before clipping."""
+        norms = self._norms(norms_out)
+        self._check(self._L.gbmuf_clip_scale(self._h, max_norm, norms.data_ptr(), self._on(stream)))
+        return norms
+
+    def _on(self, stream):
+        if stream is None:
+            return self._torch.cuda.current_stream(self.device).cuda_stream
+        return getattr(stream, "cuda_stream", stream)
+
+    def destroy(self):
+        if self._h:
+            self._L.gbmuf_clip_destroy(self._h)
+            self._h = ctypes.c_void_p()
+            self._keep = None
 
     def __del__(self):
         try:

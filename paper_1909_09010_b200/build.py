@@ -7,12 +7,12 @@ import subprocess
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-SRC = os.path.join(CSRC, "gbmuf.cu")          # the one translation unit; it includes csrc/*.cuh
+SRCS = [os.path.join(CSRC, f) for f in ("gbmuf.cu", "local_ops.cu")]    # they include csrc/*.cuh
 HDR = os.path.join(ROOT, "include", "gbmuf.h")
 LIB = os.path.join(PKG, "libgbmuf.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
+              "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
 
 
 def nvcc_path() -> str:
@@ -26,7 +26,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    sources = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]
+    sources = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))]
     return any(os.path.getmtime(f) > t for f in sources + [HDR])
 
 
@@ -35,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [nvcc_path(), *NVCC_FLAGS, "-I", os.path.join(ROOT, "include"), SRC, "-o", tmp]
+    cmd = [nvcc_path(), *NVCC_FLAGS, "-I", os.path.join(ROOT, "include"), *SRCS, "-o", tmp]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

@@ -1,7 +1,8 @@
 // libgbmuf: the random-gossip BMUF synchronisation round (Algorithm 1 of "A Random Gossip BMUF
 // Process for Neural Language Modeling") for K parameter replicas resident in one GPU's memory.
 // CUDA for sm_100a.  The interface is include/gbmuf.h; this file holds the host side and the C
-// ABI, the kernels live in the headers it includes:
+// ABI of the synchronisation round (local_ops.cu: of the operators of a worker's local step), the
+// kernels live in the headers it includes:
 //   philox.cuh           Philox4x32-10
 //   round_setup.cuh      round_setup_kernel: neighbour draws for every (worker, component) of a
 //                        round + the tile work-list prefix of the components that take part
@@ -38,6 +39,7 @@
 
 #include "gbmuf.h"
 
+#include "host_common.h"
 #include "philox.cuh"
 #include "round_setup.cuh"
 #include "primitives.cuh"
@@ -52,7 +54,7 @@ namespace {
 // =================================================================================================
 // Host side
 // =================================================================================================
-thread_local std::string g_create_error;
+thread_local std::string g_create_error;   // text of gbmuf_last_error(NULL)
 
 struct Tuning {
   int ncons = 0, T = 0, stages = 0, ring = 0, flags = 0;   // 0 = built-in choice
@@ -78,53 +80,9 @@ int host_candidates(int K, int p) {
   return (int)c;
 }
 
-// Is `st` recording a stream capture?  (The legacy default stream never is.)
-bool is_capturing(cudaStream_t st) {
-  if (!st) return false;
-  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-  if (cudaStreamIsCapturing(st, &cs) != cudaSuccess) { cudaGetLastError(); return false; }
-  return cs != cudaStreamCaptureStatusNone;
-}
-
-// Which streams a handle has put work into, as one event per stream recorded after the latest
-// piece of work.  Re-partitioning and destruction wait for these events: for the handle's own
-// work and nothing else on the device.  Events outlive the streams they were recorded in, so a
-// stream the caller has destroyed in the meantime is no problem.  Work recorded into a stream
-// capture is not tracked (an event recorded there cannot be waited for from the host); the
-// caller keeps the handle alive while such a graph can still run.
-struct WorkMarks {
-  struct Mark { cudaStream_t s; cudaEvent_t ev; };
-  std::vector<Mark> marks;
-  static constexpr size_t kMaxStreams = 16;
-  void note(cudaStream_t st) {
-    if (is_capturing(st)) return;
-    for (Mark& mk : marks)
-      if (mk.s == st) { cudaEventRecord(mk.ev, st); return; }
-    if (marks.size() == kMaxStreams) {               // many streams: retire the oldest mark
-      cudaEventSynchronize(marks.front().ev);
-      cudaEventDestroy(marks.front().ev);
-      marks.erase(marks.begin());
-    }
-    Mark mk{st, nullptr};
-    if (cudaEventCreateWithFlags(&mk.ev, cudaEventDisableTiming) != cudaSuccess) { cudaGetLastError(); return; }
-    cudaEventRecord(mk.ev, st);
-    marks.push_back(mk);
-  }
-  cudaError_t wait() {
-    cudaError_t first = cudaSuccess;
-    for (Mark& mk : marks) {
-      const cudaError_t e = cudaEventSynchronize(mk.ev);
-      if (e != cudaSuccess && first == cudaSuccess) first = e;
-    }
-    return first;
-  }
-  void release() {
-    for (Mark& mk : marks) cudaEventDestroy(mk.ev);
-    marks.clear();
-  }
-};
-
 }  // namespace
+
+void gbmuf_set_thread_error(const std::string& text) { g_create_error = text; }
 
 struct gbmuf_ctx {
   gbmuf_config cfg;
@@ -160,19 +118,6 @@ struct gbmuf_ctx {
 };
 
 namespace {
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; }
-    if (prev != dev) ok = (cudaSetDevice(dev) == cudaSuccess);
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-  }
-};
 
 gbmuf_status fail(gbmuf_ctx* ctx, gbmuf_status st, const std::string& msg) {
   if (ctx) ctx->err = msg; else g_create_error = msg;
@@ -213,23 +158,11 @@ cudaError_t ensure_kernel_attributes(int device, int max_smem) {
   return cudaSuccess;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // Tensor map for boxes of K rows x BW columns over the [K][ld] theta array.
 gbmuf_status build_tensor_maps(gbmuf_ctx* ctx, const Launch& L) {
   if (L.tmem_cols > 0 || L.ma_ring > 0) return GBMUF_OK;   // these variants stage rows by 1-D copies
-  static EncodeTiledFn encode = nullptr;
-  if (!encode) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
-    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
-      return fail(ctx, GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-    encode = reinterpret_cast<EncodeTiledFn>(fn);
-  }
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return fail(ctx, GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
   const cuuint64_t ld = (cuuint64_t)ctx->cfg.ld;
   const cuuint64_t gdim[2] = {ld, (cuuint64_t)ctx->cfg.K};
   const cuuint32_t box[2] = {(cuuint32_t)L.BW, (cuuint32_t)ctx->cfg.K};

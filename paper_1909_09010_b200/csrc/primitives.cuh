@@ -1,5 +1,5 @@
 // Bounded mbarrier waits, bulk copies, theta storage types.
-// Part of libgbmuf (CUDA, sm_100a); included by gbmuf.cu, which is the only translation unit.
+// Part of libgbmuf (CUDA, sm_100a); included by its translation units gbmuf.cu and local_ops.cu.
 #ifndef GBMUF_CSRC_PRIMITIVES_CUH
 #define GBMUF_CSRC_PRIMITIVES_CUH
 
