@@ -1,0 +1,58 @@
+// Operands of the tensor-core products that cannot be read in place.
+// Part of libgbmuf (CUDA, sm_100a); included by local_ops.cu.
+#ifndef GBMUF_CSRC_LINEAR_PACK_CUH
+#define GBMUF_CSRC_LINEAR_PACK_CUH
+
+namespace {
+
+// x as hi + mid + lo, each bf16: hi = RN(x), mid = RN(x - hi), lo = RN(x - hi - mid); the differences
+// are exact, and three times 8 bits hold all 24 of x (down to the smallest bf16).  Where RN(x)
+// overflows, hi is the largest bf16.  An infinity or NaN is in hi alone.
+__device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uint16_t& lo) {
+  __nv_bfloat16 h = __float2bfloat16_rn(x);
+  const uint32_t bits = __float_as_uint(x);
+  const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
+  uint16_t hb = __bfloat16_as_ushort(h);
+  if (finite && (hb & 0x7f80u) == 0x7f80u) hb = (uint16_t)((hb & 0x8000u) | 0x7f7fu);
+  const float r1 = finite ? x - __uint_as_float((uint32_t)hb << 16) : 0.0f;
+  const uint16_t mb = __bfloat16_as_ushort(__float2bfloat16_rn(r1));
+  const float r2 = r1 - __uint_as_float((uint32_t)mb << 16);
+  hi = hb; mid = mb; lo = __bfloat16_as_ushort(__float2bfloat16_rn(r2));
+}
+
+// src [outer][inner] with any stride and alignment -> bf16 parts [1 or 3][outer][ld_dst], ld_dst a
+// multiple of 8; columns inner .. ld_dst-1 are never read as data and get zeros.  One thread per
+// eight columns; VEC: src rows are 16-byte aligned.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) pack_kernel(const T* src, long long ld, long long outer, long long inner,
+                                                   __nv_bfloat16* dst, long long ld_dst) {
+  grid_launch_dependents();
+  const long long per_row = ld_dst / 8, n = outer * per_row, part = outer * ld_dst;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+    const long long r = i / per_row, c = (i - r * per_row) * 8;
+    const T* const s = src + r * ld + c;
+    __align__(16) T v[8];
+    if (VEC && c + 8 <= inner) {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(v)[j] = reinterpret_cast<const uint4*>(s)[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = c + j < inner ? s[j] : from_f32<T>(0.0f);
+    }
+    uint4* const d = reinterpret_cast<uint4*>(dst + r * ld_dst + c);
+    if constexpr (sizeof(T) == 2) {
+      *d = *reinterpret_cast<const uint4*>(v);
+    } else {
+      __align__(16) uint16_t p[3][8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) split3(v[j], p[0][j], p[1][j], p[2][j]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        reinterpret_cast<uint4*>(dst + q * part + r * ld_dst + c)[0] = *reinterpret_cast<const uint4*>(p[q]);
+    }
+  }
+}
+
+}  // namespace
+
+#endif  // GBMUF_CSRC_LINEAR_PACK_CUH

@@ -5,56 +5,6 @@
 
 namespace {
 
-// C[r][c] = sum_k A(r, k) B(c, k), A(r, k) = a[r * sa_r + k * sa_k], B alike; 64 x 64 outputs per
-// block of 256 threads, 4 x 4 per thread, 16 k per step through shared memory.
-struct SimtParams {
-  const void *a, *b;
-  long long sa_r, sa_k, sb_c, sb_k;
-  long long R, C, K;
-  Epilogue E;
-};
-
-template <int KIND, typename T, typename TO>
-__global__ void __launch_bounds__(256) linear_simt_kernel(const SimtParams P) {
-  __shared__ float sa[16][65], sb[16][65];
-  const T* const a = static_cast<const T*>(P.a);
-  const T* const b = static_cast<const T*>(P.b);
-  const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;
-  const long long tiles_c = (P.C + 63) / 64, tiles = tiles_c * ((P.R + 63) / 64);
-  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const long long r0 = tile / tiles_c * 64, c0 = tile % tiles_c * 64;
-    float acc[4][4] = {};
-    for (long long k0 = 0; k0 < P.K; k0 += 16) {
-      for (int i = threadIdx.x; i < 1024; i += 256) {
-        // consecutive threads along whichever index is contiguous in memory
-        const int ka = P.sa_k == 1 ? i & 15 : i >> 6, ra = P.sa_k == 1 ? i >> 4 : i & 63;
-        const int kb = P.sb_k == 1 ? i & 15 : i >> 6, cb = P.sb_k == 1 ? i >> 4 : i & 63;
-        sa[ka][ra] = r0 + ra < P.R && k0 + ka < P.K ? to_f32(a[(r0 + ra) * P.sa_r + (k0 + ka) * P.sa_k]) : 0.0f;
-        sb[kb][cb] = c0 + cb < P.C && k0 + kb < P.K ? to_f32(b[(c0 + cb) * P.sb_c + (k0 + kb) * P.sb_k]) : 0.0f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        float x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] = sa[k][tr + 16 * i]; y[i] = sb[k][tc + 16 * i]; }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const long long r = r0 + tr + 16 * i, c = c0 + tc + 16 * j;
-        if (r < P.R && c < P.C) finish_element<KIND, T, TO>(P.E, r, c, acc[i][j]);
-      }
-  }
-}
-
 // out[c] (+)= sum over the rows of a [R][C] matrix: one block per 32 columns, 8 row groups summed
 // in a fixed order.
 template <typename T, typename TO>

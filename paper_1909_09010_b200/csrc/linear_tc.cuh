@@ -1,0 +1,332 @@
+// Matrix products of the linear layer on the tensor cores.
+// Part of libgbmuf (CUDA, sm_100a); included by local_ops.cu.
+#ifndef GBMUF_CSRC_LINEAR_TC_CUH
+#define GBMUF_CSRC_LINEAR_TC_CUH
+
+namespace {
+
+// Result[r][c] = sum_k A(c, k) B(r, k), bf16 operands, fp32 sums.  Columns c of the result (they lie
+// next to one another in memory) run along the 128 lanes of tensor memory, rows r along its columns:
+//   forward       A = w, B = x,  k = n_in   (both with k contiguous)
+//   input grad    A = w, B = dz, k = n_out  (A with c contiguous)
+//   weight grad   A = x, B = dz, k = rows   (A with c contiguous, B with r contiguous)
+// so a warp that holds 32 lanes of one accumulator column stores 32 neighbouring elements, and few
+// rows (single tokens) make the tile narrow (BN), not half empty.
+//
+// fp32 operands come as three bf16 parts (hi, mid, lo: together all 24 bits) and each step along k
+// is done for the six products of parts that reach 2^-24 of the product: `products` = 6.
+//
+// A tile is 128 x BN.  Warp 0 loads 64 k of both operands per step with the copy engine (128-byte
+// swizzle), warp 1 issues the matrix instructions, warps 4..11 finish the sums.  Two accumulators:
+// one is finished while the next is summed.
+constexpr int kTcThreads = 384;
+constexpr int kTcK = 64;                       // k per step
+constexpr int kTcMaxStages = 12;
+
+struct TcParams {
+  Epilogue E;
+  int32_t* status;
+  int R, C;
+  int ksteps;            // steps of 64 along k
+  int products;          // 1 or 6
+  int tiles_r, tiles;    // row tiles; all tiles, row tiles running fastest
+  int split;             // CTAs of a cluster that share a tile's steps (1: none)
+  int stages;
+};
+
+__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn) { return (128u + (uint32_t)bn) * 128u; }
+constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
+__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int stages) {
+  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn);
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+      "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Shared-memory operand descriptor, 128-byte swizzle.  k contiguous: rows of 128 bytes (64 k), groups
+// of 8 rows 1024 bytes apart.  k strided: blocks of 64 elements x 64 k, rows of 128 bytes along the
+// operand's own dimension, 8 k 1024 bytes apart, the next 64 elements 8192 bytes on.
+template <bool K_CONTIGUOUS>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+  const uint64_t lbo = K_CONTIGUOUS ? 1 : (8192 >> 4), sbo = 1024 >> 4;
+  return (uint64_t)((addr >> 4) & 0x3fff) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor: fp32 accumulator, bf16 operands, 128 x BN.
+template <bool A_K, bool B_K>
+__device__ __forceinline__ constexpr uint32_t instr_desc(int bn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
+         ((uint32_t)(bn >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t keep) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(keep)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void st_remote(uint32_t addr, uint32_t rank, float v) {
+  asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.f32 [r], %2;\n\t}" ::"r"(addr),
+               "r"(rank), "f"(v)
+               : "memory");
+}
+// 16 accumulator columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
+  uint32_t u[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+}
+
+// Parts (0 hi, 1 mid, 2 lo) of A and B in product p of six, smallest products first: an accumulator
+// that is still small loses less to each addition.  hi lo, lo hi, mid mid, hi mid, mid hi, hi hi.
+__device__ __forceinline__ int part_of_a(int products, int p) { return products == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
+__device__ __forceinline__ int part_of_b(int products, int p) { return products == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
+
+template <int KIND, typename T, typename TO, bool PROMOTE, int BN>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
+  constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad;
+  constexpr uint32_t STAGE = tc_stage_bytes(BN), A_BYTES = 128 * 128;
+  constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
+  constexpr int NCOL = BN / 2;                 // accumulator columns per finishing warp
+  extern __shared__ unsigned char raw[];
+  unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+  const uint32_t bars = smem_u32(smem), ring = bars + kTcHead;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 128u + 8u * s; };
+  auto acc_full = [&](int b) { return bars + 256u + 8u * b; };
+  auto acc_empty = [&](int b) { return bars + 272u + 8u * b; };
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + 320);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int S = P.stages;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 256); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_slot;
+  grid_dependency_wait();
+
+  // this CTA's tiles and its share of each one's steps
+  const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;
+  const int step0 = (int)((long long)P.ksteps * rank / P.split), step1 = (int)((long long)P.ksteps * (rank + 1) / P.split);
+  const int iters = (step1 - step0) * P.products;                 // (k step, product) pairs of a tile
+  // without PROMOTE a tile is one chunk; with it the tensor cores' sum is moved into fp32 registers
+  // after every chunk of 16 (24) instructions
+  const int chunk = PROMOTE ? (P.products == 1 ? 4 : 6) : (iters > 0 ? iters : 1);
+  const int chunks = iters == 0 ? 0 : (iters + chunk - 1) / chunk;
+  const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)blockIdx.x;
+  const int tile_step = P.split > 1 ? P.tiles : (int)gridDim.x;   // a split tile: one per cluster
+
+  if (warp == 0) {
+    // -------------------------------------------------------------------- loads
+    if (lane == 0) {
+      int s = 0, issued = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+        const int c0 = tile / P.tiles_r * 128, r0 = tile % P.tiles_r * BN;
+        for (int it = 0; it < iters && ok; ++it) {
+          const int k0 = (step0 + it / P.products) * kTcK, p = it % P.products;
+          const int pa = part_of_a(P.products, p), pb = part_of_b(P.products, p);
+          if (issued >= S) ok = mbar_wait_bounded(empty(s), ph ^ 1, P.status);
+          if (!ok) break;
+          mbar_arrive_expect_tx(full(s), STAGE);
+          const uint32_t a = ring + s * STAGE, b = a + A_BYTES;
+          if (A_K) tma_load_3d(a, &map_a, k0, c0, pa, full(s));
+          else
+            for (int i = 0; i < 2; ++i) tma_load_3d(a + i * 8192, &map_a, c0 + 64 * i, k0, pa, full(s));
+          if (B_K) tma_load_3d(b, &map_b, k0, r0, pb, full(s));
+          else
+            for (int i = 0; i < BN / 64; ++i) tma_load_3d(b + i * 8192, &map_b, r0 + 64 * i, k0, pb, full(s));
+          ++issued;
+          if (++s == S) { s = 0; ph ^= 1; }
+        }
+      }
+      if (!ok) {
+        // the copies requested into this CTA's shared memory land before it ends
+        for (int j = issued > S ? issued - S : 0; j < issued; ++j) mbar_wait_bounded(full(j % S), (j / S) & 1, P.status);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // -------------------------------------------------------------------- matrix instructions
+    if (lane == 0) {
+      int s = 0, n = 0;                                            // n: chunks started
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+        for (int it = 0; it < iters && ok; ++it) {
+          const int in_chunk = it % chunk;
+          if (in_chunk == 0) {
+            if (n >= 2) ok = mbar_wait_bounded(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
+          ok = mbar_wait_bounded(full(s), ph, P.status);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t a = ring + s * STAGE, b = a + A_BYTES, d = tmem + (uint32_t)(n & 1) * ACC;
+#pragma unroll
+          for (int k = 0; k < kTcK / 16; ++k)
+            mma_bf16(d, operand_desc<A_K>(a + k * (A_K ? 32 : 2048)), operand_desc<B_K>(b + k * (B_K ? 32 : 2048)),
+                     instr_desc<A_K, B_K>(BN), in_chunk > 0 || k > 0);
+          mma_commit(empty(s));
+          if (in_chunk == chunk - 1 || it == iters - 1) { mma_commit(acc_full(n & 1)); ++n; }
+          if (++s == S) { s = 0; ph ^= 1; }
+        }
+      }
+    }
+    __syncwarp();
+  }
+
+  // ---------------------------------------------------------------------- finishing warps
+  const int quad = warp & 3, half = (warp - 4) >> 2;
+  const uint32_t my_tmem = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NCOL);
+  if (warp >= 4 && P.split == 1) {
+    int n = 0;
+    bool ok = true;
+    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+      const int c = tile / P.tiles_r * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + half * NCOL;
+      if (PROMOTE) {
+        float acc[NCOL];
+#pragma unroll
+        for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
+        for (int ch = 0; ch < chunks; ++ch, ++n) {
+          ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+          if (!__all_sync(~0u, ok)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+          for (int j = 0; j < NCOL; j += 16) {
+            float v[16];
+            tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[j + i] += v[i];
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          mbar_arrive(acc_empty(n & 1));
+        }
+        if (!ok) break;
+        if (c < P.C) {
+#pragma unroll
+          for (int i = 0; i < NCOL; ++i)
+            if (r0 + i < P.R) finish_element<KIND, T, TO>(P.E, r0 + i, c, acc[i]);
+        }
+        __syncwarp();
+      } else {
+        if (chunks > 0) {
+          ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+          if (!__all_sync(~0u, ok)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
+#pragma unroll 1
+        for (int j = 0; j < NCOL; j += 16) {
+          float v[16] = {};
+          if (chunks > 0) tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+          if (c < P.C) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (r0 + j + i < P.R) finish_element<KIND, T, TO>(P.E, r0 + j + i, c, v[i]);
+          }
+          __syncwarp();
+        }
+        if (chunks > 0) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          mbar_arrive(acc_empty(n & 1));
+          ++n;
+        }
+      }
+    }
+  }
+  if (P.split > 1) {
+    // The cluster's CTAs hold partial sums of one tile.  CTA j finishes accumulator columns
+    // [j, j + 1) BN / split: everybody writes its sums of those columns into CTA j's shared memory
+    // (the operand ring, idle by then) and CTA j adds them in the order of the ranks.
+    const int cols = BN / P.split;
+    float acc[PROMOTE ? NCOL : 1];
+    if (warp >= 4) {
+      bool ok = true;
+      if (PROMOTE)
+#pragma unroll
+        for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
+      for (int n = 0; n < chunks && ok; ++n) {
+        ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+        ok = __all_sync(~0u, ok);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (PROMOTE && ok) {
+#pragma unroll
+          for (int j = 0; j < NCOL; j += 16) {
+            float v[16];
+            tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[j + i] += v[i];
+          }
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          mbar_arrive(acc_empty(n & 1));
+        }
+      }
+    }
+    cluster_sync();                                                // every ring is idle
+    if (warp >= 4) {
+      const uint32_t mine = ring + 4u * (uint32_t)(rank * cols * 128 + quad * 32 + lane);
+#pragma unroll
+      for (int j = 0; j < NCOL; j += 16) {
+        float v[16];
+        if (!PROMOTE) tmem_ld16(my_tmem + j, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int col = half * NCOL + j + i, owner = col / cols;
+          st_remote(mine + 512u * (uint32_t)(col - owner * cols), (uint32_t)owner, PROMOTE ? acc[PROMOTE ? j + i : 0] : v[i]);
+        }
+      }
+    }
+    cluster_sync();                                                // everybody's sums have arrived
+    if (warp >= 4 && first_tile < P.tiles) {
+      const float* const part = reinterpret_cast<const float*>(smem + kTcHead);
+      const int c = first_tile / P.tiles_r * 128 + quad * 32 + lane;
+      for (int i = half; i < cols; i += 2) {
+        const int r = first_tile % P.tiles_r * BN + rank * cols + i;
+        float v = part[i * 128 + quad * 32 + lane];
+        for (int q = 1; q < P.split; ++q) v += part[(q * cols + i) * 128 + quad * 32 + lane];
+        if (r < P.R && c < P.C) finish_element<KIND, T, TO>(P.E, r, c, v);
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
+  }
+}
+
+}  // namespace
+
+#endif  // GBMUF_CSRC_LINEAR_TC_CUH

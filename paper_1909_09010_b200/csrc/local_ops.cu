@@ -2,6 +2,8 @@
 // the gradient norm and clipping.  The interface is the last section of include/gbmuf.h; this file
 // holds the host side and the C ABI, the kernels live in the headers it includes:
 //   linear_epilogue.cuh  activations, and what happens to a finished sum of a matrix product
+//   linear_tc.cuh        matrix products on the tensor cores
+//   linear_pack.cuh      operands that cannot be read in place: other alignments, fp32 as bf16 parts
 //   linear_simt.cuh      matrix products on the fp32 units for any strides, column sums
 //   cross_entropy.cuh    cross-entropy over a vocabulary with its gradient
 //   grad_clip.cuh        norms over many tensors and the clipped copies
@@ -24,6 +26,8 @@
 #include "host_common.h"
 #include "primitives.cuh"
 #include "linear_epilogue.cuh"
+#include "linear_pack.cuh"
+#include "linear_tc.cuh"
 #include "linear_simt.cuh"
 #include "cross_entropy.cuh"
 #include "grad_clip.cuh"
@@ -31,6 +35,7 @@
 struct gbmuf_ops {
   int device = 0;
   int num_sms = 0;
+  int max_smem = 0;              // opt-in dynamic shared memory per block
   int32_t* d_status = nullptr;
 };
 
@@ -88,11 +93,146 @@ gbmuf_status check_sizes(const gbmuf_ops* ops, int64_t rows, int64_t n_in, int64
   return GBMUF_OK;
 }
 
+#define DISPATCH_DTYPE(dtype, T, ...)                       \
+  if ((dtype) == GBMUF_F32) { using T = float; __VA_ARGS__; } \
+  else { using T = __nv_bfloat16; __VA_ARGS__; }
+
+// An operand as it lies in memory: [outer][inner] of the call's type, row stride ld; k_inner: the
+// summed index is the inner one.
+struct Operand {
+  const void* p;
+  long long outer, inner, ld;
+  bool k_inner;
+};
+// A product of two operands: result [R][C], K terms.
+struct Product {
+  Operand a, b;
+  long long R, C, K;
+  int32_t dtype;
+  Epilogue E;
+};
+
+bool in_place(const Operand& o, int32_t dtype) {
+  return dtype == GBMUF_BF16 && (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || (o.ld % 8 == 0 && o.ld < ((long long)1 << 38)));
+}
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+long long packed_bytes(const Operand& o, int32_t dtype) {
+  return in_place(o, dtype) ? 0 : round_up((dtype == GBMUF_F32 ? 3 : 1) * o.outer * round_up(o.inner, 8) * 2, 256);
+}
+long long product_workspace(const Product& q) {
+  return q.K == 0 || q.R == 0 || q.C == 0 ? 0 : packed_bytes(q.a, q.dtype) + packed_bytes(q.b, q.dtype);
+}
+
+template <typename T>
+void pack(const gbmuf_ops* ops, const Operand& o, void* dst, cudaStream_t st) {
+  const long long ld_dst = round_up(o.inner, 8), n = o.outer * (ld_dst / 8);
+  const int grid = (int)std::min<long long>((n + 255) / 256, (long long)ops->num_sms * 16);
+  const bool vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)sizeof(T) % 16 == 0);
+  if (vec)
+    pack_kernel<T, true><<<grid, 256, 0, st>>>(static_cast<const T*>(o.p), o.ld, o.outer, o.inner, static_cast<__nv_bfloat16*>(dst), ld_dst);
+  else
+    pack_kernel<T, false><<<grid, 256, 0, st>>>(static_cast<const T*>(o.p), o.ld, o.outer, o.inner, static_cast<__nv_bfloat16*>(dst), ld_dst);
+}
+
+// Tensor map of an operand (packed at `packed` if it cannot be read in place): [parts][outer][inner],
+// boxes of 64 inner elements by `box` outer ones.
+gbmuf_status operand_map(const Operand& o, int32_t dtype, const void* packed, int box, CUtensorMap* map) {
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return refuse(GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
+  const bool here = in_place(o, dtype);
+  const long long ld = here && o.outer > 1 ? o.ld : round_up(o.inner, 8);
+  const cuuint64_t dim[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)(dtype == GBMUF_F32 ? 3 : 1)};
+  const cuuint64_t stride[2] = {(cuuint64_t)ld * 2, dtype == GBMUF_F32 ? (cuuint64_t)(o.outer * ld) * 2 : (cuuint64_t)ld * 2};
+  const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, one[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(here ? o.p : packed), dim, stride, boxes,
+                            one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return refuse(GBMUF_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
+  return GBMUF_OK;
+}
+
+struct TcShape { int bn, split; };
+TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int products, bool rows_64) {
+  TcShape best{256, 1};
+  double best_t = 1e300;
+  const long long ksteps = (q.K + 63) / 64;
+  for (int bn = rows_64 ? 64 : 32; bn <= 256; bn *= 2)
+    for (int split = 1; split <= 8; split *= 2) {
+      if (split > 1 && split * 2 > ksteps) break;
+      const long long tiles = ((q.C + 127) / 128) * ((q.R + bn - 1) / bn);
+      if (split > 1 && tiles * split > ops->num_sms) break;
+      const long long waves = (tiles * split + ops->num_sms - 1) / ops->num_sms;
+      const double step = std::max(2.0 * bn, 64.0 + bn);
+      const double t = waves * ((double)((ksteps + split - 1) / split) * products * step + 600.0 + bn * 4.0 / split) + (split > 1 ? 1500.0 : 0.0);
+      if (t < best_t) { best_t = t; best = {bn, split}; }
+    }
+  return best;
+}
+
+template <int KIND, typename T, typename TO, bool PROMOTE, int BN>
+gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
+  const auto kernel = linear_tc_kernel<KIND, T, TO, PROMOTE, BN>;
+  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN));
+  const uint32_t smem = tc_smem_bytes(BN, P.stages);
+  static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
+  const uint64_t bit = 1ull << (ops->device & 63);
+  if (!(ready.load() & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ops->max_smem);
+    if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the linear-layer kernel", e);
+    if (ops->device < 64) ready.fetch_or(bit);
+  }
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.blockDim = dim3(kTcThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  if (P.split > 1) {
+    cfg.gridDim = dim3((unsigned)(P.tiles * P.split));
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)P.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  } else {
+    cfg.gridDim = dim3((unsigned)std::min(P.tiles, ops->num_sms));
+  }
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ma, mb, P);
+  return e == cudaSuccess ? GBMUF_OK : cuda_refuse("launch of the linear-layer kernel", e);
+}
+
+// Runs a product: operands that cannot be read in place are packed into the workspace first.
 template <int KIND, typename T, typename TO>
-void launch_simt(const gbmuf_ops* ops, const SimtParams& P, cudaStream_t st) {
-  const long long tiles = ((P.C + 63) / 64) * ((P.R + 63) / 64);
-  const int grid = (int)std::min<long long>(tiles, (long long)ops->num_sms * 8);
-  linear_simt_kernel<KIND, T, TO><<<grid, 256, 0, st>>>(P);
+gbmuf_status run_product(const gbmuf_ops* ops, const Product& q, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
+  const long long need = product_workspace(q);
+  if (need > workspace_bytes || (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)))
+    return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
+  constexpr bool PROMOTE = sizeof(TO) == 4;
+  TcParams P{};
+  P.E = q.E; P.status = ops->d_status; P.R = (int)q.R; P.C = (int)q.C;
+  P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
+  P.products = q.dtype == GBMUF_F32 ? 6 : 1;
+  const TcShape shape = choose_shape(ops, q, P.products, KIND == kWeightGrad);
+  P.split = shape.split;
+  P.tiles_r = (int)((q.R + shape.bn - 1) / shape.bn);
+  const long long tiles = (long long)P.tiles_r * ((q.C + 127) / 128);
+  if (tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles");
+  P.tiles = (int)tiles;
+  CUtensorMap ma{}, mb{};
+  if (q.K > 0) {
+    unsigned char* const ws = static_cast<unsigned char*>(workspace);
+    void* const pa = ws;
+    void* const pb = ws + packed_bytes(q.a, q.dtype);
+    if (!in_place(q.a, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.a, pa, st))); }
+    if (!in_place(q.b, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.b, pb, st))); }
+    if (gbmuf_status rc = operand_map(q.a, q.dtype, pa, q.a.k_inner ? 128 : 64, &ma)) return rc;
+    if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn : 64, &mb)) return rc;
+  }
+  switch (shape.bn) {
+    case 32:
+      if constexpr (KIND != kWeightGrad) return launch_tc<KIND, T, TO, PROMOTE, 32>(ops, P, ma, mb, st);
+    case 64: return launch_tc<KIND, T, TO, PROMOTE, 64>(ops, P, ma, mb, st);
+    case 128: return launch_tc<KIND, T, TO, PROMOTE, 128>(ops, P, ma, mb, st);
+    default: return launch_tc<KIND, T, TO, PROMOTE, 256>(ops, P, ma, mb, st);
+  }
 }
 
 gbmuf_status check_forward(const gbmuf_ops* ops, const gbmuf_linear_forward_args* a) {
@@ -135,25 +275,34 @@ gbmuf_status launched(const char* what) {
   return e == cudaSuccess ? GBMUF_OK : cuda_refuse(what, e);
 }
 
-#define DISPATCH_DTYPE(dtype, T, ...)                       \
-  if ((dtype) == GBMUF_F32) { using T = float; __VA_ARGS__; } \
-  else { using T = __nv_bfloat16; __VA_ARGS__; }
+Product forward_product(const gbmuf_linear_forward_args* a) {
+  Product q{};
+  q.a = {a->w, a->n_out, a->n_in, a->ld_w, true};
+  q.b = {a->x, a->rows, a->n_in, a->ld_x, true};
+  q.R = a->rows; q.C = a->n_out; q.K = a->n_in; q.dtype = a->dtype;
+  q.E.bias = a->bias; q.E.residual = a->residual; q.E.ld_residual = a->ld_residual;
+  q.E.out0 = a->y; q.E.ld_out0 = a->ld_y; q.E.out1 = a->z; q.E.ld_out1 = a->ld_z; q.E.act = a->activation;
+  return q;
+}
 
-template <typename T, typename TO>
-void backward_weight(const gbmuf_ops* ops, const gbmuf_linear_backward_weight_args* a, cudaStream_t st) {
-  if (a->dw && a->n_in > 0) {
-    SimtParams P{};
-    P.a = a->dz; P.sa_r = 1; P.sa_k = a->ld_dz;
-    P.b = a->x; P.sb_c = 1; P.sb_k = a->ld_x;
-    P.R = a->n_out; P.C = a->n_in; P.K = a->rows;
-    P.E.out0 = a->dw; P.E.ld_out0 = a->ld_dw; P.E.accumulate = a->accumulate;
-    launch_simt<kWeightGrad, T, TO>(ops, P, st);
-  }
-  if (a->dbias) {
-    const int grid = (int)std::min<long long>((a->n_out + 31) / 32, 65535);
-    column_sum_kernel<T, TO><<<grid, 256, 0, st>>>(static_cast<const T*>(a->dz), a->ld_dz, a->rows, a->n_out,
-                                                   static_cast<TO*>(a->dbias), a->accumulate);
-  }
+Product input_grad_product(const gbmuf_linear_backward_input_args* a) {
+  Product q{};
+  q.a = {a->w, a->n_out, a->n_in, a->ld_w, false};
+  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, true};
+  q.R = a->rows; q.C = a->n_in; q.K = a->n_out; q.dtype = a->dtype;
+  q.E.residual = a->residual; q.E.ld_residual = a->ld_residual; q.E.z_in = a->z_prev; q.E.ld_z_in = a->ld_z_prev;
+  q.E.out0 = a->dx; q.E.ld_out0 = a->ld_dx; q.E.out1 = a->dz_prev; q.E.ld_out1 = a->ld_dz_prev;
+  q.E.act = a->activation;
+  return q;
+}
+
+Product weight_grad_product(const gbmuf_linear_backward_weight_args* a) {
+  Product q{};
+  q.a = {a->x, a->rows, a->n_in, a->ld_x, false};
+  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, false};
+  q.R = a->dw ? a->n_out : 0; q.C = a->n_in; q.K = a->rows; q.dtype = a->dtype;
+  q.E.out0 = a->dw; q.E.ld_out0 = a->ld_dw; q.E.accumulate = a->accumulate;
+  return q;
 }
 
 }  // namespace
@@ -169,6 +318,7 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
     gbmuf_ops* ops = new gbmuf_ops;
     ops->device = device;
     cudaError_t e = cudaDeviceGetAttribute(&ops->num_sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ops->max_smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
     if (e == cudaSuccess) e = cudaMalloc(&ops->d_status, 256);
     if (e == cudaSuccess) e = cudaMemset(ops->d_status, 0, 256);
     if (e != cudaSuccess) {
@@ -214,7 +364,7 @@ gbmuf_status gbmuf_linear_forward_workspace(gbmuf_ops* ops, const gbmuf_linear_f
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check_forward(ops, a)) return st;
-    *bytes = 0;
+    *bytes = product_workspace(forward_product(a));
     return GBMUF_OK;
   });
 }
@@ -225,14 +375,8 @@ gbmuf_status gbmuf_linear_forward(gbmuf_ops* ops, const gbmuf_linear_forward_arg
     if (a->rows == 0 || a->n_out == 0) return GBMUF_OK;
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    SimtParams P{};
-    P.a = a->x; P.sa_r = a->ld_x; P.sa_k = 1;
-    P.b = a->w; P.sb_c = a->ld_w; P.sb_k = 1;
-    P.R = a->rows; P.C = a->n_out; P.K = a->n_in;
-    P.E.bias = a->bias; P.E.residual = a->residual; P.E.ld_residual = a->ld_residual;
-    P.E.out0 = a->y; P.E.ld_out0 = a->ld_y; P.E.out1 = a->z; P.E.ld_out1 = a->ld_z; P.E.act = a->activation;
-    DISPATCH_DTYPE(a->dtype, T, (launch_simt<kForward, T, T>(ops, P, (cudaStream_t)stream)));
-    return launched("launch of the linear-layer kernel");
+    const Product q = forward_product(a);
+    DISPATCH_DTYPE(a->dtype, T, return run_product<kForward, T, T>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
   });
 }
 
@@ -241,7 +385,7 @@ gbmuf_status gbmuf_linear_backward_input_workspace(gbmuf_ops* ops, const gbmuf_l
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check_backward_input(ops, a)) return st;
-    *bytes = 0;
+    *bytes = product_workspace(input_grad_product(a));
     return GBMUF_OK;
   });
 }
@@ -253,15 +397,8 @@ gbmuf_status gbmuf_linear_backward_input(gbmuf_ops* ops, const gbmuf_linear_back
     if (a->rows == 0 || a->n_in == 0) return GBMUF_OK;
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    SimtParams P{};
-    P.a = a->dz; P.sa_r = a->ld_dz; P.sa_k = 1;
-    P.b = a->w; P.sb_c = 1; P.sb_k = a->ld_w;
-    P.R = a->rows; P.C = a->n_in; P.K = a->n_out;
-    P.E.residual = a->residual; P.E.ld_residual = a->ld_residual; P.E.z_in = a->z_prev; P.E.ld_z_in = a->ld_z_prev;
-    P.E.out0 = a->dx; P.E.ld_out0 = a->ld_dx; P.E.out1 = a->dz_prev; P.E.ld_out1 = a->ld_dz_prev;
-    P.E.act = a->activation;
-    DISPATCH_DTYPE(a->dtype, T, (launch_simt<kInputGrad, T, T>(ops, P, (cudaStream_t)stream)));
-    return launched("launch of the input-gradient kernel");
+    const Product q = input_grad_product(a);
+    DISPATCH_DTYPE(a->dtype, T, return run_product<kInputGrad, T, T>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
   });
 }
 
@@ -270,7 +407,7 @@ gbmuf_status gbmuf_linear_backward_weight_workspace(gbmuf_ops* ops, const gbmuf_
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check_backward_weight(ops, a)) return st;
-    *bytes = 0;
+    *bytes = product_workspace(weight_grad_product(a));
     return GBMUF_OK;
   });
 }
@@ -282,8 +419,19 @@ gbmuf_status gbmuf_linear_backward_weight(gbmuf_ops* ops, const gbmuf_linear_bac
     if (a->n_out == 0 || (a->accumulate && a->rows == 0)) return GBMUF_OK;
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    DISPATCH_DTYPE(a->dtype, T,
-                   DISPATCH_DTYPE(a->grad_dtype, TO, (backward_weight<T, TO>(ops, a, (cudaStream_t)stream))));
+    cudaStream_t st = (cudaStream_t)stream;
+    if (a->dw && a->n_in > 0) {
+      const Product q = weight_grad_product(a);
+      gbmuf_status rc = GBMUF_OK;
+      DISPATCH_DTYPE(a->grad_dtype, TO, (rc = run_product<kWeightGrad, TO, TO>(ops, q, a->workspace, a->workspace_bytes, st)));
+      if (rc != GBMUF_OK) return rc;
+    }
+    if (a->dbias) {
+      const int grid = (int)std::min<long long>((a->n_out + 31) / 32, 65535);
+      DISPATCH_DTYPE(a->dtype, T, DISPATCH_DTYPE(a->grad_dtype, TO,
+          (column_sum_kernel<T, TO><<<grid, 256, 0, st>>>(static_cast<const T*>(a->dz), a->ld_dz, a->rows, a->n_out,
+                                                          static_cast<TO*>(a->dbias), a->accumulate))));
+    }
     return launched("launch of the weight-gradient kernels");
   });
 }
