@@ -17,9 +17,10 @@ namespace {
 // is done for the six products of parts that reach 2^-24 of the product: `products` = 6.
 //
 // A tile is 128 x BN.  Warp 0 loads 64 k of both operands per step with the copy engine (128-byte
-// swizzle), warp 1 issues the matrix instructions, warps 4..11 finish the sums.  Two accumulators:
+// swizzle), warp 1 issues the matrix instructions, the warps from 4 on finish the sums.  Two accumulators:
 // one is finished while the next is summed.
-constexpr int kTcThreads = 384;
+constexpr int kTcFinishers = 16;               // warps
+constexpr int kTcThreads = 128 + 32 * kTcFinishers;
 constexpr int kTcK = 64;                       // k per step
 constexpr int kTcMaxStages = 12;
 
@@ -81,17 +82,23 @@ __device__ __forceinline__ void st_remote(uint32_t addr, uint32_t rank, float v)
                "r"(rank), "f"(v)
                : "memory");
 }
-// 16 accumulator columns of this warp's 32 lanes.
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16]) {
-  uint32_t u[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-      : "r"(addr));
+// N accumulator columns of this warp's 32 lanes.
+template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[N]) {
+  static_assert(N == 8 || N == 16, "");
+  uint32_t u[N];
+  if constexpr (N == 16)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+          "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+        : "r"(addr));
+  else
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+                 : "r"(addr));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(u[i]);
 }
 
 // Parts (0 hi, 1 mid, 2 lo) of A and B in product p of six, smallest products first: an accumulator
@@ -105,7 +112,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad;
   constexpr uint32_t STAGE = tc_stage_bytes(BN), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
-  constexpr int NCOL = BN / 2;                 // accumulator columns per finishing warp
+  constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
+  constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
   extern __shared__ unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const uint32_t bars = smem_u32(smem), ring = bars + kTcHead;
@@ -119,7 +127,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 256); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 32 * kTcFinishers); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -208,13 +216,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
 
   // ---------------------------------------------------------------------- finishing warps
-  const int quad = warp & 3, half = (warp - 4) >> 2;
-  const uint32_t my_tmem = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(half * NCOL);
+  const int quad = warp & 3, part = (warp - 4) >> 2;
+  const uint32_t my_tmem = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * NCOL);
+  auto bias_of = [&](int c) {
+    return KIND == kForward && P.E.bias && c < P.C ? to_f32(static_cast<const T*>(P.E.bias)[c]) : 0.0f;
+  };
   if (warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
     for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-      const int c = tile / P.tiles_r * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + half * NCOL;
+      const int c = tile / P.tiles_r * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + part * NCOL;
+      const float bias = bias_of(c);
       if (PROMOTE) {
         float acc[NCOL];
 #pragma unroll
@@ -224,38 +236,41 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (!__all_sync(~0u, ok)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-          for (int j = 0; j < NCOL; j += 16) {
-            float v[16];
-            tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+          for (int j = 0; j < NCOL; j += N) {
+            float v[N];
+            tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j + i] += v[i];
+            for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           mbar_arrive(acc_empty(n & 1));
         }
         if (!ok) break;
-        if (c < P.C) {
 #pragma unroll
-          for (int i = 0; i < NCOL; ++i)
-            if (r0 + i < P.R) finish_element<KIND, T, TO>(P.E, r0 + i, c, acc[i]);
+        for (int j = 0; j < NCOL; j += N) {
+          Finisher<KIND, T, TO, N> F;
+          float v[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[i] = acc[j + i];
+          F.ask(P.E, r0 + j, c, P.R, P.C, lane);
+          F.finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
         }
-        __syncwarp();
       } else {
+        // what the epilogue reads is requested one strip ahead, the first one during the sums
+        Finisher<KIND, T, TO, N> F;
+        F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
           ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
           if (!__all_sync(~0u, ok)) { ok = false; break; }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
 #pragma unroll 1
-        for (int j = 0; j < NCOL; j += 16) {
-          float v[16] = {};
-          if (chunks > 0) tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
-          if (c < P.C) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (r0 + j + i < P.R) finish_element<KIND, T, TO>(P.E, r0 + j + i, c, v[i]);
-          }
-          __syncwarp();
+        for (int j = 0; j < NCOL; j += N) {
+          float v[N] = {};
+          if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+          const Finisher<KIND, T, TO, N> now = F;
+          if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
+          Finisher<KIND, T, TO, N>(now).finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -282,11 +297,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (PROMOTE && ok) {
 #pragma unroll
-          for (int j = 0; j < NCOL; j += 16) {
-            float v[16];
-            tmem_ld16(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+          for (int j = 0; j < NCOL; j += N) {
+            float v[N];
+            tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j + i] += v[i];
+            for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           mbar_arrive(acc_empty(n & 1));
@@ -297,25 +312,33 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (warp >= 4) {
       const uint32_t mine = ring + 4u * (uint32_t)(rank * cols * 128 + quad * 32 + lane);
 #pragma unroll
-      for (int j = 0; j < NCOL; j += 16) {
-        float v[16];
-        if (!PROMOTE) tmem_ld16(my_tmem + j, v);
+      for (int j = 0; j < NCOL; j += N) {
+        float v[N];
+        if (!PROMOTE) tmem_ld<N>(my_tmem + j, v);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int col = half * NCOL + j + i, owner = col / cols;
+        for (int i = 0; i < N; ++i) {
+          const int col = part * NCOL + j + i, owner = col / cols;
           st_remote(mine + 512u * (uint32_t)(col - owner * cols), (uint32_t)owner, PROMOTE ? acc[PROMOTE ? j + i : 0] : v[i]);
         }
       }
     }
     cluster_sync();                                                // everybody's sums have arrived
-    if (warp >= 4 && first_tile < P.tiles) {
-      const float* const part = reinterpret_cast<const float*>(smem + kTcHead);
+    if (warp >= 4) {
+      // strips of 4 rows (BN / split is a multiple of 4)
+      const float* const sums = reinterpret_cast<const float*>(smem + kTcHead) + quad * 32 + lane;
       const int c = first_tile / P.tiles_r * 128 + quad * 32 + lane;
-      for (int i = half; i < cols; i += 2) {
+      const float bias = bias_of(c);
+      for (int i = 4 * part; i < cols; i += kTcFinishers) {
         const int r = first_tile % P.tiles_r * BN + rank * cols + i;
-        float v = part[i * 128 + quad * 32 + lane];
-        for (int q = 1; q < P.split; ++q) v += part[(q * cols + i) * 128 + quad * 32 + lane];
-        if (r < P.R && c < P.C) finish_element<KIND, T, TO>(P.E, r, c, v);
+        Finisher<KIND, T, TO, 4> F;
+        F.ask(P.E, r, c, P.R, P.C, lane);
+        float v[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          v[x] = sums[(i + x) * 128];
+          for (int q = 1; q < P.split; ++q) v[x] += sums[(q * cols + i + x) * 128];
+        }
+        F.finish(P.E, r, c, P.R, P.C, lane, bias, v);
       }
     }
   }

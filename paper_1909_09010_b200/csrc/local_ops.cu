@@ -151,6 +151,16 @@ gbmuf_status operand_map(const Operand& o, int32_t dtype, const void* packed, in
   return GBMUF_OK;
 }
 
+// Whether the epilogue's matrices can be accessed two bf16 columns at a time.
+int may_pair(const Product& q) {
+  const Epilogue& E = q.E;
+  const void* const p[] = {E.residual, E.z_in, E.out0, E.out1};
+  const long long ld[] = {E.ld_residual, E.ld_z_in, E.ld_out0, E.ld_out1};
+  bool ok = q.C % 2 == 0;
+  for (int i = 0; i < 4; ++i) ok = ok && (!p[i] || ((uintptr_t)p[i] % 4 == 0 && (q.R == 1 || ld[i] % 2 == 0)));
+  return ok;
+}
+
 struct TcShape { int bn, split; };
 TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int products, bool rows_64) {
   TcShape best{256, 1};
@@ -201,11 +211,12 @@ gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma,
 
 // Runs a product: operands that cannot be read in place are packed into the workspace first.
 template <int KIND, typename T, typename TO>
-gbmuf_status run_product(const gbmuf_ops* ops, const Product& q, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
+gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
   const long long need = product_workspace(q);
   if (need > workspace_bytes || (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)))
     return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
   constexpr bool PROMOTE = sizeof(TO) == 4;
+  q.E.pairs = may_pair(q);
   TcParams P{};
   P.E = q.E; P.status = ops->d_status; P.R = (int)q.R; P.C = (int)q.C;
   P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
