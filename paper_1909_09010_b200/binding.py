@@ -32,7 +32,8 @@ EXPORTS = ["gbmuf_create", "gbmuf_set_partition", "gbmuf_init", "gbmuf_local_per
            "gbmuf_linear_backward_input_workspace", "gbmuf_linear_backward_input",
            "gbmuf_linear_backward_weight_workspace", "gbmuf_linear_backward_weight",
            "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_clip_create",
-           "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_destroy"]
+           "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_device_status",
+           "gbmuf_clip_destroy"]
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 
 
@@ -140,6 +141,7 @@ def lib() -> ctypes.CDLL:
     L.gbmuf_clip_set_tensors.argtypes = [vp, i64, vp]
     L.gbmuf_clip_norms.argtypes = [vp, vp, vp]
     L.gbmuf_clip_scale.argtypes = [vp, f32, vp, vp]
+    L.gbmuf_clip_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
     L.gbmuf_clip_destroy.argtypes = [vp]
     L.gbmuf_last_error.argtypes = [vp]
     L.gbmuf_last_error.restype = ctypes.c_char_p
@@ -753,6 +755,12 @@ class GradClip:
         norms = self._norms(norms_out)
         self._check(self._L.gbmuf_clip_scale(self._h, max_norm, norms.data_ptr(), self._on(stream)))
         return norms
+
+    def device_status(self, stream=None) -> int:
+        """Waits for the stream; reads and clears the status word."""
+        v = ctypes.c_int32(-1)
+        self._check(self._L.gbmuf_clip_device_status(self._h, self._on(stream), ctypes.byref(v)))
+        return v.value
 
     def _on(self, stream):
         if stream is None:

@@ -5,26 +5,48 @@
 
 namespace {
 
-// out[c] (+)= sum over the rows of a [R][C] matrix: one block per 32 columns, 8 row groups summed
-// in a fixed order.
-template <typename T, typename TO>
-__global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long ld, long long R, long long C,
-                                                         TO* out, int accumulate) {
-  __shared__ float part[8][33];
-  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
-  for (long long c0 = (long long)blockIdx.x * 32; c0 < C; c0 += (long long)gridDim.x * 32) {
-    const long long c = c0 + lane;
-    float s = 0.0f;
-    if (c < C)
-      for (long long r = g; r < R; r += 8) s += to_f32(a[r * ld + c]);
-    part[g][lane] = s;
-    __syncthreads();
-    if (g == 0 && c < C) {
-      float t = part[0][lane];
-      for (int i = 1; i < 8; ++i) t += part[i][lane];
-      out[c] = from_f32<TO>(accumulate ? t + to_f32(out[c]) : t);
+// out[c] (+)= sum over the rows of a [R][C] matrix.  A cluster takes a strip of columns (VEC: 128
+// bytes wide, 16 bytes per thread; else 32 columns) and shares its rows; sums are joined through
+// shared memory and rank 0's shared memory, in a fixed order.
+template <typename T, typename TO, bool VEC>
+__global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long ld, long long R, long long C, TO* out,
+                                                         int accumulate) {
+  constexpr int W = VEC ? 16 / (int)sizeof(T) : 1, L = VEC ? 8 : 32, ROWS = 256 / L, COLS = L * W;
+  __shared__ float part[ROWS][COLS + 1];
+  __shared__ float ranks[8][COLS];
+  uint32_t share, rank;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(share));
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const long long c0 = (long long)(blockIdx.x / share) * COLS;
+  const int lane = threadIdx.x % L, row = threadIdx.x / L;
+  const long long c = c0 + lane * W;
+  float s[W] = {};
+  if (c < C) {                                              // VEC: C is a multiple of W
+    const T* p = a + c;
+    const long long step = (long long)share * ROWS;
+#pragma unroll 8
+    for (long long r = (long long)rank * ROWS + row; r < R; r += step) {
+      __align__(16) T v[W];
+      if constexpr (VEC) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p + r * ld);
+      else v[0] = p[r * ld];
+#pragma unroll
+      for (int i = 0; i < W; ++i) s[i] += to_f32(v[i]);
     }
-    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) part[row][lane * W + i] = s[i];
+  __syncthreads();
+  if (threadIdx.x < COLS) {
+    float t = part[0][threadIdx.x];
+    for (int i = 1; i < ROWS; ++i) t += part[i][threadIdx.x];
+    st_remote(smem_u32(&ranks[rank][threadIdx.x]), 0, t);
+  }
+  cluster_sync();
+  if (rank == 0 && threadIdx.x < COLS && c0 + threadIdx.x < C) {
+    float t = ranks[0][threadIdx.x];
+    for (uint32_t q = 1; q < share; ++q) t += ranks[q][threadIdx.x];
+    TO* const o = out + c0 + threadIdx.x;
+    *o = from_f32<TO>(accumulate ? t + to_f32(*o) : t);
   }
 }
 

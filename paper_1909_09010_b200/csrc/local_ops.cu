@@ -44,8 +44,9 @@ struct gbmuf_clip {
   int64_t count = 0;             // tensors with elements
   long long chunks = 0;
   int blocks = 0;
-  void* table = nullptr;         // [ClipTensor][slots][partial sums]
+  void* table = nullptr;         // status word, [ClipEntry][slots][partial sums]
   size_t table_bytes = 0, slots_off = 0, partial_off = 0;
+  int32_t* status() const { return static_cast<int32_t*>(table); }
   WorkMarks work;
 };
 
@@ -316,6 +317,45 @@ Product weight_grad_product(const gbmuf_linear_backward_weight_args* a) {
   return q;
 }
 
+template <typename T, typename TO>
+cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t st) {
+  const bool vec = (uintptr_t)a->dz % 16 == 0 && a->n_out % (16 / sizeof(T)) == 0 &&
+                   (a->rows <= 1 || a->ld_dz * sizeof(T) % 16 == 0);
+  const int cols = vec ? 128 / (int)sizeof(T) : 32, rows_at_once = vec ? 32 : 8;
+  // a cluster shares the rows of a column tile: as many CTAs as have four rows per thread, 8 at most
+  unsigned share = 1;
+  while (share < 8 && a->rows >= (long long)share * 2 * rows_at_once * 4) share *= 2;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = share; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(share * (unsigned)((a->n_out + cols - 1) / cols));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const T* const dz = static_cast<const T*>(a->dz);
+  TO* const out = static_cast<TO*>(a->dbias);
+  const long long R = a->rows, C = a->n_out, ld = a->ld_dz;
+  return vec ? cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, true>, dz, ld, R, C, out, (int)a->accumulate)
+             : cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, false>, dz, ld, R, C, out, (int)a->accumulate);
+}
+
+// Reads and clears a status word, once the stream has got there.
+gbmuf_status read_status(int device, int32_t* word, void* stream, int32_t* out) {
+  DeviceGuard guard(device);
+  if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
+  cudaStream_t st = (cudaStream_t)stream;
+  if (is_capturing(st)) return refuse(GBMUF_ERR_BAD_STATE, "the status word cannot be read inside a stream capture");
+  int32_t v = 0;
+  cudaError_t e = cudaMemcpyAsync(&v, word, sizeof(v), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof(v), st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return cuda_refuse("read of the device status word", e);
+  *out = v;
+  return GBMUF_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -346,17 +386,7 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
 gbmuf_status gbmuf_ops_device_status(gbmuf_ops* ops, void* stream, int32_t* out) {
   return guarded([&]() -> gbmuf_status {
     if (!ops || !out) return invalid("ops and out must not be NULL");
-    DeviceGuard guard(ops->device);
-    if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    cudaStream_t st = (cudaStream_t)stream;
-    if (is_capturing(st)) return refuse(GBMUF_ERR_BAD_STATE, "the status word cannot be read inside a stream capture");
-    int32_t v = 0;
-    cudaError_t e = cudaMemcpyAsync(&v, ops->d_status, sizeof(v), cudaMemcpyDeviceToHost, st);
-    if (e == cudaSuccess) e = cudaMemsetAsync(ops->d_status, 0, sizeof(v), st);
-    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-    if (e != cudaSuccess) return cuda_refuse("read of the device status word", e);
-    *out = v;
-    return GBMUF_OK;
+    return read_status(ops->device, ops->d_status, stream, out);
   });
 }
 
@@ -438,12 +468,11 @@ gbmuf_status gbmuf_linear_backward_weight(gbmuf_ops* ops, const gbmuf_linear_bac
       if (rc != GBMUF_OK) return rc;
     }
     if (a->dbias) {
-      const int grid = (int)std::min<long long>((a->n_out + 31) / 32, 65535);
-      DISPATCH_DTYPE(a->dtype, T, DISPATCH_DTYPE(a->grad_dtype, TO,
-          (column_sum_kernel<T, TO><<<grid, 256, 0, st>>>(static_cast<const T*>(a->dz), a->ld_dz, a->rows, a->n_out,
-                                                          static_cast<TO*>(a->dbias), a->accumulate))));
+      cudaError_t e = cudaSuccess;
+      DISPATCH_DTYPE(a->dtype, T, DISPATCH_DTYPE(a->grad_dtype, TO, (e = column_sum<T, TO>(a, st))));
+      if (e != cudaSuccess) return cuda_refuse("launch of the bias-gradient kernel", e);
     }
-    return launched("launch of the weight-gradient kernels");
+    return GBMUF_OK;
   });
 }
 
@@ -520,7 +549,8 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
     }
     std::stable_sort(order.begin(), order.end(),
                      [&](int64_t i, int64_t j) { return tensors[i].group < tensors[j].group; });
-    std::vector<ClipTensor> table(order.size());
+    std::vector<ClipEntry> table;
+    table.reserve(order.size());
     std::vector<long long> group_first(h->groups, -1), group_end(h->groups, -1);
     std::vector<int> group_run(h->groups, 0);
     long long chunks = 0;
@@ -528,17 +558,29 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
     for (size_t i = 0; i < order.size(); ++i) {
       const gbmuf_grad_tensor& t = tensors[order[i]];
       if (i == 0 || tensors[order[i - 1]].group != t.group) ++run;
-      ClipTensor& d = table[i];
-      d.grad = t.grad; d.out = t.out; d.n = t.rows * t.cols; d.cols = t.cols;
-      // a tensor of one row, or of rows that follow one another, is one run of elements
-      d.ld_grad = t.rows == 1 ? t.cols : t.ld_grad;
-      d.ld_out = t.rows == 1 ? t.cols : t.ld_out;
-      d.dtype = t.dtype; d.out_dtype = t.out_dtype; d.group = t.group; d.run = run; d.chunk0 = chunks;
+      // rows that follow one another are one run of elements, long rows are a run each; short
+      // strided rows stay together and are read element by element
+      const bool whole = t.rows == 1 || (t.ld_grad == t.cols && (!t.out || t.ld_out == t.cols));
+      const bool split = !whole && t.cols >= 512;
+      const int64_t runs = split ? t.rows : 1;
       if (group_first[t.group] < 0) { group_first[t.group] = chunks; group_run[t.group] = run; }
-      chunks += (d.n + kClipChunk - 1) / kClipChunk;
+      if (runs + (int64_t)table.size() > (1 << 26)) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^26 runs of elements");
+      for (int64_t r = 0; r < runs; ++r) {
+        ClipEntry d{};
+        d.grad = static_cast<const char*>(t.grad) + r * t.ld_grad * (int64_t)size_of(t.dtype);
+        d.out = t.out ? static_cast<char*>(t.out) + r * t.ld_out * (int64_t)size_of(t.out_dtype) : nullptr;
+        d.n = split ? t.cols : t.rows * t.cols;
+        d.cols = t.cols; d.ld_grad = t.ld_grad; d.ld_out = t.ld_out;
+        d.dtype = t.dtype; d.out_dtype = t.out ? t.out_dtype : t.dtype; d.group = t.group; d.run = run; d.chunk0 = chunks;
+        d.direct = !whole && !split;
+        d.shift = d.direct ? 0 : (int32_t)((uintptr_t)d.grad % 16 / size_of(t.dtype));
+        const int64_t ch = kClipSlot / (int64_t)size_of(t.dtype);
+        chunks += (d.n + d.shift + ch - 1) / ch;
+        table.push_back(d);
+      }
       group_end[t.group] = chunks;
     }
-    const int blocks = (int)std::max<long long>(1, std::min<long long>(chunks, (long long)h->num_sms * 4));
+    const int blocks = (int)std::max<long long>(1, std::min<long long>(chunks, (long long)h->num_sms * kClipBlocksPerSm));
     std::vector<int> slots(2 * (size_t)h->groups, 0);
     auto block_of = [&](long long c) {      // the block whose chunks [b C / G, (b + 1) C / G) hold c
       long long b = c * blocks / chunks;
@@ -554,7 +596,7 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
       }
     DeviceGuard guard(h->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    const size_t slots_off = (table.size() * sizeof(ClipTensor) + 255) / 256 * 256;
+    const size_t slots_off = 256 + (table.size() * sizeof(ClipEntry) + 255) / 256 * 256;
     const size_t partial_off = slots_off + (slots.size() * sizeof(int) + 255) / 256 * 256;
     const size_t bytes = partial_off + ((size_t)blocks + h->groups) * sizeof(double);
     cudaError_t e = h->work.wait();
@@ -568,7 +610,7 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
       h->table_bytes = bytes;
     }
     std::vector<unsigned char> image(partial_off, 0);
-    if (!table.empty()) memcpy(image.data(), table.data(), table.size() * sizeof(ClipTensor));
+    if (!table.empty()) memcpy(image.data() + 256, table.data(), table.size() * sizeof(ClipEntry));
     if (!slots.empty()) memcpy(image.data() + slots_off, slots.data(), slots.size() * sizeof(int));
     h->count = 0;                            // no usable table until the upload has succeeded
     h->chunks = 0;
@@ -591,7 +633,9 @@ gbmuf_status gbmuf_clip_create(int32_t device, int32_t groups, int64_t count, co
     gbmuf_clip* h = new gbmuf_clip;
     h->device = device; h->groups = groups;
     gbmuf_status st = GBMUF_OK;
-    const cudaError_t e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, device);
+    cudaError_t e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)clip_norm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)clip_scale_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipSmem);
     if (e != cudaSuccess) { cudaGetLastError(); st = cuda_refuse("device properties", e); }
     if (st == GBMUF_OK) st = gbmuf_clip_set_tensors(h, count, tensors);
     if (st != GBMUF_OK) { cudaFree(h->table); delete h; return st; }
@@ -610,17 +654,33 @@ static gbmuf_status clip_run(gbmuf_clip* h, bool scale, float max_norm, float* n
     cudaStream_t st = (cudaStream_t)stream;
     ClipParams P{};
     unsigned char* const base = static_cast<unsigned char*>(h->table);
-    P.tensors = reinterpret_cast<const ClipTensor*>(base);
+    P.status = h->status();
+    P.entries = reinterpret_cast<const ClipEntry*>(base + 256);
     P.slots = reinterpret_cast<const int*>(base + h->slots_off);
     P.partial = reinterpret_cast<double*>(base + h->partial_off);
     P.norms = norms; P.chunks = h->chunks; P.count = (int)h->count; P.groups = h->groups; P.blocks = h->blocks;
     P.max_norm = max_norm;
-    if (h->chunks > 0) clip_norm_kernel<<<h->blocks, 256, 0, st>>>(P);
-    if (scale) clip_scale_kernel<<<h->blocks, 256, 0, st>>>(P);
-    else clip_finish_kernel<<<std::min(h->groups, h->num_sms), 256, 0, st>>>(P);
-    const gbmuf_status rc = launched("launch of the gradient-norm kernels");
-    if (rc == GBMUF_OK) h->work.note(st);
-    return rc;
+    if (h->chunks > 0) clip_norm_kernel<<<h->blocks, kClipThreads, kClipSmem, st>>>(P);
+    if (gbmuf_status rc = launched("launch of the gradient-norm kernel")) return rc;
+    // the second kernel's blocks may become resident while the first one ends
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = h->chunks > 0 ? 1 : 0;
+    cudaError_t e;
+    if (scale) {
+      cfg.gridDim = dim3(h->blocks); cfg.blockDim = dim3(kClipThreads); cfg.dynamicSmemBytes = kClipSmem;
+      e = cudaLaunchKernelEx(&cfg, clip_scale_kernel, P);
+    } else {
+      cfg.gridDim = dim3(std::min(h->groups, h->num_sms)); cfg.blockDim = dim3(kClipWorkers);
+      e = cudaLaunchKernelEx(&cfg, clip_finish_kernel, P);
+    }
+    if (e != cudaSuccess) return cuda_refuse("launch of the gradient-norm kernels", e);
+    h->work.note(st);
+    return GBMUF_OK;
   });
 }
 
@@ -629,6 +689,13 @@ gbmuf_status gbmuf_clip_norms(gbmuf_clip* h, float* norms, void* stream) {
 }
 gbmuf_status gbmuf_clip_scale(gbmuf_clip* h, float max_norm, float* norms, void* stream) {
   return clip_run(h, true, max_norm, norms, stream);
+}
+
+gbmuf_status gbmuf_clip_device_status(gbmuf_clip* h, void* stream, int32_t* out) {
+  return guarded([&]() -> gbmuf_status {
+    if (!h || !out) return invalid("handle and out must not be NULL");
+    return read_status(h->device, h->status(), stream, out);
+  });
 }
 
 gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h) {
