@@ -37,6 +37,7 @@ struct gbmuf_ops {
   int num_sms = 0;
   int max_smem = 0;              // opt-in dynamic shared memory per block
   int32_t* d_status = nullptr;
+  int loss_clusters[2][4] = {};  // clusters of 1, 2, 4, 8 CTAs of the cross-entropy kernel (fp32, bf16) that fit at once
 };
 
 struct gbmuf_clip {
@@ -341,6 +342,52 @@ cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t 
              : cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, false>, dz, ld, R, C, out, (int)a->accumulate);
 }
 
+template <typename T>
+cudaLaunchConfig_t loss_config(int split, int clusters, cudaLaunchAttribute* attr, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(clusters * split)); cfg.blockDim = dim3(kLossThreads); cfg.dynamicSmemBytes = kLossSmem;
+  cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
+  attr->id = cudaLaunchAttributeClusterDimension;
+  attr->val.clusterDim.x = (unsigned)split; attr->val.clusterDim.y = 1; attr->val.clusterDim.z = 1;
+  return cfg;
+}
+
+template <typename T> cudaError_t prepare_loss(gbmuf_ops* ops, int (&clusters)[4]) {
+  cudaError_t e = cudaFuncSetAttribute((const void*)cross_entropy_ring_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLossSmem);
+  for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = loss_config<T>(1 << i, ops->num_sms >> i, &attr, nullptr);
+    e = cudaOccupancyMaxActiveClusters(&clusters[i], cross_entropy_ring_kernel<T>, &cfg);
+    if (clusters[i] < 1) clusters[i] = 1;
+  }
+  return e;
+}
+
+// Short rows: a warp each.  Rows of up to 8 x 147 KB: in the shared memory of as few CTAs as hold
+// them, or of more where there are too few rows for all SMs.  Longer ones are read twice.
+template <typename T> cudaError_t launch_loss(const gbmuf_ops* ops, LossParams& P, cudaStream_t st) {
+  if (P.vocab <= kWarpVocab) {
+    const unsigned grid = (unsigned)((P.rows + 3) / 4);
+    if (P.vocab <= 256) cross_entropy_warp_kernel<T, 8><<<grid, 128, 0, st>>>(P);
+    else if (P.vocab <= 1024) cross_entropy_warp_kernel<T, 32><<<grid, 128, 0, st>>>(P);
+    else cross_entropy_warp_kernel<T, kWarpRegs><<<grid, 128, 0, st>>>(P);
+    return cudaGetLastError();
+  }
+  const long long pieces = (P.vocab * (long long)sizeof(T) + 15) / 16, most = (long long)kLossMostChunks * kLossChunk / 16;
+  int log = 0;
+  while (log < 3 && (pieces >> log) > most - 1) ++log;
+  if ((pieces >> log) > most - 1) {
+    cross_entropy_twice_kernel<T><<<(unsigned)std::min<long long>(P.rows, ops->num_sms * 4), 512, 0, st>>>(P);
+    return cudaGetLastError();
+  }
+  while (log < 3 && P.rows << (log + 1) <= ops->num_sms && (pieces >> log) >= 2 * kLossChunk / 16) ++log;
+  P.split = 1 << log;
+  cudaLaunchAttribute attr;
+  const int clusters = (int)std::min<long long>(P.rows, ops->loss_clusters[sizeof(T) == 2][log]);
+  const cudaLaunchConfig_t cfg = loss_config<T>(P.split, clusters, &attr, st);
+  return cudaLaunchKernelEx(&cfg, cross_entropy_ring_kernel<T>, P);
+}
+
 // Reads and clears a status word, once the stream has got there.
 gbmuf_status read_status(int device, int32_t* word, void* stream, int32_t* out) {
   DeviceGuard guard(device);
@@ -370,6 +417,8 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
     ops->device = device;
     cudaError_t e = cudaDeviceGetAttribute(&ops->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ops->max_smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
+    if (e == cudaSuccess) e = prepare_loss<float>(ops, ops->loss_clusters[0]);
+    if (e == cudaSuccess) e = prepare_loss<__nv_bfloat16>(ops, ops->loss_clusters[1]);
     if (e == cudaSuccess) e = cudaMalloc(&ops->d_status, 256);
     if (e == cudaSuccess) e = cudaMemset(ops->d_status, 0, 256);
     if (e != cudaSuccess) {
@@ -520,9 +569,9 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
     P.loss = a->loss; P.lse = a->lse; P.dlogits = a->dlogits;
     P.rows = a->rows; P.vocab = a->vocab; P.ld = a->ld_logits; P.ld_d = a->ld_dlogits;
     P.ignore_index = a->ignore_index; P.scale = a->scale; P.status = ops->d_status;
-    const int grid = (int)std::min<long long>(a->rows, (long long)ops->num_sms * 8);
-    DISPATCH_DTYPE(a->dtype, T, (cross_entropy_kernel<T><<<grid, 256, 0, (cudaStream_t)stream>>>(P)));
-    return launched("launch of the cross-entropy kernel");
+    cudaError_t e = cudaSuccess;
+    DISPATCH_DTYPE(a->dtype, T, e = launch_loss<T>(ops, P, (cudaStream_t)stream));
+    return e == cudaSuccess ? GBMUF_OK : cuda_refuse("launch of the cross-entropy kernel", e);
   });
 }
 
