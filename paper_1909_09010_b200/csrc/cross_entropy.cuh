@@ -7,8 +7,7 @@ namespace {
 
 // Per row: m = max x, s = sum exp(x - m), then d = s_i (exp(x - m) / s - [target]).  Every logit is
 // needed twice with the whole row between, so the row stays on the chip from its one read to its
-// one write: in the registers of a warp (short rows), or in the shared memory of 1 to 8 CTAs of a
-// cluster (16 KB to 1.1 MB of it).  Only longer rows are read twice.
+// one write: in the registers of a warp (short rows), or in shared memory and the L2 cache.
 struct LossParams {
   const void* logits;
   const int64_t* targets;
@@ -84,14 +83,6 @@ template <bool FAST> struct Shift {
   }
 };
 
-// (m, s): s = sum of exp(x - m) over some logits.  m = -inf: nothing but -inf (s = 0), or NaN (s).
-__device__ __forceinline__ void softmax_merge(float& m, float& s, float m2, float s2) {
-  const float top = fmaxf(m, m2);
-  if (top == -INFINITY) { s += s2; return; }
-  s = s * expf(m - top) + s2 * expf(m2 - top);
-  m = top;
-}
-
 // What the statistics of a row say: its loss and whether its gradient is zero.
 struct RowOutcome { float lse, loss; bool zero; };
 __device__ __forceinline__ bool target_ignored(const LossParams& P, long long t, float w) { return t == P.ignore_index || w == 0.0f; }
@@ -161,19 +152,22 @@ __global__ void __launch_bounds__(128) cross_entropy_warp_kernel(const LossParam
   }
 }
 
-// ---- rows in shared memory.  A cluster of `split` CTAs takes a row; each holds a slice of its
-// 16-byte pieces as chunks in a ring of slots that a producer warp keeps filled by bulk copies.  A
-// group of 8 warps goes through the chunks as they land (two pieces per thread and chunk) and keeps a
-// running maximum and sum, the CTAs exchange theirs, and a second walk over the same slots writes the
-// gradient and frees the slots one by one.  Two groups take alternate rows: while one waits for the
-// other CTAs, or writes, the other one's chunks arrive and are summed.
-constexpr int kLossGroups = 2;
-constexpr int kLossWorkers = 256;                          // threads of a group
-constexpr int kLossThreads = kLossGroups * kLossWorkers + 32;
-constexpr int kLossChunk = 32 * kLossWorkers;              // bytes: two pieces per thread
-constexpr int kLossRing = 26;
-constexpr int kLossMostChunks = 18;                        // of one row in one CTA: the rest is ahead
-constexpr uint32_t kLossHead = 1280;
+// ---- longer rows.  A cluster of `split` CTAs takes a row; each goes through a slice of its 16-byte
+// pieces in chunks that a producer warp fetches into a ring of slots by bulk copies.  256 threads sum
+// the chunks as they land (four pieces per thread), the CTAs exchange their maxima and sums, and a
+// second walk writes the gradient: first over the slice's last kLossKept chunks, which have stayed in
+// their slots, then over the others, last to first, which the producer has fetched again -- from the
+// L2 cache: what was read last is needed first, and the host splits rows so that all slices in flight
+// fit it.  Two CTAs per SM: one sums while the other one writes or waits.
+constexpr int kLossWorkers = 256;
+constexpr int kLossWarps = kLossWorkers / 32;
+constexpr int kLossThreads = kLossWorkers + 32;
+constexpr int kLossPieces = 4;                              // per thread and chunk
+constexpr int kLossChunk = 16 * kLossPieces * kLossWorkers; // 16 KB
+constexpr int kLossRing = 6;
+constexpr int kLossKept = 4;
+constexpr int kLossBlocksPerSm = 2;
+constexpr uint32_t kLossHead = 512;
 constexpr uint32_t kLossSmem = kLossHead + kLossRing * kLossChunk;
 
 struct RowSpan {
@@ -181,6 +175,7 @@ struct RowSpan {
   int pieces;                // whole pieces of the row
   int p0, n;                 // this CTA's pieces
 };
+__device__ __forceinline__ void loss_workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kLossWorkers) : "memory"); }
 template <typename T> __device__ __forceinline__ RowSpan row_span(const LossParams& P, long long row, int rank) {
   constexpr int E = 16 / (int)sizeof(T);
   RowSpan r;
@@ -230,147 +225,157 @@ __device__ __forceinline__ void piece_values(uint4 u, float (&v)[8]) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads, 1) cross_entropy_ring_kernel(const LossParams P) {
+__global__ void __launch_bounds__(kLossThreads, kLossBlocksPerSm) cross_entropy_ring_kernel(const LossParams P) {
   constexpr bool FAST = sizeof(T) == 2;
   constexpr int E = 16 / (int)sizeof(T);
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t bars = smem_u32(smem), ring = bars + kLossHead;
   auto full = [&](int s) { return bars + 8u * s; };
-  auto empty = [&](int s) { return bars + 256u + 8u * s; };
-  auto heard = [&](int b) { return bars + 512u + 8u * b; };            // [group][2]
-  float2* const told = reinterpret_cast<float2*>(smem + 576);          // [group][2][8]: statistics of the ranks
-  float2* const warp_stat = reinterpret_cast<float2*>(smem + 896);     // [group][8]
+  auto empty = [&](int s) { return bars + 64u + 8u * s; };
+  auto heard = [&](int b) { return bars + 128u + 8u * b; };
+  float2* const told = reinterpret_cast<float2*>(smem + 144);          // [2][8]: statistics of the ranks
+  float2* const warp_stat = reinterpret_cast<float2*>(smem + 288);     // [8]
   const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;
   const long long first = blockIdx.x / (unsigned)P.split, step = gridDim.x / (unsigned)P.split;
-  const int lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kLossRing; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kLossWorkers); }
-    for (int b = 0; b < 2 * kLossGroups; ++b) mbar_init(heard(b), 1);
+  const int thread = threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (thread == 0) {
+    for (int s = 0; s < kLossRing; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kLossWarps); }
+    for (int b = 0; b < 2; ++b) mbar_init(heard(b), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
   if (P.split > 1) cluster_sync();                         // barriers exist before a peer uses them
 
-  if (threadIdx.x >= kLossGroups * kLossWorkers) {
+  int slot = 0;                                            // next slot of the ring and its phase
+  uint32_t phase = 0;
+  auto advance = [&] { if (++slot == kLossRing) { slot = 0; phase ^= 1; } };
+  if (thread >= kLossWorkers) {
     // ------------------------------------------------------------------ producer
     if (lane == 0) {
-      int n = 0, slot = 0;
-      uint32_t round = 0;
+      int filled = 0;
       bool ok = true;
       for (long long row = first; row < P.rows && ok; row += step) {
         const RowSpan r = row_span<T>(P, row, rank);
-        const char* src = reinterpret_cast<const char*>(static_cast<const T*>(P.logits) + row * P.ld + r.a0) + 16ll * r.p0;
-        for (int left = 16 * r.n; left > 0; left -= kLossChunk, src += kLossChunk) {
-          if (n >= kLossRing) ok = mbar_wait_bounded(empty(slot), round ^ 1, P.status);
+        const char* const src = reinterpret_cast<const char*>(static_cast<const T*>(P.logits) + row * P.ld + r.a0) + 16ll * r.p0;
+        const int chunks = (16 * r.n + kLossChunk - 1) / kLossChunk, again = P.dlogits ? chunks - kLossKept : 0;
+        for (int i = 0; i < chunks + (again > 0 ? again : 0) && ok; ++i) {
+          const int c = i < chunks ? i : again - 1 - (i - chunks);
+          if (filled == kLossRing) ok = mbar_wait_bounded(empty(slot), phase ^ 1, P.status);
+          else ++filled;
           if (!ok) break;
+          const int left = 16 * r.n - c * kLossChunk;
           const uint32_t bytes = left < kLossChunk ? left : kLossChunk;
           mbar_arrive_expect_tx(full(slot), bytes);
-          bulk_load_row(ring + slot * kLossChunk, src, bytes, full(slot));
-          if (n < kLossRing) ++n;
-          if (++slot == kLossRing) { slot = 0; round ^= 1; }
+          bulk_load_row(ring + slot * kLossChunk, src + (long long)c * kLossChunk, bytes, full(slot));
+          advance();
         }
       }
       if (!ok)                                             // copies requested into this CTA's memory land first
-        for (int j = 0; j < kLossRing; ++j) {
-          const int s = (slot + j) % kLossRing;
-          mbar_wait_bounded(full(s), s >= slot ? round ^ 1 : round, P.status);
-        }
+        for (int j = 0; j < kLossRing; ++j) { mbar_wait_bounded(full(slot), phase ^ 1, P.status); advance(); }
     }
     __syncwarp();
   } else {
-    // ------------------------------------------------------------------ two groups of 8 warps
-    const int group = threadIdx.x / kLossWorkers, thread = threadIdx.x % kLossWorkers, warp = thread >> 5;
-    auto group_sync = [&] { asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(kLossWorkers) : "memory"); };
-    int slot = 0, turn = 0;
-    uint32_t round = 0;
-    auto advance = [&](int& s, uint32_t& rd, int by) {
-      s += by;
-      while (s >= kLossRing) { s -= kLossRing; rd ^= 1; }
-    };
-    auto chunks_of = [&](const RowSpan& r) { return (r.n + 2 * kLossWorkers - 1) / (2 * kLossWorkers); };
+    // ------------------------------------------------------------------ 8 worker warps
     bool ok = true;
-    long long row = first + group * step;
-    if (group == 1 && first < P.rows) advance(slot, round, chunks_of(row_span<T>(P, first, rank)));
     RowAhead<T> ahead;
-    ahead.ask(P, row, rank, thread);
-    for (; row < P.rows; row += kLossGroups * step, ++turn) {
+    ahead.ask(P, first, rank, thread);
+    int turn = 0;
+    for (long long row = first; row < P.rows; row += step, ++turn) {
       const RowSpan r = row_span<T>(P, row, rank);
       const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
-      const int chunks = chunks_of(r);
+      const int chunks = (r.n + kLossPieces * kLossWorkers - 1) / (kLossPieces * kLossWorkers);
+      const int again = P.dlogits && chunks > kLossKept ? chunks - kLossKept : 0;      // chunks that are fetched twice
       const RowAhead<T> now = ahead;
       const long long t = now.t;
       const float w = P.scale * now.weight;
+      // of the pieces of a slice, this thread's part in chunk c, and the slot's values
+      auto left_in = [&](int c) { return r.n - c * kLossPieces * kLossWorkers - thread; };
+      auto pieces_in = [&](int s) { return reinterpret_cast<const uint4*>(smem + kLossHead + s * kLossChunk) + thread; };
+      auto release = [&](int s) {
+        __syncwarp();                                      // one arrival per warp: they are serialised
+        if (lane == 0) mbar_arrive(empty(s));
+      };
 
       Shift<FAST> e;
       float m = now.own == now.own ? now.own : -INFINITY;
       e.set(m);
-      Two s01 = two(now.at >= 0 && now.own != -INFINITY ? 1.0f + (now.own - now.own) : 0.0f, 0.0f);
-      int sl = slot;
-      uint32_t rd = round;
+      Two s01 = two(now.at >= 0 && now.own != -INFINITY ? 1.0f + (now.own - now.own) : 0.0f, 0.0f), s23 = two(0.0f, 0.0f);
+      // the target's place: chunk and element of the slice, if it is in a whole piece of this CTA's
+      const int ti = target_inside(P, t) ? (int)t - r.a0 - r.p0 * E : -1;
+      const bool mine = ti >= 0 && ti < r.n * E;
+      float xt = 0.0f;                                     // of thread 0
+      if (thread == 0 && rank == 0 && target_inside(P, t) && ((int)t < r.a0 || (int)t >= r.a0 + r.pieces * E)) xt = to_f32(x[t]);
+      const bool owns = rank == 0 ? (mine || !target_inside(P, t) || (int)t < r.a0 || (int)t >= r.a0 + r.pieces * E) : mine;
+      int kept_slot = 0;                                   // slot of the first chunk that stays
       for (int c = 0; c < chunks; ++c) {
-        ok = ok && mbar_wait_bounded(full(sl), rd, P.status);
-        const int piece = c * 2 * kLossWorkers + thread;
-        const uint4* const p = reinterpret_cast<const uint4*>(smem + kLossHead + sl * kLossChunk) + thread;
-        if (ok && piece < r.n) {
-          const bool both = piece + kLossWorkers < r.n;
-          const uint4 u = p[0], u2 = both ? p[kLossWorkers] : u;
-          float v[E], v2[E];
-          const float top = fmaxf(piece_max(u, v), piece_max(u2, v2));
+        ok = ok && mbar_wait_bounded(full(slot), phase, P.status);
+        const int left = left_in(c);
+        const uint4* const p = pieces_in(slot);
+        if (ok && left > 0) {
+          uint4 u[kLossPieces];
+#pragma unroll
+          for (int h = 0; h < kLossPieces; ++h) u[h] = p[h * kLossWorkers < left ? h * kLossWorkers : 0];
+          float v[E];
+          float top = piece_max(u[0], v);
+#pragma unroll
+          for (int h = 1; h < kLossPieces; ++h) top = fmaxf(top, piece_max(u[h], v));
           if (top > m) {
             const float before = m;
             m = top;
             e.set(m);
-            if (before != -INFINITY) { const float k = e(before); s01 = s01 * two(k, k); }   // else s is 0 or NaN
+            if (before != -INFINITY) {                     // else the sums are 0 or NaN
+              const float k = e(before);
+              s01 = s01 * two(k, k);
+              s23 = s23 * two(k, k);
+            }
           }
-          piece_values(u, v);
+          // whole chunks without a branch between the pieces: their latencies overlap
+          auto add = [&](uint4 piece) {
+            piece_values(piece, v);
 #pragma unroll
-          for (int i = 0; i < E; i += 2) s01 = s01 + e(v[i], v[i + 1]);
-          if (both) {
-            piece_values(u2, v2);
+            for (int i = 0; i < E; i += 4) {
+              s01 = s01 + e(v[i], v[i + 1]);
+              s23 = s23 + e(v[i + 2], v[i + 3]);
+            }
+          };
+          if ((kLossPieces - 1) * kLossWorkers < left) {
 #pragma unroll
-            for (int i = 0; i < E; i += 2) s01 = s01 + e(v2[i], v2[i + 1]);
+            for (int h = 0; h < kLossPieces; ++h) add(u[h]);
+          } else {
+#pragma unroll
+            for (int h = 0; h < kLossPieces; ++h)
+              if (h * kLossWorkers < left) add(u[h]);
           }
         }
-        advance(sl, rd, 1);
+        if (thread == 0 && mine && ti / (kLossChunk / (int)sizeof(T)) == c)
+          xt = to_f32(reinterpret_cast<const T*>(smem + kLossHead + slot * kLossChunk)[ti % (kLossChunk / (int)sizeof(T))]);
+        if (c == again) kept_slot = slot;
+        if (c < again || !P.dlogits) release(slot);
+        advance();
       }
       float s, s1;
-      apart(s01, s, s1);
+      apart(s01 + s23, s, s1);
       s += s1;
-      // the target's logit, before anything of the row may be overwritten, and whether this CTA has it
-      bool owns = rank == 0;
-      float xt = 0.0f;
-      if (thread == 0 && target_inside(P, t)) {
-        const int i = (int)t - r.a0;
-        if (i < 0 || i >= r.pieces * E) {
-          if (owns) xt = to_f32(x[t]);
-        } else {
-          const int piece = i / E - r.p0;
-          owns = piece >= 0 && piece < r.n;
-          if (owns) {
-            int at = slot;
-            uint32_t unused = 0;
-            advance(at, unused, piece / (2 * kLossWorkers));
-            xt = to_f32(reinterpret_cast<const T*>(smem + kLossHead + at * kLossChunk)[piece % (2 * kLossWorkers) * E + i % E]);
-          }
-        }
-      }
-      ahead.ask(P, row + kLossGroups * step, rank, thread);
+      ahead.ask(P, row + step, rank, thread);
       // statistics of the warp, the CTA, the row: every thread ends with the same bits
       float wm = m;
       for (int d = 16; d > 0; d >>= 1) wm = fmaxf(wm, __shfl_xor_sync(~0u, wm, d));
       if (wm != -INFINITY && m != -INFINITY) s *= expf(m - wm);
       for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-      if (lane == 0) warp_stat[group * 8 + warp] = make_float2(wm, s);
-      group_sync();
-      const float2 st = warp_stat[group * 8 + (lane & 7)];
-      float top = st.x;
-      for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-      float sum = st.x == -INFINITY ? st.y : st.y * expf(st.x - top);
-      for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+      if (lane == 0) warp_stat[warp] = make_float2(wm, s);
+      loss_workers_sync();
+      auto join = [&](float2 st, float& top, float& sum) { // over eight lanes
+        top = st.x;
+        for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        sum = st.x == -INFINITY ? st.y : st.y * expf(st.x - top);
+        for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+      };
+      float top, sum;
+      join(warp_stat[lane & 7], top, sum);
       if (P.split > 1) {
-        // to every rank; two sets per group: a peer's group is one of its rows ahead at most
-        const int b = 2 * group + (turn & 1);
+        // to every rank; two sets: a peer is one row ahead at most
+        const int b = turn & 1;
         if (thread == 0) mbar_arrive_expect_tx(heard(b), 8u * P.split);
         if (thread < P.split)
           asm volatile(
@@ -381,110 +386,72 @@ __global__ void __launch_bounds__(kLossThreads, 1) cross_entropy_ring_kernel(con
               "r"(heard(b)), "r"(thread), "f"(top), "f"(sum)
               : "memory");
         ok = mbar_wait_bounded(heard(b), (turn >> 1) & 1, P.status) && ok;
-        const float2 all = (lane & 7) < P.split ? told[b * 8 + (lane & 7)] : make_float2(-INFINITY, 0.0f);
-        top = all.x;
-        for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        sum = all.x == -INFINITY ? all.y : all.y * expf(all.x - top);
-        for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+        join((lane & 7) < P.split ? told[b * 8 + (lane & 7)] : make_float2(-INFINITY, 0.0f), top, sum);
       }
       const RowOutcome o = row_outcome(P, top, sum, xt, t, w);
       if (thread == 0) {
         if (rank == 0) { report_target(P, t, w); if (P.lse) P.lse[row] = o.lse; }
         if (owns && P.loss) P.loss[row] = o.loss;
       }
-      e.set(top);
-      const float k = w / sum;
-      T* const d = static_cast<T*>(P.dlogits) + row * P.ld_d;
-      const bool wide = (uintptr_t)(d + r.a0) % 16 == 0;
-      if (P.dlogits && now.at >= 0) d[now.at] = from_f32<T>(o.zero ? 0.0f : e(now.own) * k - (now.at == t ? w : 0.0f));
-      for (int c = 0; c < chunks; ++c) {
-        const uint4* const p = reinterpret_cast<const uint4*>(smem + kLossHead + slot * kLossChunk) + thread;
-        const int piece = c * 2 * kLossWorkers + thread;
-        if (P.dlogits) {
+      if (P.dlogits) {
+        e.set(top);
+        const float k = w / sum;
+        T* const d = static_cast<T*>(P.dlogits) + row * P.ld_d;
+        const bool wide = (uintptr_t)(d + r.a0) % 16 == 0;
+        if (now.at >= 0) d[now.at] = from_f32<T>(o.zero ? 0.0f : e(now.own) * k - (now.at == t ? w : 0.0f));
+        for (int i = 0; i < chunks; ++i) {
+          // kept chunks, oldest first, then those that come again
+          const bool kept = i < chunks - again;
+          const int c = kept ? again + i : chunks - 1 - i, sl = kept ? kept_slot : slot;
+          if (!kept) ok = ok && mbar_wait_bounded(full(slot), phase, P.status);
+          const int left = left_in(c);
+          const uint4* const p = pieces_in(sl);
+          if (left > 0 && ok) {
+            const int c0 = r.a0 + (r.p0 + c * kLossPieces * kLossWorkers + thread) * E;
+            T* const dc = d + c0;
+            auto gradient = [&](uint4 piece, float (&v)[E]) {
+              piece_values(piece, v);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (piece + h * kLossWorkers >= r.n) break;
-            float v[E];
-            piece_values(p[h * kLossWorkers], v);
-            const int c0 = r.a0 + (r.p0 + piece + h * kLossWorkers) * E;
-            const unsigned hit = (unsigned)((int)t - c0);  // t is inside the vocabulary, or o.zero
-            if (o.zero) {
+              for (int j = 0; j < E; j += 2) apart(e(v[j], v[j + 1]) * two(k, k), v[j], v[j + 1]);
+            };
+            if (wide && !o.zero && (kLossPieces - 1) * kLossWorkers < left) {
+              uint4 u[kLossPieces];
 #pragma unroll
-              for (int i = 0; i < E; ++i) v[i] = 0.0f;
+              for (int h = 0; h < kLossPieces; ++h) u[h] = p[h * kLossWorkers];
+#pragma unroll
+              for (int h = 0; h < kLossPieces; ++h) {
+                float v[E];
+                gradient(u[h], v);
+                ThetaTraits<T>::stg(dc + h * kLossWorkers * E, v);
+              }
             } else {
+              for (int h = 0; h * kLossWorkers < left && h < kLossPieces; ++h) {
+                float v[E] = {};
+                if (!o.zero) gradient(p[h * kLossWorkers], v);
+                if (wide) ThetaTraits<T>::stg(dc + h * kLossWorkers * E, v);
+                else {
 #pragma unroll
-              for (int i = 0; i < E; i += 2) apart(e(v[i], v[i + 1]) * two(k, k), v[i], v[i + 1]);
-              if (hit < E) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) v[i] -= (int)hit == i ? w : 0.0f;
+                  for (int j = 0; j < E; ++j) dc[h * kLossWorkers * E + j] = from_f32<T>(v[j]);
+                }
               }
             }
-            if (wide) ThetaTraits<T>::stg(d + c0, v);
-            else {
-#pragma unroll
-              for (int i = 0; i < E; ++i) d[c0 + i] = from_f32<T>(v[i]);
+            // the target: the thread that has just stored its piece stores it once more
+            const int off = mine ? ti - c * (kLossChunk / (int)sizeof(T)) : -1;
+            if (off >= 0 && off < kLossChunk / (int)sizeof(T) && off / E % kLossWorkers == thread && !o.zero) {
+              const float y = to_f32(reinterpret_cast<const T*>(smem + kLossHead + sl * kLossChunk)[off]);
+              d[t] = from_f32<T>(e(y) * k - w);
             }
           }
+          release(sl);
+          if (kept) { if (++kept_slot == kLossRing) kept_slot = 0; }
+          else advance();
         }
-        mbar_arrive(empty(slot));
-        advance(slot, round, 1);
       }
-      // past the other group's next row
-      if (row + step < P.rows) advance(slot, round, chunks_of(row_span<T>(P, row + step, rank)));
-      group_sync();                                        // warp_stat may be written again
+      loss_workers_sync();                                 // warp_stat may be written again
     }
   }
   __syncwarp();
   if (P.split > 1) cluster_sync();                         // no peer writes to a CTA that has ended
-}
-
-// ---- rows longer than that: read twice, one block per row
-template <typename T>
-__global__ void __launch_bounds__(512) cross_entropy_twice_kernel(const LossParams P) {
-  constexpr bool FAST = sizeof(T) == 2;
-  __shared__ float2 stat[16];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (long long row = blockIdx.x; row < P.rows; row += gridDim.x) {
-    const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
-    float m = -INFINITY, s = 0.0f;
-    Shift<FAST> e;
-    e.set(m);
-#pragma unroll 4
-    for (long long v = threadIdx.x; v < P.vocab; v += 512) {
-      const float y = to_f32(x[v]);
-      if (y > m) {
-        s *= m == -INFINITY ? 1.0f : expf(m - y);
-        m = y;
-        e.set(m);
-      }
-      s += e(y);
-    }
-    for (int d = 16; d > 0; d >>= 1) {
-      const float m2 = __shfl_xor_sync(~0u, m, d), s2 = __shfl_xor_sync(~0u, s, d);
-      softmax_merge(m, s, m2, s2);
-    }
-    if (lane == 0) stat[warp] = make_float2(m, s);
-    __syncthreads();
-    m = stat[0].x; s = stat[0].y;
-    for (int i = 1; i < 16; ++i) softmax_merge(m, s, stat[i].x, stat[i].y);
-    const long long t = P.targets[row];
-    const float w = P.scale * (P.row_weight ? P.row_weight[row] : 1.0f);
-    const float xt = target_inside(P, t) ? to_f32(x[t]) : 0.0f;
-    __syncthreads();                                       // dlogits may be the logits
-    const RowOutcome o = row_outcome(P, m, s, xt, t, w);
-    if (threadIdx.x == 0) {
-      report_target(P, t, w);
-      if (P.loss) P.loss[row] = o.loss;
-      if (P.lse) P.lse[row] = o.lse;
-    }
-    if (!P.dlogits) continue;
-    T* const d = static_cast<T*>(P.dlogits) + row * P.ld_d;
-    e.set(m);
-    const float k = w / s;
-#pragma unroll 4
-    for (long long v = threadIdx.x; v < P.vocab; v += 512)
-      d[v] = from_f32<T>(o.zero ? 0.0f : e(to_f32(x[v])) * k - (v == t ? w : 0.0f));
-  }
 }
 
 }  // namespace

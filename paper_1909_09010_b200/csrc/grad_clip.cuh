@@ -176,7 +176,7 @@ template <bool UP> __device__ __forceinline__ void clip_produce(const ClipParams
 __device__ __forceinline__ void clip_prologue(unsigned char* smem) {
   if (threadIdx.x == 0) {
     const uint32_t bars = smem_u32(smem);
-    for (int r = 0; r < kClipRing; ++r) { mbar_init(bars + 8 * r, 1); mbar_init(bars + 64 + 8 * r, kClipWorkers); }
+    for (int r = 0; r < kClipRing; ++r) { mbar_init(bars + 8 * r, 1); mbar_init(bars + 64 + 8 * r, kClipWorkers / 32); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_norm_kern
           for (int j = 0; j < 4; ++j) u[j] = k + j * kClipWorkers < pieces ? p[k + j * kClipWorkers] : make_uint4(0, 0, 0, 0);
           s0 += w.t.dtype == GBMUF_F32 ? square_sum<true>(u) : square_sum<false>(u);
         }
-      mbar_arrive(bars + 64 + 8 * slot);
+      __syncwarp();                              // one arrival per warp: they are serialised
+      if ((threadIdx.x & 31) == 0) mbar_arrive(bars + 64 + 8 * slot);
       ++n;
     }
     const long long rest = (s.e1 - s.e0) - (s.a1 - s.a0);
@@ -322,7 +323,8 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_scale_ker
           each([&](int k, float (&v)[4]) { ThetaTraits<__nv_bfloat16>::lds_quad(x + k, v); }, [&](int k) { return to_f32(x[k]); });
         }
       }
-      mbar_arrive(bars + 64 + 8 * slot);
+      __syncwarp();                              // one arrival per warp: they are serialised
+      if ((threadIdx.x & 31) == 0) mbar_arrive(bars + 64 + 8 * slot);
       ++n;
     }
     const long long rest = (s.e1 - s.e0) - (s.a1 - s.a0);

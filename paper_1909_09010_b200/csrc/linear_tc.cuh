@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), 32 * kTcFinishers); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), kTcFinishers); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -243,7 +243,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          mbar_arrive(acc_empty(n & 1));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
         }
         if (!ok) break;
 #pragma unroll
@@ -274,7 +275,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          mbar_arrive(acc_empty(n & 1));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
           ++n;
         }
       }
@@ -304,7 +306,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          mbar_arrive(acc_empty(n & 1));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
         }
       }
     }

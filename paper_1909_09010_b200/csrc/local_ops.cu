@@ -342,6 +342,8 @@ cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t 
              : cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, false>, dz, ld, R, C, out, (int)a->accumulate);
 }
 
+constexpr long long kLossCacheBytes = 64ll << 20;   // of the 126 MB: the gradient passes through as well
+
 template <typename T>
 cudaLaunchConfig_t loss_config(int split, int clusters, cudaLaunchAttribute* attr, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
@@ -356,15 +358,15 @@ template <typename T> cudaError_t prepare_loss(gbmuf_ops* ops, int (&clusters)[4
   cudaError_t e = cudaFuncSetAttribute((const void*)cross_entropy_ring_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLossSmem);
   for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = loss_config<T>(1 << i, ops->num_sms >> i, &attr, nullptr);
+    const cudaLaunchConfig_t cfg = loss_config<T>(1 << i, (ops->num_sms * kLossBlocksPerSm) >> i, &attr, nullptr);
     e = cudaOccupancyMaxActiveClusters(&clusters[i], cross_entropy_ring_kernel<T>, &cfg);
     if (clusters[i] < 1) clusters[i] = 1;
   }
   return e;
 }
 
-// Short rows: a warp each.  Rows of up to 8 x 147 KB: in the shared memory of as few CTAs as hold
-// them, or of more where there are too few rows for all SMs.  Longer ones are read twice.
+// Short rows: a warp each.  Longer ones: a cluster of CTAs each, of more CTAs where there are too few
+// rows to fill the GPU, or where the slices that are fetched twice would not fit the L2 cache.
 template <typename T> cudaError_t launch_loss(const gbmuf_ops* ops, LossParams& P, cudaStream_t st) {
   if (P.vocab <= kWarpVocab) {
     const unsigned grid = (unsigned)((P.rows + 3) / 4);
@@ -373,14 +375,14 @@ template <typename T> cudaError_t launch_loss(const gbmuf_ops* ops, LossParams& 
     else cross_entropy_warp_kernel<T, kWarpRegs><<<grid, 128, 0, st>>>(P);
     return cudaGetLastError();
   }
-  const long long pieces = (P.vocab * (long long)sizeof(T) + 15) / 16, most = (long long)kLossMostChunks * kLossChunk / 16;
+  const long long bytes = P.vocab * (long long)sizeof(T), ctas = (long long)ops->num_sms * kLossBlocksPerSm;
   int log = 0;
-  while (log < 3 && (pieces >> log) > most - 1) ++log;
-  if ((pieces >> log) > most - 1) {
-    cross_entropy_twice_kernel<T><<<(unsigned)std::min<long long>(P.rows, ops->num_sms * 4), 512, 0, st>>>(P);
-    return cudaGetLastError();
+  while (log < 3) {
+    const long long twice = (bytes - ((long long)kLossKept * kLossChunk << log)) * (ctas >> log);
+    const bool few = P.rows << (log + 1) <= ctas && bytes >> (log + 1) >= kLossChunk / 2;
+    if (!few && twice < kLossCacheBytes) break;
+    ++log;
   }
-  while (log < 3 && P.rows << (log + 1) <= ops->num_sms && (pieces >> log) >= 2 * kLossChunk / 16) ++log;
   P.split = 1 << log;
   cudaLaunchAttribute attr;
   const int clusters = (int)std::min<long long>(P.rows, ops->loss_clusters[sizeof(T) == 2][log]);
