@@ -165,10 +165,22 @@ constexpr int kLossThreads = kLossWorkers + 32;
 constexpr int kLossPieces = 4;                              // per thread and chunk
 constexpr int kLossChunk = 16 * kLossPieces * kLossWorkers; // 16 KB
 constexpr int kLossRing = 6;
-constexpr int kLossKept = 4;
+constexpr int kLossKept = 5;
 constexpr int kLossBlocksPerSm = 2;
 constexpr uint32_t kLossHead = 512;
 constexpr uint32_t kLossSmem = kLossHead + kLossRing * kLossChunk;
+
+// A bulk copy that says whether its source will be fetched again soon: the L2 cache then keeps it
+// rather than the gradient that passes through (2,048 x 267,735 bf16: 464 -> 422 us).
+__device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, bool again) {
+  uint64_t keep, pass;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pass));
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar), "l"(again ? keep : pass)
+      : "memory");
+}
 
 struct RowSpan {
   int a0;                    // elements before the first whole piece
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(kLossThreads, kLossBlocksPerSm) cross_entropy_
           const int left = 16 * r.n - c * kLossChunk;
           const uint32_t bytes = left < kLossChunk ? left : kLossChunk;
           mbar_arrive_expect_tx(full(slot), bytes);
-          bulk_load_row(ring + slot * kLossChunk, src + (long long)c * kLossChunk, bytes, full(slot));
+          bulk_load_hint(ring + slot * kLossChunk, src + (long long)c * kLossChunk, bytes, full(slot), c < again && i < chunks);
           advance();
         }
       }
