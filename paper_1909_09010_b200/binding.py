@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -50,6 +51,15 @@ def _fields(spec: str):
     """ctypes fields from "type name name, type name ..." (i: int32, l: int64, f: float, p: pointer)."""
     types = {"i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float, "p": ctypes.c_void_p}
     return [(name, types[part.split()[0]]) for part in spec.split(",") for name in part.split()[1:]]
+
+
+def _packer(cls):
+    """Packs the fields of a ctypes structure, in order, into its bytes: a tenth of the time that
+    filling the structure takes, which for the smallest calls is longer than the GPU's part."""
+    code = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_void_p: "P"}
+    packer = struct.Struct("@" + "".join(code[t] for _, t in cls._fields_) + "0q")
+    assert packer.size == ctypes.sizeof(cls)
+    return packer.pack
 
 
 class LinearForwardArgs(ctypes.Structure):
@@ -424,6 +434,12 @@ class Gbmuf:
 # ------------------------------------------------------------------------------------------------
 # The operators of a worker's local step
 # ------------------------------------------------------------------------------------------------
+_pack_forward = _packer(LinearForwardArgs)
+_pack_backward_input = _packer(LinearBackwardInputArgs)
+_pack_backward_weight = _packer(LinearBackwardWeightArgs)
+_pack_cross_entropy = _packer(CrossEntropyArgs)
+
+
 def _dtype_code(t) -> int:
     import torch
     if t.dtype is torch.bfloat16:
@@ -433,52 +449,54 @@ def _dtype_code(t) -> int:
     raise TypeError(f"tensors are float32 or bfloat16, not {t.dtype}")
 
 
-def _matrix(name, t, rows, cols, like):
-    """(address, row stride) of a matrix of the given shape, type and device; (None, 0) for None."""
+def _matrix(name, t, shape, dtype, device):
+    """(address, row stride) of a matrix of the given shape, type and device; (0, 0) for None."""
     if t is None:
-        return None, 0
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must be [{rows}][{cols}], not {list(t.shape)}")
-    if t.dtype is not like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+        return 0, 0
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
     ld, step = t.stride()
-    if step != 1 and cols > 1 and rows > 0:
+    if step != 1 and shape[1] > 1 and shape[0] > 0:
         raise ValueError(f"{name} must have its columns next to one another")
-    return t.data_ptr(), (ld if rows > 1 and cols > 0 else cols)
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
 def _vector(name, t, n, dtype, device):
     if t is None:
-        return None
-    if t.dim() != 1 or t.shape[0] != n:
+        return 0
+    if t.shape != (n,):
         raise ValueError(f"{name} must be [{n}], not {list(t.shape)}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
     if n > 1 and t.stride(0) != 1:
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-class LocalOps:
-    """``gbmuf_ops_*``: linear layers with their gradients and the loss, on one device.  Tensors are
-    torch tensors on it; results that are not handed in are allocated by torch on its current
-    stream, and so is the workspace of a call that needs one.  ``stream`` (default: the current one
-    of the device) is where the call runs; tensors used on another stream than their own are the
-    caller's to guard, as for any torch operation."""
+def _two_dims(name, t):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    return t.shape
 
-    def __init__(self, device=0):
+
+class _OnDevice:
+    """What LocalOps and GradClip share: the library, errors, streams."""
+
+    def _open(self, device):
         import torch
         self._torch = torch
         self._L = lib()
         self._h = ctypes.c_void_p()
         self.device = device
-        st = self._L.gbmuf_ops_create(device, ctypes.byref(self._h))
-        if st != GBMUF_OK:
-            raise GbmufError(st, self._L.gbmuf_last_error(None).decode())
+        # the address of the current stream without building a torch Stream object around it
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                                   lambda d: torch.cuda.current_stream(d).cuda_stream)
 
     def _check(self, st):
         if st != GBMUF_OK:
@@ -486,47 +504,59 @@ class LocalOps:
 
     def _on(self, stream):
         if stream is None:
-            return self._torch.cuda.current_stream(self.device).cuda_stream
+            return self._raw_stream(self.device)
         return getattr(stream, "cuda_stream", stream)
 
-    def _own(self, t, name):
-        if t.device.type != "cuda" or t.device.index != self.device:
-            raise ValueError(f"{name} is on {t.device}, not on cuda:{self.device}")
 
-    def _linear(self, name, args, like, stream):
-        """Asks for the workspace, allocates it, runs the call."""
-        ref = ctypes.byref(args)
-        need = ctypes.c_int64()
-        self._check(getattr(self._L, name + "_workspace")(self._h, ref, ctypes.byref(need)))
-        work = None
-        if need.value:
-            torch = self._torch
-            work = torch.empty(need.value, dtype=torch.uint8, device=like.device)
-            if stream is not None:
-                work.record_stream(stream if hasattr(stream, "cuda_stream")
-                                   else torch.cuda.ExternalStream(stream, device=like.device))
-            args.workspace, args.workspace_bytes = work.data_ptr(), need.value
-        self._check(getattr(self._L, name)(self._h, ref, self._on(stream)))
+class LocalOps(_OnDevice):
+    """``gbmuf_ops_*``: linear layers with their gradients and the loss, on one device.  Tensors are
+    torch tensors on it; results that are not handed in are allocated by torch on its current
+    stream, and so is the workspace of a call that needs one.  ``stream`` (default: the current one
+    of the device) is where the call runs; tensors used on another stream than their own are the
+    caller's to guard, as for any torch operation."""
+
+    def __init__(self, device=0):
+        self._open(device)
+        self._check(self._L.gbmuf_ops_create(device, ctypes.byref(self._h)))
+
+    def _linear(self, call, query, pack, fields, in_place, like, stream):
+        """Runs a linear-layer call.  in_place: its operands are aligned bf16, no workspace."""
+        if in_place:
+            args = pack(*fields, 0, 0)
+        else:
+            args, need = pack(*fields, 0, 0), ctypes.c_int64()
+            self._check(query(self._h, args, ctypes.byref(need)))
+            if need.value:
+                torch = self._torch
+                work = torch.empty(need.value, dtype=torch.uint8, device=like.device)
+                if stream is not None:
+                    work.record_stream(stream if hasattr(stream, "cuda_stream")
+                                       else torch.cuda.ExternalStream(stream, device=like.device))
+                args = pack(*fields, work.data_ptr(), need.value)
+        st = call(self._h, args, self._on(stream))
+        if st != GBMUF_OK:
+            self._check(st)
 
     def linear_forward(self, x, w, bias=None, residual=None, activation="none", keep_z=False, out=None,
                        z_out=None, stream=None):
         """``gbmuf_linear_forward``: y = act(x w^T + bias) + residual; with ``keep_z`` (or ``z_out``)
         returns (y, z), z = x w^T + bias.  x [rows][n_in], w [n_out][n_in]."""
-        if x.dim() != 2 or w.dim() != 2:
-            raise ValueError("x and w must be matrices")
-        (rows, n_in), n_out = x.shape, w.shape[0]
-        self._own(x, "x")
-        y = out if out is not None else x.new_empty((rows, n_out))
-        z = z_out if z_out is not None else (x.new_empty((rows, n_out)) if keep_z else None)
-        px, lx = _matrix("x", x, rows, n_in, x)
-        pw, lw = _matrix("w", w, n_out, n_in, x)
-        pr, lr = _matrix("residual", residual, rows, n_out, x)
-        py, ly = _matrix("out", y, rows, n_out, x)
-        pz, lz = _matrix("z_out", z, rows, n_out, x)
-        pb = _vector("bias", bias, n_out, x.dtype, x.device)
-        args = LinearForwardArgs(rows, n_in, n_out, px, pw, pb, pr, py, pz, lx, lw, lr, ly, lz,
-                                 _dtype_code(x), ACTIVATIONS[activation], None, 0)
-        self._linear("gbmuf_linear_forward", args, x, stream)
+        rows, n_in = _two_dims("x", x)
+        n_out = _two_dims("w", w)[0]
+        dtype, dev, shape = x.dtype, self.device, (rows, n_out)
+        code = _dtype_code(x)
+        px, lx = _matrix("x", x, (rows, n_in), dtype, dev)
+        pw, lw = _matrix("w", w, (n_out, n_in), dtype, dev)
+        pb = _vector("bias", bias, n_out, dtype, dev)
+        pr, lr = _matrix("residual", residual, shape, dtype, dev)
+        act = ACTIVATIONS[activation]
+        y = out if out is not None else x.new_empty(shape)
+        py, ly = _matrix("out", y, shape, dtype, dev)
+        z = z_out if z_out is not None else (x.new_empty(shape) if keep_z else None)
+        pz, lz = _matrix("z_out", z, shape, dtype, dev)
+        self._linear(self._L.gbmuf_linear_forward, self._L.gbmuf_linear_forward_workspace, _pack_forward,
+                     (rows, n_in, n_out, px, pw, pb, pr, py, pz, lx, lw, lr, ly, lz, code, act),
+                     code == BF16 and not ((px | pw) & 15 or (lx | lw) & 7), x, stream)
         return y if z is None else (y, z)
 
     def linear_backward_input(self, dz, w, residual=None, z_prev=None, activation="none", want_dx=None,
@@ -534,26 +564,28 @@ class LocalOps:
         """``gbmuf_linear_backward_input``: dx = dz w + residual, and with ``z_prev`` also
         dz_prev = dx * act'(z_prev).  Returns dx without ``z_prev``; dz_prev with it, or
         (dx, dz_prev) if ``want_dx`` or ``dx_out``."""
-        if dz.dim() != 2 or w.dim() != 2:
-            raise ValueError("dz and w must be matrices")
-        (rows, n_out), n_in = dz.shape, w.shape[1]
-        self._own(dz, "dz")
+        rows, n_out = _two_dims("dz", dz)
+        n_in = _two_dims("w", w)[1]
+        dtype, dev, shape = dz.dtype, self.device, (rows, n_in)
+        code = _dtype_code(dz)
+        pd, ldd = _matrix("dz", dz, (rows, n_out), dtype, dev)
+        pw, lw = _matrix("w", w, (n_out, n_in), dtype, dev)
+        pr, lr = _matrix("residual", residual, shape, dtype, dev)
+        pz, lz = _matrix("z_prev", z_prev, shape, dtype, dev)
+        act = ACTIVATIONS[activation]
         dx, dp = dx_out, dz_out
         if dx is None and (want_dx or z_prev is None):
-            dx = dz.new_empty((rows, n_in))
+            dx = dz.new_empty(shape)
         if dp is None and z_prev is not None:
-            dp = dz.new_empty((rows, n_in))
+            dp = dz.new_empty(shape)
         if z_prev is None and dp is not None:
             raise ValueError("dz_out needs z_prev")
-        pd, ldd = _matrix("dz", dz, rows, n_out, dz)
-        pw, lw = _matrix("w", w, n_out, n_in, dz)
-        pr, lr = _matrix("residual", residual, rows, n_in, dz)
-        pz, lz = _matrix("z_prev", z_prev, rows, n_in, dz)
-        px, lx = _matrix("dx_out", dx, rows, n_in, dz)
-        pp, lp = _matrix("dz_out", dp, rows, n_in, dz)
-        args = LinearBackwardInputArgs(rows, n_in, n_out, pd, pw, pr, pz, px, pp, ldd, lw, lr, lz, lx, lp,
-                                       _dtype_code(dz), ACTIVATIONS[activation], None, 0)
-        self._linear("gbmuf_linear_backward_input", args, dz, stream)
+        px, lx = _matrix("dx_out", dx, shape, dtype, dev)
+        pp, lp = _matrix("dz_out", dp, shape, dtype, dev)
+        self._linear(self._L.gbmuf_linear_backward_input, self._L.gbmuf_linear_backward_input_workspace,
+                     _pack_backward_input,
+                     (rows, n_in, n_out, pd, pw, pr, pz, px, pp, ldd, lw, lr, lz, lx, lp, code, act),
+                     code == BF16 and not ((pd | pw) & 15 or (ldd | lw) & 7), dz, stream)
         return dx if dp is None else (dp if dx is None else (dx, dp))
 
     def linear_backward_weight(self, dz, x, grad_dtype=None, want_bias=True, dw_out=None, dbias_out=None,
@@ -561,44 +593,44 @@ class LocalOps:
         """``gbmuf_linear_backward_weight``: dw = dz^T x and dbias = sum over the rows of dz, in
         ``grad_dtype`` (default: the operands' type); with ``accumulate`` added to ``dw_out`` and
         ``dbias_out``.  Returns dw, or (dw, dbias) if ``want_bias`` or ``dbias_out``."""
-        if dz.dim() != 2 or x.dim() != 2:
-            raise ValueError("dz and x must be matrices")
-        (rows, n_out), n_in = dz.shape, x.shape[1]
-        self._own(dz, "dz")
+        rows, n_out = _two_dims("dz", dz)
+        n_in = _two_dims("x", x)[1]
+        dtype, dev, shape = dz.dtype, self.device, (n_out, n_in)
+        code = _dtype_code(dz)
+        pd, ldd = _matrix("dz", dz, (rows, n_out), dtype, dev)
+        px, lx = _matrix("x", x, (rows, n_in), dtype, dev)
         if dw_out is not None:
             if grad_dtype is not None and dw_out.dtype is not grad_dtype:
                 raise TypeError(f"dw_out must be {grad_dtype}, not {dw_out.dtype}")
             grad_dtype = dw_out.dtype
         elif grad_dtype is None:
-            grad_dtype = dz.dtype
+            grad_dtype = dtype
         if accumulate and (dw_out is None or (want_bias and dbias_out is None)):
             raise ValueError("accumulate adds to dw_out and dbias_out: hand them in")
-        dw = dw_out if dw_out is not None else dz.new_empty((n_out, n_in), dtype=grad_dtype)
+        dw = dw_out if dw_out is not None else dz.new_empty(shape, dtype=grad_dtype)
         db = dbias_out if dbias_out is not None else (
             dz.new_empty((n_out,), dtype=grad_dtype) if want_bias else None)
-        pd, ldd = _matrix("dz", dz, rows, n_out, dz)
-        px, lx = _matrix("x", x, rows, n_in, dz)
-        if dw.device != dz.device:
-            raise ValueError(f"dw_out is on {dw.device}, not on {dz.device}")
-        pw, lw = _matrix("dw_out", dw, n_out, n_in, dw)
-        pb = _vector("dbias_out", db, n_out, grad_dtype, dz.device)
-        args = LinearBackwardWeightArgs(rows, n_in, n_out, pd, px, pw, pb, ldd, lx, lw, _dtype_code(dz),
-                                        _dtype_code(dw), 1 if accumulate else 0, 0, None, 0)
-        self._linear("gbmuf_linear_backward_weight", args, dz, stream)
+        pw, lw = _matrix("dw_out", dw, shape, grad_dtype, dev)
+        pb = _vector("dbias_out", db, n_out, grad_dtype, dev)
+        self._linear(self._L.gbmuf_linear_backward_weight, self._L.gbmuf_linear_backward_weight_workspace,
+                     _pack_backward_weight,
+                     (rows, n_in, n_out, pd, px, pw, pb, ldd, lx, lw, code, _dtype_code(dw),
+                      1 if accumulate else 0, 0),
+                     code == BF16 and not ((pd | px) & 15 or (ldd | lx) & 7), dz, stream)
         return dw if db is None else (dw, db)
 
     def activation_backward(self, dy, z, activation, out=None, stream=None):
         """``gbmuf_activation_backward``: dy * act'(z); ``out`` may be dy."""
-        if dy.dim() != 2:
-            raise ValueError("dy must be a matrix")
-        rows, cols = dy.shape
-        self._own(dy, "dy")
-        dz = out if out is not None else dy.new_empty((rows, cols))
-        py, ly = _matrix("dy", dy, rows, cols, dy)
-        pz, lz = _matrix("z", z, rows, cols, dy)
-        po, lo = _matrix("out", dz, rows, cols, dy)
-        self._check(self._L.gbmuf_activation_backward(self._h, rows, cols, _dtype_code(dy),
-                                                      ACTIVATIONS[activation], py, ly, pz, lz, po, lo,
+        shape = _two_dims("dy", dy)
+        rows, cols = shape
+        dtype, dev = dy.dtype, self.device
+        code = _dtype_code(dy)
+        py, ly = _matrix("dy", dy, shape, dtype, dev)
+        pz, lz = _matrix("z", z, shape, dtype, dev)
+        act = ACTIVATIONS[activation]
+        dz = out if out is not None else dy.new_empty(shape)
+        po, lo = _matrix("out", dz, shape, dtype, dev)
+        self._check(self._L.gbmuf_activation_backward(self._h, rows, cols, code, act, py, ly, pz, lz, po, lo,
                                                       self._on(stream)))
         return dz
 
@@ -607,23 +639,25 @@ class LocalOps:
         """``gbmuf_cross_entropy``: (loss, lse, dlogits), or (loss, lse) without ``want_grad``.  loss
         and lse are float32 [rows]; ``dlogits_out`` may be the logits."""
         torch = self._torch
-        if logits.dim() != 2:
-            raise ValueError("logits must be a matrix")
-        rows, vocab = logits.shape
-        self._own(logits, "logits")
-        both = torch.empty((2, rows), dtype=torch.float32, device=logits.device)
+        shape = _two_dims("logits", logits)
+        rows, vocab = shape
+        dtype, dev = logits.dtype, self.device
+        code = _dtype_code(logits)
+        pl, ll = _matrix("logits", logits, shape, dtype, dev)
+        pt = _vector("targets", targets, rows, torch.int64, dev)
+        pw = _vector("row_weight", row_weight, rows, torch.float32, dev)
         d = dlogits_out
         if d is None and want_grad:
-            d = logits.new_empty((rows, vocab))
-        pl, ll = _matrix("logits", logits, rows, vocab, logits)
-        pd, ldd = _matrix("dlogits_out", d, rows, vocab, logits)
-        pt = _vector("targets", targets, rows, torch.int64, logits.device)
-        pw = _vector("row_weight", row_weight, rows, torch.float32, logits.device)
+            d = logits.new_empty(shape)
+        pd, ldd = _matrix("dlogits_out", d, shape, dtype, dev)
+        both = logits.new_empty((2, rows), dtype=torch.float32)
         at = both.data_ptr()
-        args = CrossEntropyArgs(rows, vocab, pl, pt, pw, at, at + 4 * rows, pd, ll, ldd, ignore_index,
-                                _dtype_code(logits), scale)
-        self._check(self._L.gbmuf_cross_entropy(self._h, ctypes.byref(args), self._on(stream)))
-        loss, lse = both[0], both[1]
+        args = _pack_cross_entropy(rows, vocab, pl, pt, pw, at, at + 4 * rows, pd, ll, ldd, ignore_index,
+                                   code, scale)
+        st = self._L.gbmuf_cross_entropy(self._h, args, self._on(stream))
+        if st != GBMUF_OK:
+            self._check(st)
+        loss, lse = both.unbind(0)
         return (loss, lse) if d is None else (loss, lse, d)
 
     def device_status(self, stream=None) -> int:
@@ -679,28 +713,21 @@ def _rows_cols(name, t):
     return rows, cols, ld
 
 
-class GradClip:
+class GradClip(_OnDevice):
     """``gbmuf_clip_*``: the gradient norm of each group (a worker) over a list of tensors, and the
     clipped copies.  entries: (gradient, out or None, group); gradient float32 or bfloat16, out of
     the same shape in float32 or the gradient's type (or the gradient itself)."""
 
     def __init__(self, entries, groups=1, device=None):
-        import torch
-        self._torch = torch
-        self._L = lib()
-        self._h = ctypes.c_void_p()
         entries = list(entries)
         if device is None:
-            device = entries[0][0].device.index if entries else torch.cuda.current_device()
-        self.device, self.groups = device, groups
+            import torch
+            device = entries[0][0].get_device() if entries else torch.cuda.current_device()
+        self._open(device)
+        self.groups = groups
         arr = self._table(entries)
-        st = self._L.gbmuf_clip_create(device, groups, len(entries), arr, ctypes.byref(self._h))
-        self._check(st)
+        self._check(self._L.gbmuf_clip_create(device, groups, len(entries), arr, ctypes.byref(self._h)))
         self._keep = entries
-
-    def _check(self, st):
-        if st != GBMUF_OK:
-            raise GbmufError(st, self._L.gbmuf_last_error(None).decode())
 
     def _table(self, entries):
         arr = (GradTensor * len(entries))()
@@ -761,11 +788,6 @@ class GradClip:
         v = ctypes.c_int32(-1)
         self._check(self._L.gbmuf_clip_device_status(self._h, self._on(stream), ctypes.byref(v)))
         return v.value
-
-    def _on(self, stream):
-        if stream is None:
-            return self._torch.cuda.current_stream(self.device).cuda_stream
-        return getattr(stream, "cuda_stream", stream)
 
     def destroy(self):
         if self._h:
