@@ -1,7 +1,7 @@
-// Matrix products on the fp32 units, for any strides.
+// Column sums, and the gradient of an activation by itself.
 // Part of libgbmuf (CUDA, sm_100a); included by local_ops.cu.
-#ifndef GBMUF_CSRC_LINEAR_SIMT_CUH
-#define GBMUF_CSRC_LINEAR_SIMT_CUH
+#ifndef GBMUF_CSRC_COLUMN_SUM_CUH
+#define GBMUF_CSRC_COLUMN_SUM_CUH
 
 namespace {
 
@@ -63,4 +63,4 @@ __global__ void __launch_bounds__(256) activation_backward_kernel(const T* dy, l
 
 }  // namespace
 
-#endif  // GBMUF_CSRC_LINEAR_SIMT_CUH
+#endif  // GBMUF_CSRC_COLUMN_SUM_CUH

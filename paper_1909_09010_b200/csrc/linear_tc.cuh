@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
-  extern __shared__ unsigned char raw[];
+  extern __shared__ __align__(128) unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const uint32_t bars = smem_u32(smem), ring = bars + kTcHead;
   auto full = [&](int s) { return bars + 8u * s; };

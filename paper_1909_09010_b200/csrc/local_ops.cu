@@ -4,7 +4,8 @@
 //   linear_epilogue.cuh  activations, and what happens to a finished sum of a matrix product
 //   linear_tc.cuh        matrix products on the tensor cores
 //   linear_pack.cuh      operands that cannot be read in place: other alignments, fp32 as bf16 parts
-//   linear_simt.cuh      matrix products on the fp32 units for any strides, column sums
+//   linear_rows.cuh      the layer for a few rows, on the fp32 units
+//   column_sum.cuh       column sums (bias gradients), gradient of an activation by itself
 //   cross_entropy.cuh    cross-entropy over a vocabulary with its gradient
 //   grad_clip.cuh        norms over many tensors and the clipped copies
 
@@ -19,6 +20,7 @@
 #include <new>
 #include <numeric>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "gbmuf.h"
@@ -28,7 +30,8 @@
 #include "linear_epilogue.cuh"
 #include "linear_pack.cuh"
 #include "linear_tc.cuh"
-#include "linear_simt.cuh"
+#include "linear_rows.cuh"
+#include "column_sum.cuh"
 #include "cross_entropy.cuh"
 #include "grad_clip.cuh"
 
@@ -298,6 +301,39 @@ Product forward_product(const gbmuf_linear_forward_args* a) {
   return q;
 }
 
+// Whether the few-rows kernel takes a layer.
+bool few_rows(const gbmuf_linear_forward_args* a) {
+  const bool direct = in_place(forward_product(a).a, a->dtype) && in_place(forward_product(a).b, a->dtype);
+  const int64_t most = a->dtype == GBMUF_F32 ? 16 : direct ? 8 : 8;
+  const int64_t rows = a->rows <= 1 ? 1 : a->rows <= 2 ? 2 : a->rows <= 4 ? 4 : a->rows <= 8 ? 8 : 16;
+  return a->rows <= most && rows * ((a->n_in + 7) / 8 * 8) * (int64_t)size_of(a->dtype) <= kRowsMostBytes;
+}
+
+template <typename T, int ROWS> gbmuf_status launch_rows(const gbmuf_ops* ops, const RowsParams& P, bool vec, cudaStream_t st) {
+  constexpr int NF = ROWS >= 16 ? 2 : 4, per_block = NF * kRowsThreads / 32;
+  const uint32_t smem = (uint32_t)(ROWS * ((P.K + 7) / 8 * 8) * (int)sizeof(T));
+  const auto kernel = vec ? linear_rows_kernel<T, ROWS, true> : linear_rows_kernel<T, ROWS, false>;
+  if (smem > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsMostBytes);
+    if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the few-rows kernel", e);
+  }
+  const int grid = (int)std::min<long long>(((long long)P.C + per_block - 1) / per_block, ops->num_sms * 2);
+  kernel<<<grid, kRowsThreads, smem, st>>>(P);
+  return launched("launch of the few-rows kernel");
+}
+template <typename T> gbmuf_status forward_rows(const gbmuf_ops* ops, const gbmuf_linear_forward_args* a, cudaStream_t st) {
+  RowsParams P{};
+  P.E = forward_product(a).E;
+  P.x = a->x; P.w = a->w; P.ld_x = a->ld_x; P.ld_w = a->ld_w;
+  P.R = (int)a->rows; P.C = (int)a->n_out; P.K = (int)a->n_in;
+  const bool vec = (uintptr_t)a->w % 16 == 0 && (a->n_out == 1 || a->ld_w * (int64_t)sizeof(T) % 16 == 0);
+  if (a->rows <= 1) return launch_rows<T, 1>(ops, P, vec, st);
+  if (a->rows <= 2) return launch_rows<T, 2>(ops, P, vec, st);
+  if (a->rows <= 4) return launch_rows<T, 4>(ops, P, vec, st);
+  if (a->rows <= 8) return launch_rows<T, 8>(ops, P, vec, st);
+  return launch_rows<T, 16>(ops, P, vec, st);
+}
+
 Product input_grad_product(const gbmuf_linear_backward_input_args* a) {
   Product q{};
   q.a = {a->w, a->n_out, a->n_in, a->ld_w, false};
@@ -456,7 +492,7 @@ gbmuf_status gbmuf_linear_forward_workspace(gbmuf_ops* ops, const gbmuf_linear_f
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check_forward(ops, a)) return st;
-    *bytes = product_workspace(forward_product(a));
+    *bytes = few_rows(a) ? 0 : product_workspace(forward_product(a));
     return GBMUF_OK;
   });
 }
@@ -467,6 +503,7 @@ gbmuf_status gbmuf_linear_forward(gbmuf_ops* ops, const gbmuf_linear_forward_arg
     if (a->rows == 0 || a->n_out == 0) return GBMUF_OK;
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
+    if (few_rows(a)) { DISPATCH_DTYPE(a->dtype, T, return forward_rows<T>(ops, a, (cudaStream_t)stream)); }
     const Product q = forward_product(a);
     DISPATCH_DTYPE(a->dtype, T, return run_product<kForward, T, T>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
   });
