@@ -57,7 +57,10 @@ __global__ void __launch_bounds__(256) activation_backward_kernel(const T* dy, l
   const long long n = rows * cols;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
     const long long r = i / cols, c = i - r * cols;
-    dz[r * ld_dz + c] = from_f32<T>(to_f32(dy[r * ld_dy + c]) * activate_slope<sizeof(T) == 2>(to_f32(z[r * ld_z + c]), act));
+    float v[2] = {to_f32(dy[r * ld_dy + c]), 0.0f};
+    const float y = to_f32(z[r * ld_z + c]), at[2] = {y, y};
+    slope_all<sizeof(T) == 2>(v, at, act);
+    dz[r * ld_dz + c] = from_f32<T>(v[0]);
   }
 }
 

@@ -21,30 +21,6 @@ struct LossParams {
   int split;           // CTAs per row (ring kernel)
 };
 
-// Two fp32 operations per instruction.
-struct Two { unsigned long long u; };
-__device__ __forceinline__ Two two(float x, float y) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ void apart(Two t, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(t.u)); }
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-  Two r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-  return r;
-}
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-  return r;
-}
-__device__ __forceinline__ Two fma_two(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
-  return r;
-}
-
 // exp(x - m) for a fixed m, two at a time; m = -inf counts as 0.  2^y with y = (x - m) log2 e from the
 // special-function unit.  The difference comes first (and not x log2 e - m log2 e in one operation)
 // so that x = m gives 1 exactly and no finite logit overflows.  bf16 logits (FAST): the rounding of y,
@@ -53,11 +29,6 @@ __device__ __forceinline__ Two fma_two(Two a, Two b, Two c) {
 template <bool FAST> struct Shift {
   float m;
   __device__ __forceinline__ void set(float top) { m = top == -INFINITY ? 0.0f : top; }
-  __device__ __forceinline__ static float exp2_unit(float y) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-    return r;
-  }
   __device__ __forceinline__ Two operator()(float x0, float x1) const {
     constexpr float kHi = 1.44269502f, kLo = 1.925963033e-8f, kLn2 = 0.693147181f;     // log2 e = kHi + kLo
     Two t = two(x0, x1) + two(-m, -m);
@@ -67,9 +38,7 @@ template <bool FAST> struct Shift {
       return two(exp2_unit(y0), exp2_unit(y1));
     }
     apart(t, y0, y1);                                      // -inf would give inf - inf below; NaN stays
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-200.0f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-200.0f));
-    t = two(y0, y1);
+    t = two(max_nan(y0, -200.0f), max_nan(y1, -200.0f));
     const Two y = t * two(kHi, kHi);
     const Two f = fma_two(t, two(kLo, kLo), fma_two(t, two(kHi, kHi), y * two(-1.0f, -1.0f)));
     apart(y, y0, y1);

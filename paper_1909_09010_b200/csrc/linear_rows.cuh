@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const Rows
     }
     constexpr int SPARE = NA >= 32 ? 0 : 32 / NA - 1;      // lanes that hold the same sum
     const int c = c0 + index / ROWS, r = index % ROWS;
-    if ((lane & SPARE) == 0 && c < P.C && r < P.R) finish_element<kForward, T, T>(P.E, r, c, acc[0]);
+    if ((lane & SPARE) == 0 && c < P.C && r < P.R) finish_element<T>(P.E, r, c, acc[0]);
   }
 }
 

@@ -161,8 +161,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       bool ok = true;
       for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
         const int c0 = tile / P.tiles_r * 128, r0 = tile % P.tiles_r * BN;
-        for (int it = 0; it < iters && ok; ++it) {
-          const int k0 = (step0 + it / P.products) * kTcK, p = it % P.products;
+        int k0 = step0 * kTcK, p = 0;
+        for (int it = 0; it < iters; ++it) {
           const int pa = part_of_a(P.products, p), pb = part_of_b(P.products, p);
           if (issued >= S) ok = mbar_wait_bounded(empty(s), ph ^ 1, P.status);
           if (!ok) break;
@@ -174,6 +174,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (B_K) tma_load_3d(b, &map_b, k0, r0, pb, full(s));
           else
             for (int i = 0; i < BN / 64; ++i) tma_load_3d(b + i * 8192, &map_b, r0 + 64 * i, k0, pb, full(s));
+          if (++p == P.products) { p = 0; k0 += kTcK; }
           ++issued;
           if (++s == S) { s = 0; ph ^= 1; }
         }
@@ -191,8 +192,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       uint32_t ph = 0;
       bool ok = true;
       for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-        for (int it = 0; it < iters && ok; ++it) {
-          const int in_chunk = it % chunk;
+        int in_chunk = 0;
+        for (int it = 0; it < iters; ++it) {
           if (in_chunk == 0) {
             if (n >= 2) ok = mbar_wait_bounded(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
             if (!ok) break;
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             mma_bf16(d, operand_desc<A_K>(a + k * (A_K ? 32 : 2048)), operand_desc<B_K>(b + k * (B_K ? 32 : 2048)),
                      instr_desc<A_K, B_K>(BN), in_chunk > 0 || k > 0);
           mma_commit(empty(s));
-          if (in_chunk == chunk - 1 || it == iters - 1) { mma_commit(acc_full(n & 1)); ++n; }
+          if (++in_chunk == chunk || it == iters - 1) { mma_commit(acc_full(n & 1)); ++n; in_chunk = 0; }
           if (++s == S) { s = 0; ph ^= 1; }
         }
       }

@@ -1,6 +1,7 @@
 // libgbmuf: the operators of a worker's local step -- linear layers with their gradients, the loss,
 // the gradient norm and clipping.  The interface is the last section of include/gbmuf.h; this file
 // holds the host side and the C ABI, the kernels live in the headers it includes:
+//   packed_math.cuh      two fp32 operations per instruction
 //   linear_epilogue.cuh  activations, and what happens to a finished sum of a matrix product
 //   linear_tc.cuh        matrix products on the tensor cores
 //   linear_pack.cuh      operands that cannot be read in place: other alignments, fp32 as bf16 parts
@@ -27,6 +28,7 @@
 
 #include "host_common.h"
 #include "primitives.cuh"
+#include "packed_math.cuh"
 #include "linear_epilogue.cuh"
 #include "linear_pack.cuh"
 #include "linear_tc.cuh"
