@@ -51,25 +51,32 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 
 // Shared-memory operand descriptor, 128-byte swizzle.  k contiguous: rows of 128 bytes (64 k), groups
 // of 8 rows 1024 bytes apart.  k strided: blocks of 64 elements x 64 k, rows of 128 bytes along the
-// operand's own dimension, 8 k 1024 bytes apart, the next 64 elements 8192 bytes on.
-template <bool K_CONTIGUOUS>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-  const uint64_t lbo = K_CONTIGUOUS ? 1 : (8192 >> 4), sbo = 1024 >> 4;
-  return (uint64_t)((addr >> 4) & 0x3fff) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
+// operand's own dimension, 8 k 1024 bytes apart, the next 64 elements 8192 bytes on.  The upper word is
+// a constant, the lower one the address / 16 (14 bits) and the block stride.
+constexpr uint32_t kDescUpper = (1024u >> 4) | (1u << 14) | (2u << 29);
+template <bool K_CONTIGUOUS> __device__ __forceinline__ uint32_t desc_lower(uint32_t addr) {
+  return ((addr >> 4) & 0x3fffu) | ((K_CONTIGUOUS ? 1u : 8192u >> 4) << 16);
 }
+template <bool K_CONTIGUOUS> constexpr uint32_t kDescStep = (K_CONTIGUOUS ? 32u : 2048u) >> 4;     // 16 k
 // Instruction descriptor: fp32 accumulator, bf16 operands, 128 x BN.
 template <bool A_K, bool B_K>
 __device__ __forceinline__ constexpr uint32_t instr_desc(int bn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
          ((uint32_t)(bn >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t keep) {
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t keep) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
       "setp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(keep)
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(keep), "r"(kDescUpper)
       : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -122,7 +129,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   auto acc_full = [&](int b) { return bars + 256u + 8u * b; };
   auto acc_empty = [&](int b) { return bars + 272u + 8u * b; };
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + 320);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int S = P.stages;
 
   if (threadIdx.x == 0) {
@@ -139,7 +146,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
   grid_dependency_wait();
 
   // this CTA's tiles and its share of each one's steps
@@ -154,66 +161,67 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int tile_step = P.split > 1 ? P.tiles : (int)gridDim.x;   // a split tile: one per cluster
 
   if (warp == 0) {
-    // -------------------------------------------------------------------- loads
-    if (lane == 0) {
-      int s = 0, issued = 0;
-      uint32_t ph = 0;
-      bool ok = true;
-      for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-        const int c0 = tile / P.tiles_r * 128, r0 = tile % P.tiles_r * BN;
-        int k0 = step0 * kTcK, p = 0;
-        for (int it = 0; it < iters; ++it) {
-          const int pa = part_of_a(P.products, p), pb = part_of_b(P.products, p);
-          if (issued >= S) ok = mbar_wait_bounded(empty(s), ph ^ 1, P.status);
-          if (!ok) break;
-          mbar_arrive_expect_tx(full(s), STAGE);
-          const uint32_t a = ring + s * STAGE, b = a + A_BYTES;
-          if (A_K) tma_load_3d(a, &map_a, k0, c0, pa, full(s));
-          else
-            for (int i = 0; i < 2; ++i) tma_load_3d(a + i * 8192, &map_a, c0 + 64 * i, k0, pa, full(s));
-          if (B_K) tma_load_3d(b, &map_b, k0, r0, pb, full(s));
-          else
-            for (int i = 0; i < BN / 64; ++i) tma_load_3d(b + i * 8192, &map_b, r0 + 64 * i, k0, pb, full(s));
-          if (++p == P.products) { p = 0; k0 += kTcK; }
-          ++issued;
-          if (++s == S) { s = 0; ph ^= 1; }
-        }
-      }
-      if (!ok) {
-        // the copies requested into this CTA's shared memory land before it ends
-        for (int j = issued > S ? issued - S : 0; j < issued; ++j) mbar_wait_bounded(full(j % S), (j / S) & 1, P.status);
+    // -------------------------------------------------------------------- loads: a box per lane
+    constexpr int BOXES_A = A_K ? 1 : 2, BOXES_B = B_K ? 1 : BN / 64;
+    const bool is_a = lane < BOXES_A, is_b = !is_a && lane < BOXES_A + BOXES_B;
+    const int box = is_a ? lane : lane - BOXES_A;
+    const uint32_t offset = is_a ? box * 8192u : A_BYTES + box * 8192u;
+    int s = 0, issued = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+      const int c0 = tile / P.tiles_r * 128, r0 = tile % P.tiles_r * BN;
+      const int own = (is_a ? c0 : r0) + 64 * box;                 // along the operand's own dimension
+      int k0 = step0 * kTcK, p = 0;
+      for (int it = 0; it < iters; ++it) {
+        if (issued >= S) ok = mbar_wait_bounded(empty(s), ph ^ 1, P.status);
+        ok = __all_sync(~0u, ok);
+        if (!ok) break;
+        if (lane == 0) mbar_arrive_expect_tx(full(s), STAGE);
+        __syncwarp();
+        if (is_a) tma_load_3d(ring + s * STAGE + offset, &map_a, A_K ? k0 : own, A_K ? own : k0, part_of_a(P.products, p), full(s));
+        if (is_b) tma_load_3d(ring + s * STAGE + offset, &map_b, B_K ? k0 : own, B_K ? own : k0, part_of_b(P.products, p), full(s));
+        if (++p == P.products) { p = 0; k0 += kTcK; }
+        ++issued;
+        if (++s == S) { s = 0; ph ^= 1; }
       }
     }
+    if (!ok)                                                       // the copies requested into this CTA's memory land first
+      for (int j = issued > S ? issued - S : 0; j < issued; ++j) mbar_wait_bounded(full(j % S), (j / S) & 1, P.status);
     __syncwarp();
   } else if (warp == 1) {
     // -------------------------------------------------------------------- matrix instructions
-    if (lane == 0) {
-      int s = 0, n = 0;                                            // n: chunks started
-      uint32_t ph = 0;
-      bool ok = true;
-      for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-        int in_chunk = 0;
-        for (int it = 0; it < iters; ++it) {
-          if (in_chunk == 0) {
-            if (n >= 2) ok = mbar_wait_bounded(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
-            if (!ok) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          }
-          ok = mbar_wait_bounded(full(s), ph, P.status);
-          if (!ok) break;
+    // The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers;
+    // one lane issues.
+    int s = 0, n = 0;                                              // n: chunks started
+    uint32_t ph = 0;
+    bool ok = true;
+    const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + A_BYTES);
+    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+      int in_chunk = 0;
+      for (int it = 0; it < iters; ++it) {
+        if (in_chunk == 0) {
+          if (n >= 2) ok = mbar_wait_bounded(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t a = ring + s * STAGE, b = a + A_BYTES, d = tmem + (uint32_t)(n & 1) * ACC;
+        }
+        ok = mbar_wait_bounded(full(s), ph, P.status) && ok;
+        ok = __all_sync(~0u, ok);
+        if (!ok) break;
+        const uint32_t a = a0 + s * (STAGE >> 4), b = b0 + s * (STAGE >> 4), d = tmem + (uint32_t)(n & 1) * ACC;
+        const bool last = in_chunk + 1 == chunk || it == iters - 1;
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < kTcK / 16; ++k)
-            mma_bf16(d, operand_desc<A_K>(a + k * (A_K ? 32 : 2048)), operand_desc<B_K>(b + k * (B_K ? 32 : 2048)),
-                     instr_desc<A_K, B_K>(BN), in_chunk > 0 || k > 0);
+            mma_bf16(d, a + k * kDescStep<A_K>, b + k * kDescStep<B_K>, instr_desc<A_K, B_K>(BN), k > 0 ? 1u : (uint32_t)in_chunk);
           mma_commit(empty(s));
-          if (++in_chunk == chunk || it == iters - 1) { mma_commit(acc_full(n & 1)); ++n; in_chunk = 0; }
-          if (++s == S) { s = 0; ph ^= 1; }
+          if (last) mma_commit(acc_full(n & 1));
         }
+        __syncwarp();
+        ++in_chunk;
+        if (last) { ++n; in_chunk = 0; }
+        if (++s == S) { s = 0; ph ^= 1; }
       }
     }
-    __syncwarp();
   }
 
   // ---------------------------------------------------------------------- finishing warps
@@ -234,7 +242,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
         for (int ch = 0; ch < chunks; ++ch, ++n) {
           ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
-          if (!__all_sync(~0u, ok)) { ok = false; break; }
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
           for (int j = 0; j < NCOL; j += N) {
@@ -263,7 +272,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
           ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
-          if (!__all_sync(~0u, ok)) { ok = false; break; }
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
 #pragma unroll 1
