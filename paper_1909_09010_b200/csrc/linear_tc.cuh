@@ -16,7 +16,9 @@ namespace {
 // fp32 operands come as three bf16 parts (hi, mid, lo: together all 24 bits) and each step along k
 // is done for the six products of parts that reach 2^-24 of the product: `products` = 6.
 //
-// A tile is 128 x BN.  Warp 0 loads 64 k of both operands per step with the copy engine (128-byte
+// A tile is 128 x BN, or 256 x BN for a pair of CTAs whose tensor cores work as one (PAIR 2): each
+// holds half of the accumulator and loads half of B, a third less to fetch from L2 per product at
+// BN = 256, which is what bounds a single CTA.  Warp 0 loads 64 k of both operands per step with the copy engine (128-byte
 // swizzle), warp 1 issues the matrix instructions, the warps from 4 on finish the sums.  Two accumulators:
 // one is finished while the next is summed.
 constexpr int kTcFinishers = 16;               // warps
@@ -35,18 +37,29 @@ struct TcParams {
   int stages;
 };
 
-__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn) { return (128u + (uint32_t)bn) * 128u; }
+// PAIR CTAs of a cluster work on one tile of PAIR * 128 x BN: each loads 128 of A's rows and BN / PAIR
+// of B's.
+__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
-__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int stages) {
-  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn);
+__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
+  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
 }
 
+// PAIR 2: the barrier may be the other CTA's.
+template <int PAIR>
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
-      "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-      : "memory");
+  if (PAIR == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+        "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], "
+        "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
 }
 
 // Shared-memory operand descriptor, 128-byte swizzle.  k contiguous: rows of 128 bytes (64 k), groups
@@ -58,28 +71,47 @@ template <bool K_CONTIGUOUS> __device__ __forceinline__ uint32_t desc_lower(uint
   return ((addr >> 4) & 0x3fffu) | ((K_CONTIGUOUS ? 1u : 8192u >> 4) << 16);
 }
 template <bool K_CONTIGUOUS> constexpr uint32_t kDescStep = (K_CONTIGUOUS ? 32u : 2048u) >> 4;     // 16 k
-// Instruction descriptor: fp32 accumulator, bf16 operands, 128 x BN.
+// Instruction descriptor: fp32 accumulator, bf16 operands, PAIR * 128 x BN.
 template <bool A_K, bool B_K>
-__device__ __forceinline__ constexpr uint32_t instr_desc(int bn) {
+__device__ __forceinline__ constexpr uint32_t instr_desc(int bn, int pair) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (A_K ? 0u : 1u << 15) | (B_K ? 0u : 1u << 16) |
-         ((uint32_t)(bn >> 3) << 17) | ((128u >> 4) << 24);
+         ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(pair * 128 >> 4) << 24);
 }
+template <int PAIR>
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t keep) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "setp.ne.u32 p, %4, 0;\n\t"
-      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "r"(b), "r"(idesc), "r"(keep), "r"(kDescUpper)
-      : "memory");
+#define MMA(GROUP)                                                                                       \
+  asm volatile(                                                                                          \
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"                                                    \
+      "setp.ne.u32 p, %4, 0;\n\t"                                                                        \
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"                                              \
+      "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d),                   \
+      "r"(a), "r"(b), "r"(idesc), "r"(keep), "r"(kDescUpper)                                             \
+      : "memory")
+  if (PAIR == 1) MMA("1"); else MMA("2");
+#undef MMA
 }
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
   return one != 0;
 }
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// Arrives on a barrier once the matrix instructions issued so far are done; PAIR 2: in both CTAs.
+template <int PAIR> __device__ __forceinline__ void mma_commit(uint32_t bar) {
+  if (PAIR == 1)
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+// The address of rank 0's copy of a shared-memory location.
+__device__ __forceinline__ uint32_t in_leader(uint32_t addr) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ void arrive_remote(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -113,11 +145,12 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 __device__ __forceinline__ int part_of_a(int products, int p) { return products == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
 __device__ __forceinline__ int part_of_b(int products, int p) { return products == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
 
-template <int KIND, typename T, typename TO, bool PROMOTE, int BN>
+template <int KIND, typename T, typename TO, bool PROMOTE, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
   constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad;
-  constexpr uint32_t STAGE = tc_stage_bytes(BN), A_BYTES = 128 * 128;
+  constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
+  constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
@@ -134,99 +167,117 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), kTcFinishers); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), PAIR * kTcFinishers); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (PAIR == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (PAIR == 2) cluster_sync();                                   // both CTAs' barriers exist
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
   grid_dependency_wait();
 
   // this CTA's tiles and its share of each one's steps
-  const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;
+  const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;      // among the CTAs that share the steps
+  const int side = PAIR == 2 ? (int)(blockIdx.x & 1) : 0;                        // of the pair that shares the tile
   const int step0 = (int)((long long)P.ksteps * rank / P.split), step1 = (int)((long long)P.ksteps * (rank + 1) / P.split);
   const int iters = (step1 - step0) * P.products;                 // (k step, product) pairs of a tile
   // without PROMOTE a tile is one chunk; with it the tensor cores' sum is moved into fp32 registers
   // after every chunk of 16 (24) instructions
   const int chunk = PROMOTE ? (P.products == 1 ? 4 : 6) : (iters > 0 ? iters : 1);
   const int chunks = iters == 0 ? 0 : (iters + chunk - 1) / chunk;
-  const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)blockIdx.x;
-  const int tile_step = P.split > 1 ? P.tiles : (int)gridDim.x;   // a split tile: one per cluster
+  const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)(blockIdx.x / PAIR);
+  const int tile_step = P.split > 1 ? P.tiles : (int)(gridDim.x / PAIR);   // a split tile: one per cluster
 
   if (warp == 0) {
-    // -------------------------------------------------------------------- loads: a box per lane
-    constexpr int BOXES_A = A_K ? 1 : 2, BOXES_B = B_K ? 1 : BN / 64;
-    const bool is_a = lane < BOXES_A, is_b = !is_a && lane < BOXES_A + BOXES_B;
-    const int box = is_a ? lane : lane - BOXES_A;
-    const uint32_t offset = is_a ? box * 8192u : A_BYTES + box * 8192u;
+    // -------------------------------------------------------------------- loads
+    // The whole warp goes through the loops of this and the next role, so that addresses, coordinates
+    // and descriptors stay in uniform registers; an elected lane waits and issues.  Where a wait gives
+    // up, the rest of the loop does nothing.
+    constexpr int BOXES_A = A_K ? 1 : 2, BOXES_B = B_K ? 1 : OWN_R / 64;
     int s = 0, issued = 0;
     uint32_t ph = 0;
     bool ok = true;
-    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-      const int c0 = tile / P.tiles_r * 128, r0 = tile % P.tiles_r * BN;
-      const int own = (is_a ? c0 : r0) + 64 * box;                 // along the operand's own dimension
+    for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
+      const int c0 = tile / P.tiles_r * TILE_C + side * 128, r0 = tile % P.tiles_r * BN + side * OWN_R;
       int k0 = step0 * kTcK, p = 0;
       for (int it = 0; it < iters; ++it) {
-        if (issued >= S) ok = mbar_wait_bounded(empty(s), ph ^ 1, P.status);
-        ok = __all_sync(~0u, ok);
-        if (!ok) break;
-        if (lane == 0) mbar_arrive_expect_tx(full(s), STAGE);
-        __syncwarp();
-        if (is_a) tma_load_3d(ring + s * STAGE + offset, &map_a, A_K ? k0 : own, A_K ? own : k0, part_of_a(P.products, p), full(s));
-        if (is_b) tma_load_3d(ring + s * STAGE + offset, &map_b, B_K ? k0 : own, B_K ? own : k0, part_of_b(P.products, p), full(s));
+        // the leader's barrier counts both CTAs' bytes
+        const uint32_t bar = PAIR == 2 ? in_leader(full(s)) : full(s), a = ring + s * STAGE, b = a + A_BYTES;
+        const int pa = part_of_a(P.products, p), pb = part_of_b(P.products, p);
+        if (elect_one()) {
+          if (issued >= S) ok = ok && wait_phase(empty(s), ph ^ 1, P.status);
+          if (ok) {
+            if (side == 0) mbar_arrive_expect_tx(full(s), PAIR * STAGE);
+#pragma unroll
+            for (int i = 0; i < BOXES_A; ++i)
+              tma_load_3d<PAIR>(a + i * 8192, &map_a, A_K ? k0 : c0 + 64 * i, A_K ? c0 : k0, pa, bar);
+#pragma unroll
+            for (int i = 0; i < BOXES_B; ++i)
+              tma_load_3d<PAIR>(b + i * 8192, &map_b, B_K ? k0 : r0 + 64 * i, B_K ? r0 : k0, pb, bar);
+          }
+        }
         if (++p == P.products) { p = 0; k0 += kTcK; }
         ++issued;
         if (++s == S) { s = 0; ph ^= 1; }
       }
     }
-    if (!ok)                                                       // the copies requested into this CTA's memory land first
-      for (int j = issued > S ? issued - S : 0; j < issued; ++j) mbar_wait_bounded(full(j % S), (j / S) & 1, P.status);
+    // the copies requested so far land before the CTAs end; the leader's barriers count both CTAs'
+    if (!ok && side == 0)
+      for (int j = 0; j < S; ++j) { mbar_wait_bounded(full(j), 0, P.status); mbar_wait_bounded(full(j), 1, P.status); }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == 1 && side == 0) {
     // -------------------------------------------------------------------- matrix instructions
-    // The whole warp goes through the loop, so that addresses and descriptors stay in uniform registers;
-    // one lane issues.
     int s = 0, n = 0;                                              // n: chunks started
     uint32_t ph = 0;
     bool ok = true;
     const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + A_BYTES);
-    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
+    for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
       int in_chunk = 0;
       for (int it = 0; it < iters; ++it) {
-        if (in_chunk == 0) {
-          if (n >= 2) ok = mbar_wait_bounded(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        }
-        ok = mbar_wait_bounded(full(s), ph, P.status) && ok;
-        ok = __all_sync(~0u, ok);
-        if (!ok) break;
         const uint32_t a = a0 + s * (STAGE >> 4), b = b0 + s * (STAGE >> 4), d = tmem + (uint32_t)(n & 1) * ACC;
         const bool last = in_chunk + 1 == chunk || it == iters - 1;
         if (elect_one()) {
+          if (in_chunk == 0) {
+            if (n >= 2) ok = ok && wait_phase(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
+          ok = ok && wait_phase(full(s), ph, P.status);
+          if (ok) {
 #pragma unroll
-          for (int k = 0; k < kTcK / 16; ++k)
-            mma_bf16(d, a + k * kDescStep<A_K>, b + k * kDescStep<B_K>, instr_desc<A_K, B_K>(BN), k > 0 ? 1u : (uint32_t)in_chunk);
-          mma_commit(empty(s));
-          if (last) mma_commit(acc_full(n & 1));
+            for (int k = 0; k < kTcK / 16; ++k)
+              mma_bf16<PAIR>(d, a + k * kDescStep<A_K>, b + k * kDescStep<B_K>, instr_desc<A_K, B_K>(BN, PAIR), k > 0 ? 1u : (uint32_t)in_chunk);
+            mma_commit<PAIR>(empty(s));
+            if (last) mma_commit<PAIR>(acc_full(n & 1));
+          }
         }
-        __syncwarp();
         ++in_chunk;
         if (last) { ++n; in_chunk = 0; }
         if (++s == S) { s = 0; ph ^= 1; }
       }
     }
+    __syncwarp();
   }
 
   // ---------------------------------------------------------------------- finishing warps
   const int quad = warp & 3, part = (warp - 4) >> 2;
   const uint32_t my_tmem = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * NCOL);
+  auto release = [&](int b) {                                      // one arrival per warp, at the leader's barrier
+    if (lane == 0) {
+      if (PAIR == 2) arrive_remote(in_leader(acc_empty(b)));
+      else mbar_arrive(acc_empty(b));
+    }
+  };
   auto bias_of = [&](int c) {
     return KIND == kForward && P.E.bias && c < P.C ? to_f32(static_cast<const T*>(P.E.bias)[c]) : 0.0f;
   };
@@ -234,7 +285,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     int n = 0;
     bool ok = true;
     for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-      const int c = tile / P.tiles_r * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + part * NCOL;
+      const int c = tile / P.tiles_r * TILE_C + side * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + part * NCOL;
       const float bias = bias_of(c);
       if (PROMOTE) {
         float acc[NCOL];
@@ -254,7 +305,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
+          release(n & 1);
         }
         if (!ok) break;
 #pragma unroll
@@ -287,13 +338,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
+          release(n & 1);
           ++n;
         }
       }
     }
   }
-  if (P.split > 1) {
+  if (PAIR == 1 && P.split > 1) {
     // The cluster's CTAs hold partial sums of one tile.  CTA j finishes accumulator columns
     // [j, j + 1) BN / split: everybody writes its sums of those columns into CTA j's shared memory
     // (the operand ring, idle by then) and CTA j adds them in the order of the ranks.
@@ -318,7 +369,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty(n & 1));     // per warp: arrivals are serialised
+          release(n & 1);
         }
       }
     }
@@ -358,9 +409,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (PAIR == 2) cluster_sync();                                   // nothing of this CTA is used any more
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
+    if (PAIR == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
   }
 }
 

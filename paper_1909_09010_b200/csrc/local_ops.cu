@@ -168,29 +168,36 @@ int may_pair(const Product& q) {
   return ok;
 }
 
-struct TcShape { int bn, split; };
+// Tile width, CTAs that share a tile's steps, CTAs that share a tile: the choice with the least time
+// by a model in clock cycles, fitted to measurements.
+struct TcShape { int bn, split, pair; };
 TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int products, bool rows_64) {
-  TcShape best{256, 1};
+  TcShape best{256, 1, 1};
   double best_t = 1e300;
   const long long ksteps = (q.K + 63) / 64;
-  for (int bn = rows_64 ? 64 : 32; bn <= 256; bn *= 2)
-    for (int split = 1; split <= 8; split *= 2) {
-      if (split > 1 && split * 2 > ksteps) break;
-      const long long tiles = ((q.C + 127) / 128) * ((q.R + bn - 1) / bn);
-      if (split > 1 && tiles * split > ops->num_sms) break;
-      const long long waves = (tiles * split + ops->num_sms - 1) / ops->num_sms;
-      const double step = std::max(2.0 * bn, 64.0 + bn);
-      const double t = waves * ((double)((ksteps + split - 1) / split) * products * step + 600.0 + bn * 4.0 / split) + (split > 1 ? 1500.0 : 0.0);
-      if (t < best_t) { best_t = t; best = {bn, split}; }
-    }
+  for (int pair = 1; pair <= 2; ++pair)
+    for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= 256; bn *= 2)
+      for (int split = 1; split <= (pair == 2 ? 1 : 8); split *= 2) {
+        if (split > 1 && split * 2 > ksteps) break;
+        const long long tiles = ((q.C + 128 * pair - 1) / (128 * pair)) * ((q.R + bn - 1) / bn);
+        if (split > 1 && tiles * split > ops->num_sms) break;
+        const long long waves = (tiles * split * pair + ops->num_sms - 1) / ops->num_sms;
+        const double step = std::max(std::max(330.0, 2.0 * bn), tc_stage_bytes(bn, pair) / 53.0);
+        const double steps = (double)((ksteps + split - 1) / split) * products;
+        const double t = waves * std::max(steps * step, bn * 8.0 / split) + bn * 8.0 / split + (split > 1 ? 2000.0 : 0.0);
+        if (t < best_t) { best_t = t; best = {bn, split, pair}; }
+      }
+#ifdef FORCE_SHAPE
+  if (const char* f = getenv("SHAPE")) sscanf(f, "%d,%d,%d", &best.bn, &best.split, &best.pair);
+#endif
   return best;
 }
 
-template <int KIND, typename T, typename TO, bool PROMOTE, int BN>
+template <int KIND, typename T, typename TO, bool PROMOTE, int BN, int PAIR>
 gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
-  const auto kernel = linear_tc_kernel<KIND, T, TO, PROMOTE, BN>;
-  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN));
-  const uint32_t smem = tc_smem_bytes(BN, P.stages);
+  const auto kernel = linear_tc_kernel<KIND, T, TO, PROMOTE, BN, PAIR>;
+  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR));
+  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages);
   static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
   const uint64_t bit = 1ull << (ops->device & 63);
   if (!(ready.load() & bit)) {
@@ -204,14 +211,13 @@ gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma,
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cfg.attrs = attr;
-  if (P.split > 1) {
-    cfg.gridDim = dim3((unsigned)(P.tiles * P.split));
+  const int cluster = PAIR * P.split;
+  if (cluster > 1) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)P.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
-  } else {
-    cfg.gridDim = dim3((unsigned)std::min(P.tiles, ops->num_sms));
   }
+  cfg.gridDim = dim3((unsigned)(P.split > 1 ? P.tiles * P.split : PAIR * std::min(P.tiles, ops->num_sms / PAIR)));
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ma, mb, P);
   return e == cudaSuccess ? GBMUF_OK : cuda_refuse("launch of the linear-layer kernel", e);
 }
@@ -231,7 +237,7 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
   const TcShape shape = choose_shape(ops, q, P.products, KIND == kWeightGrad);
   P.split = shape.split;
   P.tiles_r = (int)((q.R + shape.bn - 1) / shape.bn);
-  const long long tiles = (long long)P.tiles_r * ((q.C + 127) / 128);
+  const long long tiles = (long long)P.tiles_r * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
   if (tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles");
   P.tiles = (int)tiles;
   CUtensorMap ma{}, mb{};
@@ -242,14 +248,17 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
     if (!in_place(q.a, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.a, pa, st))); }
     if (!in_place(q.b, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.b, pb, st))); }
     if (gbmuf_status rc = operand_map(q.a, q.dtype, pa, q.a.k_inner ? 128 : 64, &ma)) return rc;
-    if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn : 64, &mb)) return rc;
+    if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn / shape.pair : 64, &mb)) return rc;
   }
+  if (shape.pair == 2)
+    return shape.bn == 128 ? launch_tc<KIND, T, TO, PROMOTE, 128, 2>(ops, P, ma, mb, st)
+                           : launch_tc<KIND, T, TO, PROMOTE, 256, 2>(ops, P, ma, mb, st);
   switch (shape.bn) {
     case 32:
-      if constexpr (KIND != kWeightGrad) return launch_tc<KIND, T, TO, PROMOTE, 32>(ops, P, ma, mb, st);
-    case 64: return launch_tc<KIND, T, TO, PROMOTE, 64>(ops, P, ma, mb, st);
-    case 128: return launch_tc<KIND, T, TO, PROMOTE, 128>(ops, P, ma, mb, st);
-    default: return launch_tc<KIND, T, TO, PROMOTE, 256>(ops, P, ma, mb, st);
+      if constexpr (KIND != kWeightGrad) return launch_tc<KIND, T, TO, PROMOTE, 32, 1>(ops, P, ma, mb, st);
+    case 64: return launch_tc<KIND, T, TO, PROMOTE, 64, 1>(ops, P, ma, mb, st);
+    case 128: return launch_tc<KIND, T, TO, PROMOTE, 128, 1>(ops, P, ma, mb, st);
+    default: return launch_tc<KIND, T, TO, PROMOTE, 256, 1>(ops, P, ma, mb, st);
   }
 }
 

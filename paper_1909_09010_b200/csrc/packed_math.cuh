@@ -51,6 +51,14 @@ __device__ __forceinline__ float min_nan(float x, float y) {
   return r;
 }
 
+// mbar_wait_bounded with the first try in line.
+__device__ __noinline__ bool wait_slowly(uint32_t bar, uint32_t parity, int32_t* status) {
+  return mbar_wait_bounded(bar, parity, status);
+}
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, int32_t* status) {
+  return mbar_try_wait(bar, parity) || wait_slowly(bar, parity, status);
+}
+
 }  // namespace
 
 #endif  // GBMUF_CSRC_PACKED_MATH_CUH
