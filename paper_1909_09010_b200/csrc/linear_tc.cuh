@@ -13,8 +13,8 @@ namespace {
 // so a warp that holds 32 lanes of one accumulator column stores 32 neighbouring elements, and few
 // rows (single tokens) make the tile narrow (BN), not half empty.
 //
-// fp32 operands come as three bf16 parts (hi, mid, lo: together all 24 bits) and each step along k
-// is done for the six products of parts that reach 2^-24 of the product: `products` = 6.
+// fp32 operands come as three bf16 parts (hi, mid, lo: together all 24 bits; PARTS 3), and each step
+// along k does the six products of parts that reach 2^-24 of the product.
 //
 // A tile is 128 x BN, or 256 x BN for a pair of CTAs whose tensor cores work as one (PAIR 2): each
 // holds half of the accumulator and loads half of B, a third less to fetch from L2 per product at
@@ -31,7 +31,6 @@ struct TcParams {
   int32_t* status;
   int R, C;
   int ksteps;            // steps of 64 along k
-  int products;          // 1 or 6
   int tiles_r, tiles;    // row tiles; all tiles, row tiles running fastest
   int split;             // CTAs of a cluster that share a tile's steps (1: none)
   int stages;
@@ -39,10 +38,12 @@ struct TcParams {
 
 // PAIR CTAs of a cluster work on one tile of PAIR * 128 x BN: each loads 128 of A's rows and BN / PAIR
 // of B's.
-__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
+__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair, int parts) {
+  return (uint32_t)parts * (128u + (uint32_t)(bn / pair)) * 128u;
+}
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
-__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
-  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
+__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int parts, int stages) {
+  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair, parts);
 }
 
 // PAIR 2: the barrier may be the other CTA's.
@@ -142,15 +143,18 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 
 // Parts (0 hi, 1 mid, 2 lo) of A and B in product p of six, smallest products first: an accumulator
 // that is still small loses less to each addition.  hi lo, lo hi, mid mid, hi mid, mid hi, hi hi.
-__device__ __forceinline__ int part_of_a(int products, int p) { return products == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
-__device__ __forceinline__ int part_of_b(int products, int p) { return products == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
+__device__ __forceinline__ constexpr uint32_t part_of_a(int p) { return (0x010120u >> (4 * p)) & 15u; }
+__device__ __forceinline__ constexpr uint32_t part_of_b(int p) { return (0x001102u >> (4 * p)) & 15u; }
 
-template <int KIND, typename T, typename TO, bool PROMOTE, int BN, int PAIR>
+// PROMOTE (results that stay fp32): the tensor cores' sum is moved into fp32 registers, and added there
+// with rounding to nearest, after every 16 (24) instructions: in the accumulator every addition cuts
+// towards zero, which over thousands of them would cost a few units of 2^-18.
+template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
-  constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad;
-  constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
+  constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad, PROMOTE = sizeof(TO) == 4;
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
+  constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR, PARTS), A_BYTES = 128 * 128, B_BYTES = OWN_R * 128;   // A and B of a part
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
@@ -191,10 +195,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;      // among the CTAs that share the steps
   const int side = PAIR == 2 ? (int)(blockIdx.x & 1) : 0;                        // of the pair that shares the tile
   const int step0 = (int)((long long)P.ksteps * rank / P.split), step1 = (int)((long long)P.ksteps * (rank + 1) / P.split);
-  const int iters = (step1 - step0) * P.products;                 // (k step, product) pairs of a tile
-  // without PROMOTE a tile is one chunk; with it the tensor cores' sum is moved into fp32 registers
-  // after every chunk of 16 (24) instructions
-  const int chunk = PROMOTE ? (P.products == 1 ? 4 : 6) : (iters > 0 ? iters : 1);
+  const int iters = step1 - step0;
+  // without PROMOTE a tile is one chunk
+  const int chunk = PROMOTE ? (PARTS == 1 ? 4 : 1) : (iters > 0 ? iters : 1);
   const int chunks = iters == 0 ? 0 : (iters + chunk - 1) / chunk;
   const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)(blockIdx.x / PAIR);
   const int tile_step = P.split > 1 ? P.tiles : (int)(gridDim.x / PAIR);   // a split tile: one per cluster
@@ -210,24 +213,25 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     bool ok = true;
     for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
       const int c0 = tile / P.tiles_r * TILE_C + side * 128, r0 = tile % P.tiles_r * BN + side * OWN_R;
-      int k0 = step0 * kTcK, p = 0;
       for (int it = 0; it < iters; ++it) {
+        const int k0 = (step0 + it) * kTcK;
         // the leader's barrier counts both CTAs' bytes
-        const uint32_t bar = PAIR == 2 ? in_leader(full(s)) : full(s), a = ring + s * STAGE, b = a + A_BYTES;
-        const int pa = part_of_a(P.products, p), pb = part_of_b(P.products, p);
+        const uint32_t bar = PAIR == 2 ? in_leader(full(s)) : full(s), a = ring + s * STAGE, b = a + PARTS * A_BYTES;
         if (elect_one()) {
           if (issued >= S) ok = ok && wait_phase(empty(s), ph ^ 1, P.status);
           if (ok) {
             if (side == 0) mbar_arrive_expect_tx(full(s), PAIR * STAGE);
 #pragma unroll
-            for (int i = 0; i < BOXES_A; ++i)
-              tma_load_3d<PAIR>(a + i * 8192, &map_a, A_K ? k0 : c0 + 64 * i, A_K ? c0 : k0, pa, bar);
+            for (int p = 0; p < PARTS; ++p) {
 #pragma unroll
-            for (int i = 0; i < BOXES_B; ++i)
-              tma_load_3d<PAIR>(b + i * 8192, &map_b, B_K ? k0 : r0 + 64 * i, B_K ? r0 : k0, pb, bar);
+              for (int i = 0; i < BOXES_A; ++i)
+                tma_load_3d<PAIR>(a + p * A_BYTES + i * 8192, &map_a, A_K ? k0 : c0 + 64 * i, A_K ? c0 : k0, p, bar);
+#pragma unroll
+              for (int i = 0; i < BOXES_B; ++i)
+                tma_load_3d<PAIR>(b + p * B_BYTES + i * 8192, &map_b, B_K ? k0 : r0 + 64 * i, B_K ? r0 : k0, p, bar);
+            }
           }
         }
-        if (++p == P.products) { p = 0; k0 += kTcK; }
         ++issued;
         if (++s == S) { s = 0; ph ^= 1; }
       }
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     int s = 0, n = 0;                                              // n: chunks started
     uint32_t ph = 0;
     bool ok = true;
-    const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + A_BYTES);
+    const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + PARTS * A_BYTES);
     for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
       int in_chunk = 0;
       for (int it = 0; it < iters; ++it) {
@@ -255,8 +259,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           ok = ok && wait_phase(full(s), ph, P.status);
           if (ok) {
 #pragma unroll
-            for (int k = 0; k < kTcK / 16; ++k)
-              mma_bf16<PAIR>(d, a + k * kDescStep<A_K>, b + k * kDescStep<B_K>, instr_desc<A_K, B_K>(BN, PAIR), k > 0 ? 1u : (uint32_t)in_chunk);
+            for (int p = PARTS == 1 ? 5 : 0; p < 6; ++p)
+#pragma unroll
+              for (int k = 0; k < kTcK / 16; ++k)
+                mma_bf16<PAIR>(d, a + part_of_a(p) * (A_BYTES >> 4) + k * kDescStep<A_K>, b + part_of_b(p) * (B_BYTES >> 4) + k * kDescStep<B_K>,
+                               instr_desc<A_K, B_K>(BN, PAIR), k > 0 || (PARTS == 3 && p > 0) ? 1u : (uint32_t)in_chunk);
             mma_commit<PAIR>(empty(s));
             if (last) mma_commit<PAIR>(acc_full(n & 1));
           }

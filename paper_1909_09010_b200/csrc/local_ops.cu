@@ -171,19 +171,19 @@ int may_pair(const Product& q) {
 // Tile width, CTAs that share a tile's steps, CTAs that share a tile: the choice with the least time
 // by a model in clock cycles, fitted to measurements.
 struct TcShape { int bn, split, pair; };
-TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int products, bool rows_64) {
+TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64) {
   TcShape best{256, 1, 1};
   double best_t = 1e300;
   const long long ksteps = (q.K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
-    for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= 256; bn *= 2)
+    for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2)
       for (int split = 1; split <= (pair == 2 ? 1 : 8); split *= 2) {
         if (split > 1 && split * 2 > ksteps) break;
         const long long tiles = ((q.C + 128 * pair - 1) / (128 * pair)) * ((q.R + bn - 1) / bn);
         if (split > 1 && tiles * split > ops->num_sms) break;
         const long long waves = (tiles * split * pair + ops->num_sms - 1) / ops->num_sms;
-        const double step = std::max(std::max(330.0, 2.0 * bn), tc_stage_bytes(bn, pair) / 53.0);
-        const double steps = (double)((ksteps + split - 1) / split) * products;
+        const double step = std::max(std::max(330.0, 2.0 * bn * (parts == 3 ? 6 : 1)), tc_stage_bytes(bn, pair, parts) / 53.0);
+        const double steps = (double)((ksteps + split - 1) / split);
         const double t = waves * std::max(steps * step, bn * 8.0 / split) + bn * 8.0 / split + (split > 1 ? 2000.0 : 0.0);
         if (t < best_t) { best_t = t; best = {bn, split, pair}; }
       }
@@ -193,11 +193,11 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int products, bool 
   return best;
 }
 
-template <int KIND, typename T, typename TO, bool PROMOTE, int BN, int PAIR>
+template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
-  const auto kernel = linear_tc_kernel<KIND, T, TO, PROMOTE, BN, PAIR>;
-  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR));
-  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages);
+  const auto kernel = linear_tc_kernel<KIND, T, TO, PARTS, BN, PAIR>;
+  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR, PARTS));
+  const uint32_t smem = tc_smem_bytes(BN, PAIR, PARTS, P.stages);
   static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
   const uint64_t bit = 1ull << (ops->device & 63);
   if (!(ready.load() & bit)) {
@@ -223,18 +223,16 @@ gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma,
 }
 
 // Runs a product: operands that cannot be read in place are packed into the workspace first.
-template <int KIND, typename T, typename TO>
+template <int KIND, typename T, typename TO, int PARTS>
 gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
   const long long need = product_workspace(q);
   if (need > workspace_bytes || (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)))
     return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
-  constexpr bool PROMOTE = sizeof(TO) == 4;
   q.E.pairs = may_pair(q);
   TcParams P{};
   P.E = q.E; P.status = ops->d_status; P.R = (int)q.R; P.C = (int)q.C;
   P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
-  P.products = q.dtype == GBMUF_F32 ? 6 : 1;
-  const TcShape shape = choose_shape(ops, q, P.products, KIND == kWeightGrad);
+  const TcShape shape = choose_shape(ops, q, PARTS, KIND == kWeightGrad);
   P.split = shape.split;
   P.tiles_r = (int)((q.R + shape.bn - 1) / shape.bn);
   const long long tiles = (long long)P.tiles_r * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
@@ -251,15 +249,14 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
     if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn / shape.pair : 64, &mb)) return rc;
   }
   if (shape.pair == 2)
-    return shape.bn == 128 ? launch_tc<KIND, T, TO, PROMOTE, 128, 2>(ops, P, ma, mb, st)
-                           : launch_tc<KIND, T, TO, PROMOTE, 256, 2>(ops, P, ma, mb, st);
-  switch (shape.bn) {
-    case 32:
-      if constexpr (KIND != kWeightGrad) return launch_tc<KIND, T, TO, PROMOTE, 32, 1>(ops, P, ma, mb, st);
-    case 64: return launch_tc<KIND, T, TO, PROMOTE, 64, 1>(ops, P, ma, mb, st);
-    case 128: return launch_tc<KIND, T, TO, PROMOTE, 128, 1>(ops, P, ma, mb, st);
-    default: return launch_tc<KIND, T, TO, PROMOTE, 256, 1>(ops, P, ma, mb, st);
-  }
+    return shape.bn == 128 ? launch_tc<KIND, T, TO, PARTS, 128, 2>(ops, P, ma, mb, st)
+                           : launch_tc<KIND, T, TO, PARTS, 256, 2>(ops, P, ma, mb, st);
+  if constexpr (KIND != kWeightGrad)
+    if (shape.bn == 32) return launch_tc<KIND, T, TO, PARTS, 32, 1>(ops, P, ma, mb, st);
+  if constexpr (PARTS == 1)
+    if (shape.bn == 256) return launch_tc<KIND, T, TO, PARTS, 256, 1>(ops, P, ma, mb, st);
+  return shape.bn == 64 ? launch_tc<KIND, T, TO, PARTS, 64, 1>(ops, P, ma, mb, st)
+                        : launch_tc<KIND, T, TO, PARTS, 128, 1>(ops, P, ma, mb, st);
 }
 
 gbmuf_status check_forward(const gbmuf_ops* ops, const gbmuf_linear_forward_args* a) {
@@ -516,7 +513,7 @@ gbmuf_status gbmuf_linear_forward(gbmuf_ops* ops, const gbmuf_linear_forward_arg
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
     if (few_rows(a)) { DISPATCH_DTYPE(a->dtype, T, return forward_rows<T>(ops, a, (cudaStream_t)stream)); }
     const Product q = forward_product(a);
-    DISPATCH_DTYPE(a->dtype, T, return run_product<kForward, T, T>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
+    DISPATCH_DTYPE(a->dtype, T, return run_product<kForward, T, T, (sizeof(T) == 4 ? 3 : 1)>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
   });
 }
 
@@ -538,7 +535,7 @@ gbmuf_status gbmuf_linear_backward_input(gbmuf_ops* ops, const gbmuf_linear_back
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
     const Product q = input_grad_product(a);
-    DISPATCH_DTYPE(a->dtype, T, return run_product<kInputGrad, T, T>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
+    DISPATCH_DTYPE(a->dtype, T, return run_product<kInputGrad, T, T, (sizeof(T) == 4 ? 3 : 1)>(ops, q, a->workspace, a->workspace_bytes, (cudaStream_t)stream));
   });
 }
 
@@ -563,7 +560,8 @@ gbmuf_status gbmuf_linear_backward_weight(gbmuf_ops* ops, const gbmuf_linear_bac
     if (a->dw && a->n_in > 0) {
       const Product q = weight_grad_product(a);
       gbmuf_status rc = GBMUF_OK;
-      DISPATCH_DTYPE(a->grad_dtype, TO, (rc = run_product<kWeightGrad, TO, TO>(ops, q, a->workspace, a->workspace_bytes, st)));
+      DISPATCH_DTYPE(a->dtype, T, DISPATCH_DTYPE(a->grad_dtype, TO,
+          (rc = run_product<kWeightGrad, TO, TO, (sizeof(T) == 4 ? 3 : 1)>(ops, q, a->workspace, a->workspace_bytes, st))));
       if (rc != GBMUF_OK) return rc;
     }
     if (a->dbias) {
