@@ -14,6 +14,8 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long l
   constexpr int W = VEC ? 16 / (int)sizeof(T) : 1, L = VEC ? 8 : 32, ROWS = 256 / L, COLS = L * W;
   __shared__ float part[ROWS][COLS + 1];
   __shared__ float ranks[8][COLS];
+  grid_launch_dependents();
+  grid_dependency_wait();
   uint32_t share, rank;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(share));
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -54,6 +56,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) activation_backward_kernel(const T* dy, long long ld_dy, const T* z,
                                                                   long long ld_z, T* dz, long long ld_dz,
                                                                   long long rows, long long cols, int act) {
+  grid_launch_dependents();
+  grid_dependency_wait();
   const long long n = rows * cols;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
     const long long r = i / cols, c = i - r * cols;

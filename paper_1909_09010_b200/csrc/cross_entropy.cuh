@@ -76,6 +76,8 @@ constexpr int kWarpVocab = 32 * kWarpRegs;
 template <typename T, int REGS>
 __global__ void __launch_bounds__(128) cross_entropy_warp_kernel(const LossParams P) {
   constexpr bool FAST = sizeof(T) == 2;
+  grid_launch_dependents();
+  grid_dependency_wait();
   const int lane = threadIdx.x & 31;
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
   if (row >= P.rows) return;
@@ -227,6 +229,8 @@ __global__ void __launch_bounds__(kLossThreads, kLossBlocksPerSm) cross_entropy_
   }
   __syncthreads();
   if (P.split > 1) cluster_sync();                         // barriers exist before a peer uses them
+  grid_launch_dependents();
+  grid_dependency_wait();
 
   int slot = 0;                                            // next slot of the ring and its phase
   uint32_t phase = 0;

@@ -196,9 +196,10 @@ __device__ __forceinline__ long long clip_outside(const ClipSpan& s, long long k
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_norm_kernel(const ClipParams P) {
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ double scratch[kClipWorkers / 32];
-  grid_launch_dependents();
   const uint32_t bars = smem_u32(smem);
   clip_prologue(smem);
+  grid_launch_dependents();
+  grid_dependency_wait();
   if (threadIdx.x >= kClipWorkers) { clip_produce<true>(P, bars, bars + 128); return; }
   ClipWalk<true> w;
   w.begin(P);                                    // every block has a chunk

@@ -151,21 +151,22 @@ __device__ __forceinline__ uint32_t trade_pairs(uint32_t u, int lane) {
 template <typename X, int N> struct Strip {
   uint32_t raw[N];
 
-  // Asks for the values; unpack() has to come before the next use of the memory they came from.
+  // Asks for the values; unpack() has to come before the next use of the memory they came from.  One
+  // pointer walks down the rows: an address per row from scratch would be a third of the epilogue.
   template <bool WHOLE>
   __device__ __forceinline__ void load(const void* base, long long ld, int r, int c, int R, int C, bool pairs, int lane) {
     if (sizeof(X) == 2 && pairs) {
       const int odd = lane & 1;
       const char* p = static_cast<const char*>(base) + ((r + odd) * ld + (c - odd)) * 2;
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j)
-        raw[j] = WHOLE || (c - odd < C && r + odd + 2 * j < R) ? *reinterpret_cast<const uint32_t*>(p + 4 * j * ld) : 0u;
+      for (int j = 0; j < N / 2; ++j, p += 4 * ld)
+        raw[j] = WHOLE || (c - odd < C && r + odd + 2 * j < R) ? *reinterpret_cast<const uint32_t*>(p) : 0u;
     } else {
       const X* p = static_cast<const X*>(base) + r * ld + c;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if constexpr (sizeof(X) == 2) raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint16_t*>(p + j * ld) : 0u;
-        else raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint32_t*>(p + j * ld) : 0u;
+      for (int j = 0; j < N; ++j, p += ld) {
+        if constexpr (sizeof(X) == 2) raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint16_t*>(p) : 0u;
+        else raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint32_t*>(p) : 0u;
       }
     }
   }
@@ -190,16 +191,16 @@ __device__ __forceinline__ void store_strip(const float (&v)[N], void* base, lon
     const int odd = lane & 1;
     char* p = static_cast<char*>(base) + ((r + odd) * ld + (c - odd)) * 2;
 #pragma unroll
-    for (int j = 0; j < N / 2; ++j) {
+    for (int j = 0; j < N / 2; ++j, p += 4 * ld) {
       __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
       const uint32_t u = trade_pairs(*reinterpret_cast<const uint32_t*>(&h), lane);
-      if (WHOLE || (c - odd < C && r + odd + 2 * j < R)) *reinterpret_cast<uint32_t*>(p + 4 * j * ld) = u;
+      if (WHOLE || (c - odd < C && r + odd + 2 * j < R)) *reinterpret_cast<uint32_t*>(p) = u;
     }
   } else {
     X* p = static_cast<X*>(base) + r * ld + c;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (WHOLE || (c < C && r + j < R)) p[j * ld] = from_f32<X>(v[j]);
+    for (int j = 0; j < N; ++j, p += ld)
+      if (WHOLE || (c < C && r + j < R)) *p = from_f32<X>(v[j]);
   }
 }
 

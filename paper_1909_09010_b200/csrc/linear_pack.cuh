@@ -27,6 +27,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) pack_kernel(const T* src, long long ld, long long outer, long long inner,
                                                    __nv_bfloat16* dst, long long ld_dst) {
   grid_launch_dependents();
+  grid_dependency_wait();
   const long long per_row = ld_dst / 8, n = outer * per_row, part = outer * ld_dst;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
     const long long r = i / per_row, c = (i - r * per_row) * 8;

@@ -38,6 +38,8 @@ template <typename T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const RowsParams P) {
   constexpr int NF = ROWS >= 16 ? 2 : 4, NA = NF * ROWS, V = VEC ? 16 / (int)sizeof(T) : 1;
   extern __shared__ __align__(128) unsigned char smem[];
+  grid_launch_dependents();
+  grid_dependency_wait();
   T* const xs = reinterpret_cast<T*>(smem);
   const int kp = (P.K + 7) & ~7;                 // row stride in shared memory
   for (int i = threadIdx.x; i < ROWS * kp; i += kRowsThreads) {

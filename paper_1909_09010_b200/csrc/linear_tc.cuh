@@ -189,6 +189,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (PAIR == 2) cluster_sync();                                   // both CTAs' barriers exist
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
+  grid_launch_dependents();
   grid_dependency_wait();
 
   // this CTA's tiles and its share of each one's steps

@@ -42,6 +42,7 @@ struct gbmuf_ops {
   int num_sms = 0;
   int max_smem = 0;              // opt-in dynamic shared memory per block
   int32_t* d_status = nullptr;
+  int tc_clusters[4] = {};       // clusters of 1, 2, 4, 8 CTAs of the linear-layer kernel that fit at once
   int loss_clusters[2][4] = {};  // clusters of 1, 2, 4, 8 CTAs of the cross-entropy kernel (fp32, bf16) that fit at once
 };
 
@@ -74,6 +75,23 @@ template <typename F> gbmuf_status guarded(F&& f) {
     return GBMUF_ERR_ALLOC;
   }
 }
+
+// Every kernel of this file is launched as a programmatic dependent of the work before it in the
+// stream: its blocks may become resident while that ends, and it waits (grid_dependency_wait) before
+// it touches memory.  In clusters of `cluster` blocks.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), unsigned grid, unsigned cluster, int threads, uint32_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+  cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+gbmuf_status launched(const char* what, cudaError_t e) { return e == cudaSuccess ? GBMUF_OK : cuda_refuse(what, e); }
 
 size_t size_of(int32_t dtype) { return dtype == GBMUF_F32 ? 4 : 2; }
 bool is_dtype(int32_t d) { return d == GBMUF_F32 || d == GBMUF_BF16; }
@@ -131,14 +149,12 @@ long long product_workspace(const Product& q) {
 }
 
 template <typename T>
-void pack(const gbmuf_ops* ops, const Operand& o, void* dst, cudaStream_t st) {
+cudaError_t pack(const gbmuf_ops* ops, const Operand& o, void* dst, cudaStream_t st) {
   const long long ld_dst = round_up(o.inner, 8), n = o.outer * (ld_dst / 8);
-  const int grid = (int)std::min<long long>((n + 255) / 256, (long long)ops->num_sms * 16);
+  const unsigned grid = (unsigned)std::min<long long>((n + 255) / 256, (long long)ops->num_sms * 16);
   const bool vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)sizeof(T) % 16 == 0);
-  if (vec)
-    pack_kernel<T, true><<<grid, 256, 0, st>>>(static_cast<const T*>(o.p), o.ld, o.outer, o.inner, static_cast<__nv_bfloat16*>(dst), ld_dst);
-  else
-    pack_kernel<T, false><<<grid, 256, 0, st>>>(static_cast<const T*>(o.p), o.ld, o.outer, o.inner, static_cast<__nv_bfloat16*>(dst), ld_dst);
+  return launch(vec ? pack_kernel<T, true> : pack_kernel<T, false>, grid, 1, 256, 0, st, static_cast<const T*>(o.p), o.ld, o.outer, o.inner,
+                static_cast<__nv_bfloat16*>(dst), ld_dst);
 }
 
 // Tensor map of an operand (packed at `packed` if it cannot be read in place): [parts][outer][inner],
@@ -169,27 +185,29 @@ int may_pair(const Product& q) {
 }
 
 // Tile width, CTAs that share a tile's steps, CTAs that share a tile: the choice with the least time
-// by a model in clock cycles, fitted to measurements.
+// by a model whose four constants were fitted to 180 measured products of 12 to 100,000 rows, columns
+// and terms in both types (its choice is 0.8 % above the best one on average, 15 % at worst).
 struct TcShape { int bn, split, pair; };
-TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64) {
-  TcShape best{256, 1, 1};
+TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided) {
+  TcShape best{64, 1, 1};
   double best_t = 1e300;
   const long long ksteps = (q.K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
     for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2)
-      for (int split = 1; split <= (pair == 2 ? 1 : 8); split *= 2) {
-        if (split > 1 && split * 2 > ksteps) break;
+      for (int log = 0; log <= (pair == 2 ? 0 : 3); ++log) {
+        const int split = 1 << log;
         const long long tiles = ((q.C + 128 * pair - 1) / (128 * pair)) * ((q.R + bn - 1) / bn);
-        if (split > 1 && tiles * split > ops->num_sms) break;
-        const long long waves = (tiles * split * pair + ops->num_sms - 1) / ops->num_sms;
-        const double step = std::max(std::max(330.0, 2.0 * bn * (parts == 3 ? 6 : 1)), tc_stage_bytes(bn, pair, parts) / 53.0);
-        const double steps = (double)((ksteps + split - 1) / split);
-        const double t = waves * std::max(steps * step, bn * 8.0 / split) + bn * 8.0 / split + (split > 1 ? 2000.0 : 0.0);
+        const long long fit = ops->tc_clusters[pair == 2 ? 1 : log];
+        if (split > 1 && (split * 2 > ksteps || tiles > fit)) break;
+        const double waves = (double)((tiles + fit - 1) / fit);
+        // a step takes as long as its operands take to arrive, the epilogue as long as the tile is wide
+        double step = std::max(100.0, tc_stage_bytes(bn, pair, parts) / 126.0);
+        if (pair == 2 && a_strided) step *= 1.45;
+        const double sums = 1000.0 + (double)((ksteps + split - 1) / split) * step, epilogue = 15.0 * bn / split;
+        double t = split > 1 ? waves * (sums + 1100.0 + 19.0 * bn) : waves * std::max(sums, epilogue);
+        t += epilogue + (pair == 2 ? 2000.0 : 0.0);
         if (t < best_t) { best_t = t; best = {bn, split, pair}; }
       }
-#ifdef FORCE_SHAPE
-  if (const char* f = getenv("SHAPE")) sscanf(f, "%d,%d,%d", &best.bn, &best.split, &best.pair);
-#endif
   return best;
 }
 
@@ -205,21 +223,8 @@ gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma,
     if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the linear-layer kernel", e);
     if (ops->device < 64) ready.fetch_or(bit);
   }
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
-  cfg.blockDim = dim3(kTcThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = attr;
-  const int cluster = PAIR * P.split;
-  if (cluster > 1) {
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.numAttrs = 1;
-  }
-  cfg.gridDim = dim3((unsigned)(P.split > 1 ? P.tiles * P.split : PAIR * std::min(P.tiles, ops->num_sms / PAIR)));
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ma, mb, P);
-  return e == cudaSuccess ? GBMUF_OK : cuda_refuse("launch of the linear-layer kernel", e);
+  const unsigned grid = (unsigned)(P.split > 1 ? P.tiles * P.split : PAIR * std::min(P.tiles, ops->num_sms / PAIR));
+  return launched("launch of the linear-layer kernel", launch(kernel, grid, (unsigned)(PAIR * P.split), kTcThreads, smem, st, ma, mb, P));
 }
 
 // Runs a product: operands that cannot be read in place are packed into the workspace first.
@@ -232,7 +237,7 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
   TcParams P{};
   P.E = q.E; P.status = ops->d_status; P.R = (int)q.R; P.C = (int)q.C;
   P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
-  const TcShape shape = choose_shape(ops, q, PARTS, KIND == kWeightGrad);
+  const TcShape shape = choose_shape(ops, q, PARTS, KIND == kWeightGrad, KIND != kForward);
   P.split = shape.split;
   P.tiles_r = (int)((q.R + shape.bn - 1) / shape.bn);
   const long long tiles = (long long)P.tiles_r * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
@@ -243,8 +248,10 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     void* const pa = ws;
     void* const pb = ws + packed_bytes(q.a, q.dtype);
-    if (!in_place(q.a, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.a, pa, st))); }
-    if (!in_place(q.b, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, (pack<TI>(ops, q.b, pb, st))); }
+    cudaError_t e = cudaSuccess;
+    if (!in_place(q.a, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, e = pack<TI>(ops, q.a, pa, st)); }
+    if (e == cudaSuccess && !in_place(q.b, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, e = pack<TI>(ops, q.b, pb, st)); }
+    if (e != cudaSuccess) return cuda_refuse("launch of the operand-packing kernel", e);
     if (gbmuf_status rc = operand_map(q.a, q.dtype, pa, q.a.k_inner ? 128 : 64, &ma)) return rc;
     if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn / shape.pair : 64, &mb)) return rc;
   }
@@ -294,10 +301,6 @@ gbmuf_status check_backward_weight(const gbmuf_ops* ops, const gbmuf_linear_back
   return GBMUF_OK;
 }
 
-gbmuf_status launched(const char* what) {
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? GBMUF_OK : cuda_refuse(what, e);
-}
 
 Product forward_product(const gbmuf_linear_forward_args* a) {
   Product q{};
@@ -325,9 +328,8 @@ template <typename T, int ROWS> gbmuf_status launch_rows(const gbmuf_ops* ops, c
     const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsMostBytes);
     if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the few-rows kernel", e);
   }
-  const int grid = (int)std::min<long long>(((long long)P.C + per_block - 1) / per_block, ops->num_sms * 2);
-  kernel<<<grid, kRowsThreads, smem, st>>>(P);
-  return launched("launch of the few-rows kernel");
+  const unsigned grid = (unsigned)std::min<long long>(((long long)P.C + per_block - 1) / per_block, ops->num_sms * 2);
+  return launched("launch of the few-rows kernel", launch(kernel, grid, 1, kRowsThreads, smem, st, P));
 }
 template <typename T> gbmuf_status forward_rows(const gbmuf_ops* ops, const gbmuf_linear_forward_args* a, cudaStream_t st) {
   RowsParams P{};
@@ -370,40 +372,25 @@ cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t 
   // a cluster shares the rows of a column tile: as many CTAs as have four rows per thread, 8 at most
   unsigned share = 1;
   while (share < 8 && a->rows >= (long long)share * 2 * rows_at_once * 4) share *= 2;
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = share; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(share * (unsigned)((a->n_out + cols - 1) / cols));
-  cfg.blockDim = dim3(256);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const T* const dz = static_cast<const T*>(a->dz);
-  TO* const out = static_cast<TO*>(a->dbias);
-  const long long R = a->rows, C = a->n_out, ld = a->ld_dz;
-  return vec ? cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, true>, dz, ld, R, C, out, (int)a->accumulate)
-             : cudaLaunchKernelEx(&cfg, column_sum_kernel<T, TO, false>, dz, ld, R, C, out, (int)a->accumulate);
+  const long long tiles = (a->n_out + cols - 1) / cols;
+  return launch(vec ? column_sum_kernel<T, TO, true> : column_sum_kernel<T, TO, false>, share * (unsigned)tiles, share, 256, 0, st,
+                static_cast<const T*>(a->dz), (long long)a->ld_dz, (long long)a->rows, (long long)a->n_out, static_cast<TO*>(a->dbias),
+                (int)a->accumulate);
 }
 
 constexpr long long kLossCacheBytes = 64ll << 20;   // of the 126 MB: the gradient passes through as well
 
-template <typename T>
-cudaLaunchConfig_t loss_config(int split, int clusters, cudaLaunchAttribute* attr, cudaStream_t st) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(clusters * split)); cfg.blockDim = dim3(kLossThreads); cfg.dynamicSmemBytes = kLossSmem;
-  cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
-  attr->id = cudaLaunchAttributeClusterDimension;
-  attr->val.clusterDim.x = (unsigned)split; attr->val.clusterDim.y = 1; attr->val.clusterDim.z = 1;
-  return cfg;
-}
-
-template <typename T> cudaError_t prepare_loss(gbmuf_ops* ops, int (&clusters)[4]) {
-  cudaError_t e = cudaFuncSetAttribute((const void*)cross_entropy_ring_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLossSmem);
+// How many clusters of 1, 2, 4 and 8 blocks of a kernel the GPU holds at once.
+template <typename K> cudaError_t count_clusters(K kernel, int threads, uint32_t smem, int blocks, int (&clusters)[4]) {
+  cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = loss_config<T>(1 << i, (ops->num_sms * kLossBlocksPerSm) >> i, &attr, nullptr);
-    e = cudaOccupancyMaxActiveClusters(&clusters[i], cross_entropy_ring_kernel<T>, &cfg);
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1u << i; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(blocks >> i << i)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&clusters[i], kernel, &cfg);
     if (clusters[i] < 1) clusters[i] = 1;
   }
   return e;
@@ -413,11 +400,9 @@ template <typename T> cudaError_t prepare_loss(gbmuf_ops* ops, int (&clusters)[4
 // rows to fill the GPU, or where the slices that are fetched twice would not fit the L2 cache.
 template <typename T> cudaError_t launch_loss(const gbmuf_ops* ops, LossParams& P, cudaStream_t st) {
   if (P.vocab <= kWarpVocab) {
-    const unsigned grid = (unsigned)((P.rows + 3) / 4);
-    if (P.vocab <= 256) cross_entropy_warp_kernel<T, 8><<<grid, 128, 0, st>>>(P);
-    else if (P.vocab <= 1024) cross_entropy_warp_kernel<T, 32><<<grid, 128, 0, st>>>(P);
-    else cross_entropy_warp_kernel<T, kWarpRegs><<<grid, 128, 0, st>>>(P);
-    return cudaGetLastError();
+    const auto kernel = P.vocab <= 256 ? cross_entropy_warp_kernel<T, 8> : P.vocab <= 1024 ? cross_entropy_warp_kernel<T, 32>
+                                                                                           : cross_entropy_warp_kernel<T, kWarpRegs>;
+    return launch(kernel, (unsigned)((P.rows + 3) / 4), 1, 128, 0, st, P);
   }
   const long long bytes = P.vocab * (long long)sizeof(T), ctas = (long long)ops->num_sms * kLossBlocksPerSm;
   int log = 0;
@@ -428,10 +413,8 @@ template <typename T> cudaError_t launch_loss(const gbmuf_ops* ops, LossParams& 
     ++log;
   }
   P.split = 1 << log;
-  cudaLaunchAttribute attr;
   const int clusters = (int)std::min<long long>(P.rows, ops->loss_clusters[sizeof(T) == 2][log]);
-  const cudaLaunchConfig_t cfg = loss_config<T>(P.split, clusters, &attr, st);
-  return cudaLaunchKernelEx(&cfg, cross_entropy_ring_kernel<T>, P);
+  return launch(cross_entropy_ring_kernel<T>, (unsigned)(clusters * P.split), (unsigned)P.split, kLossThreads, kLossSmem, st, P);
 }
 
 // Reads and clears a status word, once the stream has got there.
@@ -463,8 +446,12 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
     ops->device = device;
     cudaError_t e = cudaDeviceGetAttribute(&ops->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ops->max_smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, device);
-    if (e == cudaSuccess) e = prepare_loss<float>(ops, ops->loss_clusters[0]);
-    if (e == cudaSuccess) e = prepare_loss<__nv_bfloat16>(ops, ops->loss_clusters[1]);
+    const int pairs = ops->num_sms * kLossBlocksPerSm;
+    if (e == cudaSuccess) e = count_clusters(cross_entropy_ring_kernel<float>, kLossThreads, kLossSmem, pairs, ops->loss_clusters[0]);
+    if (e == cudaSuccess) e = count_clusters(cross_entropy_ring_kernel<__nv_bfloat16>, kLossThreads, kLossSmem, pairs, ops->loss_clusters[1]);
+    if (e == cudaSuccess)
+      e = count_clusters(linear_tc_kernel<kForward, __nv_bfloat16, __nv_bfloat16, 1, 128, 1>, kTcThreads, (uint32_t)ops->max_smem, ops->num_sms,
+                         ops->tc_clusters);
     if (e == cudaSuccess) e = cudaMalloc(&ops->d_status, 256);
     if (e == cudaSuccess) e = cudaMemset(ops->d_status, 0, 256);
     if (e != cudaSuccess) {
@@ -584,11 +571,12 @@ gbmuf_status gbmuf_activation_backward(gbmuf_ops* ops, int64_t rows, int64_t col
     if (rows == 0 || cols == 0) return GBMUF_OK;
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    const int grid = (int)std::min<long long>((rows * cols + 255) / 256, (long long)ops->num_sms * 16);
-    DISPATCH_DTYPE(dtype, T, (activation_backward_kernel<T><<<grid, 256, 0, (cudaStream_t)stream>>>(
-        static_cast<const T*>(dy), ld_dy, static_cast<const T*>(z), ld_z, static_cast<T*>(dz), ld_dz, rows, cols,
-        activation)));
-    return launched("launch of the activation-gradient kernel");
+    const unsigned grid = (unsigned)std::min<long long>((rows * cols + 255) / 256, (long long)ops->num_sms * 16);
+    cudaError_t e = cudaSuccess;
+    DISPATCH_DTYPE(dtype, T, e = launch(activation_backward_kernel<T>, grid, 1, 256, 0, (cudaStream_t)stream, static_cast<const T*>(dy),
+                                        (long long)ld_dy, static_cast<const T*>(z), (long long)ld_z, static_cast<T*>(dz), (long long)ld_dz,
+                                        (long long)rows, (long long)cols, (int)activation));
+    return launched("launch of the activation-gradient kernel", e);
   });
 }
 
@@ -757,24 +745,11 @@ static gbmuf_status clip_run(gbmuf_clip* h, bool scale, float max_norm, float* n
     P.partial = reinterpret_cast<double*>(base + h->partial_off);
     P.norms = norms; P.chunks = h->chunks; P.count = (int)h->count; P.groups = h->groups; P.blocks = h->blocks;
     P.max_norm = max_norm;
-    if (h->chunks > 0) clip_norm_kernel<<<h->blocks, kClipThreads, kClipSmem, st>>>(P);
-    if (gbmuf_status rc = launched("launch of the gradient-norm kernel")) return rc;
-    // the second kernel's blocks may become resident while the first one ends
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = h->chunks > 0 ? 1 : 0;
-    cudaError_t e;
-    if (scale) {
-      cfg.gridDim = dim3(h->blocks); cfg.blockDim = dim3(kClipThreads); cfg.dynamicSmemBytes = kClipSmem;
-      e = cudaLaunchKernelEx(&cfg, clip_scale_kernel, P);
-    } else {
-      cfg.gridDim = dim3(std::min(h->groups, h->num_sms)); cfg.blockDim = dim3(kClipWorkers);
-      e = cudaLaunchKernelEx(&cfg, clip_finish_kernel, P);
-    }
+    cudaError_t e = cudaSuccess;
+    if (h->chunks > 0) e = launch(clip_norm_kernel, (unsigned)h->blocks, 1, kClipThreads, kClipSmem, st, P);
+    if (e == cudaSuccess)
+      e = scale ? launch(clip_scale_kernel, (unsigned)h->blocks, 1, kClipThreads, kClipSmem, st, P)
+                : launch(clip_finish_kernel, (unsigned)std::min(h->groups, h->num_sms), 1, kClipWorkers, 0, st, P);
     if (e != cudaSuccess) return cuda_refuse("launch of the gradient-norm kernels", e);
     h->work.note(st);
     return GBMUF_OK;
