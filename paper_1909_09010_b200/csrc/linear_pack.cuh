@@ -22,36 +22,46 @@ __device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uin
 
 // src [outer][inner] with any stride and alignment -> bf16 parts [1 or 3][outer][ld_dst], ld_dst a
 // multiple of 8; columns inner .. ld_dst-1 are never read as data and get zeros.  One thread per
-// eight columns; VEC: src rows are 16-byte aligned.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) pack_kernel(const T* src, long long ld, long long outer, long long inner,
-                                                   __nv_bfloat16* dst, long long ld_dst) {
-  grid_launch_dependents();
-  grid_dependency_wait();
-  const long long per_row = ld_dst / 8, n = outer * per_row, part = outer * ld_dst;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+// eight columns; vec: src rows are 16-byte aligned.
+struct PackJob {
+  const void* src;
+  __nv_bfloat16* dst;
+  long long ld, outer, inner, ld_dst;
+  int vec, blocks;             // blocks: of the grid, 0: nothing to do
+};
+template <typename T, bool VEC> __device__ __forceinline__ void pack_run(const PackJob& J, int block) {
+  const long long per_row = J.ld_dst / 8, n = J.outer * per_row, part = J.outer * J.ld_dst;
+  for (long long i = (long long)block * 256 + threadIdx.x; i < n; i += (long long)J.blocks * 256) {
     const long long r = i / per_row, c = (i - r * per_row) * 8;
-    const T* const s = src + r * ld + c;
+    const T* const s = static_cast<const T*>(J.src) + r * J.ld + c;
     __align__(16) T v[8];
-    if (VEC && c + 8 <= inner) {
+    if (VEC && c + 8 <= J.inner) {
 #pragma unroll
       for (int j = 0; j < (int)sizeof(T) / 2; ++j) reinterpret_cast<uint4*>(v)[j] = reinterpret_cast<const uint4*>(s)[j];
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = c + j < inner ? s[j] : from_f32<T>(0.0f);
+      for (int j = 0; j < 8; ++j) v[j] = c + j < J.inner ? s[j] : from_f32<T>(0.0f);
     }
-    uint4* const d = reinterpret_cast<uint4*>(dst + r * ld_dst + c);
+    __nv_bfloat16* const d = J.dst + r * J.ld_dst + c;
     if constexpr (sizeof(T) == 2) {
-      *d = *reinterpret_cast<const uint4*>(v);
+      *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(v);
     } else {
       __align__(16) uint16_t p[3][8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) split3(v[j], p[0][j], p[1][j], p[2][j]);
 #pragma unroll
-      for (int q = 0; q < 3; ++q)
-        reinterpret_cast<uint4*>(dst + q * part + r * ld_dst + c)[0] = *reinterpret_cast<const uint4*>(p[q]);
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(d + q * part) = *reinterpret_cast<const uint4*>(p[q]);
     }
   }
+}
+// Both operands of a product in one launch.
+template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const PackJob a, const PackJob b) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const bool first = (int)blockIdx.x < a.blocks;
+  const PackJob& J = first ? a : b;
+  const int block = first ? blockIdx.x : blockIdx.x - a.blocks;
+  if (J.vec) pack_run<T, true>(J, block); else pack_run<T, false>(J, block);
 }
 
 }  // namespace

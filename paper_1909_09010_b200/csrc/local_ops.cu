@@ -148,13 +148,13 @@ long long product_workspace(const Product& q) {
   return q.K == 0 || q.R == 0 || q.C == 0 ? 0 : packed_bytes(q.a, q.dtype) + packed_bytes(q.b, q.dtype);
 }
 
-template <typename T>
-cudaError_t pack(const gbmuf_ops* ops, const Operand& o, void* dst, cudaStream_t st) {
-  const long long ld_dst = round_up(o.inner, 8), n = o.outer * (ld_dst / 8);
-  const unsigned grid = (unsigned)std::min<long long>((n + 255) / 256, (long long)ops->num_sms * 16);
-  const bool vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)sizeof(T) % 16 == 0);
-  return launch(vec ? pack_kernel<T, true> : pack_kernel<T, false>, grid, 1, 256, 0, st, static_cast<const T*>(o.p), o.ld, o.outer, o.inner,
-                static_cast<__nv_bfloat16*>(dst), ld_dst);
+PackJob pack_job(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst) {
+  PackJob j{};
+  if (in_place(o, dtype)) return j;
+  j.src = o.p; j.dst = static_cast<__nv_bfloat16*>(dst); j.ld = o.ld; j.outer = o.outer; j.inner = o.inner; j.ld_dst = round_up(o.inner, 8);
+  j.vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)size_of(dtype) % 16 == 0);
+  j.blocks = (int)std::min<long long>((o.outer * (j.ld_dst / 8) + 255) / 256, (long long)ops->num_sms * 16);
+  return j;
 }
 
 // Tensor map of an operand (packed at `packed` if it cannot be read in place): [parts][outer][inner],
@@ -248,10 +248,12 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     void* const pa = ws;
     void* const pb = ws + packed_bytes(q.a, q.dtype);
-    cudaError_t e = cudaSuccess;
-    if (!in_place(q.a, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, e = pack<TI>(ops, q.a, pa, st)); }
-    if (e == cudaSuccess && !in_place(q.b, q.dtype)) { DISPATCH_DTYPE(q.dtype, TI, e = pack<TI>(ops, q.b, pb, st)); }
-    if (e != cudaSuccess) return cuda_refuse("launch of the operand-packing kernel", e);
+    const PackJob ja = pack_job(ops, q.a, q.dtype, pa), jb = pack_job(ops, q.b, q.dtype, pb);
+    if (ja.blocks + jb.blocks > 0) {
+      const cudaError_t e = launch(q.dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)(ja.blocks + jb.blocks), 1,
+                                   256, 0, st, ja, jb);
+      if (e != cudaSuccess) return cuda_refuse("launch of the operand-packing kernel", e);
+    }
     if (gbmuf_status rc = operand_map(q.a, q.dtype, pa, q.a.k_inner ? 128 : 64, &ma)) return rc;
     if (gbmuf_status rc = operand_map(q.b, q.dtype, pb, q.b.k_inner ? shape.bn / shape.pair : 64, &mb)) return rc;
   }
