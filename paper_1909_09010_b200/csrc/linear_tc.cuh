@@ -32,6 +32,7 @@ struct TcParams {
   int R, C;
   int ksteps;            // steps of 64 along k
   int tiles_r, tiles;    // row tiles; all tiles, row tiles running fastest
+  int tile_step, step_c, step_r;   // from a CTA's tile to its next: tiles, and as column and row tiles
   int split;             // CTAs of a cluster that share a tile's steps (1: none)
   int stages;
 };
@@ -138,7 +139,10 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
                  : "r"(addr));
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(u[i]);
+  for (int i = 0; i < N; ++i) {
+    asm volatile("" : "+r"(u[i]));                                 // no use of the values moves before the wait
+    v[i] = __uint_as_float(u[i]);
+  }
 }
 
 // Parts (0 hi, 1 mid, 2 lo) of A and B in product p of six, smallest products first: an accumulator
@@ -169,6 +173,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int warp = __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int S = P.stages;
 
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), PAIR * kTcFinishers); }
@@ -195,13 +203,23 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   // this CTA's tiles and its share of each one's steps
   const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;      // among the CTAs that share the steps
   const int side = PAIR == 2 ? (int)(blockIdx.x & 1) : 0;                        // of the pair that shares the tile
-  const int step0 = (int)((long long)P.ksteps * rank / P.split), step1 = (int)((long long)P.ksteps * (rank + 1) / P.split);
+  const int step0 = P.split > 1 ? (int)((unsigned)P.ksteps * (unsigned)rank / (unsigned)P.split) : 0;
+  const int step1 = P.split > 1 ? (int)((unsigned)P.ksteps * (unsigned)(rank + 1) / (unsigned)P.split) : P.ksteps;
   const int iters = step1 - step0;
   // without PROMOTE a tile is one chunk
   const int chunk = PROMOTE ? (PARTS == 1 ? 4 : 1) : (iters > 0 ? iters : 1);
   const int chunks = iters == 0 ? 0 : (iters + chunk - 1) / chunk;
   const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)(blockIdx.x / PAIR);
-  const int tile_step = P.split > 1 ? P.tiles : (int)(gridDim.x / PAIR);   // a split tile: one per cluster
+  struct Walk {                                                    // tile number, column tile, row tile
+    int tile, c, r;
+  };
+  auto first = [&] { return Walk{first_tile, first_tile / P.tiles_r, first_tile % P.tiles_r}; };
+  auto next = [&](Walk& w) {
+    w.tile += P.tile_step;
+    w.c += P.step_c;
+    w.r += P.step_r;
+    if (w.r >= P.tiles_r) { w.r -= P.tiles_r; ++w.c; }
+  };
 
   if (warp == 0) {
     // -------------------------------------------------------------------- loads
@@ -212,8 +230,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     int s = 0, issued = 0;
     uint32_t ph = 0;
     bool ok = true;
-    for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
-      const int c0 = tile / P.tiles_r * TILE_C + side * 128, r0 = tile % P.tiles_r * BN + side * OWN_R;
+    for (Walk w = first(); w.tile < P.tiles; next(w)) {
+      const int c0 = w.c * TILE_C + side * 128, r0 = w.r * BN + side * OWN_R;
       for (int it = 0; it < iters; ++it) {
         const int k0 = (step0 + it) * kTcK;
         // the leader's barrier counts both CTAs' bytes
@@ -247,7 +265,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     uint32_t ph = 0;
     bool ok = true;
     const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + PARTS * A_BYTES);
-    for (int tile = first_tile; tile < P.tiles; tile += tile_step) {
+    for (int tile = first_tile; tile < P.tiles; tile += P.tile_step) {
       int in_chunk = 0;
       for (int it = 0; it < iters; ++it) {
         const uint32_t a = a0 + s * (STAGE >> 4), b = b0 + s * (STAGE >> 4), d = tmem + (uint32_t)(n & 1) * ACC;
@@ -292,8 +310,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
-    for (int tile = first_tile; tile < P.tiles && ok; tile += tile_step) {
-      const int c = tile / P.tiles_r * TILE_C + side * 128 + quad * 32 + lane, r0 = tile % P.tiles_r * BN + part * NCOL;
+    for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
+      const int c = w.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL;
       const float bias = bias_of(c);
       if (PROMOTE) {
         float acc[NCOL];
@@ -339,9 +357,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int j = 0; j < NCOL; j += N) {
           float v[N] = {};
           if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
-          const Finisher<KIND, T, TO, N> now = F;
+          Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
-          Finisher<KIND, T, TO, N>(now).finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
+          now.finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -399,10 +417,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (warp >= 4) {
       // strips of 4 rows (BN / split is a multiple of 4)
       const float* const sums = reinterpret_cast<const float*>(smem + kTcHead) + quad * 32 + lane;
-      const int c = first_tile / P.tiles_r * 128 + quad * 32 + lane;
+      const Walk w = first();
+      const int c = w.c * 128 + quad * 32 + lane;
       const float bias = bias_of(c);
       for (int i = 4 * part; i < cols; i += kTcFinishers) {
-        const int r = first_tile % P.tiles_r * BN + rank * cols + i;
+        const int r = w.r * BN + rank * cols + i;
         Finisher<KIND, T, TO, 4> F;
         F.ask(P.E, r, c, P.R, P.C, lane);
         float v[4];

@@ -223,7 +223,9 @@ gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma,
     if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the linear-layer kernel", e);
     if (ops->device < 64) ready.fetch_or(bit);
   }
-  const unsigned grid = (unsigned)(P.split > 1 ? P.tiles * P.split : PAIR * std::min(P.tiles, ops->num_sms / PAIR));
+  const int at_once = P.split > 1 ? P.tiles : std::min(P.tiles, ops->num_sms / PAIR);     // a split tile: one per cluster
+  P.tile_step = at_once; P.step_c = at_once / P.tiles_r; P.step_r = at_once % P.tiles_r;
+  const unsigned grid = (unsigned)(at_once * PAIR * P.split);
   return launched("launch of the linear-layer kernel", launch(kernel, grid, (unsigned)(PAIR * P.split), kTcThreads, smem, st, ma, mb, P));
 }
 
