@@ -149,7 +149,7 @@ __device__ __forceinline__ uint32_t trade_pairs(uint32_t u, int lane) {
   return __byte_perm(u, __shfl_xor_sync(~0u, u, 1), lane & 1 ? 0x3276 : 0x5410);
 }
 template <typename X, int N> struct Strip {
-  uint32_t raw[N];
+  uint32_t raw[sizeof(X) == 2 ? N / 2 : N];          // bf16: two rows to a word
 
   // Asks for the values; unpack() has to come before the next use of the memory they came from.  One
   // pointer walks down the rows: an address per row from scratch would be a third of the epilogue.
@@ -165,22 +165,27 @@ template <typename X, int N> struct Strip {
       const X* p = static_cast<const X*>(base) + r * ld + c;
 #pragma unroll
       for (int j = 0; j < N; ++j, p += ld) {
-        if constexpr (sizeof(X) == 2) raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint16_t*>(p) : 0u;
-        else raw[j] = WHOLE || (c < C && r + j < R) ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+        const bool there = WHOLE || (c < C && r + j < R);
+        if constexpr (sizeof(X) == 2) {
+          const uint32_t h = there ? *reinterpret_cast<const uint16_t*>(p) : 0u;
+          raw[j / 2] = j & 1 ? raw[j / 2] | h << 16 : h;
+        } else {
+          raw[j] = there ? *reinterpret_cast<const uint32_t*>(p) : 0u;
+        }
       }
     }
   }
   __device__ __forceinline__ void unpack(float (&v)[N], bool pairs, int lane) const {
-    if (sizeof(X) == 2 && pairs) {
+    if constexpr (sizeof(X) == 2) {
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
-        const uint32_t u = trade_pairs(raw[j], lane);
+        const uint32_t u = pairs ? trade_pairs(raw[j], lane) : raw[j];
         v[2 * j] = __uint_as_float(u << 16);
         v[2 * j + 1] = __uint_as_float(u & 0xffff0000u);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = __uint_as_float(sizeof(X) == 2 ? raw[j] << 16 : raw[j]);
+      for (int j = 0; j < N; ++j) v[j] = __uint_as_float(raw[j]);
     }
   }
 };
