@@ -38,13 +38,11 @@ struct TcParams {
 };
 
 // PAIR CTAs of a cluster work on one tile of PAIR * 128 x BN: each loads 128 of A's rows and BN / PAIR
-// of B's.
-__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair, int parts) {
-  return (uint32_t)parts * (128u + (uint32_t)(bn / pair)) * 128u;
-}
+// of B's.  A stage of the ring holds 64 k of one part of both.
+__host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
-__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int parts, int stages) {
-  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair, parts);
+__host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
+  return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
 }
 
 // PAIR 2: the barrier may be the other CTA's.
@@ -145,11 +143,6 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
   }
 }
 
-// Parts (0 hi, 1 mid, 2 lo) of A and B in product p of six, smallest products first: an accumulator
-// that is still small loses less to each addition.  hi lo, lo hi, mid mid, hi mid, mid hi, hi hi.
-__device__ __forceinline__ constexpr uint32_t part_of_a(int p) { return (0x010120u >> (4 * p)) & 15u; }
-__device__ __forceinline__ constexpr uint32_t part_of_b(int p) { return (0x001102u >> (4 * p)) & 15u; }
-
 // PROMOTE (results that stay fp32): the tensor cores' sum is moved into fp32 registers, and added there
 // with rounding to nearest, after every 16 (24) instructions: in the accumulator every addition cuts
 // towards zero, which over thousands of them would cost a few units of 2^-18.
@@ -158,7 +151,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
   constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad, PROMOTE = sizeof(TO) == 4;
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
-  constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR, PARTS), A_BYTES = 128 * 128, B_BYTES = OWN_R * 128;   // A and B of a part
+  constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
@@ -234,25 +227,26 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const int c0 = w.c * TILE_C + side * 128, r0 = w.r * BN + side * OWN_R;
       for (int it = 0; it < iters; ++it) {
         const int k0 = (step0 + it) * kTcK;
-        // the leader's barrier counts both CTAs' bytes
-        const uint32_t bar = PAIR == 2 ? in_leader(full(s)) : full(s), a = ring + s * STAGE, b = a + PARTS * A_BYTES;
-        if (elect_one()) {
-          if (issued >= S) ok = ok && wait_phase(empty(s), ph ^ 1, P.status);
-          if (ok) {
-            if (side == 0) mbar_arrive_expect_tx(full(s), PAIR * STAGE);
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
+        for (int q = 0; q < PARTS; ++q) {                          // parts in the order of their use: hi, lo, mid
+          const int part = q == 0 ? 0 : 3 - q;
+          // the leader's barrier counts both CTAs' bytes
+          const uint32_t bar = PAIR == 2 ? in_leader(full(s)) : full(s), a = ring + s * STAGE, b = a + A_BYTES;
+          if (elect_one()) {
+            if (issued >= S) ok = ok && wait_phase(empty(s), ph ^ 1, P.status);
+            if (ok) {
+              if (side == 0) mbar_arrive_expect_tx(full(s), PAIR * STAGE);
 #pragma unroll
               for (int i = 0; i < BOXES_A; ++i)
-                tma_load_3d<PAIR>(a + p * A_BYTES + i * 8192, &map_a, A_K ? k0 : c0 + 64 * i, A_K ? c0 : k0, p, bar);
+                tma_load_3d<PAIR>(a + i * 8192, &map_a, A_K ? k0 : c0 + 64 * i, A_K ? c0 : k0, part, bar);
 #pragma unroll
               for (int i = 0; i < BOXES_B; ++i)
-                tma_load_3d<PAIR>(b + p * B_BYTES + i * 8192, &map_b, B_K ? k0 : r0 + 64 * i, B_K ? r0 : k0, p, bar);
+                tma_load_3d<PAIR>(b + i * 8192, &map_b, B_K ? k0 : r0 + 64 * i, B_K ? r0 : k0, part, bar);
             }
           }
+          ++issued;
+          if (++s == S) { s = 0; ph ^= 1; }
         }
-        ++issued;
-        if (++s == S) { s = 0; ph ^= 1; }
       }
     }
     // the copies requested so far land before the CTAs end; the leader's barriers count both CTAs'
@@ -264,32 +258,60 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     int s = 0, n = 0;                                              // n: chunks started
     uint32_t ph = 0;
     bool ok = true;
-    const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + PARTS * A_BYTES);
+    const uint32_t a0 = desc_lower<A_K>(ring), b0 = desc_lower<B_K>(ring + A_BYTES);
+    // 64 k of A in one stage against B in another
+    auto multiply = [&](uint32_t d, int sa, int sb, uint32_t keep) {
+      const uint32_t a = a0 + sa * (STAGE >> 4), b = b0 + sb * (STAGE >> 4);
+#pragma unroll
+      for (int k = 0; k < kTcK / 16; ++k)
+        mma_bf16<PAIR>(d, a + k * kDescStep<A_K>, b + k * kDescStep<B_K>, instr_desc<A_K, B_K>(BN, PAIR), k > 0 ? 1u : keep);
+    };
     for (int tile = first_tile; tile < P.tiles; tile += P.tile_step) {
       int in_chunk = 0;
       for (int it = 0; it < iters; ++it) {
-        const uint32_t a = a0 + s * (STAGE >> 4), b = b0 + s * (STAGE >> 4), d = tmem + (uint32_t)(n & 1) * ACC;
+        const uint32_t d = tmem + (uint32_t)(n & 1) * ACC;
         const bool last = in_chunk + 1 == chunk || it == iters - 1;
+        // with three parts: hi in stage s, lo in s1, mid in s2
+        int s1 = s + 1, s2 = s + 2;
+        uint32_t ph1 = ph, ph2 = ph;
+        if (PARTS == 3) {
+          if (s1 >= S) { s1 -= S; ph1 ^= 1; }
+          if (s2 >= S) { s2 -= S; ph2 ^= 1; }
+        }
         if (elect_one()) {
           if (in_chunk == 0) {
             if (n >= 2) ok = ok && wait_phase(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           }
           ok = ok && wait_phase(full(s), ph, P.status);
+          if constexpr (PARTS == 1) {
+            if (ok) multiply(d, s, s, (uint32_t)in_chunk);
+          } else {
+            // smallest products first: an accumulator that is still small loses less to each addition
+            ok = ok && wait_phase(full(s1), ph1, P.status);
+            if (ok) {
+              multiply(d, s, s1, (uint32_t)in_chunk);
+              multiply(d, s1, s, 1);
+              mma_commit<PAIR>(empty(s1));
+            }
+            ok = ok && wait_phase(full(s2), ph2, P.status);
+            if (ok) {
+              multiply(d, s2, s2, 1);
+              multiply(d, s, s2, 1);
+              multiply(d, s2, s, 1);
+              mma_commit<PAIR>(empty(s2));
+              multiply(d, s, s, 1);
+            }
+          }
           if (ok) {
-#pragma unroll
-            for (int p = PARTS == 1 ? 5 : 0; p < 6; ++p)
-#pragma unroll
-              for (int k = 0; k < kTcK / 16; ++k)
-                mma_bf16<PAIR>(d, a + part_of_a(p) * (A_BYTES >> 4) + k * kDescStep<A_K>, b + part_of_b(p) * (B_BYTES >> 4) + k * kDescStep<B_K>,
-                               instr_desc<A_K, B_K>(BN, PAIR), k > 0 || (PARTS == 3 && p > 0) ? 1u : (uint32_t)in_chunk);
             mma_commit<PAIR>(empty(s));
             if (last) mma_commit<PAIR>(acc_full(n & 1));
           }
         }
         ++in_chunk;
         if (last) { ++n; in_chunk = 0; }
-        if (++s == S) { s = 0; ph ^= 1; }
+        s += PARTS;
+        if (s >= S) { s -= S; ph ^= 1; }
       }
     }
     __syncwarp();

@@ -201,7 +201,7 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
         if (split > 1 && (split * 2 > ksteps || tiles > fit)) break;
         const double waves = (double)((tiles + fit - 1) / fit);
         // a step takes as long as its operands take to arrive, the epilogue as long as the tile is wide
-        double step = std::max(100.0, tc_stage_bytes(bn, pair, parts) / 126.0);
+        double step = std::max(100.0, parts * tc_stage_bytes(bn, pair) / 126.0);
         if (pair == 2 && a_strided) step *= 1.45;
         const double sums = 1000.0 + (double)((ksteps + split - 1) / split) * step, epilogue = 15.0 * bn / split;
         double t = split > 1 ? waves * (sums + 1100.0 + 19.0 * bn) : waves * std::max(sums, epilogue);
@@ -214,8 +214,8 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
   const auto kernel = linear_tc_kernel<KIND, T, TO, PARTS, BN, PAIR>;
-  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR, PARTS));
-  const uint32_t smem = tc_smem_bytes(BN, PAIR, PARTS, P.stages);
+  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR));
+  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages);
   static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
   const uint64_t bit = 1ull << (ops->device & 63);
   if (!(ready.load() & bit)) {
