@@ -335,7 +335,7 @@ gbmuf_status gbmuf_peer_destroy(gbmuf_peer* h);
  *     infinite gives NaN where the plain product would give an infinity), epilogues are computed
  *     in fp32 from the unrounded sum, and every output is rounded once, to nearest even.
  *   - Outputs may not overlap inputs or each other, except where a call says so.
- *   - A zero in rows, n_in or n_out is allowed: an empty sum is 0.
+ *   - A zero in rows, n_in or n_out is allowed: an empty sum is 0.  At most 2^31 - 2^16 each.
  *   - workspace: device memory of at least the bytes that the _workspace call of the same arguments
  *     gives (256-byte aligned; may be NULL when that is 0), not shared by calls that can overlap.
  *   - Calls only launch kernels and may be recorded into a stream capture.

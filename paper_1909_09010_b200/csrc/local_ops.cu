@@ -48,6 +48,7 @@ struct gbmuf_ops {
 
 struct gbmuf_clip {
   int device = 0, groups = 0, num_sms = 0;
+  bool ready = false;            // the table holds what set_tensors was last given
   int64_t count = 0;             // tensors with elements
   long long chunks = 0;
   int blocks = 0;
@@ -94,6 +95,7 @@ cudaError_t launch(void (*kernel)(P...), unsigned grid, unsigned cluster, int th
 gbmuf_status launched(const char* what, cudaError_t e) { return e == cudaSuccess ? GBMUF_OK : cuda_refuse(what, e); }
 
 size_t size_of(int32_t dtype) { return dtype == GBMUF_F32 ? 4 : 2; }
+constexpr int64_t kMostDim = 0x7fffffff - 0xffff;     // indices stay in 32 bits past the last tile
 bool is_dtype(int32_t d) { return d == GBMUF_F32 || d == GBMUF_BF16; }
 
 // A [rows][cols] operand: NULL only where allowed, aligned to its elements, rows that do not
@@ -102,7 +104,7 @@ const char* check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, 
   if (!p) return optional || rows == 0 || cols == 0 ? nullptr : "is NULL";
   if ((uintptr_t)p % size_of(dtype) != 0) return "is not aligned to its element type";
   if (rows > 0 && cols > 0 && ld < cols) return "has a row stride below its columns";
-  if (ld > ((int64_t)1 << 40)) return "has a row stride above 2^40";
+  if ((rows > 1 && ld > ((int64_t)1 << 40)) || (__int128)rows * std::max(ld, cols) > ((__int128)1 << 56)) return "has an extent above 2^56 elements";
   return nullptr;
 }
 #define CHECK_MATRIX(name, p, rows, cols, ld, dtype, optional)                                   \
@@ -111,8 +113,8 @@ const char* check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, 
 gbmuf_status check_sizes(const gbmuf_ops* ops, int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype, int32_t act) {
   if (!ops) return invalid("ops is NULL");
   if (rows < 0 || n_in < 0 || n_out < 0) return invalid("rows, n_in and n_out must not be negative");
-  if (rows > 0x7fffffff || n_in > 0x7fffffff || n_out > 0x7fffffff)
-    return refuse(GBMUF_ERR_UNSUPPORTED, "rows, n_in and n_out must be below 2^31");
+  if (rows > kMostDim || n_in > kMostDim || n_out > kMostDim)
+    return refuse(GBMUF_ERR_UNSUPPORTED, "rows, n_in and n_out must be at most 2^31 - 2^16");
   if (!is_dtype(dtype)) return invalid("dtype must be GBMUF_F32 or GBMUF_BF16");
   if (act < GBMUF_ACT_NONE || act > GBMUF_ACT_SIGMOID) return invalid("unknown activation");
   return GBMUF_OK;
@@ -588,8 +590,8 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
   return guarded([&]() -> gbmuf_status {
     if (!ops || !a) return invalid("ops and args must not be NULL");
     if (a->rows < 0 || a->vocab < 0) return invalid("rows and vocab must not be negative");
-    if (a->rows > 0x7fffffff || a->vocab > 0x7fffffff)
-      return refuse(GBMUF_ERR_UNSUPPORTED, "rows and vocab must be below 2^31");
+    if (a->rows > kMostDim || a->vocab > kMostDim)
+      return refuse(GBMUF_ERR_UNSUPPORTED, "rows and vocab must be at most 2^31 - 2^16");
     if (a->rows > 0 && a->vocab == 0) return invalid("vocab must not be 0");
     if (!is_dtype(a->dtype)) return invalid("dtype must be GBMUF_F32 or GBMUF_BF16");
     if (!(a->scale == a->scale)) return invalid("scale must not be NaN");
@@ -701,12 +703,11 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
     std::vector<unsigned char> image(partial_off, 0);
     if (!table.empty()) memcpy(image.data() + 256, table.data(), table.size() * sizeof(ClipEntry));
     if (!slots.empty()) memcpy(image.data() + slots_off, slots.data(), slots.size() * sizeof(int));
-    h->count = 0;                            // no usable table until the upload has succeeded
-    h->chunks = 0;
+    h->ready = false;                        // until the upload has succeeded
     if (!image.empty()) e = cudaMemcpy(h->table, image.data(), image.size(), cudaMemcpyHostToDevice);
     if (e != cudaSuccess) return cuda_refuse("upload of the gradient tensors' table", e);
     h->count = (int64_t)table.size(); h->chunks = chunks; h->blocks = blocks;
-    h->slots_off = slots_off; h->partial_off = partial_off;
+    h->slots_off = slots_off; h->partial_off = partial_off; h->ready = true;
     return GBMUF_OK;
   });
 }
@@ -738,6 +739,7 @@ static gbmuf_status clip_run(gbmuf_clip* h, bool scale, float max_norm, float* n
     if (!h) return invalid("handle is NULL");
     if (!norms || (uintptr_t)norms % 4 != 0) return invalid("norms must be a device pointer to fp32");
     if (!(max_norm == max_norm)) return invalid("max_norm must not be NaN");
+    if (!h->ready) return refuse(GBMUF_ERR_BAD_STATE, "the last set_tensors failed");
     DeviceGuard guard(h->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
     cudaStream_t st = (cudaStream_t)stream;
