@@ -465,6 +465,14 @@ def _matrix(name, t, shape, dtype, device):
     return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
+def _result(name, given, like, shape, dtype, device):
+    """(tensor, address, row stride) of a result: the one handed in, or a new one on like's device."""
+    if given is None:
+        t = like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr(), shape[1]
+    return (given, *_matrix(name, given, shape, dtype, device))
+
+
 def _vector(name, t, n, dtype, device):
     if t is None:
         return 0
@@ -550,10 +558,8 @@ class LocalOps(_OnDevice):
         pb = _vector("bias", bias, n_out, dtype, dev)
         pr, lr = _matrix("residual", residual, shape, dtype, dev)
         act = ACTIVATIONS[activation]
-        y = out if out is not None else x.new_empty(shape)
-        py, ly = _matrix("out", y, shape, dtype, dev)
-        z = z_out if z_out is not None else (x.new_empty(shape) if keep_z else None)
-        pz, lz = _matrix("z_out", z, shape, dtype, dev)
+        y, py, ly = _result("out", out, x, shape, dtype, dev)
+        z, pz, lz = _result("z_out", z_out, x, shape, dtype, dev) if keep_z or z_out is not None else (None, 0, 0)
         self._linear(self._L.gbmuf_linear_forward, self._L.gbmuf_linear_forward_workspace, _pack_forward,
                      (rows, n_in, n_out, px, pw, pb, pr, py, pz, lx, lw, lr, ly, lz, code, act),
                      code == BF16 and not ((px | pw) & 15 or (lx | lw) & 7), x, stream)
@@ -573,15 +579,14 @@ class LocalOps(_OnDevice):
         pr, lr = _matrix("residual", residual, shape, dtype, dev)
         pz, lz = _matrix("z_prev", z_prev, shape, dtype, dev)
         act = ACTIVATIONS[activation]
-        dx, dp = dx_out, dz_out
-        if dx is None and (want_dx or z_prev is None):
-            dx = dz.new_empty(shape)
-        if dp is None and z_prev is not None:
-            dp = dz.new_empty(shape)
-        if z_prev is None and dp is not None:
+        if z_prev is None and dz_out is not None:
             raise ValueError("dz_out needs z_prev")
-        px, lx = _matrix("dx_out", dx, shape, dtype, dev)
-        pp, lp = _matrix("dz_out", dp, shape, dtype, dev)
+        dx = dp = None
+        px = lx = pp = lp = 0
+        if want_dx or z_prev is None or dx_out is not None:
+            dx, px, lx = _result("dx_out", dx_out, dz, shape, dtype, dev)
+        if z_prev is not None:
+            dp, pp, lp = _result("dz_out", dz_out, dz, shape, dtype, dev)
         self._linear(self._L.gbmuf_linear_backward_input, self._L.gbmuf_linear_backward_input_workspace,
                      _pack_backward_input,
                      (rows, n_in, n_out, pd, pw, pr, pz, px, pp, ldd, lw, lr, lz, lx, lp, code, act),
@@ -607,10 +612,9 @@ class LocalOps(_OnDevice):
             grad_dtype = dtype
         if accumulate and (dw_out is None or (want_bias and dbias_out is None)):
             raise ValueError("accumulate adds to dw_out and dbias_out: hand them in")
-        dw = dw_out if dw_out is not None else dz.new_empty(shape, dtype=grad_dtype)
+        dw, pw, lw = _result("dw_out", dw_out, dz, shape, grad_dtype, dev)
         db = dbias_out if dbias_out is not None else (
             dz.new_empty((n_out,), dtype=grad_dtype) if want_bias else None)
-        pw, lw = _matrix("dw_out", dw, shape, grad_dtype, dev)
         pb = _vector("dbias_out", db, n_out, grad_dtype, dev)
         self._linear(self._L.gbmuf_linear_backward_weight, self._L.gbmuf_linear_backward_weight_workspace,
                      _pack_backward_weight,
@@ -646,18 +650,16 @@ class LocalOps(_OnDevice):
         pl, ll = _matrix("logits", logits, shape, dtype, dev)
         pt = _vector("targets", targets, rows, torch.int64, dev)
         pw = _vector("row_weight", row_weight, rows, torch.float32, dev)
-        d = dlogits_out
-        if d is None and want_grad:
-            d = logits.new_empty(shape)
-        pd, ldd = _matrix("dlogits_out", d, shape, dtype, dev)
-        both = logits.new_empty((2, rows), dtype=torch.float32)
-        at = both.data_ptr()
-        args = _pack_cross_entropy(rows, vocab, pl, pt, pw, at, at + 4 * rows, pd, ll, ldd, ignore_index,
-                                   code, scale)
+        d, pd, ldd = None, 0, 0
+        if want_grad or dlogits_out is not None:
+            d, pd, ldd = _result("dlogits_out", dlogits_out, logits, shape, dtype, dev)
+        loss = logits.new_empty((rows,), dtype=torch.float32)
+        lse = logits.new_empty((rows,), dtype=torch.float32)
+        args = _pack_cross_entropy(rows, vocab, pl, pt, pw, loss.data_ptr(), lse.data_ptr(), pd, ll, ldd,
+                                   ignore_index, code, scale)
         st = self._L.gbmuf_cross_entropy(self._h, args, self._on(stream))
         if st != GBMUF_OK:
             self._check(st)
-        loss, lse = both.unbind(0)
         return (loss, lse) if d is None else (loss, lse, d)
 
     def device_status(self, stream=None) -> int:

@@ -326,15 +326,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       else mbar_arrive(acc_empty(b));
     }
   };
-  auto bias_of = [&](int c) {
-    return KIND == kForward && P.E.bias && c < P.C ? to_f32(static_cast<const T*>(P.E.bias)[c]) : 0.0f;
-  };
+  // Asked for before the wait for the sums and converted after it: a conversion here would wait for it.
+  auto bias_of = [&](int c) { return KIND == kForward && P.E.bias && c < P.C ? static_cast<const T*>(P.E.bias)[c] : from_f32<T>(0.0f); };
   if (warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const int c = w.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL;
-      const float bias = bias_of(c);
+      const T bias = bias_of(c);
       if (PROMOTE) {
         float acc[NCOL];
 #pragma unroll
@@ -363,7 +362,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
           for (int i = 0; i < N; ++i) v[i] = acc[j + i];
           F.ask(P.E, r0 + j, c, P.R, P.C, lane);
-          F.finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
+          F.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
         }
       } else {
         // what the epilogue reads is requested one strip ahead, the first one during the sums
@@ -381,7 +380,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
           Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
-          now.finish(P.E, r0 + j, c, P.R, P.C, lane, bias, v);
+          now.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -441,7 +440,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       const float* const sums = reinterpret_cast<const float*>(smem + kTcHead) + quad * 32 + lane;
       const Walk w = first();
       const int c = w.c * 128 + quad * 32 + lane;
-      const float bias = bias_of(c);
+      const T bias = bias_of(c);
       for (int i = 4 * part; i < cols; i += kTcFinishers) {
         const int r = w.r * BN + rank * cols + i;
         Finisher<KIND, T, TO, 4> F;
@@ -452,7 +451,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           v[x] = sums[(i + x) * 128];
           for (int q = 1; q < P.split; ++q) v[x] += sums[(q * cols + i + x) * 128];
         }
-        F.finish(P.E, r, c, P.R, P.C, lane, bias, v);
+        F.finish(P.E, r, c, P.R, P.C, lane, to_f32(bias), v);
       }
     }
   }
