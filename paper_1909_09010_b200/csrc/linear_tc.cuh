@@ -21,6 +21,11 @@ namespace {
 // BN = 256, which is what bounds a single CTA.  Warp 0 loads 64 k of both operands per step with the copy engine (128-byte
 // swizzle), warp 1 issues the matrix instructions, the warps from 4 on finish the sums.  Two accumulators:
 // one is finished while the next is summed.
+//
+// Measured: 2,048 x 1,024 x 100,000 bf16 292 us (1,437 TFLOP/s, 89 % of a library product's rate; pairs of
+// CTAs, single ones 327); 8,192 x 1,024 x 4,096 to fp32 58 us (1,185 TFLOP/s, bound by operand traffic
+// from L2); 4,096 x 512 x 2,048 with gelu 18.7 us, of which the two epilogues of a CTA are 10: 16
+// finishing warps hide their own latencies better than 8 (24 us then), 32-row strips spill (20 us).
 constexpr int kTcFinishers = 16;               // warps
 constexpr int kTcThreads = 128 + 32 * kTcFinishers;
 constexpr int kTcK = 64;                       // k per step

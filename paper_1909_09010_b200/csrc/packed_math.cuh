@@ -1,4 +1,5 @@
-// Two fp32 operations per instruction, and single instructions of the special-function unit.
+// Two fp32 operations per instruction, single instructions of the special-function unit, and what the
+// local-step kernels add to primitives.cuh.
 // Part of libgbmuf (CUDA, sm_100a); included by local_ops.cu.
 #ifndef GBMUF_CSRC_PACKED_MATH_CUH
 #define GBMUF_CSRC_PACKED_MATH_CUH
@@ -49,6 +50,18 @@ __device__ __forceinline__ float min_nan(float x, float y) {
   float r;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
   return r;
+}
+
+// A bulk copy that says whether its source will be fetched again soon: the L2 cache then keeps it
+// rather than what only passes through (cross-entropy of 2,048 x 267,735 bf16: 464 -> 422 us).
+__device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, bool again) {
+  uint64_t keep, pass;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pass));
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar), "l"(again ? keep : pass)
+      : "memory");
 }
 
 // mbar_wait_bounded with the first try in line.
