@@ -582,3 +582,52 @@ def test_refusals(ops):
     clip = binding.GradClip([(x, None, 0)])
     with pytest.raises(binding.GbmufError):
         clip.clip(math.nan)
+
+
+# ------------------------------------------------------- products large enough for every launch shape
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,n_in,n_out", [(2048, 1024, 20000), (4096, 512, 2048), (8192, 4096, 1024),
+                                             (64, 4096, 1024), (128, 4096, 1024), (16, 2048, 2048), (256, 1024, 30000),
+                                             (8200, 264, 250), (1000, 4104, 1032), (33, 8192, 100)])
+def test_linear_large(ops, dtype, rows, n_in, n_out):
+    g = gen(rows + n_in + n_out)
+    x, w, b = rnd(g, (rows, n_in), dtype), rnd(g, (n_out, n_in), dtype, n_in ** -0.5), rnd(g, (n_out,), dtype, 0.2)
+    dz, res = rnd(g, (rows, n_out), dtype, 1e-2), rnd(g, (rows, n_in), dtype, 1e-2)
+    xd, wd, dd = x.double(), w.double(), dz.double()
+    y, z = ops.linear_forward(x, w, bias=b, activation="silu", keep_z=True)
+    ref = xd @ wd.t() + b.double()
+    tol = sum_error(xd.abs(), wd.abs().t(), n_in)
+    check(z, ref, tol + 2.0 ** -23 * ref.abs(), dtype, "z")
+    check(y, act64(ref, "silu"), 1.25 * tol + 1e-6 * (1 + ref.abs()), dtype, "y")
+    dx, dp = ops.linear_backward_input(dz, w, residual=res, z_prev=x, activation="tanh", want_dx=True)
+    ref = dd @ wd
+    tol = sum_error(dd.abs(), wd.abs(), n_out) + 2.0 ** -23 * (ref.abs() + res.double().abs())
+    ref = ref + res.double()
+    check(dx, ref, tol, dtype, "dx")
+    check(dp, ref * slope64(xd, "tanh"), 1.25 * tol + ref.abs() * 1e-6 * (1 + xd.abs()), dtype, "dz_prev")
+    for grad in (F, BF):
+        dw, db = ops.linear_backward_weight(dz, x, grad_dtype=grad)
+        check(dw, dd.t() @ xd, sum_error(dd.abs().t(), xd.abs(), rows), grad, "dw")
+        check(db, dd.sum(0), (rows + 8) * 2.0 ** -23 * dd.abs().sum(0), grad, "dbias")
+    assert ops.device_status() == 0
+
+
+def test_two_streams_at_once(ops):
+    """Calls on two streams share the handle; results are those of calls one after the other."""
+    g = gen(77)
+    jobs = []
+    for i in range(2):
+        x, w = rnd(g, (700 + i, 515), F), rnd(g, (333, 515), F)
+        logits, t = rnd(g, (40, 50_001), BF, 3.0), torch.randint(0, 50_001, (40,), generator=g, device="cuda")
+        jobs.append((x, w, logits, t))
+    ref = [(ops.linear_forward(x, w, activation="gelu"), *ops.cross_entropy(l, t)) for x, w, l, t in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for s, (x, w, l, t) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                got.append((ops.linear_forward(x, w, activation="gelu"), *ops.cross_entropy(l, t)))
+        torch.cuda.synchronize()
+        for a, b in zip(got, ref):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
