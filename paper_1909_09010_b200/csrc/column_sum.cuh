@@ -7,7 +7,9 @@ namespace {
 
 // out[c] (+)= sum over the rows of a [R][C] matrix.  A cluster takes a strip of columns (VEC: 128
 // bytes wide, 16 bytes per thread; else 32 columns) and shares its rows; sums are joined through
-// shared memory and rank 0's shared memory, in a fixed order.  Bound by memory: 8,192 x 4,096 bf16 in 12 to
+// shared memory and rank 0's shared memory, in a fixed order; every rank arrives at the cluster's barrier
+// first thing and waits for it after its rows, so that rank 0 has started before anybody writes there.
+// Bound by memory: 8,192 x 4,096 bf16 in 12 to
 // 14 us (5 TB/s); one block per strip without a cluster took 366.
 template <typename T, typename TO, bool VEC>
 __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long ld, long long R, long long C, TO* out,
@@ -15,6 +17,7 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long l
   constexpr int W = VEC ? 16 / (int)sizeof(T) : 1, L = VEC ? 8 : 32, ROWS = 256 / L, COLS = L * W;
   __shared__ float part[ROWS][COLS + 1];
   __shared__ float ranks[8][COLS];
+  cluster_arrive();
   grid_launch_dependents();
   grid_dependency_wait();
   uint32_t share, rank;
@@ -39,6 +42,7 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long l
 #pragma unroll
   for (int i = 0; i < W; ++i) part[row][lane * W + i] = s[i];
   __syncthreads();
+  cluster_wait();
   if (threadIdx.x < COLS) {
     float t = part[0][threadIdx.x];
     for (int i = 1; i < ROWS; ++i) t += part[i][threadIdx.x];

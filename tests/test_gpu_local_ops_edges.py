@@ -1,0 +1,40 @@
+"""Cases of the local-step operators that once went wrong or were never reached, against 64-bit values."""
+import pytest
+import torch
+
+from paper_1909_09010_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ops():
+    return binding.local_ops(0)
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def rnd(g, shape, dtype, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n_out", [8, 33, 1024, 40_000])
+@pytest.mark.parametrize("rows", [1, 63, 64, 255, 300, 700, 4096])
+def test_bias_gradient_of_every_cluster_size(ops, dtype, rows, n_out):
+    """Column sums by clusters of 1, 2, 4 and 8 CTAs, by pieces and element by element, many times over."""
+    dz = rnd(gen(rows + n_out), (rows, n_out), dtype)
+    x = torch.ones((rows, 8), dtype=dtype, device="cuda")
+    ref, size = dz.double().sum(0), dz.double().abs().sum(0)
+    first = ops.linear_backward_weight(dz, x, grad_dtype=F)[1]
+    # an fp32 sum of `rows` terms in any order, each addition off by half a unit of a partial sum
+    assert bool(((first.double() - ref).abs() <= rows * 2.0 ** -24 * size).all())
+    for _ in range(20):
+        assert torch.equal(ops.linear_backward_weight(dz, x, grad_dtype=F)[1], first)
+    assert ops.device_status() == 0
