@@ -460,6 +460,7 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
                          ops->tc_clusters);
     if (e == cudaSuccess) e = cudaMalloc(&ops->d_status, 256);
     if (e == cudaSuccess) e = cudaMemset(ops->d_status, 0, 256);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);          // other streams do not wait for the default one
     if (e != cudaSuccess) {
       cudaGetLastError();
       cudaFree(ops->d_status);
@@ -705,6 +706,9 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
     if (!slots.empty()) memcpy(image.data() + slots_off, slots.data(), slots.size() * sizeof(int));
     h->ready = false;                        // until the upload has succeeded
     if (!image.empty()) e = cudaMemcpy(h->table, image.data(), image.size(), cudaMemcpyHostToDevice);
+    // a copy from pageable memory may return before it has landed, and streams other than the default one
+    // would not wait for it
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) return cuda_refuse("upload of the gradient tensors' table", e);
     h->count = (int64_t)table.size(); h->chunks = chunks; h->blocks = blocks;
     h->slots_off = slots_off; h->partial_off = partial_off; h->ready = true;

@@ -1,4 +1,6 @@
 """Cases of the local-step operators that once went wrong or were never reached, against 64-bit values."""
+import math
+
 import pytest
 import torch
 
@@ -38,3 +40,31 @@ def test_bias_gradient_of_every_cluster_size(ops, dtype, rows, n_out):
     for _ in range(20):
         assert torch.equal(ops.linear_backward_weight(dz, x, grad_dtype=F)[1], first)
     assert ops.device_status() == 0
+
+
+def test_clip_on_another_stream_right_after_new_tensors():
+    """The table of the tensors is on the GPU when create and set_tensors return, whatever stream comes next
+    and however much the default stream still has to do."""
+    g = gen(11)
+    sets = [[(rnd(g, s, F), torch.zeros(s, device="cuda"), i % 2) for i, s in enumerate(shapes)]
+            for shapes in ([(50_000,), (7, 9)], [(3,), (1000, 40), (123,)], [(9001,), (5,), (64, 64), (2,)])]
+    refs = [[math.sqrt(sum(float((t.double() ** 2).sum()) for t, _, k in e if k == j)) for j in range(2)] for e in sets]
+    norms = torch.zeros(2, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for turn in range(30):
+        i = turn % 3
+        torch.cuda._sleep(1_000_000)                       # half a millisecond of work on the default stream
+        if turn % 10 == 0:
+            clip = binding.GradClip(sets[i], groups=2)
+        else:
+            clip.set_tensors(sets[i])
+        clip.clip(1.0, norms_out=norms, stream=side)
+        side.synchronize()
+        assert all(abs(float(n) - r) <= 2.0 ** -22 * r for n, r in zip(norms, refs[i]))
+        for t, out, k in sets[i]:
+            assert torch.allclose(out.double(), t.double() / refs[i][k], rtol=2.0 ** -20, atol=0)
+        for _, out, _ in sets[i]:
+            out.zero_()
+        torch.cuda.synchronize()
+    assert clip.device_status() == 0
