@@ -460,7 +460,10 @@ gbmuf_status gbmuf_clip_create(int32_t device, int32_t groups, int64_t count,
 gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_grad_tensor* tensors_host);
 gbmuf_status gbmuf_clip_norms(gbmuf_clip* h, float* norms_device, void* stream);
 gbmuf_status gbmuf_clip_scale(gbmuf_clip* h, float max_norm, float* norms_device, void* stream);
-gbmuf_status gbmuf_clip_device_status(gbmuf_clip* h, void* stream, int32_t* out); /* as gbmuf_device_status */
+/* As gbmuf_device_status.  set_tensors leaves the word as it is. */
+gbmuf_status gbmuf_clip_device_status(gbmuf_clip* h, void* stream, int32_t* out);
+/* As gbmuf_selftest_wait_timeout, on this handle's status word; does not wait for the kernel. */
+gbmuf_status gbmuf_clip_selftest_wait_timeout(gbmuf_clip* h, void* stream);
 gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h);
 
 /* Sentence about the last error on this context ("" if none); valid until the next call on it.

@@ -34,7 +34,7 @@ EXPORTS = ["gbmuf_create", "gbmuf_set_partition", "gbmuf_init", "gbmuf_local_per
            "gbmuf_linear_backward_weight_workspace", "gbmuf_linear_backward_weight",
            "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_clip_create",
            "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_device_status",
-           "gbmuf_clip_destroy"]
+           "gbmuf_clip_selftest_wait_timeout", "gbmuf_clip_destroy"]
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 
 
@@ -152,6 +152,7 @@ def lib() -> ctypes.CDLL:
     L.gbmuf_clip_norms.argtypes = [vp, vp, vp]
     L.gbmuf_clip_scale.argtypes = [vp, f32, vp, vp]
     L.gbmuf_clip_device_status.argtypes = [vp, vp, ctypes.POINTER(i32)]
+    L.gbmuf_clip_selftest_wait_timeout.argtypes = [vp, vp]
     L.gbmuf_clip_destroy.argtypes = [vp]
     L.gbmuf_last_error.argtypes = [vp]
     L.gbmuf_last_error.restype = ctypes.c_char_p
@@ -790,6 +791,10 @@ class GradClip(_OnDevice):
         v = ctypes.c_int32(-1)
         self._check(self._L.gbmuf_clip_device_status(self._h, self._on(stream), ctypes.byref(v)))
         return v.value
+
+    def selftest_wait_timeout(self, stream=None):
+        """``gbmuf_clip_selftest_wait_timeout``: a wait that expires, after which ``device_status`` says so."""
+        self._check(self._L.gbmuf_clip_selftest_wait_timeout(self._h, self._on(stream)))
 
     def destroy(self):
         if self._h:

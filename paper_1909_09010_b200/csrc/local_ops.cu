@@ -52,9 +52,9 @@ struct gbmuf_clip {
   int64_t count = 0;             // tensors with elements
   long long chunks = 0;
   int blocks = 0;
-  void* table = nullptr;         // status word, [ClipEntry][slots][partial sums]
+  int32_t* d_status = nullptr;
+  void* table = nullptr;         // [ClipEntry][slots][partial sums]
   size_t table_bytes = 0, slots_off = 0, partial_off = 0;
-  int32_t* status() const { return static_cast<int32_t*>(table); }
   WorkMarks work;
 };
 
@@ -688,7 +688,7 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
       }
     DeviceGuard guard(h->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    const size_t slots_off = 256 + (table.size() * sizeof(ClipEntry) + 255) / 256 * 256;
+    const size_t slots_off = (table.size() * sizeof(ClipEntry) + 255) / 256 * 256;
     const size_t partial_off = slots_off + (slots.size() * sizeof(int) + 255) / 256 * 256;
     const size_t bytes = partial_off + ((size_t)blocks + h->groups) * sizeof(double);
     cudaError_t e = h->work.wait();
@@ -702,7 +702,7 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
       h->table_bytes = bytes;
     }
     std::vector<unsigned char> image(partial_off, 0);
-    if (!table.empty()) memcpy(image.data() + 256, table.data(), table.size() * sizeof(ClipEntry));
+    if (!table.empty()) memcpy(image.data(), table.data(), table.size() * sizeof(ClipEntry));
     if (!slots.empty()) memcpy(image.data() + slots_off, slots.data(), slots.size() * sizeof(int));
     h->ready = false;                        // until the upload has succeeded
     if (!image.empty()) e = cudaMemcpy(h->table, image.data(), image.size(), cudaMemcpyHostToDevice);
@@ -730,9 +730,11 @@ gbmuf_status gbmuf_clip_create(int32_t device, int32_t groups, int64_t count, co
     cudaError_t e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)clip_norm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)clip_scale_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipSmem);
-    if (e != cudaSuccess) { cudaGetLastError(); st = cuda_refuse("device properties", e); }
+    if (e == cudaSuccess) e = cudaMalloc(&h->d_status, 256);
+    if (e == cudaSuccess) e = cudaMemset(h->d_status, 0, 256);         // set_tensors waits for it
+    if (e != cudaSuccess) { cudaGetLastError(); st = cuda_refuse("set-up of the clipping handle", e); }
     if (st == GBMUF_OK) st = gbmuf_clip_set_tensors(h, count, tensors);
-    if (st != GBMUF_OK) { cudaFree(h->table); delete h; return st; }
+    if (st != GBMUF_OK) { cudaFree(h->d_status); cudaFree(h->table); delete h; return st; }
     *out = h;
     return GBMUF_OK;
   });
@@ -749,8 +751,8 @@ static gbmuf_status clip_run(gbmuf_clip* h, bool scale, float max_norm, float* n
     cudaStream_t st = (cudaStream_t)stream;
     ClipParams P{};
     unsigned char* const base = static_cast<unsigned char*>(h->table);
-    P.status = h->status();
-    P.entries = reinterpret_cast<const ClipEntry*>(base + 256);
+    P.status = h->d_status;
+    P.entries = reinterpret_cast<const ClipEntry*>(base);
     P.slots = reinterpret_cast<const int*>(base + h->slots_off);
     P.partial = reinterpret_cast<double*>(base + h->partial_off);
     P.norms = norms; P.chunks = h->chunks; P.count = (int)h->count; P.groups = h->groups; P.blocks = h->blocks;
@@ -776,7 +778,19 @@ gbmuf_status gbmuf_clip_scale(gbmuf_clip* h, float max_norm, float* norms, void*
 gbmuf_status gbmuf_clip_device_status(gbmuf_clip* h, void* stream, int32_t* out) {
   return guarded([&]() -> gbmuf_status {
     if (!h || !out) return invalid("handle and out must not be NULL");
-    return read_status(h->device, h->status(), stream, out);
+    return read_status(h->device, h->d_status, stream, out);
+  });
+}
+
+gbmuf_status gbmuf_clip_selftest_wait_timeout(gbmuf_clip* h, void* stream) {
+  return guarded([&]() -> gbmuf_status {
+    if (!h) return invalid("handle is NULL");
+    DeviceGuard guard(h->device);
+    if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
+    wait_timeout_selftest_kernel<<<1, 32, 0, (cudaStream_t)stream>>>(h->d_status, h->d_status + 1);
+    const cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) h->work.note((cudaStream_t)stream);
+    return launched("launch of the wait-timeout self-test", e);
   });
 }
 
@@ -788,6 +802,7 @@ gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h) {
     if (guard.ok) {
       if (h->work.wait() != cudaSuccess) rc = GBMUF_ERR_CUDA;
       h->work.release();
+      cudaFree(h->d_status);
       cudaFree(h->table);
     } else {
       rc = GBMUF_ERR_CUDA;

@@ -63,8 +63,18 @@ def test_clip_on_another_stream_right_after_new_tensors():
         side.synchronize()
         assert all(abs(float(n) - r) <= 2.0 ** -22 * r for n, r in zip(norms, refs[i]))
         for t, out, k in sets[i]:
-            assert torch.allclose(out.double(), t.double() / refs[i][k], rtol=2.0 ** -20, atol=0)
+            assert torch.allclose(out.double(), t.double() / max(1.0, refs[i][k]), rtol=2.0 ** -20, atol=0)
         for _, out, _ in sets[i]:
             out.zero_()
         torch.cuda.synchronize()
     assert clip.device_status() == 0
+
+
+def test_new_tensors_keep_a_status_nobody_has_read():
+    x, out = torch.ones(1000, device="cuda"), torch.zeros(1000, device="cuda")
+    clip = binding.GradClip([(x, out, 0)])
+    assert clip.device_status() == binding.GBMUF_OK
+    clip.selftest_wait_timeout()                           # two seconds, then the word is set
+    clip.set_tensors([(x[:500], None, 0), (x[500:], out[500:], 0)])
+    assert clip.device_status() == binding.ERR_TIMEOUT and clip.device_status() == binding.GBMUF_OK
+    assert abs(float(clip.clip(1.0)[0]) - 1000 ** 0.5) < 1e-5
