@@ -447,7 +447,8 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
  *   gbmuf_clip_scale: the norms, and out = grad * (max_norm / max(norm_g, max_norm)); max_norm <= 0
  *     copies without clipping.  A group whose norm is not finite has its outputs filled with zeros,
  *     so that the worker's step leaves theta and the accumulator as they are; its norm tells.
- * Both may be recorded into a stream capture. */
+ * Both may be recorded into a stream capture: a graph goes on with the tensors that the handle had
+ * then, also after set_tensors, until the handle is destroyed. */
 typedef struct gbmuf_clip gbmuf_clip;
 typedef struct {
   const void* grad;

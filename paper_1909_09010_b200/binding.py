@@ -760,7 +760,8 @@ class GradClip(_OnDevice):
         return arr
 
     def set_tensors(self, entries):
-        """New tensors (and groups) for the same number of groups; waits for this handle's work."""
+        """New tensors (and groups) for the same number of groups; waits for this handle's work.  A graph
+        recorded before goes on with the tensors of then, which the caller keeps alive for it."""
         entries = list(entries)
         self._check(self._L.gbmuf_clip_set_tensors(self._h, len(entries), self._table(entries)))
         self._keep = entries

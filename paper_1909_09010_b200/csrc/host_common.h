@@ -47,19 +47,21 @@ struct WorkMarks {
   struct Mark { cudaStream_t s; cudaEvent_t ev; };
   std::vector<Mark> marks;
   static constexpr size_t kMaxStreams = 16;
-  void note(cudaStream_t st) {
-    if (is_capturing(st)) return;
+  // false: the work went into a stream capture
+  bool note(cudaStream_t st) {
+    if (is_capturing(st)) return false;
     for (Mark& mk : marks)
-      if (mk.s == st) { cudaEventRecord(mk.ev, st); return; }
+      if (mk.s == st) { cudaEventRecord(mk.ev, st); return true; }
     if (marks.size() == kMaxStreams) {               // many streams: retire the oldest mark
       cudaEventSynchronize(marks.front().ev);
       cudaEventDestroy(marks.front().ev);
       marks.erase(marks.begin());
     }
     Mark mk{st, nullptr};
-    if (cudaEventCreateWithFlags(&mk.ev, cudaEventDisableTiming) != cudaSuccess) { cudaGetLastError(); return; }
+    if (cudaEventCreateWithFlags(&mk.ev, cudaEventDisableTiming) != cudaSuccess) { cudaGetLastError(); return true; }
     cudaEventRecord(mk.ev, st);
     marks.push_back(mk);
+    return true;
   }
   cudaError_t wait() {
     cudaError_t first = cudaSuccess;

@@ -55,6 +55,8 @@ struct gbmuf_clip {
   int32_t* d_status = nullptr;
   void* table = nullptr;         // [ClipEntry][slots][partial sums]
   size_t table_bytes = 0, slots_off = 0, partial_off = 0;
+  bool in_graph = false;         // a stream capture has recorded the table's address and sizes
+  std::vector<void*> earlier;    // tables that graphs may still read
   WorkMarks work;
 };
 
@@ -693,13 +695,15 @@ gbmuf_status gbmuf_clip_set_tensors(gbmuf_clip* h, int64_t count, const gbmuf_gr
     const size_t bytes = partial_off + ((size_t)blocks + h->groups) * sizeof(double);
     cudaError_t e = h->work.wait();
     if (e != cudaSuccess) return cuda_refuse("wait for the handle's earlier work", e);
-    if (bytes > h->table_bytes) {
+    if (bytes > h->table_bytes || h->in_graph) {
+      if (h->in_graph) h->earlier.reserve(h->earlier.size() + 1);
       void* fresh = nullptr;
       e = cudaMalloc(&fresh, bytes);
       if (e != cudaSuccess) { cudaGetLastError(); return refuse(GBMUF_ERR_ALLOC, "table of the gradient tensors"); }
-      cudaFree(h->table);
+      if (h->in_graph) h->earlier.push_back(h->table); else cudaFree(h->table);
       h->table = fresh;
       h->table_bytes = bytes;
+      h->in_graph = false;
     }
     std::vector<unsigned char> image(partial_off, 0);
     if (!table.empty()) memcpy(image.data(), table.data(), table.size() * sizeof(ClipEntry));
@@ -763,7 +767,7 @@ static gbmuf_status clip_run(gbmuf_clip* h, bool scale, float max_norm, float* n
       e = scale ? launch(clip_scale_kernel, (unsigned)h->blocks, 1, kClipThreads, kClipSmem, st, P)
                 : launch(clip_finish_kernel, (unsigned)std::min(h->groups, h->num_sms), 1, kClipWorkers, 0, st, P);
     if (e != cudaSuccess) return cuda_refuse("launch of the gradient-norm kernels", e);
-    h->work.note(st);
+    if (!h->work.note(st)) h->in_graph = true;
     return GBMUF_OK;
   });
 }
@@ -804,6 +808,7 @@ gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h) {
       h->work.release();
       cudaFree(h->d_status);
       cudaFree(h->table);
+      for (void* t : h->earlier) cudaFree(t);
     } else {
       rc = GBMUF_ERR_CUDA;
     }

@@ -78,3 +78,31 @@ def test_new_tensors_keep_a_status_nobody_has_read():
     clip.set_tensors([(x[:500], None, 0), (x[500:], out[500:], 0)])
     assert clip.device_status() == binding.ERR_TIMEOUT and clip.device_status() == binding.GBMUF_OK
     assert abs(float(clip.clip(1.0)[0]) - 1000 ** 0.5) < 1e-5
+
+
+@pytest.mark.parametrize("more", [False, True])
+def test_graph_keeps_the_tensors_it_was_recorded_with(more):
+    """New tensors, fewer or many more, neither change nor invalidate what a graph does."""
+    g = gen(13)
+    first = [(rnd(g, s, F), torch.zeros(s, device="cuda"), 0) for s in [(300_000,), (41, 7)]]
+    shapes = [(777,)] * 500 if more else [(5,)]
+    second = [(rnd(g, s, F), torch.zeros(s, device="cuda"), 0) for s in shapes]
+    length = lambda e: math.sqrt(sum(float((t.double() ** 2).sum()) for t, _, _ in e))              # noqa: E731
+    clip = binding.GradClip(first)
+    norms, graph = torch.zeros(1, device="cuda"), torch.cuda.CUDAGraph()
+    clip.clip(0.5)
+    with torch.cuda.graph(graph):
+        clip.clip(0.5, norms_out=norms)
+    want = [out.clone() for _, out, _ in first]
+    clip.set_tensors(second)
+    for _ in range(2):
+        for _, out, _ in first:
+            out.zero_()
+        graph.replay()
+        assert abs(float(clip.clip(0.5)[0]) - length(second)) <= 2.0 ** -22 * length(second)
+        assert abs(float(norms[0]) - length(first)) <= 2.0 ** -22 * length(first)
+        assert all(torch.equal(out, w) for (_, out, _), w in zip(first, want))
+        clip.set_tensors(second[:1])
+        clip.set_tensors(second)
+    torch.cuda.synchronize()
+    del graph
