@@ -516,19 +516,36 @@ class _OnDevice:
             return self._raw_stream(self.device)
         return getattr(stream, "cuda_stream", stream)
 
+    def _on_stream(self, stream, given, call, *args):
+        """``call(*args)`` with ``stream`` as torch's current one: what it allocates (results, workspace)
+        then comes from memory whose earlier uses are ordered before the call.  New results (not among
+        ``given``) may be used, and dropped, on the caller's stream."""
+        torch = self._torch
+        if not hasattr(stream, "cuda_stream"):                      # a handle; 1 and 0 name the same stream
+            stream = torch.cuda.ExternalStream(0 if stream == 1 else stream, device=self.device)
+        caller = torch.cuda.current_stream(self.device)
+        if stream.device.index != self.device:
+            raise ValueError(f"stream is on {stream.device}, not on cuda:{self.device}")
+        with torch.cuda.stream(stream):
+            results = call(*args)
+        for t in results if isinstance(results, tuple) else (results,):
+            if not any(t is g for g in given):
+                t.record_stream(caller)
+        return results
+
 
 class LocalOps(_OnDevice):
     """``gbmuf_ops_*``: linear layers with their gradients and the loss, on one device.  Tensors are
-    torch tensors on it; results that are not handed in are allocated by torch on its current
-    stream, and so is the workspace of a call that needs one.  ``stream`` (default: the current one
-    of the device) is where the call runs; tensors used on another stream than their own are the
-    caller's to guard, as for any torch operation."""
+    torch tensors on it.  ``stream`` (default: the current one of the device) is where a call runs and
+    where torch allocates what it needs: results that are not handed in, and the workspace.  Tensors
+    handed in that were last used on another stream are the caller's to guard, and a result has to
+    be waited for before another stream reads it, as for any torch operation."""
 
     def __init__(self, device=0):
         self._open(device)
         self._check(self._L.gbmuf_ops_create(device, ctypes.byref(self._h)))
 
-    def _linear(self, call, query, pack, fields, in_place, like, stream):
+    def _linear(self, call, query, pack, fields, in_place, like):
         """Runs a linear-layer call.  in_place: its operands are aligned bf16, no workspace."""
         if in_place:
             args = pack(*fields, 0, 0)
@@ -536,13 +553,9 @@ class LocalOps(_OnDevice):
             args, need = pack(*fields, 0, 0), ctypes.c_int64()
             self._check(query(self._h, args, ctypes.byref(need)))
             if need.value:
-                torch = self._torch
-                work = torch.empty(need.value, dtype=torch.uint8, device=like.device)
-                if stream is not None:
-                    work.record_stream(stream if hasattr(stream, "cuda_stream")
-                                       else torch.cuda.ExternalStream(stream, device=like.device))
+                work = self._torch.empty(need.value, dtype=self._torch.uint8, device=like.device)
                 args = pack(*fields, work.data_ptr(), need.value)
-        st = call(self._h, args, self._on(stream))
+        st = call(self._h, args, self._raw_stream(self.device))
         if st != GBMUF_OK:
             self._check(st)
 
@@ -550,6 +563,9 @@ class LocalOps(_OnDevice):
                        z_out=None, stream=None):
         """``gbmuf_linear_forward``: y = act(x w^T + bias) + residual; with ``keep_z`` (or ``z_out``)
         returns (y, z), z = x w^T + bias.  x [rows][n_in], w [n_out][n_in]."""
+        if stream is not None:
+            return self._on_stream(stream, (out, z_out), self.linear_forward, x, w, bias, residual, activation,
+                                   keep_z, out, z_out)
         rows, n_in = _two_dims("x", x)
         n_out = _two_dims("w", w)[0]
         dtype, dev, shape = x.dtype, self.device, (rows, n_out)
@@ -563,7 +579,7 @@ class LocalOps(_OnDevice):
         z, pz, lz = _result("z_out", z_out, x, shape, dtype, dev) if keep_z or z_out is not None else (None, 0, 0)
         self._linear(self._L.gbmuf_linear_forward, self._L.gbmuf_linear_forward_workspace, _pack_forward,
                      (rows, n_in, n_out, px, pw, pb, pr, py, pz, lx, lw, lr, ly, lz, code, act),
-                     code == BF16 and not ((px | pw) & 15 or (lx | lw) & 7), x, stream)
+                     code == BF16 and not ((px | pw) & 15 or (lx | lw) & 7), x)
         return y if z is None else (y, z)
 
     def linear_backward_input(self, dz, w, residual=None, z_prev=None, activation="none", want_dx=None,
@@ -571,6 +587,9 @@ class LocalOps(_OnDevice):
         """``gbmuf_linear_backward_input``: dx = dz w + residual, and with ``z_prev`` also
         dz_prev = dx * act'(z_prev).  Returns dx without ``z_prev``; dz_prev with it, or
         (dx, dz_prev) if ``want_dx`` or ``dx_out``."""
+        if stream is not None:
+            return self._on_stream(stream, (dx_out, dz_out), self.linear_backward_input, dz, w, residual, z_prev,
+                                   activation, want_dx, dx_out, dz_out)
         rows, n_out = _two_dims("dz", dz)
         n_in = _two_dims("w", w)[1]
         dtype, dev, shape = dz.dtype, self.device, (rows, n_in)
@@ -591,7 +610,7 @@ class LocalOps(_OnDevice):
         self._linear(self._L.gbmuf_linear_backward_input, self._L.gbmuf_linear_backward_input_workspace,
                      _pack_backward_input,
                      (rows, n_in, n_out, pd, pw, pr, pz, px, pp, ldd, lw, lr, lz, lx, lp, code, act),
-                     code == BF16 and not ((pd | pw) & 15 or (ldd | lw) & 7), dz, stream)
+                     code == BF16 and not ((pd | pw) & 15 or (ldd | lw) & 7), dz)
         return dx if dp is None else (dp if dx is None else (dx, dp))
 
     def linear_backward_weight(self, dz, x, grad_dtype=None, want_bias=True, dw_out=None, dbias_out=None,
@@ -599,6 +618,9 @@ class LocalOps(_OnDevice):
         """``gbmuf_linear_backward_weight``: dw = dz^T x and dbias = sum over the rows of dz, in
         ``grad_dtype`` (default: the operands' type); with ``accumulate`` added to ``dw_out`` and
         ``dbias_out``.  Returns dw, or (dw, dbias) if ``want_bias`` or ``dbias_out``."""
+        if stream is not None:
+            return self._on_stream(stream, (dw_out, dbias_out), self.linear_backward_weight, dz, x, grad_dtype,
+                                   want_bias, dw_out, dbias_out, accumulate)
         rows, n_out = _two_dims("dz", dz)
         n_in = _two_dims("x", x)[1]
         dtype, dev, shape = dz.dtype, self.device, (n_out, n_in)
@@ -621,11 +643,13 @@ class LocalOps(_OnDevice):
                      _pack_backward_weight,
                      (rows, n_in, n_out, pd, px, pw, pb, ldd, lx, lw, code, _dtype_code(dw),
                       1 if accumulate else 0, 0),
-                     code == BF16 and not ((pd | px) & 15 or (ldd | lx) & 7), dz, stream)
+                     code == BF16 and not ((pd | px) & 15 or (ldd | lx) & 7), dz)
         return dw if db is None else (dw, db)
 
     def activation_backward(self, dy, z, activation, out=None, stream=None):
         """``gbmuf_activation_backward``: dy * act'(z); ``out`` may be dy."""
+        if stream is not None:
+            return self._on_stream(stream, (out,), self.activation_backward, dy, z, activation, out)
         shape = _two_dims("dy", dy)
         rows, cols = shape
         dtype, dev = dy.dtype, self.device
@@ -636,13 +660,16 @@ class LocalOps(_OnDevice):
         dz = out if out is not None else dy.new_empty(shape)
         po, lo = _matrix("out", dz, shape, dtype, dev)
         self._check(self._L.gbmuf_activation_backward(self._h, rows, cols, code, act, py, ly, pz, lz, po, lo,
-                                                      self._on(stream)))
+                                                      self._raw_stream(self.device)))
         return dz
 
     def cross_entropy(self, logits, targets, ignore_index=-100, row_weight=None, scale=1.0,
                       want_grad=True, dlogits_out=None, stream=None):
         """``gbmuf_cross_entropy``: (loss, lse, dlogits), or (loss, lse) without ``want_grad``.  loss
         and lse are float32 [rows]; ``dlogits_out`` may be the logits."""
+        if stream is not None:
+            return self._on_stream(stream, (dlogits_out,), self.cross_entropy, logits, targets, ignore_index,
+                                   row_weight, scale, want_grad, dlogits_out)
         torch = self._torch
         shape = _two_dims("logits", logits)
         rows, vocab = shape
@@ -658,7 +685,7 @@ class LocalOps(_OnDevice):
         lse = logits.new_empty((rows,), dtype=torch.float32)
         args = _pack_cross_entropy(rows, vocab, pl, pt, pw, loss.data_ptr(), lse.data_ptr(), pd, ll, ldd,
                                    ignore_index, code, scale)
-        st = self._L.gbmuf_cross_entropy(self._h, args, self._on(stream))
+        st = self._L.gbmuf_cross_entropy(self._h, args, self._raw_stream(self.device))
         if st != GBMUF_OK:
             self._check(st)
         return (loss, lse) if d is None else (loss, lse, d)
@@ -776,15 +803,20 @@ class GradClip(_OnDevice):
         return out
 
     def norms(self, norms_out=None, stream=None):
-        """``gbmuf_clip_norms``: float32 [groups]."""
+        """``gbmuf_clip_norms``: float32 [groups].  ``stream`` as for :class:`LocalOps`."""
+        if stream is not None:
+            return self._on_stream(stream, (norms_out,), self.norms, norms_out)
         norms = self._norms(norms_out)
-        self._check(self._L.gbmuf_clip_norms(self._h, norms.data_ptr(), self._on(stream)))
+        self._check(self._L.gbmuf_clip_norms(self._h, norms.data_ptr(), self._raw_stream(self.device)))
         return norms
 
     def clip(self, max_norm, norms_out=None, stream=None):
-        """``gbmuf_clip_scale``: writes every entry's out; returns the norms before clipping."""
+        """``gbmuf_clip_scale``: writes every entry's out; returns the norms before clipping.  ``stream`` as
+        for :class:`LocalOps`."""
+        if stream is not None:
+            return self._on_stream(stream, (norms_out,), self.clip, max_norm, norms_out)
         norms = self._norms(norms_out)
-        self._check(self._L.gbmuf_clip_scale(self._h, max_norm, norms.data_ptr(), self._on(stream)))
+        self._check(self._L.gbmuf_clip_scale(self._h, max_norm, norms.data_ptr(), self._raw_stream(self.device)))
         return norms
 
     def device_status(self, stream=None) -> int:

@@ -106,3 +106,54 @@ def test_graph_keeps_the_tensors_it_was_recorded_with(more):
         clip.set_tensors(second)
     torch.cuda.synchronize()
     del graph
+
+
+def test_calls_on_a_side_stream_leave_the_memory_of_pending_work_alone(ops):
+    """Blocks that the current stream's pending work still reads are free for that stream's next
+    allocation, not for a call that runs on another stream at once."""
+    g = gen(17)
+    x, w, b = rnd(g, (300, 131), F), rnd(g, (77, 131), F), rnd(g, (77,), F)
+    xb, wb = rnd(g, (640, 512), BF), rnd(g, (1024, 512), BF)
+    logits, t = rnd(g, (60, 5003), BF, 3.0), torch.randint(0, 5003, (60,), generator=g, device="cuda")
+    dz, clip = rnd(g, (60, 77), F), binding.GradClip([(x, None, 0)], groups=65_536)
+    work = [lambda s: ops.linear_forward(x, w, bias=b, activation="gelu", keep_z=True, stream=s),
+            lambda s: ops.linear_forward(xb, wb, stream=s),
+            lambda s: ops.linear_backward_input(dz, w, stream=s),
+            lambda s: ops.linear_backward_weight(xb, xb, grad_dtype=F, stream=s),
+            lambda s: ops.cross_entropy(logits, t, stream=s), lambda s: ops.activation_backward(xb, xb, "tanh", stream=s),
+            lambda s: clip.norms(stream=s)]
+    flat = lambda r: r if isinstance(r, tuple) else (r,)                            # noqa: E731
+    refs = [flat(f(None)) for f in work]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for f, ref in zip(work, refs):
+        # a block of the size of each result and of typical workspaces, read late by the current stream
+        blocks = [torch.full((n,), 3.0, device="cuda") for n in {(r.numel() * r.element_size() + 3) // 4 for r in ref} |
+                  {80_000, 120_000, 170_000, 250_000}]
+        late = [torch.empty_like(v) for v in blocks]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)                      # ten milliseconds
+        for v, out in zip(blocks, late):
+            out.copy_(v)
+        blocks.clear()
+        del v
+        got = flat(f(side.cuda_stream if f is work[0] else side))
+        side.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, ref))
+        torch.cuda.synchronize()
+        assert all(bool((out == 3.0).all()) for out in late), "memory of pending work was overwritten"
+        del got
+    assert ops.device_status() == 0
+
+
+def test_calls_on_side_streams_in_turn(ops):
+    """fp32 products (with a workspace each) on the current stream and on two others, nothing between them."""
+    g = gen(19)
+    jobs = [(rnd(g, (700 + i, 515), F), rnd(g, (333, 515), F)) for i in range(6)]
+    refs = [ops.linear_forward(x, w) for x, w in jobs]
+    streams = [None, torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [ops.linear_forward(x, w, stream=streams[i % 3]) for i, (x, w) in enumerate(jobs)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, refs))
