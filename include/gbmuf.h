@@ -445,7 +445,7 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
  *   gbmuf_clip_norms: norms[g] = sqrt(sum of squares over the tensors of group g), squares and sums
  *     in double in a fixed order; 0 for a group without elements.  norms: device fp32 [groups].
  *   gbmuf_clip_scale: the norms, and out = grad * (max_norm / max(norm_g, max_norm)); max_norm <= 0
- *     copies without clipping.  A group whose norm is not finite has its outputs filled with zeros,
+ *     or infinite copies without clipping.  A group whose norm is not finite has its outputs filled with zeros,
  *     so that the worker's step leaves theta and the accumulator as they are; its norm tells.
  * Both may be recorded into a stream capture: a graph goes on with the tensors that the handle had
  * then, also after set_tensors, until the handle is destroyed. */

@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_scale_ker
       group = w.t.group;
       const float norm = clip_group_norm(P, group, scratch);
       zero = !(norm <= 3.402823466e38f);
-      factor = P.max_norm > 0.0f ? __fdiv_rn(P.max_norm, norm > P.max_norm ? norm : P.max_norm) : 1.0f;
+      factor = P.max_norm > 0.0f && norm > P.max_norm ? __fdiv_rn(P.max_norm, norm) : 1.0f;
     }
     if (!w.t.out) continue;
     const ClipSpan s = clip_span(w.t, w.c - w.t.chunk0);

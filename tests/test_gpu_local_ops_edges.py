@@ -157,3 +157,18 @@ def test_calls_on_side_streams_in_turn(ops):
         got = [ops.linear_forward(x, w, stream=streams[i % 3]) for i, (x, w) in enumerate(jobs)]
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, refs))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_clip_with_infinite_bound_copies(dtype):
+    """max_norm = inf: nothing is longer than that, so outputs are the gradients."""
+    g = gen(3)
+    grads = [rnd(g, s, dtype) for s in [(70_001,), (33, 5), (9,)]]
+    outs = [torch.full_like(t, 7.0, dtype=F) for t in grads]
+    bad, zeroed = rnd(g, (50,), dtype), torch.ones(50, device="cuda")
+    bad[3] = math.inf
+    clip = binding.GradClip([(t, o, 0) for t, o in zip(grads, outs)] + [(bad, zeroed, 1)], groups=2)
+    norms = clip.clip(math.inf)
+    ref = math.sqrt(sum(float((t.double() ** 2).sum()) for t in grads))
+    assert abs(float(norms[0]) - ref) <= 2.0 ** -22 * ref and float(norms[1]) == math.inf
+    assert all(torch.equal(o, t.float()) for t, o in zip(grads, outs)) and not bool(zeroed.any())
