@@ -331,8 +331,9 @@ gbmuf_status gbmuf_peer_destroy(gbmuf_peer* h);
  *     others are first copied into the workspace.)
  *   - `dtype` is the type of activations, weights, biases and their gradients with respect to
  *     activations.  Products are summed in fp32 (fp32 operands as three bf16 parts each, whose
- *     six leading products carry at least the 24 bits of an fp32 product; an fp32 operand that is
- *     infinite gives NaN where the plain product would give an infinity), epilogues are computed
+ *     six leading products carry at least the 24 bits of an fp32 product; infinite and NaN operands
+ *     give what the plain product gives, whichever kernel takes the call; finite operands whose
+ *     product leaves the range of fp32 give an infinity or NaN), epilogues are computed
  *     in fp32 from the unrounded sum, and every output is rounded once, to nearest even.
  *   - Outputs may not overlap inputs or each other, except where a call says so.
  *   - A zero in rows, n_in or n_out is allowed: an empty sum is 0.  At most 2^31 - 2^16 each.

@@ -7,7 +7,10 @@ namespace {
 
 // x as hi + mid + lo, each bf16: hi = RN(x), mid = RN(x - hi), lo = RN(x - hi - mid); the differences
 // are exact, and three times 8 bits hold all 24 of x (down to the smallest bf16).  Where RN(x)
-// overflows, hi is the largest bf16.  An infinity or NaN is in hi alone.
+// overflows, hi is the largest bf16.  A NaN is in hi alone.  An infinity is in lo, with 1 of its sign in
+// hi: lo meets hi of the other operand only, whose sign is the operand's and which is not 0 unless that is,
+// so the sum of the six products is what the plain product gives (in hi it would meet mid and lo of
+// the other operand as well, which can be 0 or of the other sign: NaN).
 __device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uint16_t& lo) {
   __nv_bfloat16 h = __float2bfloat16_rn(x);
   const uint32_t bits = __float_as_uint(x);
@@ -17,7 +20,10 @@ __device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uin
   const float r1 = finite ? x - __uint_as_float((uint32_t)hb << 16) : 0.0f;
   const uint16_t mb = __bfloat16_as_ushort(__float2bfloat16_rn(r1));
   const float r2 = r1 - __uint_as_float((uint32_t)mb << 16);
-  hi = hb; mid = mb; lo = __bfloat16_as_ushort(__float2bfloat16_rn(r2));
+  const bool infinite = (bits & 0x7fffffffu) == 0x7f800000u;
+  hi = infinite ? (uint16_t)(bits >> 16 & 0x8000u | 0x3f80u) : hb;
+  mid = mb;
+  lo = infinite ? hb : __bfloat16_as_ushort(__float2bfloat16_rn(r2));
 }
 
 // src [outer][inner] with any stride and alignment -> bf16 parts [1 or 3][outer][ld_dst], ld_dst a

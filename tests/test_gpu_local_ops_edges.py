@@ -172,3 +172,27 @@ def test_clip_with_infinite_bound_copies(dtype):
     ref = math.sqrt(sum(float((t.double() ** 2).sum()) for t in grads))
     assert abs(float(norms[0]) - ref) <= 2.0 ** -22 * ref and float(norms[1]) == math.inf
     assert all(torch.equal(o, t.float()) for t, o in zip(grads, outs)) and not bool(zeroed.any())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows", [4, 16, 17, 200])
+def test_infinite_operands_give_what_the_plain_product_gives(ops, dtype, rows):
+    """An infinity times a finite value is an infinity of the product's sign, infinities of both signs in
+    one sum or one times zero are NaN -- whichever kernel takes the call."""
+    g = gen(rows)
+    x, w = rnd(g, (rows, 320), dtype), rnd(g, (160, 320), dtype, 0.1)
+    dz = rnd(g, (rows, 160), dtype)
+    x[0, 7], x[1, 300] = math.inf, -math.inf
+    x[2, 5] = x[2, 11] = math.inf
+    x[3, 0] = math.nan
+    w[9, 7], w[11, 300] = 0.0, -math.inf
+    w[13, 17] = w[14, 17] = math.inf
+    dz[0, 3], dz[1, 13] = -math.inf, math.inf
+    wide = lambda *t: [v.double().cpu() for v in t]                                 # noqa: E731
+    xd, wd, dd = wide(x, w, dz)
+    for got, ref in [(ops.linear_forward(x, w), xd @ wd.t()), (ops.linear_backward_input(dz, w), dd @ wd),
+                     (ops.linear_backward_weight(dz, x, want_bias=False), dd.t() @ xd)]:
+        got = got.double().cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
+        assert bool(torch.isinf(ref).any())
