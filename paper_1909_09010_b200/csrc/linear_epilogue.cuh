@@ -14,19 +14,27 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 
 // Activations and their slopes, two values at a time.  Values beyond +-100 count as +-100 where an
 // activation is flat there in fp32 (its exponentials are 0 or its limit is reached), so that infinities
-// give the limits and not inf * 0; NaN stays NaN.
+// give the limits and not inf * 0; NaN stays NaN.  A slope that goes to 0 is formed as a product of what
+// goes to 0, not as a difference of numbers near 1, so that its last digits hold (fp32).
 //
 // FAST (results that are rounded to bf16): exponentials and reciprocals are single instructions of the
 // special-function unit, off by a few units of 2^-22; the accurate functions took twice the
 // instructions of everything else in the epilogue and made it the bound.
 __device__ __forceinline__ float clamp100(float z) { return z > 100.0f ? 100.0f : (z < -100.0f ? -100.0f : z); }
 
-template <bool FAST> __device__ __forceinline__ Two logistic(float a, float b) {
-  if (!FAST) return two(1.0f / (1.0f + expf(-a)), 1.0f / (1.0f + expf(-b)));
+template <bool FAST> __device__ __forceinline__ Two decay(float a, float b) {          // exp(-a), exp(-b)
+  if (!FAST) return two(expf(-a), expf(-b));
   float x, y;
   apart(two(a, b) * two(-1.44269504f, -1.44269504f), x, y);
-  apart(two(exp2_unit(x), exp2_unit(y)) + two(1.0f, 1.0f), x, y);
-  return two(rcp_unit(x), rcp_unit(y));
+  return two(exp2_unit(x), exp2_unit(y));
+}
+template <bool FAST> __device__ __forceinline__ Two reciprocal(Two t) {
+  float x, y;
+  apart(t, x, y);
+  return FAST ? two(rcp_unit(x), rcp_unit(y)) : two(1.0f / x, 1.0f / y);
+}
+template <bool FAST> __device__ __forceinline__ Two logistic(float a, float b) {
+  return reciprocal<FAST>(decay<FAST>(a, b) + two(1.0f, 1.0f));
 }
 // For a, b >= 0: q = 1 - Phi = erfc(x / sqrt 2) / 2 (Phi the normal distribution function) and
 // g = exp(-x^2 / 2).  FAST: Abramowitz and Stegun 7.1.26, erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2),
@@ -79,25 +87,27 @@ template <bool FAST, int ACT> __device__ __forceinline__ void activate_two(float
 template <bool FAST, int ACT> __device__ __forceinline__ Two slope_two(float a, float b) {
   const Two one = two(1.0f, 1.0f);
   if (ACT == GBMUF_ACT_RELU) return two(a > 0.0f ? 1.0f : (a <= 0.0f ? 0.0f : a), b > 0.0f ? 1.0f : (b <= 0.0f ? 0.0f : b));
-  if (ACT == GBMUF_ACT_GELU) {                             // Phi(z) + z phi(z), Phi = 1/2 + sign(z) (1/2 - q)
+  if (ACT == GBMUF_ACT_GELU) {                             // Phi(z) + z phi(z), Phi = q or 1 - q by the sign
     const float x = min_nan(fabsf(a), 100.0f), y = min_nan(fabsf(b), 100.0f);
     Two g;
-    float u, v;
-    apart(two(0.5f, 0.5f) - normal_tail<FAST>(x, y, g), u, v);
-    const Two phi = two(copysignf(u, a), copysignf(v, b)) + two(0.5f, 0.5f);
+    float u, v, cu, cv;
+    const Two q = normal_tail<FAST>(x, y, g);
+    apart(q, u, v);
+    apart(one - q, cu, cv);
+    const Two phi = two(a < 0.0f ? u : cu, b < 0.0f ? v : cv);
     return fma_two(two(copysignf(x, a), copysignf(y, b)) * two(0.39894228f, 0.39894228f), g, phi);
   }
   if (ACT == GBMUF_ACT_SILU) {
     const Two s = logistic<FAST>(a, b);
     return s * fma_two(two(clamp100(a), clamp100(b)), one - s, one);
   }
-  if (ACT == GBMUF_ACT_TANH) {
-    const float x = tanh_of<FAST>(a), y = tanh_of<FAST>(b);
-    return fma_two(two(-x, -y), two(x, y), one);
+  if (ACT == GBMUF_ACT_TANH) {                             // 4 e / (1 + e)^2, e = exp(-2 |z|)
+    const Two e = decay<FAST>(2.0f * fabsf(a), 2.0f * fabsf(b)), r = reciprocal<FAST>(one + e);
+    return e * two(4.0f, 4.0f) * (r * r);
   }
-  if (ACT == GBMUF_ACT_SIGMOID) {
-    const Two s = logistic<FAST>(a, b);
-    return s * (one - s);
+  if (ACT == GBMUF_ACT_SIGMOID) {                          // e / (1 + e)^2, e = exp(-|z|)
+    const Two e = decay<FAST>(fabsf(a), fabsf(b)), r = reciprocal<FAST>(one + e);
+    return e * (r * r);
   }
   return one;
 }

@@ -196,3 +196,29 @@ def test_infinite_operands_give_what_the_plain_product_gives(ops, dtype, rows):
         assert torch.equal(torch.isnan(got), torch.isnan(ref))
         assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
         assert bool(torch.isinf(ref).any())
+
+
+@pytest.mark.parametrize("act,far", [("gelu", 12.0), ("sigmoid", 80.0), ("tanh", 40.0)])
+def test_slopes_keep_their_digits_in_the_tails(ops, act, far):
+    """Relative errors, where the slope itself is tiny: it is not formed as a difference of numbers near 1."""
+    z = torch.linspace(-far, far, 30_000, device="cuda").view(-1, 16)
+    zd = z.double()
+    if act == "gelu":
+        tail, bell = torch.special.erfc(-zd / 2 ** 0.5) / 2, zd * torch.exp(-zd * zd / 2) / math.sqrt(2 * math.pi)
+        # both parts are exponentials of z^2 / 2, which is rounded: z^2 2^-24 twice over; 2^-20 for the rest
+        ref, tol = tail + bell, (zd * zd * 2.0 ** -23 + 2.0 ** -20) * (tail + bell.abs())
+    else:
+        e = torch.exp(-zd.abs() * (1 if act == "sigmoid" else 2))
+        ref = e / (1 + e) ** 2 * (1 if act == "sigmoid" else 4)
+        tol = 2.0 ** -20 * ref               # an exponential of 2 units and five roundings
+    eye = torch.eye(16, device="cuda")
+    for got in (ops.activation_backward(torch.ones_like(z), z, act),
+                ops.linear_backward_input(torch.ones_like(z), eye, z_prev=z, activation=act)):
+        err = (got.double() - ref).abs()
+        assert bool((err <= tol).all()), float((err / ref.abs()).max())
+    if act != "gelu":                        # bf16: single instructions, off by 2^-22 and by |z| 2^-23; then one rounding
+        zb = z.to(BF)
+        e = torch.exp(-zb.double().abs() * (1 if act == "sigmoid" else 2))
+        ref = e / (1 + e) ** 2 * (1 if act == "sigmoid" else 4)
+        got = ops.activation_backward(torch.ones_like(zb), zb, act).double()
+        assert bool(((got - ref).abs() <= 2.0 ** -8 * ref).all())
