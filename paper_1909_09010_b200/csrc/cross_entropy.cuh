@@ -63,10 +63,12 @@ __device__ __forceinline__ bool target_inside(const LossParams& P, long long t) 
 __device__ __forceinline__ RowOutcome row_outcome(const LossParams& P, float m, float sum, float x_target, long long t, float w) {
   RowOutcome o;
   const bool empty = m == -INFINITY && sum == 0.0f;
-  o.lse = empty ? -INFINITY : m + logf(sum);
+  const float l = logf(sum);
+  o.lse = empty ? -INFINITY : m + l;
   const bool ignored = target_ignored(P, t, w), outside = !ignored && !target_inside(P, t);
   o.zero = ignored || outside || empty;
-  o.loss = ignored ? 0.0f : outside ? NAN : empty ? INFINITY : w * (o.lse - x_target);
+  // not lse - x_target: what the logits have in common would take digits from the logarithm
+  o.loss = ignored ? 0.0f : outside ? NAN : empty ? INFINITY : w * ((m - x_target) + l);
   return o;
 }
 __device__ __forceinline__ void report_target(const LossParams& P, long long t, float w) {

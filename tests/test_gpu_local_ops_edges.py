@@ -222,3 +222,19 @@ def test_slopes_keep_their_digits_in_the_tails(ops, act, far):
         ref = e / (1 + e) ** 2 * (1 if act == "sigmoid" else 4)
         got = ops.activation_backward(torch.ones_like(zb), zb, act).double()
         assert bool(((got - ref).abs() <= 2.0 ** -8 * ref).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("vocab", [1000, 30_001, 267_735])
+def test_loss_of_rows_with_a_large_common_offset(ops, dtype, vocab):
+    """The loss does not see what all logits of a row have in common, up to rows of the lowest value."""
+    x = torch.round(rnd(gen(vocab), (4, vocab), F, 2.0) * 4) / 4            # exact in fp32 beside the offsets below
+    offset = torch.tensor([0.0, 2.0 ** 20, -2.0 ** 21, 0.0], device="cuda")[:, None]
+    x = x + offset if dtype is F else x.to(dtype)
+    x[3, :] = torch.finfo(dtype).min
+    t = torch.tensor([1, vocab - 1, vocab // 2, 0], device="cuda")
+    loss, lse, d = ops.cross_entropy(x, t, scale=0.5)
+    ref = 0.5 * (torch.logsumexp(x.double(), 1) - x.double()[torch.arange(4), t])
+    ref[3] = 0.5 * math.log(vocab)                                           # lost in 64 bits as well
+    # a sum in chains of at most 300 terms is off by 2^-15 of itself, its log by that; then sums of numbers below 64
+    assert bool(((loss.double() - ref).abs() <= 0.5 * (2.0 ** -15 + 64 * 2.0 ** -22)).all()), loss - ref
