@@ -443,8 +443,10 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
  * gbmuf_clip_create and gbmuf_clip_set_tensors read the host table before they return; the device
  * memory it names must stay valid while the handle is used with it.  set_tensors waits for the
  * work that this handle has enqueued.  Work of one handle is kept on one stream at a time.
- *   gbmuf_clip_norms: norms[g] = sqrt(sum of squares over the tensors of group g), squares and sums
- *     in double in a fixed order; 0 for a group without elements.  norms: device fp32 [groups].
+ *   gbmuf_clip_norms: norms[g] = sqrt(sum of squares over the tensors of group g); 0 for a group
+ *     without elements.  norms: device fp32 [groups].  Squares are summed in fp32 in groups of at
+ *     most 32, in double where that would leave the range of fp32, and the groups' sums in double,
+ *     all in a fixed order: a norm is within 2^-22 of the exact one, and two calls give the same bits.
  *   gbmuf_clip_scale: the norms, and out = grad * (max_norm / max(norm_g, max_norm)); max_norm <= 0
  *     or infinite copies without clipping.  A group whose norm is not finite has its outputs filled with zeros,
  *     so that the worker's step leaves theta and the accumulator as they are; its norm tells.

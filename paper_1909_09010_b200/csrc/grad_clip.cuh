@@ -95,8 +95,10 @@ __device__ __forceinline__ double workers_sum(double v, double* scratch) {
 
 // Sum of squares of up to four 16-byte pieces (raw words; zeros where there is none): in fp32, unless
 // that leaves the range in which fp32 squares are exact to their last bits; then in double, as are the
-// sums of these sums, so that every norm that fp32 can hold comes out right.  (Every square in double
-// made the conversions the bound; one range test per four squares made each wait for the one before.)
+// sums of these sums, so that every norm that fp32 can hold comes out right.  A sum has passed at most
+// five fp32 roundings (fp32) or six (bf16, whose squares are exact), 6 x 2^-24; the square root halves that,
+// and rounding the norm adds 2^-24: 2^-22 in all.  (Every square in double made the conversions the
+// bound; one range test per four squares made each wait for the one before.)
 template <bool F32> __device__ __forceinline__ float piece_value(uint4 u, int i) {
   const uint32_t w = i / (F32 ? 1 : 2) == 0 ? u.x : i / (F32 ? 1 : 2) == 1 ? u.y : i / (F32 ? 1 : 2) == 2 ? u.z : u.w;
   return __uint_as_float(F32 ? w : i & 1 ? w & 0xffff0000u : w << 16);

@@ -238,3 +238,15 @@ def test_loss_of_rows_with_a_large_common_offset(ops, dtype, vocab):
     ref[3] = 0.5 * math.log(vocab)                                           # lost in 64 bits as well
     # a sum in chains of at most 300 terms is off by 2^-15 of itself, its log by that; then sums of numbers below 64
     assert bool(((loss.double() - ref).abs() <= 0.5 * (2.0 ** -15 + 64 * 2.0 ** -22)).all()), loss - ref
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_norms_of_equal_elements(dtype):
+    """Every fp32 rounding of a sum of equal squares goes the same way: five of them (six for bf16) and
+    the norm's own stay within 2^-22, at any length and across the range."""
+    values = [1.0, 1.1, 1.0 + 2.0 ** -7, 1.7, 0.3, 1.9921875, 1e-3, 3e-12, 1e-13, 1e-20, 1e18, 3e19, 1e25, 1e-30]
+    grads = [torch.full((n,), v, device="cuda").to(dtype) for v in values for n in (1, 3, 33, 4096, 100_003)]
+    norms = binding.GradClip([(t, None, i) for i, t in enumerate(grads)], groups=len(grads)).norms().cpu()
+    for t, n in zip(grads, norms):
+        ref = math.sqrt(t.numel()) * float(t[0].double())
+        assert abs(float(n) - ref) <= 2.0 ** -22 * ref, (t.numel(), float(t[0]), float(n), ref)
