@@ -322,8 +322,7 @@ Product forward_product(const gbmuf_linear_forward_args* a) {
 
 // Whether the few-rows kernel takes a layer.
 bool few_rows(const gbmuf_linear_forward_args* a) {
-  const bool direct = in_place(forward_product(a).a, a->dtype) && in_place(forward_product(a).b, a->dtype);
-  const int64_t most = a->dtype == GBMUF_F32 ? 16 : direct ? 8 : 8;
+  const int64_t most = a->dtype == GBMUF_F32 ? 16 : 8;
   const int64_t rows = a->rows <= 1 ? 1 : a->rows <= 2 ? 2 : a->rows <= 4 ? 4 : a->rows <= 8 ? 8 : 16;
   return a->rows <= most && rows * ((a->n_in + 7) / 8 * 8) * (int64_t)size_of(a->dtype) <= kRowsMostBytes;
 }
