@@ -6,24 +6,46 @@
 namespace {
 
 // x as hi + mid + lo, each bf16: hi = RN(x), mid = RN(x - hi), lo = RN(x - hi - mid); the differences
-// are exact, and three times 8 bits hold all 24 of x (down to the smallest bf16).  Where RN(x)
-// overflows, hi is the largest bf16.  A NaN is in hi alone.  An infinity is in lo, with 1 of its sign in
-// hi: lo meets hi of the other operand only, whose sign is the operand's and which is not 0 unless that is,
-// so the sum of the six products is what the plain product gives (in hi it would meet mid and lo of
-// the other operand as well, which can be 0 or of the other sign: NaN).
-__device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uint16_t& lo) {
-  __nv_bfloat16 h = __float2bfloat16_rn(x);
-  const uint32_t bits = __float_as_uint(x);
-  const bool finite = (bits & 0x7f800000u) != 0x7f800000u;
-  uint16_t hb = __bfloat16_as_ushort(h);
-  if (finite && (hb & 0x7f80u) == 0x7f80u) hb = (uint16_t)((hb & 0x8000u) | 0x7f7fu);
-  const float r1 = finite ? x - __uint_as_float((uint32_t)hb << 16) : 0.0f;
-  const uint16_t mb = __bfloat16_as_ushort(__float2bfloat16_rn(r1));
-  const float r2 = r1 - __uint_as_float((uint32_t)mb << 16);
-  const bool infinite = (bits & 0x7fffffffu) == 0x7f800000u;
-  hi = infinite ? (uint16_t)(bits >> 16 & 0x8000u | 0x3f80u) : hb;
-  mid = mb;
-  lo = infinite ? hb : __bfloat16_as_ushort(__float2bfloat16_rn(r2));
+// are exact, and three times 8 bits hold all 24 of x (down to the smallest bf16).  Two values at a time, the
+// parts of both in a word.
+__device__ __forceinline__ uint32_t pair_bf16(Two t) {
+  float x, y;
+  apart(t, x, y);
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ Two pair_f32(uint32_t u) { return two(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
+__device__ __forceinline__ void split3(Two x, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  hi = pair_bf16(x);
+  x = x - pair_f32(hi);
+  mid = pair_bf16(x);
+  lo = pair_bf16(x - pair_f32(mid));
+}
+// The same for n elements among which there are magnitudes that round to a bf16 that is not finite.  The hi
+// of a finite one is the largest bf16.  A NaN is in hi alone.  An infinity is in lo, with 1 of its sign in hi:
+// lo meets hi of the other operand only, whose sign is the operand's and which is not 0 unless that is, so
+// the sum of the six products is what the plain product gives (in hi it would meet mid and lo of the other
+// operand as well, which can be 0 or of the other sign: NaN).  Not in line: the loop it is called from stays
+// short (tests of every element in that loop cost 2.6 us of 9 at 5 M elements).
+__device__ __noinline__ void split3_edges(const float* s, __nv_bfloat16* d, long long part, int n) {
+  for (int j = 0; j < n; ++j) {
+    const float x = s[j];
+    const uint32_t bits = __float_as_uint(x), size = bits & 0x7fffffffu;
+    const uint16_t sign = (uint16_t)(bits >> 16 & 0x8000u);
+    uint16_t hi = __bfloat16_as_ushort(__float2bfloat16_rn(x)), mid = 0, lo = 0;
+    if (size == 0x7f800000u) {
+      lo = hi;
+      hi = sign | 0x3f80u;
+    } else if (size < 0x7f800000u) {
+      if ((hi & 0x7f80u) == 0x7f80u) hi = sign | 0x7f7fu;
+      const float r1 = x - __uint_as_float((uint32_t)hi << 16);
+      mid = __bfloat16_as_ushort(__float2bfloat16_rn(r1));
+      lo = __bfloat16_as_ushort(__float2bfloat16_rn(r1 - __uint_as_float((uint32_t)mid << 16)));
+    }
+    d[j] = __ushort_as_bfloat16(hi);
+    d[part + j] = __ushort_as_bfloat16(mid);
+    d[2 * part + j] = __ushort_as_bfloat16(lo);
+  }
 }
 
 // src [outer][inner] with any stride and alignment -> bf16 parts [1 or 3][outer][ld_dst], ld_dst a
@@ -52,15 +74,20 @@ template <typename T, bool VEC> __device__ __forceinline__ void pack_run(const P
     if constexpr (sizeof(T) == 2) {
       *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(v);
     } else {
-      __align__(16) uint16_t p[3][8];
+      __align__(16) uint32_t p[3][4];
+      uint32_t edge = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) split3(v[j], p[0][j], p[1][j], p[2][j]);
+      for (int j = 0; j < 4; ++j) {
+        split3(two(v[2 * j], v[2 * j + 1]), p[0][j], p[1][j], p[2][j]);
+        edge |= (p[0][j] & 0x7f807f80u) + 0x00800080u;     // an exponent of ones carries into the sign's place
+      }
 #pragma unroll
       for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(d + q * part) = *reinterpret_cast<const uint4*>(p[q]);
+      if (edge & 0x80008000u) split3_edges(s, d, part, J.inner - c < 8 ? (int)(J.inner - c) : 8);
     }
   }
 }
-// Both operands of a product in one launch.  Bound by memory: 21 MB of fp32 to 31 MB of parts in 11 us.
+// Both operands of a product in one launch.  Bound by memory: 21 MB of fp32 to 31 MB of parts in 8 us.
 template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const PackJob a, const PackJob b) {
   grid_launch_dependents();
   grid_dependency_wait();
