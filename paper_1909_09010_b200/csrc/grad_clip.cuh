@@ -344,6 +344,18 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_scale_ker
   } while (w.next(P));
 }
 
+// A wait for a barrier that nothing signals: it expires, sets the status word and returns.
+__global__ void clip_expired_wait_kernel(int32_t* status) {
+  __shared__ __align__(8) unsigned long long barrier;
+  const uint32_t bar = smem_u32(&barrier);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  mbar_wait_bounded(bar, 0, status);
+}
+
 }  // namespace
 
 #endif  // GBMUF_CSRC_GRAD_CLIP_CUH

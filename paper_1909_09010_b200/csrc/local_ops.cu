@@ -790,7 +790,7 @@ gbmuf_status gbmuf_clip_selftest_wait_timeout(gbmuf_clip* h, void* stream) {
     if (!h) return invalid("handle is NULL");
     DeviceGuard guard(h->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    wait_timeout_selftest_kernel<<<1, 32, 0, (cudaStream_t)stream>>>(h->d_status, h->d_status + 1);
+    clip_expired_wait_kernel<<<1, 32, 0, (cudaStream_t)stream>>>(h->d_status);
     const cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess) h->work.note((cudaStream_t)stream);
     return launched("launch of the wait-timeout self-test", e);

@@ -70,20 +70,6 @@ __device__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, int32_t* status
   atomicExch(status, (int32_t)GBMUF_ERR_TIMEOUT);
   return false;
 }
-// Self-test of the bounded wait: one warp waits on a barrier that nothing will ever signal.  The
-// wait must expire, set the status word and return; nothing here can hang or trap.
-__global__ void wait_timeout_selftest_kernel(int32_t* status, int32_t* returned) {
-  __shared__ __align__(8) unsigned long long bar_storage;
-  const uint32_t bar = smem_u32(&bar_storage);
-  if (threadIdx.x == 0) {
-    mbar_init(bar, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncwarp();
-  const bool ok = mbar_wait_bounded(bar, 0, status);
-  if (threadIdx.x == 0) *returned = ok ? 1 : 2;
-}
-
 // Two-dimensional tiled TMA load: the box [rows 0..K) x [columns x, x + box width) of a row-major
 // [K][ld] array lands in shared memory as K consecutive rows of box-width elements.  One request
 // per box, delivered to this CTA only; completion is counted in bytes on the mbarrier, out-of-range columns

@@ -521,6 +521,20 @@ __global__ void __launch_bounds__(256) divide_selftest_kernel(float b, float y, 
   }
 }
 
+// Self-test of the bounded wait: one warp waits on a barrier that nothing will ever signal.  The
+// wait must expire, set the status word and return; nothing here can hang or trap.
+__global__ void wait_timeout_selftest_kernel(int32_t* status, int32_t* returned) {
+  __shared__ __align__(8) unsigned long long bar_storage;
+  const uint32_t bar = smem_u32(&bar_storage);
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  const bool ok = mbar_wait_bounded(bar, 0, status);
+  if (threadIdx.x == 0) *returned = ok ? 1 : 2;
+}
+
 }  // namespace
 
 #endif  // GBMUF_CSRC_SYNC_FUSED_TMEM_CUH
