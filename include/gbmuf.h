@@ -129,7 +129,7 @@ gbmuf_status gbmuf_local_perturb(gbmuf_ctx* ctx, uint64_t step, float lr, float 
  * clip_mask byte is non-zero) (double accumulation, fixed order); inside those components
  * g' = g * (clip_norm / max(norm_k, clip_norm)), elsewhere g' = g; a <- a + g'g';
  * theta <- store(theta - (lr * g') / (sqrt(a) + eps)).  clip_mask: host, m bytes, or NULL (no
- * clipping; clip_norm <= 0 also switches it off); at most 16 separate runs of adjacent masked
+ * clipping; clip_norm <= 0 or infinite also switches it off); at most 16 separate runs of adjacent masked
  * components.  lr is the caller's alpha_t (the paper decays 0.1 by 0.9 per epoch).
  * Errors: INVALID_ARG, BAD_STATE (mask without set_partition), UNSUPPORTED, ALLOC, CUDA. */
 gbmuf_status gbmuf_local_adagrad(gbmuf_ctx* ctx, const float* grad_device, float* accum_device,

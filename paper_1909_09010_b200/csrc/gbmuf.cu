@@ -31,6 +31,7 @@
 
 #include <cstdio>
 #include <cstring>
+#include <limits>
 #include <mutex>
 #include <new>
 #include <string>
@@ -819,7 +820,7 @@ gbmuf_status gbmuf_local_adagrad(gbmuf_ctx* ctx, const float* grad, float* accum
   const int K = ctx->cfg.K;
   cudaError_t e;
   const float* scale = nullptr;
-  if (clip && R.n > 0) {
+  if (clip && R.n > 0 && clip_norm <= std::numeric_limits<float>::max()) {   // inf / max(norm, inf) is no number
     if (!ctx->d_norm_partial) {
       e = cudaMalloc(&ctx->d_norm_partial, (size_t)K * kNormBlocks * sizeof(double));
       if (e == cudaSuccess) e = cudaMalloc(&ctx->d_clip_scale, (size_t)K * sizeof(float));

@@ -250,3 +250,19 @@ def test_norms_of_equal_elements(dtype):
     for t, n in zip(grads, norms):
         ref = math.sqrt(t.numel()) * float(t[0].double())
         assert abs(float(n) - ref) <= 2.0 ** -22 * ref, (t.numel(), float(t[0]), float(n), ref)
+
+
+def test_adagrad_with_an_infinite_clip_norm_does_not_clip():
+    states = []
+    for clip_norm in (math.inf, 0.0):
+        theta, accum = torch.ones((2, 4096), device="cuda"), torch.full((2, 4096), 0.1, device="cuda")
+        omega, delta = torch.zeros_like(theta), torch.zeros_like(theta)
+        ctx = binding.Gbmuf(theta, omega, delta, K=2, N=4096, ld=4096, p=0, q=0, eta=0.9, zeta=1.0)
+        ctx.set_partition([0, 1000, 4096])
+        grad = rnd(gen(31), (2, 4096), F, 5.0)
+        ctx.local_adagrad(grad, accum, 0.1, eps=1e-8, clip_norm=clip_norm, clip_mask=[1, 0])
+        torch.cuda.synchronize()
+        ctx.destroy()
+        states.append((theta, accum))
+    assert bool(torch.isfinite(states[0][0]).all())
+    assert all(torch.equal(p, q) for p, q in zip(*states))
