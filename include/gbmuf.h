@@ -330,11 +330,18 @@ gbmuf_status gbmuf_peer_destroy(gbmuf_peer* h);
  *     (16-byte aligned pointers and strides that are multiples of 16 bytes are read in place;
  *     others are first copied into the workspace.)
  *   - `dtype` is the type of activations, weights, biases and their gradients with respect to
- *     activations.  Products are summed in fp32 (fp32 operands as three bf16 parts each, whose
- *     six leading products carry at least the 24 bits of an fp32 product; infinite and NaN operands
+ *     activations.  Products are summed in fp32, in an order that does not depend on timing.  A sum
+ *     that is stored as fp32 is rounded to nearest at every addition but those within 16 to 24 matrix
+ *     instructions; one that is stored as bf16 stays in the matrix unit's accumulator, whose
+ *     additions (one per 16 terms) cut towards zero: up to about 1.3e-3 of the result in the 2-norm
+ *     at 267,735 terms, less in proportion for fewer.  fp32 operands are taken as three bf16 parts
+ *     each, whose six leading products miss at most 2^-23 of a product; infinite and NaN operands
  *     give what the plain product gives, whichever kernel takes the call; finite operands whose
- *     product leaves the range of fp32 give an infinity or NaN), epilogues are computed
- *     in fp32 from the unrounded sum, and every output is rounded once, to nearest even.
+ *     product leaves the range of fp32 give an infinity or NaN.
+ *   - Epilogues are computed in fp32 from the unrounded sum, and every output is rounded once, to
+ *     nearest even.  For bf16 outputs exponentials and reciprocals are the GPU's approximate ones
+ *     (a few 2^-22), and gelu's normal distribution function is off by up to 7.5e-8: far below bf16
+ *     but for the tail beyond z = -4, where gelu itself is below 2e-4.
  *   - Outputs may not overlap inputs or each other, except where a call says so.
  *   - A zero in rows, n_in or n_out is allowed: an empty sum is 0.  At most 2^31 - 2^16 each.
  *   - workspace: device memory of at least the bytes that the _workspace call of the same arguments
@@ -422,7 +429,9 @@ gbmuf_status gbmuf_activation_backward(gbmuf_ops* ops, int64_t rows, int64_t col
  * a zero gradient (whatever its logits hold).  A logit of -inf is a word that cannot occur; a row of nothing else
  * has lse -inf, loss +inf and a zero gradient.  A row with a NaN or a +inf gives NaN throughout.
  * A target outside 0 .. vocab-1 gives loss NaN and a zero gradient, and GBMUF_ERR_INVALID_ARG in
- * the status word.  vocab = 0 is refused unless rows = 0. */
+ * the status word.  vocab = 0 is refused unless rows = 0.  Statistics and sums are fp32; of bf16
+ * logits the exponent (x - max) log2 e is rounded to fp32 (2^-24 of it), of fp32 logits it is exact
+ * to the last bits of the exponential. */
 typedef struct {
   int64_t rows, vocab;
   const void* logits;
@@ -471,7 +480,8 @@ gbmuf_status gbmuf_clip_selftest_wait_timeout(gbmuf_clip* h, void* stream);
 gbmuf_status gbmuf_clip_destroy(gbmuf_clip* h);
 
 /* Sentence about the last error on this context ("" if none); valid until the next call on it.
- * With ctx == NULL: the last error of a failed gbmuf_create on this thread. */
+ * With ctx == NULL: the last error of a failed gbmuf_create, or of a call on a gbmuf_ops or gbmuf_clip
+ * handle, on this thread. */
 const char* gbmuf_last_error(const gbmuf_ctx* ctx);
 
 /* Waits for the work this context has enqueued (not for the whole device), frees the library's

@@ -536,7 +536,8 @@ class _OnDevice:
 
 class LocalOps(_OnDevice):
     """``gbmuf_ops_*``: linear layers with their gradients and the loss, on one device.  Tensors are
-    torch tensors on it.  ``stream`` (default: the current one of the device) is where a call runs and
+    torch tensors on it; autograd does not see the calls (results have no history, whatever the
+    arguments' ``requires_grad`` says).  ``stream`` (default: the current one of the device) is where a call runs and
     where torch allocates what it needs: results that are not handed in, and the workspace.  Tensors
     handed in that were last used on another stream are the caller's to guard, and a result has to
     be waited for before another stream reads it, as for any torch operation."""

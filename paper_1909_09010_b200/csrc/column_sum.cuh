@@ -9,8 +9,8 @@ namespace {
 // bytes wide, 16 bytes per thread; else 32 columns) and shares its rows; sums are joined through
 // shared memory and rank 0's shared memory, in a fixed order; every rank arrives at the cluster's barrier
 // first thing and waits for it after its rows, so that rank 0 has started before anybody writes there.
-// Bound by memory: 8,192 x 4,096 bf16 in 12 to
-// 14 us (5 TB/s); one block per strip without a cluster took 366.
+// Bound by memory latency: 8,192 x 4,096 bf16 in 10 to 14 us (5 to 6.7 TB/s, part of it from L2 behind the
+// product that reads the same matrix); one block per strip without a cluster took 366.
 template <typename T, typename TO, bool VEC>
 __global__ void __launch_bounds__(256) column_sum_kernel(const T* a, long long ld, long long R, long long C, TO* out,
                                                          int accumulate) {

@@ -8,8 +8,9 @@ namespace {
 // Per row: m = max x, s = sum exp(x - m), then d = s_i (exp(x - m) / s - [target]).  Every logit is
 // needed twice with the whole row between, so the row stays on the chip from its one read to its
 // one write: in the registers of a warp (short rows), or in shared memory and the L2 cache.
-// Measured: 2,048 x 267,735 bf16 417 us (5.3 TB/s of the bytes that have to move, 81 % of the copy rate; a third
-// of the second fetches miss L2); a row held by four CTAs' shared memory alone, one row at a time, 602:
+// Measured: 2,048 x 267,735 bf16 417 to 458 us (4.8 to 5.3 TB/s of the bytes that have to move, 73 to 80 % of the
+// copy rate; 69 % of the logits are fetched twice and 27 % of that misses L2; exponentials keep their unit 62 %
+// busy); a row held by four CTAs' shared memory alone, one row at a time, 602:
 // the exchange and the refill of the slots were exposed; one block per row that reads it twice 2,231.
 // 512 x 10,000 fp32 12 us.  A cluster of eight per row leaves SMs idle (575 us).
 struct LossParams {

@@ -12,7 +12,8 @@ namespace {
 // them from there.  The gradients' loads so never wait for arithmetic, nor for the stores (loads
 // into registers, 64 KB of them in flight per SM, reached 3.6 TB/s in the norm pass).
 //
-// Measured, 956 M bf16 elements to fp32: norms 318 us (6.0 TB/s), copy 990 us (5.8 TB/s).
+// Measured, 954 M bf16 elements to fp32: norms 290 to 318 us (6.0 to 6.6 TB/s), copy 990 to 1,000 us (5.7 to
+// 5.8 TB/s).
 //
 // The handle's table: one entry per run of elements that follow one another in memory, sorted by
 // group, cut into chunks of kClipSlot bytes at multiples of 16 bytes.  A tensor of short strided

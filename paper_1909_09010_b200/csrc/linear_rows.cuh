@@ -10,8 +10,8 @@ namespace {
 // its lane in registers, on the fp32 units: no operand is packed or split and any alignment will do
 // (VEC false: element by element).  The 32 lanes' sums are joined by exchanging halves, so that
 // NF x ROWS sums take about as many shuffles and not five each.
-// Measured: 1 x 1,024 x 4,096 bf16 4.3 us (the tensor-core kernel 9.8); 8 x 512 x 267,735 fp32 99 us, 86 %
-// of the copy rate (the tensor-core kernel, which has to pack the weights first, 478).
+// Measured: 1 x 1,024 x 4,096 bf16 4.3 to 4.6 us (the tensor-core kernel 9.8); 8 x 512 x 267,735 fp32 97 to
+// 99 us, 86 % of the copy rate (the tensor-core kernel, which has to pack the weights first, 478).
 struct RowsParams {
   Epilogue E;
   const void *x, *w;

@@ -14,7 +14,8 @@ namespace {
 // rows (single tokens) make the tile narrow (BN), not half empty.
 //
 // fp32 operands come as three bf16 parts (hi, mid, lo: together all 24 bits; PARTS 3), and each step
-// along k does the six products of parts that reach 2^-24 of the product.
+// along k does six of the nine products of parts; mid lo, lo mid and lo lo, left out, come to at most
+// 2^-23 of a product.
 //
 // A tile is 128 x BN, or 256 x BN for a pair of CTAs whose tensor cores work as one (PAIR 2): each
 // holds half of the accumulator and loads half of B, a third less to fetch from L2 per product at
@@ -22,10 +23,12 @@ namespace {
 // swizzle), warp 1 issues the matrix instructions, the warps from 4 on finish the sums.  Two accumulators:
 // one is finished while the next is summed.
 //
-// Measured: 2,048 x 1,024 x 100,000 bf16 292 us (1,437 TFLOP/s, 89 % of a library product's rate; pairs of
-// CTAs, single ones 327); 8,192 x 1,024 x 4,096 to fp32 58 us (1,185 TFLOP/s, bound by operand traffic
-// from L2); 4,096 x 512 x 2,048 with gelu 18.7 us, of which the two epilogues of a CTA are 10: 16
-// finishing warps hide their own latencies better than 8 (24 us then), 32-row strips spill (20 us).
+// Measured: 2,048 x 1,024 x 100,000 bf16 292 to 307 us in short runs (up to 1,437 TFLOP/s, 89 % of a library
+// product's rate; tensor pipe 92 % active; single CTAs 327 us), 358 to 370 back to back under the power cap
+// (up to 1,170 TFLOP/s); 8,192 x 1,024 x 4,096 to fp32 58 us in short runs (1,185 TFLOP/s; its 128 tiles
+// leave 20 of 148 SMs idle, on the others the tensor pipe is 74 % active, L2 47 % busy); 4,096 x 512 x 2,048 with
+// gelu 17.4 to 18.7 us, of which the two epilogues of a CTA are 10: 16 finishing warps hide their own
+// latencies better than 8 (24 us then), 32-row strips spill (20 us).
 constexpr int kTcFinishers = 16;               // warps
 constexpr int kTcThreads = 128 + 32 * kTcFinishers;
 constexpr int kTcK = 64;                       // k per step
@@ -153,7 +156,9 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 
 // PROMOTE (results that stay fp32): the tensor cores' sum is moved into fp32 registers, and added there
 // with rounding to nearest, after every 16 (24) instructions: in the accumulator every addition cuts
-// towards zero, which over thousands of them would cost a few units of 2^-18.
+// towards zero, which over thousands of them would cost a few units of 2^-18.  Results that are rounded
+// to bf16 stay in the accumulator: k / 16 cuts of at most 2^-23 of a sum that grows like a random walk are
+// (2/3) k / 16 x 2^-23 of the result, 1.3e-3 at k = 267,735, about what the rounding to bf16 costs.
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {

@@ -189,8 +189,9 @@ int may_pair(const Product& q) {
 }
 
 // Tile width, CTAs that share a tile's steps, CTAs that share a tile: the choice with the least time
-// by a model whose four constants were fitted to 180 measured products of 12 to 100,000 rows, columns
-// and terms in both types (its choice is 0.8 % above the best one on average, 15 % at worst).
+// by a model whose eight constants were fitted to 180 measured products of 12 to 100,000 rows, columns
+// and terms in both types (its choice was 0.8 % above the best one on average, 15 % at worst; no sum along
+// a vocabulary among them).  The 1.45 for pairs with a strided A says what was measured, not why.
 struct TcShape { int bn, split, pair; };
 TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided) {
   TcShape best{64, 1, 1};
