@@ -189,6 +189,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  // Before the wait for the kernel before: a block of it that has yet to allocate (the fused round lets
+  // its dependents start first thing) cannot be on this SM, whose registers or shared memory do not hold both.
   if (warp == 1) {
     if (PAIR == 1) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC) : "memory");

@@ -266,3 +266,52 @@ def test_adagrad_with_an_infinite_clip_norm_does_not_clip():
         states.append((theta, accum))
     assert bool(torch.isfinite(states[0][0]).all())
     assert all(torch.equal(p, q) for p, q in zip(*states))
+
+
+def test_stream_handles(ops):
+    """Streams given as torch streams, as their handles, and as the two names of the default stream."""
+    g = gen(37)
+    x, w = rnd(g, (40, 131), F), rnd(g, (77, 131), F)
+    ref = ops.linear_forward(x, w)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream, torch.cuda.default_stream(), 0, 1):
+        got = ops.linear_forward(x, w, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, ref)
+    with torch.cuda.stream(side):
+        got = ops.linear_forward(x, w, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got, ref)
+
+
+def test_round_and_linear_layers_in_turn(ops):
+    """Synchronisation rounds with their tile in tensor memory and tensor-core products, each launched
+    while the one before still runs: same results as one at a time."""
+    g = gen(41)
+    K, N = 4, 200_000
+    x, w = rnd(g, (512, 256), BF), rnd(g, (1024, 256), BF)
+    big, v = rnd(g, (4096, 512), BF), rnd(g, (2048, 512), BF)
+    refs = ops.linear_forward(x, w), ops.linear_forward(big, v)
+    start = rnd(g, (K, N), F)
+    outcomes = []
+    for wait in (True, False):
+        theta = start.clone()
+        omega, delta = start.clone(), torch.zeros_like(start)
+        ctx = binding.Gbmuf(theta, omega, delta, K=K, N=N, ld=N, p=1, q=1, eta=0.5, zeta=1.0, seed=3)
+        ctx.set_partition([0, 70_001, N])
+        torch.cuda.synchronize()
+        got = []
+        for t in range(1, 9):
+            ctx.sync_round(t)
+            if wait:
+                torch.cuda.synchronize()
+            got += [ops.linear_forward(x, w), ops.linear_forward(big, v)]
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert ctx.device_status() == 0
+        ctx.destroy()
+        assert all(torch.equal(a, refs[i % 2]) for i, a in enumerate(got))
+        outcomes.append(torch.stack([theta, omega, delta]))
+    assert torch.equal(*outcomes) and not torch.equal(outcomes[0][0], start)
