@@ -445,6 +445,38 @@ typedef struct {
 } gbmuf_cross_entropy_args;
 gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args* a, void* stream);
 
+/* The softmax layer and its cross-entropy in one call, without the logits in memory: with
+ * z = x w^T + bias, lse_i = log sum_v exp(z_iv) and s_i = scale * row_weight_i,
+ *   loss_i = s_i (lse_i - z_it), t the target of row i
+ *   d_iv = s_i (exp(z_iv - lse_i) - [v = t]),  dx = d w,  dw = d^T x,  dbias = sum over the rows of d.
+ * x [rows][n_in], w [vocab][n_in], bias [vocab] or NULL, all of dtype; targets, row_weight, loss, lse,
+ * ignore_index: as in gbmuf_cross_entropy, with its meaning of ignored rows, of words that cannot occur
+ * (a bias of -inf), of NaN and of targets outside the vocabulary.
+ * dx [rows][n_in] of dtype, dw [vocab][n_in] and dbias [vocab] of grad_dtype: each may be NULL, and with all
+ * three NULL only the loss is computed; with accumulate != 0 dw and dbias are added to what they hold.
+ * The logits are formed twice, for the statistics and for the gradients, and the second time a piece of the
+ * vocabulary at a time: `piece` words, or 0 for a choice that keeps the gradient of a piece's logits near
+ * 64 MB (2,048 words at least).  Statistics, sums over pieces and dbias's sums are fp32.  Logits are not
+ * rounded; of bf16 operands d is rounded to bf16 before it is multiplied with w and x (as the dlogits of
+ * gbmuf_cross_entropy are), of fp32 operands it is taken as three bf16 parts.  Row weights are finite.
+ * Two calls give the same bits; another `piece` may give others. */
+typedef struct {
+  int64_t rows, n_in, vocab;
+  const void *x, *w, *bias;
+  const int64_t* targets;
+  const float* row_weight;
+  float *loss, *lse;
+  void *dx, *dw, *dbias;
+  int64_t ld_x, ld_w, ld_dx, ld_dw, ignore_index, piece;
+  int32_t dtype, grad_dtype, accumulate;
+  float scale;
+  void* workspace;
+  int64_t workspace_bytes;
+} gbmuf_linear_cross_entropy_args;
+gbmuf_status gbmuf_linear_cross_entropy_workspace(gbmuf_ops* ops, const gbmuf_linear_cross_entropy_args* a,
+                                                  int64_t* bytes);
+gbmuf_status gbmuf_linear_cross_entropy(gbmuf_ops* ops, const gbmuf_linear_cross_entropy_args* a, void* stream);
+
 /* The norm of all gradients of a group (a worker), over any number of tensors, and clipping.
  * A tensor is [rows][cols] with row stride ld_grad, fp32 or bf16; out (or NULL: it only counts in
  * the norm) has row stride ld_out and is fp32 or of the gradient's own type, and may be the

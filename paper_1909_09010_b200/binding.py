@@ -32,7 +32,8 @@ EXPORTS = ["gbmuf_create", "gbmuf_set_partition", "gbmuf_init", "gbmuf_local_per
            "gbmuf_linear_forward_workspace", "gbmuf_linear_forward",
            "gbmuf_linear_backward_input_workspace", "gbmuf_linear_backward_input",
            "gbmuf_linear_backward_weight_workspace", "gbmuf_linear_backward_weight",
-           "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_clip_create",
+           "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_linear_cross_entropy_workspace",
+           "gbmuf_linear_cross_entropy", "gbmuf_clip_create",
            "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_device_status",
            "gbmuf_clip_selftest_wait_timeout", "gbmuf_clip_destroy"]
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
@@ -85,6 +86,13 @@ class CrossEntropyArgs(ctypes.Structure):
     """Mirror of ``gbmuf_cross_entropy_args``."""
     _fields_ = _fields("l rows vocab, p logits targets row_weight loss lse dlogits, "
                        "l ld_logits ld_dlogits ignore_index, i dtype, f scale")
+
+
+class LinearCrossEntropyArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_linear_cross_entropy_args``."""
+    _fields_ = _fields("l rows n_in vocab, p x w bias targets row_weight loss lse dx dw dbias, "
+                       "l ld_x ld_w ld_dx ld_dw ignore_index piece, i dtype grad_dtype accumulate, f scale, "
+                       "p workspace, l workspace_bytes")
 
 
 class GradTensor(ctypes.Structure):
@@ -147,6 +155,8 @@ def lib() -> ctypes.CDLL:
         getattr(L, "gbmuf_linear_" + name + "_workspace").argtypes = [vp, vp, vp]
     L.gbmuf_activation_backward.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
     L.gbmuf_cross_entropy.argtypes = [vp, vp, vp]
+    L.gbmuf_linear_cross_entropy_workspace.argtypes = [vp, vp, vp]
+    L.gbmuf_linear_cross_entropy.argtypes = [vp, vp, vp]
     L.gbmuf_clip_create.argtypes = [i32, i32, i64, vp, ctypes.POINTER(vp)]
     L.gbmuf_clip_set_tensors.argtypes = [vp, i64, vp]
     L.gbmuf_clip_norms.argtypes = [vp, vp, vp]
@@ -439,6 +449,7 @@ _pack_forward = _packer(LinearForwardArgs)
 _pack_backward_input = _packer(LinearBackwardInputArgs)
 _pack_backward_weight = _packer(LinearBackwardWeightArgs)
 _pack_cross_entropy = _packer(CrossEntropyArgs)
+_pack_linear_cross_entropy = _packer(LinearCrossEntropyArgs)
 
 
 def _dtype_code(t) -> int:
@@ -690,6 +701,70 @@ class LocalOps(_OnDevice):
         if st != GBMUF_OK:
             self._check(st)
         return (loss, lse) if d is None else (loss, lse, d)
+
+    def linear_cross_entropy(self, x, w, targets, bias=None, ignore_index=-100, row_weight=None, scale=1.0,
+                             want_grad=True, want_weight_grad=True, grad_dtype=None, dx_out=None, dw_out=None,
+                             dbias_out=None, accumulate=False, piece=0, stream=None):
+        """``gbmuf_linear_cross_entropy``: the softmax layer x w^T + bias and its cross-entropy without the
+        logits in memory.  Returns (loss, lse) without ``want_grad``; else (loss, lse, dx), followed with
+        ``want_weight_grad`` by dw and, with a bias, dbias, in ``grad_dtype`` (default: the operands' type);
+        with ``accumulate`` those are added to ``dw_out`` and ``dbias_out``.  loss and lse are float32 [rows].
+        ``piece``: words of the vocabulary whose gradient is in memory at a time (0: the library's choice)."""
+        if stream is not None:
+            return self._on_stream(stream, (dx_out, dw_out, dbias_out), self.linear_cross_entropy, x, w, targets,
+                                   bias, ignore_index, row_weight, scale, want_grad, want_weight_grad, grad_dtype,
+                                   dx_out, dw_out, dbias_out, accumulate, piece)
+        torch = self._torch
+        rows, n_in = _two_dims("x", x)
+        vocab = _two_dims("w", w)[0]
+        dtype, dev = x.dtype, self.device
+        code = _dtype_code(x)
+        px, lx = _matrix("x", x, (rows, n_in), dtype, dev)
+        pw, lw = _matrix("w", w, (vocab, n_in), dtype, dev)
+        pb = _vector("bias", bias, vocab, dtype, dev)
+        pt = _vector("targets", targets, rows, torch.int64, dev)
+        pr = _vector("row_weight", row_weight, rows, torch.float32, dev)
+        if not want_grad and not (dx_out is None and dw_out is None and dbias_out is None):
+            raise ValueError("dx_out, dw_out and dbias_out need want_grad")
+        if not want_weight_grad and not (dw_out is None and dbias_out is None):
+            raise ValueError("dw_out and dbias_out need want_weight_grad")
+        if dbias_out is not None and bias is None:
+            raise ValueError("dbias_out needs a bias")
+        weights = want_grad and want_weight_grad
+        for name, t in (("dw_out", dw_out), ("dbias_out", dbias_out)):
+            if t is None:
+                continue
+            if grad_dtype is None:
+                grad_dtype = t.dtype
+            elif t.dtype is not grad_dtype:
+                raise TypeError(f"{name} must be {grad_dtype}, not {t.dtype}")
+        if grad_dtype is None:
+            grad_dtype = dtype
+        if accumulate and weights and (dw_out is None or (bias is not None and dbias_out is None)):
+            raise ValueError("accumulate adds to dw_out and dbias_out: hand them in")
+        results, pdx, ldx, pdw, ldw, pdb, grad_code = [], 0, 0, 0, 0, 0, code
+        if want_grad:
+            dx, pdx, ldx = _result("dx_out", dx_out, x, (rows, n_in), dtype, dev)
+            results.append(dx)
+        if weights:
+            dw, pdw, ldw = _result("dw_out", dw_out, x, (vocab, n_in), grad_dtype, dev)
+            grad_code = _dtype_code(dw)
+            results.append(dw)
+            if bias is not None:
+                db = dbias_out if dbias_out is not None else x.new_empty((vocab,), dtype=grad_dtype)
+                pdb = _vector("dbias_out", db, vocab, grad_dtype, dev)
+                results.append(db)
+        loss = x.new_empty((rows,), dtype=torch.float32)
+        lse = x.new_empty((rows,), dtype=torch.float32)
+        fields = (rows, n_in, vocab, px, pw, pb, pt, pr, loss.data_ptr(), lse.data_ptr(), pdx, pdw, pdb, lx, lw, ldx,
+                  ldw, ignore_index, piece, code, grad_code, 1 if accumulate else 0, scale)
+        args, need = _pack_linear_cross_entropy(*fields, 0, 0), ctypes.c_int64()
+        self._check(self._L.gbmuf_linear_cross_entropy_workspace(self._h, args, ctypes.byref(need)))
+        if need.value:
+            work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+            args = _pack_linear_cross_entropy(*fields, work.data_ptr(), need.value)
+        self._check(self._L.gbmuf_linear_cross_entropy(self._h, args, self._raw_stream(dev)))
+        return (loss, lse, *results)
 
     def device_status(self, stream=None) -> int:
         """Waits for the stream; reads and clears the status word."""

@@ -1,0 +1,320 @@
+// libgbmuf: the softmax layer with its cross-entropy and all gradients, in pieces of the vocabulary, without
+// the logits in memory.  The interface is in include/gbmuf.h; this file holds the host side and the C ABI,
+// the kernels are those of linear_tc.cuh with the epilogues of linear_loss.cuh.
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <string>
+#include <type_traits>
+
+#include "gbmuf.h"
+
+#include "host_common.h"
+#include "primitives.cuh"
+#include "packed_math.cuh"
+#include "linear_epilogue.cuh"
+#include "linear_pack.cuh"
+#include "softmax_math.cuh"
+#include "linear_loss.cuh"
+#include "linear_tc.cuh"
+#include "linear_tc_host.h"
+#include "ready_product.h"
+
+namespace {
+
+typedef gbmuf_linear_cross_entropy_args Args;
+
+// The gradient of a piece's logits is written once and read twice, by the two products; it should still
+// be in the L2 cache then (126 MB, next to the piece's weights and their gradient).
+constexpr long long kPieceBytes = 64ll << 20;
+constexpr long long kPieceLeast = 2048;           // words: fewer leave the products too short
+
+gbmuf_status check(const gbmuf_ops* ops, const Args* a) {
+  if (!ops || !a) return invalid("ops and args must not be NULL");
+  if (a->rows < 0 || a->n_in < 0 || a->vocab < 0) return invalid("rows, n_in and vocab must not be negative");
+  if (a->rows > kMostDim || a->n_in > kMostDim || a->vocab > kMostDim)
+    return refuse(GBMUF_ERR_UNSUPPORTED, "rows, n_in and vocab must be at most 2^31 - 2^16");
+  if (a->rows > 0 && a->vocab == 0) return invalid("vocab must not be 0");
+  if (!is_dtype(a->dtype) || !is_dtype(a->grad_dtype)) return invalid("dtype and grad_dtype must be GBMUF_F32 or GBMUF_BF16");
+  if (!(a->scale == a->scale)) return invalid("scale must not be NaN");
+  if (a->piece < 0) return invalid("piece must not be negative");
+  CHECK_MATRIX("x", a->x, a->rows, a->n_in, a->ld_x, a->dtype, false);
+  CHECK_MATRIX("w", a->w, a->vocab, a->n_in, a->ld_w, a->dtype, false);
+  CHECK_MATRIX("bias", a->bias, 1, a->vocab, a->vocab, a->dtype, true);
+  CHECK_MATRIX("dx", a->dx, a->rows, a->n_in, a->ld_dx, a->dtype, true);
+  CHECK_MATRIX("dw", a->dw, a->vocab, a->n_in, a->ld_dw, a->grad_dtype, true);
+  CHECK_MATRIX("dbias", a->dbias, 1, a->vocab, a->vocab, a->grad_dtype, true);
+  if (a->rows > 0 && !a->targets) return invalid("targets is NULL");
+  if ((uintptr_t)a->targets % 8 != 0) return invalid("targets is not aligned to its element type");
+  if (((uintptr_t)a->row_weight | (uintptr_t)a->loss | (uintptr_t)a->lse) % 4 != 0)
+    return invalid("row_weight, loss or lse is not aligned to its element type");
+  return GBMUF_OK;
+}
+
+// Logits of `words` words for `rows` rows, statistics: launch shape, tiles side by side, slots per row.
+struct StatsShape { TcShape tc; int at_once, slots; };
+// Row tiles whose CTAs fill at least nine tenths of the GPU when each keeps to one row tile.
+int rows_at_once(int tiles, int fit) {
+  int t = std::min(tiles, fit);
+  while (fit / t * t * 10 < fit * 9) --t;
+  return t;
+}
+struct Plan {
+  int parts;                                      // bf16 parts of an operand
+  bool grad, x_ready, w_ready;                    // ready: read in place
+  long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, rows_padded, strips, slot_rows;
+  TcShape stats, tc;                              // of the two products that form the logits
+  long long x_off, w_off, row_off, target_off, slot_off, d_off, partial_off, acc_off, bytes;
+};
+
+Operand operand_x(const Args* a) { return {a->x, a->rows, a->n_in, a->ld_x, true, false, 0}; }
+Operand operand_w(const Args* a, long long v0, long long words) {
+  return {static_cast<const char*>(a->w) + v0 * a->ld_w * (long long)size_of(a->dtype), words, a->n_in, a->ld_w, true, false, 0};
+}
+Product logits_product(const Plan& p, const Args* a, bool stats, long long rows, long long words) {
+  Product q{};
+  q.R = stats ? words : rows; q.C = stats ? rows : words; q.K = a->n_in; q.dtype = a->dtype;
+  return q;
+}
+int row_tiles(const TcShape& s, long long rows) { return (int)((rows + 128 * s.pair - 1) / (128 * s.pair)); }
+// Row tiles of the next launch of the statistics, with `left` rows to do.
+int stats_rows(const gbmuf_ops* ops, const TcShape& s, long long left) { return rows_at_once(row_tiles(s, left), ops->num_sms / s.pair); }
+int stats_slots(const gbmuf_ops* ops, const TcShape& s, int tiles_c, long long words) {
+  return (int)std::min<long long>(ops->num_sms / s.pair / tiles_c, (words + s.bn - 1) / s.bn) * (kTcFinishers / 4);
+}
+
+Plan make_plan(const gbmuf_ops* ops, const Args* a) {
+  Plan p{};
+  p.parts = a->dtype == GBMUF_F32 ? 3 : 1;
+  p.grad = a->dx || a->dw || a->dbias;
+  const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * std::max<long long>(a->rows, 1)) / 256 * 256);
+  p.x_ready = in_place(operand_x(a), a->dtype);
+  p.w_ready = in_place(operand_w(a, 0, a->vocab), a->dtype);
+  p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : a->vocab;
+  if (!a->piece && (p.grad || !p.w_ready) && a->vocab > most) {
+    const long long n = (a->vocab + most - 1) / most;
+    p.piece = round_up((a->vocab + n - 1) / n, 256);
+  }
+  p.pieces = (a->vocab + p.piece - 1) / p.piece;
+  p.ld_x = p.x_ready && a->rows > 1 ? a->ld_x : round_up(a->n_in, 8);      // the stride of a single row says nothing
+  p.ld_w = p.w_ready && a->vocab > 1 ? a->ld_w : round_up(a->n_in, 8);
+  p.ld_d = round_up(p.piece, 8);
+  p.ld_acc = round_up(a->n_in, 4);
+  p.rows_padded = round_up(a->rows, kLossRowPad);
+  const long long together = p.w_ready ? a->vocab : p.piece;
+  p.stats = choose_shape(ops, logits_product(p, a, true, a->rows, together), p.parts, false, false, false);
+  p.tc = choose_shape(ops, logits_product(p, a, false, a->rows, p.piece), p.parts, false, false, false);
+  long long at = 0;
+  auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
+  p.x_off = take(p.x_ready ? 0 : packed_bytes(operand_x(a), a->dtype));
+  p.w_off = take(p.w_ready ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype));
+  p.row_off = take(p.rows_padded * (long long)sizeof(LossRow));
+  p.target_off = take(a->rows * 4);
+  long long slots = 0;                            // of the widest launch
+  for (long long r = 0; r < a->rows;) {
+    const int t = stats_rows(ops, p.stats, a->rows - r);
+    const long long n = std::min<long long>(a->rows - r, 128ll * p.stats.pair * t);
+    slots = std::max(slots, n * stats_slots(ops, p.stats, t, together) * (p.w_ready ? 1 : p.pieces));
+    r += n;
+  }
+  p.slot_off = take(slots * 8);
+  if (p.grad) {
+    p.d_off = take(a->rows * p.ld_d * 2 * p.parts);
+    p.strips = (a->rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
+    p.partial_off = take(a->dbias ? p.strips * p.ld_d * 4 : 0);
+    p.acc_off = take(a->dx && p.pieces > 1 && a->dtype == GBMUF_BF16 ? a->rows * p.ld_acc * 4 : 0);
+  }
+  p.bytes = at;
+  return p;
+}
+
+template <int KIND, typename T, int PARTS>
+gbmuf_status launch_logits(const gbmuf_ops* ops, const TcShape& s, TcParams& P, int at_once, const Operand& a, const Operand& b,
+                           int32_t dtype, cudaStream_t st) {
+  CUtensorMap ma{}, mb{};
+  if (P.ksteps > 0) {
+    if (gbmuf_status rc = operand_map(a, dtype, nullptr, 128, &ma)) return rc;
+    if (gbmuf_status rc = operand_map(b, dtype, nullptr, s.bn / s.pair, &mb)) return rc;
+  }
+  if (s.pair == 2)
+    return s.bn == 128 ? launch_tc_at<KIND, T, T, PARTS, 128, 2>(ops, P, at_once, ma, mb, st)
+                       : launch_tc_at<KIND, T, T, PARTS, 256, 2>(ops, P, at_once, ma, mb, st);
+  if (s.bn == 32) return launch_tc_at<KIND, T, T, PARTS, 32, 1>(ops, P, at_once, ma, mb, st);
+  if constexpr (PARTS == 1)
+    if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 1>(ops, P, at_once, ma, mb, st);
+  return s.bn == 64 ? launch_tc_at<KIND, T, T, PARTS, 64, 1>(ops, P, at_once, ma, mb, st)
+                    : launch_tc_at<KIND, T, T, PARTS, 128, 1>(ops, P, at_once, ma, mb, st);
+}
+
+gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, cudaStream_t st) {
+  const PackJob j = pack_job(ops, o, dtype, dst);
+  if (j.blocks == 0) return GBMUF_OK;
+  return launched("launch of the operand-packing kernel",
+                  launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)j.blocks, 1, 256, 0, st, j, PackJob{}));
+}
+
+template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cudaStream_t st) {
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  const Plan p = make_plan(ops, a);
+  if (p.bytes > a->workspace_bytes || !a->workspace || (uintptr_t)a->workspace % 256 != 0)
+    return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(p.bytes) + " bytes");
+  char* const ws = static_cast<char*>(a->workspace);
+  const long long N = a->rows, V = a->vocab, H = a->n_in, size = (long long)sizeof(T);
+  Operand x = operand_x(a);
+  if (!p.x_ready) {
+    if (gbmuf_status rc = pack(ops, x, a->dtype, ws + p.x_off, st)) return rc;
+    x.p = ws + p.x_off;
+  }
+  x.ld = p.ld_x;
+  x.ready = true;
+  x.part = N * x.ld;
+  auto weights = [&](long long v0, long long words, Operand& w) -> gbmuf_status {
+    w = operand_w(a, v0, words);
+    if (!p.w_ready) {
+      if (gbmuf_status rc = pack(ops, w, a->dtype, ws + p.w_off, st)) return rc;
+      w.p = ws + p.w_off;
+    }
+    w.ld = p.ld_w;
+    w.ready = true;
+    return GBMUF_OK;
+  };
+  auto tc_params = [&](const TcShape& s, long long R, long long C, bool stats) {
+    TcParams P{};
+    P.status = ops->d_status; P.R = (int)R; P.C = (int)C; P.split = 1;
+    P.ksteps = (int)((H + kTcK - 1) / kTcK);
+    const int tiles_r = (int)((R + s.bn - 1) / s.bn), tiles_c = (int)((C + 128 * s.pair - 1) / (128 * s.pair));
+    P.tiles_fast = stats ? tiles_c : tiles_r;
+    P.tiles = tiles_r * tiles_c;
+    return P;
+  };
+  const TcShape& s = p.stats;
+  const long long most_tiles = std::max((V / s.bn + 1) * (N / 128 + 1), (V / 128 + 1) * (N / p.tc.bn + 1));
+  if (most_tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles of logits");
+  // ---- statistics: every CTA keeps to one row tile, so its threads keep a row's running maximum and sum
+  for (long long r0 = 0; r0 < N;) {
+    const int t = stats_rows(ops, s, N - r0);
+    const long long n = std::min<long long>(N - r0, 128ll * s.pair * t), ld = n;
+    const long long step = p.w_ready ? V : p.piece;
+    int slots = 0;
+    for (long long v0 = 0; v0 < V; v0 += step) {
+      const long long words = std::min(step, V - v0);
+      Operand w;
+      if (gbmuf_status rc = weights(v0, words, w)) return rc;
+      Operand xr = x;
+      xr.p = static_cast<const char*>(x.p) + r0 * x.ld * 2;
+      xr.outer = n;
+      TcParams P = tc_params(s, words, n, true);
+      P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
+      P.E.loss_rows = a->targets + r0;
+      P.E.target_logit = reinterpret_cast<float*>(ws + p.target_off) + r0;
+      P.E.partial = reinterpret_cast<float2*>(ws + p.slot_off) + slots * ld;
+      P.E.ld_partial = ld;
+      P.E.first_word = (int)v0;
+      const int here = stats_slots(ops, s, t, words);
+      if (gbmuf_status rc = launch_logits<kLossStats, T, PARTS>(ops, s, P, here / (kTcFinishers / 4) * t, xr, w, a->dtype, st)) return rc;
+      slots += here;
+    }
+    JoinParams J{};
+    J.L.targets = a->targets + r0; J.L.row_weight = a->row_weight ? a->row_weight + r0 : nullptr;
+    J.L.loss = a->loss ? a->loss + r0 : nullptr; J.L.lse = a->lse ? a->lse + r0 : nullptr;
+    J.L.rows = n; J.L.vocab = V; J.L.ignore_index = a->ignore_index; J.L.scale = a->scale; J.L.status = ops->d_status;
+    J.slots = reinterpret_cast<const float2*>(ws + p.slot_off);
+    J.target_logit = reinterpret_cast<const float*>(ws + p.target_off) + r0;
+    J.out = p.grad ? reinterpret_cast<LossRow*>(ws + p.row_off) + r0 : nullptr;
+    J.ld = ld; J.count = slots;
+    J.rows_padded = r0 + n == N ? p.rows_padded - r0 : n;
+    const cudaError_t e = launch(loss_join_kernel, (unsigned)((J.rows_padded + 31) / 32), 1, 32 * kJoinShares, 0, st, J);
+    if (e != cudaSuccess) return cuda_refuse("launch of the loss's join kernel", e);
+    r0 += n;
+  }
+  if (!p.grad) return GBMUF_OK;
+  // ---- gradients, a piece of the vocabulary at a time
+  for (long long i = 0, v0 = 0; v0 < V; ++i, v0 += p.piece) {
+    const long long words = std::min(p.piece, V - v0);
+    const bool last = v0 + words == V;
+    Operand w;
+    if (gbmuf_status rc = weights(v0, words, w)) return rc;
+    void* const d = ws + p.d_off;
+    // an even number of columns, so that bf16 goes out two at a time: the last one may lie beyond the piece
+    TcParams P = tc_params(p.tc, N, round_up(words, 2), false);
+    P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
+    P.E.loss_rows = ws + p.row_off;
+    P.E.partial = a->dbias ? ws + p.partial_off : nullptr;
+    P.E.ld_partial = p.ld_d;
+    P.E.first_word = (int)v0; P.E.words = (int)words;
+    P.E.out0 = d; P.E.ld_out0 = p.ld_d; P.E.part = N * p.ld_d; P.E.pairs = 1;
+    const int at_once = std::min(P.tiles, ops->num_sms / p.tc.pair);
+    if (gbmuf_status rc = launch_logits<kLossGrad, T, PARTS>(ops, p.tc, P, at_once, w, x, a->dtype, st)) return rc;
+    if (a->dbias) {
+      cudaError_t e = cudaSuccess;
+      DISPATCH_DTYPE(a->grad_dtype, TO, e = launch(loss_bias_kernel<TO>, (unsigned)((words + 255) / 256), 1, 256, 0, st,
+                                                   reinterpret_cast<const float*>(ws + p.partial_off), p.ld_d, (int)p.strips, words,
+                                                   static_cast<TO*>(a->dbias) + v0, (int)a->accumulate));
+      if (e != cudaSuccess) return cuda_refuse("launch of the loss's bias-gradient kernel", e);
+    }
+    if (H == 0) continue;
+    gbmuf_ready_product r{};
+    r.dtype = a->dtype;
+    r.b = d; r.b_outer = N; r.b_inner = words; r.b_ld = p.ld_d;
+    if (a->dw) {
+      r.weight_grad = true; r.out_dtype = a->grad_dtype; r.accumulate = a->accumulate;
+      r.a = x.p; r.a_outer = N; r.a_inner = H; r.a_ld = x.ld;
+      r.rows = words; r.cols = H; r.terms = N;
+      r.out = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); r.ld_out = a->ld_dw;
+      if (gbmuf_status rc = gbmuf_run_ready_product(ops, r, st)) return rc;
+    }
+    if (a->dx) {
+      r.weight_grad = false; r.accumulate = 0;
+      r.a = w.p; r.a_outer = words; r.a_inner = H; r.a_ld = w.ld;
+      r.rows = N; r.cols = H; r.terms = words;
+      if (PARTS == 1 && p.pieces > 1) {
+        r.out_dtype = GBMUF_F32;
+        r.residual = i > 0 ? ws + p.acc_off : nullptr; r.ld_residual = p.ld_acc;
+        r.out = last ? nullptr : ws + p.acc_off; r.ld_out = p.ld_acc;
+        r.rounded = last ? a->dx : nullptr; r.ld_rounded = a->ld_dx;
+      } else {
+        r.out_dtype = a->dtype;
+        r.residual = i > 0 ? a->dx : nullptr; r.ld_residual = a->ld_dx;
+        r.out = a->dx; r.ld_out = a->ld_dx; r.rounded = nullptr;
+      }
+      if (gbmuf_status rc = gbmuf_run_ready_product(ops, r, st)) return rc;
+    }
+  }
+  return GBMUF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gbmuf_status gbmuf_linear_cross_entropy_workspace(gbmuf_ops* ops, const gbmuf_linear_cross_entropy_args* a, int64_t* bytes) {
+  return guarded([&]() -> gbmuf_status {
+    if (!bytes) return invalid("bytes is NULL");
+    if (gbmuf_status st = check(ops, a)) return st;
+    *bytes = a->rows == 0 ? 0 : make_plan(ops, a).bytes;
+    return GBMUF_OK;
+  });
+}
+
+gbmuf_status gbmuf_linear_cross_entropy(gbmuf_ops* ops, const gbmuf_linear_cross_entropy_args* a, void* stream) {
+  return guarded([&]() -> gbmuf_status {
+    if (gbmuf_status st = check(ops, a)) return st;
+    if (a->rows == 0) {                            // empty sums
+      if (a->accumulate || a->vocab == 0 || (!a->dw && !a->dbias)) return GBMUF_OK;
+      gbmuf_linear_backward_weight_args z{};
+      z.n_in = a->n_in; z.n_out = a->vocab; z.dw = a->dw; z.dbias = a->dbias; z.ld_dw = a->ld_dw;
+      z.ld_dz = a->vocab; z.ld_x = a->n_in;
+      z.dtype = a->dtype; z.grad_dtype = a->grad_dtype;
+      return gbmuf_linear_backward_weight(ops, &z, stream);
+    }
+    DeviceGuard guard(ops->device);
+    if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
+    DISPATCH_DTYPE(a->dtype, T, return run<T>(ops, a, (cudaStream_t)stream));
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,191 @@
+// The softmax layer with its cross-entropy: what happens to a tile of logits while it is in tensor memory.
+// Part of libgbmuf (CUDA, sm_100a); included before linear_tc.cuh.
+#ifndef GBMUF_CSRC_LINEAR_LOSS_CUH
+#define GBMUF_CSRC_LINEAR_LOSS_CUH
+
+namespace {
+
+// z = x w^T + bias is formed twice and never stored.  The first time (kLossStats) a thread of the finishing
+// warps owns a row of the batch and goes through that row's logits of a tile with a running maximum and
+// sum: rows of the batch lie along the lanes, words along the columns, so no two threads share a row's tile.
+// The second time (kLossGrad) words lie along the lanes and d = w (exp(z - m) / s - [target]) of a piece of
+// the vocabulary is stored, once, as the operand of the two products that follow: rounded to bf16, or for
+// fp32 as its three parts.  bf16: that rounding is off by at most 2^-9 of an element, and the products'
+// sums of many such elements by less.
+
+// kLossGrad: what it needs of a row.
+struct __align__(16) LossRow {
+  float m, k, w;             // maximum; weight / sum; weight
+  int target;                // -1: no word of the vocabulary; -2: the row's gradient is zero
+};
+constexpr int kLossRowPad = 256;   // rows of a tile, at most: there are as many LossRow as rows of all tiles
+
+template <typename T, bool PROMOTE> struct RowStats {
+  static constexpr bool FAST = sizeof(T) == 2;
+  float m = -INFINITY;
+  Two s = two(0.0f, 0.0f);
+  int row = -1, slot = 0, target = -1;
+  bool there = false;
+  Shift<FAST> e;
+
+  __device__ __forceinline__ void open(const Epilogue& E, int c, int rows, int at) {
+    if (c == row) return;
+    close(E);
+    row = c;
+    slot = at;
+    m = -INFINITY;
+    s = two(0.0f, 0.0f);
+    e.set(m);
+    there = c < rows;
+    const long long t = there ? static_cast<const long long*>(E.loss_rows)[c] : -1;
+    target = t >= 0 && t <= 0x7fffffff ? (int)t : -1;
+  }
+  // N words from r on
+  template <int N> __device__ __forceinline__ void add(const Epilogue& E, float (&v)[N], int r, int words) {
+    if (E.bias) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += r + i < words ? to_f32(static_cast<const T*>(E.bias)[r + i]) : 0.0f;
+    }
+    if (r + N > words) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (r + i >= words) v[i] = -INFINITY;
+    }
+    const int at_target = target - E.first_word - r;
+    if ((unsigned)at_target < (unsigned)N) {
+      float x = v[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) x = at_target == i ? v[i] : x;
+      E.target_logit[row] = x;
+    }
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+    if (top > m) {
+      const float before = m;
+      m = top;
+      e.set(m);
+      if (before != -INFINITY) {                           // else the sum is 0 or NaN
+        const float k = e(before);
+        s = s * two(k, k);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; i += 2) s = s + e(v[i], v[i + 1]);
+  }
+  __device__ __forceinline__ void close(const Epilogue& E) {
+    if (!there) return;
+    float a, b;
+    apart(s, a, b);
+    static_cast<float2*>(E.partial)[(long long)slot * E.ld_partial + row] = make_float2(m, a + b);
+  }
+};
+
+template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
+  float column;              // sum over the strip's rows
+
+  __device__ __forceinline__ void ask(const Epilogue&, int, int, int, int, int) {}
+  template <bool WHOLE>
+  __device__ __forceinline__ void finish_(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
+    constexpr bool FAST = sizeof(T) == 2;
+    const LossRow* const rows = static_cast<const LossRow*>(E.loss_rows) + r;
+    const int word = c + E.first_word;
+    Two sum = two(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const LossRow a = rows[i], b = rows[i + 1];
+      const Two z = two(v[i], v[i + 1]) + two(bias, bias);
+      apart(exp_of<FAST>(z + two(-a.m, -b.m)) * two(a.k, b.k), v[i], v[i + 1]);
+      if (word == a.target) v[i] -= a.w;
+      if (word == b.target) v[i + 1] -= b.w;
+      if (a.target == -2) v[i] = 0.0f;
+      if (b.target == -2) v[i + 1] = 0.0f;
+      sum = sum + two(v[i], v[i + 1]);
+    }
+    float s0, s1;
+    apart(sum, s0, s1);
+    column = s0 + s1;
+    if constexpr (FAST) {
+      store_strip<T, WHOLE>(v, E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);
+    } else {
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(E.out0);
+      float part[N];
+#pragma unroll
+      for (int q = 0; q < 3; ++q, out += E.part) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          part[i] = __bfloat162float(__float2bfloat16_rn(v[i]));
+          v[i] -= part[i];
+        }
+        store_strip<__nv_bfloat16, WHOLE>(part, out, E.ld_out0, r, c, R, C, E.pairs, lane);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
+    if (r + N <= R && c - lane + 32 <= C) finish_<true>(E, r, c, R, C, lane, bias, v);
+    else finish_<false>(E, r, c, R, C, lane, bias, v);
+  }
+};
+
+// Joins the statistics of a row's slots, in their order: loss, lse, and what kLossGrad needs (rows past the
+// last get a zero gradient).  32 rows by 16 shares of the slots per block.
+constexpr int kJoinShares = 16;
+struct JoinParams {
+  LossParams L;
+  const float2* slots;
+  const float* target_logit;
+  LossRow* out;              // or NULL
+  long long ld, rows_padded;
+  int count;
+};
+__device__ __forceinline__ void join_stats(float& m, float& s, float2 o) {
+  const float top = fmaxf(m, o.x);
+  if (top == -INFINITY) { s += o.y; return; }              // sums are 0 or NaN
+  s = (m == -INFINITY ? s : s * expf(m - top)) + (o.x == -INFINITY ? o.y : o.y * expf(o.x - top));
+  m = top;
+}
+__global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinParams P) {
+  __shared__ float2 part[kJoinShares][32];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+  const long long row = (long long)blockIdx.x * 32 + lane;
+  float m = -INFINITY, s = 0.0f;
+  if (row < P.L.rows)
+#pragma unroll 4
+    for (int i = share; i < P.count; i += kJoinShares) join_stats(m, s, P.slots[i * P.ld + row]);
+  part[share][lane] = make_float2(m, s);
+  __syncthreads();
+  if (share != 0 || row >= P.rows_padded) return;
+  LossRow out{0.0f, 0.0f, 0.0f, -2};
+  if (row < P.L.rows) {
+    for (int i = 1; i < kJoinShares; ++i) join_stats(m, s, part[i][lane]);
+    const long long t = P.L.targets[row];
+    const float w = P.L.scale * (P.L.row_weight ? P.L.row_weight[row] : 1.0f);
+    const float x = target_inside(P.L, t) ? P.target_logit[row] : 0.0f;
+    const RowOutcome o = row_outcome(P.L, m, s, x, t, w);
+    report_target(P.L, t, w);
+    if (P.L.loss) P.L.loss[row] = o.loss;
+    if (P.L.lse) P.L.lse[row] = o.lse;
+    if (!o.zero) out = LossRow{m == -INFINITY ? 0.0f : m, w / s, w, (int)t};
+  }
+  if (P.out) P.out[row] = out;
+}
+
+// dbias of a piece: the strips' sums in their order.
+template <typename TO>
+__global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, long long ld, int strips, long long words, TO* out,
+                                                        int accumulate) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const long long c = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (c >= words) return;
+  float t = 0.0f;
+#pragma unroll 8
+  for (int i = 0; i < strips; ++i) t += partial[i * ld + c];
+  out[c] = from_f32<TO>(accumulate ? t + to_f32(out[c]) : t);
+}
+
+}  // namespace
+
+#endif  // GBMUF_CSRC_LINEAR_LOSS_CUH

@@ -39,8 +39,8 @@ struct TcParams {
   int32_t* status;
   int R, C;
   int ksteps;            // steps of 64 along k
-  int tiles_r, tiles;    // row tiles; all tiles, row tiles running fastest
-  int tile_step, step_c, step_r;   // from a CTA's tile to its next: tiles, and as column and row tiles
+  int tiles_fast, tiles; // row tiles (kLossStats: column tiles), which run fastest; all tiles
+  int tile_step, step_slow, step_fast;   // from a CTA's tile to its next: tiles, and as tiles of either kind
   int split;             // CTAs of a cluster that share a tile's steps (1: none)
   int stages;
 };
@@ -162,7 +162,7 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
-  constexpr bool A_K = KIND == kForward, B_K = KIND != kWeightGrad, PROMOTE = sizeof(TO) == 4;
+  constexpr bool A_K = KIND != kInputGrad && KIND != kWeightGrad, B_K = KIND != kWeightGrad, PROMOTE = sizeof(TO) == 4;
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
@@ -220,13 +220,21 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)(blockIdx.x / PAIR);
   struct Walk {                                                    // tile number, column tile, row tile
     int tile, c, r;
+    __device__ __forceinline__ int& fast() { return KIND == kLossStats ? c : r; }
+    __device__ __forceinline__ int& slow() { return KIND == kLossStats ? r : c; }
   };
-  auto first = [&] { return Walk{first_tile, first_tile / P.tiles_r, first_tile % P.tiles_r}; };
+  auto first = [&] {
+    Walk w;
+    w.tile = first_tile;
+    w.slow() = first_tile / P.tiles_fast;
+    w.fast() = first_tile % P.tiles_fast;
+    return w;
+  };
   auto next = [&](Walk& w) {
     w.tile += P.tile_step;
-    w.c += P.step_c;
-    w.r += P.step_r;
-    if (w.r >= P.tiles_r) { w.r -= P.tiles_r; ++w.c; }
+    w.slow() += P.step_slow;
+    w.fast() += P.step_fast;
+    if (w.fast() >= P.tiles_fast) { w.fast() -= P.tiles_fast; ++w.slow(); }
   };
 
   if (warp == 0) {
@@ -342,13 +350,74 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
   };
   // Asked for before the wait for the sums and converted after it: a conversion here would wait for it.
-  auto bias_of = [&](int c) { return KIND == kForward && P.E.bias && c < P.C ? static_cast<const T*>(P.E.bias)[c] : from_f32<T>(0.0f); };
-  if (warp >= 4 && P.split == 1) {
+  auto bias_of = [&](int c) { return (KIND == kForward || KIND == kLossGrad) && P.E.bias && c < (KIND == kLossGrad ? P.E.words : P.C) ? static_cast<const T*>(P.E.bias)[c] : from_f32<T>(0.0f); };
+  if constexpr (KIND == kLossStats) {
+    if (warp >= 4) {
+      int n = 0;
+      bool ok = true;
+      RowStats<T, PROMOTE> S;
+      for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
+        S.open(P.E, w.c * TILE_C + side * 128 + quad * 32 + lane, P.C, w.r * (kTcFinishers / 4) + part);
+        const int r0 = w.r * BN + part * NCOL;
+        if (PROMOTE) {
+          float acc[NCOL];
+#pragma unroll
+          for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
+          for (int ch = 0; ch < chunks; ++ch, ++n) {
+            ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < NCOL; j += N) {
+              float v[N];
+              tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+#pragma unroll
+              for (int i = 0; i < N; ++i) acc[j + i] += v[i];
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            release(n & 1);
+          }
+          if (!ok) break;
+#pragma unroll
+          for (int j = 0; j < NCOL; j += N) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = acc[j + i];
+            S.add(P.E, v, r0 + j, P.R);
+          }
+        } else {
+          if (chunks > 0) {
+            ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
+#pragma unroll 1
+          for (int j = 0; j < NCOL; j += N) {
+            float v[N] = {};
+            if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+            S.add(P.E, v, r0 + j, P.R);
+          }
+          if (chunks > 0) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            release(n & 1);
+            ++n;
+          }
+        }
+      }
+      S.close(P.E);
+    }
+  }
+  if (KIND != kLossStats && warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const int c = w.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL;
       const T bias = bias_of(c);
+      float column = 0.0f;                                         // kLossGrad: of the gradients of column c
       if (PROMOTE) {
         float acc[NCOL];
 #pragma unroll
@@ -378,6 +447,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           for (int i = 0; i < N; ++i) v[i] = acc[j + i];
           F.ask(P.E, r0 + j, c, P.R, P.C, lane);
           F.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
+          if constexpr (KIND == kLossGrad) column += F.column;
         }
       } else {
         // what the epilogue reads is requested one strip ahead, the first one during the sums
@@ -396,6 +466,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
           now.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
+          if constexpr (KIND == kLossGrad) column += now.column;
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -404,9 +475,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           ++n;
         }
       }
+      if (KIND == kLossGrad && P.E.partial && c < P.E.words)
+        static_cast<float*>(P.E.partial)[(w.r * (kTcFinishers / 4) + part) * P.E.ld_partial + c] = column;
     }
   }
-  if (PAIR == 1 && P.split > 1) {
+  if constexpr (KIND != kLossStats && KIND != kLossGrad && PAIR == 1) if (P.split > 1) {
     // The cluster's CTAs hold partial sums of one tile.  CTA j finishes accumulator columns
     // [j, j + 1) BN / split: everybody writes its sums of those columns into CTA j's shared memory
     // (the operand ring, idle by then) and CTA j adds them in the order of the ranks.

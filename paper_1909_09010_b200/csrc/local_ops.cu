@@ -4,9 +4,11 @@
 //   packed_math.cuh      two fp32 operations per instruction
 //   linear_epilogue.cuh  activations, and what happens to a finished sum of a matrix product
 //   linear_tc.cuh        matrix products on the tensor cores
+//   linear_loss.cuh      what such a product does with the logits of a loss (linear_loss.cu)
 //   linear_pack.cuh      operands that cannot be read in place: other alignments, fp32 as bf16 parts
 //   linear_rows.cuh      the layer for a few rows, on the fp32 units
 //   column_sum.cuh       column sums (bias gradients), gradient of an activation by itself
+//   softmax_math.cuh     exponentials of logits, a row's loss
 //   cross_entropy.cuh    cross-entropy over a vocabulary with its gradient
 //   grad_clip.cuh        norms over many tensors and the clipped copies
 
@@ -31,20 +33,15 @@
 #include "packed_math.cuh"
 #include "linear_epilogue.cuh"
 #include "linear_pack.cuh"
+#include "softmax_math.cuh"
+#include "linear_loss.cuh"
 #include "linear_tc.cuh"
 #include "linear_rows.cuh"
 #include "column_sum.cuh"
 #include "cross_entropy.cuh"
 #include "grad_clip.cuh"
-
-struct gbmuf_ops {
-  int device = 0;
-  int num_sms = 0;
-  int max_smem = 0;              // opt-in dynamic shared memory per block
-  int32_t* d_status = nullptr;
-  int tc_clusters[4] = {};       // clusters of 1, 2, 4, 8 CTAs of the linear-layer kernel that fit at once
-  int loss_clusters[2][4] = {};  // clusters of 1, 2, 4, 8 CTAs of the cross-entropy kernel (fp32, bf16) that fit at once
-};
+#include "linear_tc_host.h"
+#include "ready_product.h"
 
 struct gbmuf_clip {
   int device = 0, groups = 0, num_sms = 0;
@@ -62,56 +59,6 @@ struct gbmuf_clip {
 
 namespace {
 
-gbmuf_status refuse(gbmuf_status st, const std::string& msg) {
-  gbmuf_set_thread_error(msg);
-  return st;
-}
-gbmuf_status invalid(const std::string& msg) { return refuse(GBMUF_ERR_INVALID_ARG, msg); }
-gbmuf_status cuda_refuse(const char* what, cudaError_t e) {
-  return refuse(GBMUF_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
-}
-// No C++ exception (an allocation that fails) leaves an entry point.
-template <typename F> gbmuf_status guarded(F&& f) {
-  try {
-    return f();
-  } catch (...) {
-    return GBMUF_ERR_ALLOC;
-  }
-}
-
-// Every kernel of this file is launched as a programmatic dependent of the work before it in the
-// stream: its blocks may become resident while that ends, and it waits (grid_dependency_wait) before
-// it touches memory.  In clusters of `cluster` blocks.
-template <typename... P, typename... A>
-cudaError_t launch(void (*kernel)(P...), unsigned grid, unsigned cluster, int threads, uint32_t smem, cudaStream_t st, const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
-  cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-gbmuf_status launched(const char* what, cudaError_t e) { return e == cudaSuccess ? GBMUF_OK : cuda_refuse(what, e); }
-
-size_t size_of(int32_t dtype) { return dtype == GBMUF_F32 ? 4 : 2; }
-constexpr int64_t kMostDim = 0x7fffffff - 0xffff;     // indices stay in 32 bits past the last tile
-bool is_dtype(int32_t d) { return d == GBMUF_F32 || d == GBMUF_BF16; }
-
-// A [rows][cols] operand: NULL only where allowed, aligned to its elements, rows that do not
-// overlap, extent within 63 bits.  Empty ones are not looked at.
-const char* check_matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, bool optional) {
-  if (!p) return optional || rows == 0 || cols == 0 ? nullptr : "is NULL";
-  if ((uintptr_t)p % size_of(dtype) != 0) return "is not aligned to its element type";
-  if (rows > 0 && cols > 0 && ld < cols) return "has a row stride below its columns";
-  if ((rows > 1 && ld > ((int64_t)1 << 40)) || (__int128)rows * std::max(ld, cols) > ((__int128)1 << 56)) return "has an extent above 2^56 elements";
-  return nullptr;
-}
-#define CHECK_MATRIX(name, p, rows, cols, ld, dtype, optional)                                   \
-  if (const char* why = check_matrix(p, rows, cols, ld, dtype, optional)) return invalid(std::string(name " ") + why)
-
 gbmuf_status check_sizes(const gbmuf_ops* ops, int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype, int32_t act) {
   if (!ops) return invalid("ops is NULL");
   if (rows < 0 || n_in < 0 || n_out < 0) return invalid("rows, n_in and n_out must not be negative");
@@ -120,118 +67,6 @@ gbmuf_status check_sizes(const gbmuf_ops* ops, int64_t rows, int64_t n_in, int64
   if (!is_dtype(dtype)) return invalid("dtype must be GBMUF_F32 or GBMUF_BF16");
   if (act < GBMUF_ACT_NONE || act > GBMUF_ACT_SIGMOID) return invalid("unknown activation");
   return GBMUF_OK;
-}
-
-#define DISPATCH_DTYPE(dtype, T, ...)                       \
-  if ((dtype) == GBMUF_F32) { using T = float; __VA_ARGS__; } \
-  else { using T = __nv_bfloat16; __VA_ARGS__; }
-
-// An operand as it lies in memory: [outer][inner] of the call's type, row stride ld; k_inner: the
-// summed index is the inner one.
-struct Operand {
-  const void* p;
-  long long outer, inner, ld;
-  bool k_inner;
-};
-// A product of two operands: result [R][C], K terms.
-struct Product {
-  Operand a, b;
-  long long R, C, K;
-  int32_t dtype;
-  Epilogue E;
-};
-
-bool in_place(const Operand& o, int32_t dtype) {
-  return dtype == GBMUF_BF16 && (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || (o.ld % 8 == 0 && o.ld < ((long long)1 << 38)));
-}
-long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
-long long packed_bytes(const Operand& o, int32_t dtype) {
-  return in_place(o, dtype) ? 0 : round_up((dtype == GBMUF_F32 ? 3 : 1) * o.outer * round_up(o.inner, 8) * 2, 256);
-}
-long long product_workspace(const Product& q) {
-  return q.K == 0 || q.R == 0 || q.C == 0 ? 0 : packed_bytes(q.a, q.dtype) + packed_bytes(q.b, q.dtype);
-}
-
-PackJob pack_job(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst) {
-  PackJob j{};
-  if (in_place(o, dtype)) return j;
-  j.src = o.p; j.dst = static_cast<__nv_bfloat16*>(dst); j.ld = o.ld; j.outer = o.outer; j.inner = o.inner; j.ld_dst = round_up(o.inner, 8);
-  j.vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)size_of(dtype) % 16 == 0);
-  j.blocks = (int)std::min<long long>((o.outer * (j.ld_dst / 8) + 255) / 256, (long long)ops->num_sms * 16);
-  return j;
-}
-
-// Tensor map of an operand (packed at `packed` if it cannot be read in place): [parts][outer][inner],
-// boxes of 64 inner elements by `box` outer ones.
-gbmuf_status operand_map(const Operand& o, int32_t dtype, const void* packed, int box, CUtensorMap* map) {
-  const EncodeTiledFn encode = encode_tiled_fn();
-  if (!encode) return refuse(GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-  const bool here = in_place(o, dtype);
-  const long long ld = here && o.outer > 1 ? o.ld : round_up(o.inner, 8);
-  const cuuint64_t dim[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)(dtype == GBMUF_F32 ? 3 : 1)};
-  const cuuint64_t stride[2] = {(cuuint64_t)ld * 2, dtype == GBMUF_F32 ? (cuuint64_t)(o.outer * ld) * 2 : (cuuint64_t)ld * 2};
-  const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, one[3] = {1, 1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(here ? o.p : packed), dim, stride, boxes,
-                            one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return refuse(GBMUF_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
-  return GBMUF_OK;
-}
-
-// Whether the epilogue's matrices can be accessed two bf16 columns at a time.
-int may_pair(const Product& q) {
-  const Epilogue& E = q.E;
-  const void* const p[] = {E.residual, E.z_in, E.out0, E.out1};
-  const long long ld[] = {E.ld_residual, E.ld_z_in, E.ld_out0, E.ld_out1};
-  bool ok = q.C % 2 == 0;
-  for (int i = 0; i < 4; ++i) ok = ok && (!p[i] || ((uintptr_t)p[i] % 4 == 0 && (q.R == 1 || ld[i] % 2 == 0)));
-  return ok;
-}
-
-// Tile width, CTAs that share a tile's steps, CTAs that share a tile: the choice with the least time
-// by a model whose eight constants were fitted to 180 measured products of 12 to 100,000 rows, columns
-// and terms in both types (its choice was 0.8 % above the best one on average, 15 % at worst; no sum along
-// a vocabulary among them).  The 1.45 for pairs with a strided A says what was measured, not why.
-struct TcShape { int bn, split, pair; };
-TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided) {
-  TcShape best{64, 1, 1};
-  double best_t = 1e300;
-  const long long ksteps = (q.K + 63) / 64;
-  for (int pair = 1; pair <= 2; ++pair)
-    for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2)
-      for (int log = 0; log <= (pair == 2 ? 0 : 3); ++log) {
-        const int split = 1 << log;
-        const long long tiles = ((q.C + 128 * pair - 1) / (128 * pair)) * ((q.R + bn - 1) / bn);
-        const long long fit = ops->tc_clusters[pair == 2 ? 1 : log];
-        if (split > 1 && (split * 2 > ksteps || tiles > fit)) break;
-        const double waves = (double)((tiles + fit - 1) / fit);
-        // a step takes as long as its operands take to arrive, the epilogue as long as the tile is wide
-        double step = std::max(100.0, parts * tc_stage_bytes(bn, pair) / 126.0);
-        if (pair == 2 && a_strided) step *= 1.45;
-        const double sums = 1000.0 + (double)((ksteps + split - 1) / split) * step, epilogue = 15.0 * bn / split;
-        double t = split > 1 ? waves * (sums + 1100.0 + 19.0 * bn) : waves * std::max(sums, epilogue);
-        t += epilogue + (pair == 2 ? 2000.0 : 0.0);
-        if (t < best_t) { best_t = t; best = {bn, split, pair}; }
-      }
-  return best;
-}
-
-template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
-gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
-  const auto kernel = linear_tc_kernel<KIND, T, TO, PARTS, BN, PAIR>;
-  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR));
-  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages);
-  static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
-  const uint64_t bit = 1ull << (ops->device & 63);
-  if (!(ready.load() & bit)) {
-    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ops->max_smem);
-    if (e != cudaSuccess) return cuda_refuse("shared-memory limit of the linear-layer kernel", e);
-    if (ops->device < 64) ready.fetch_or(bit);
-  }
-  const int at_once = P.split > 1 ? P.tiles : std::min(P.tiles, ops->num_sms / PAIR);     // a split tile: one per cluster
-  P.tile_step = at_once; P.step_c = at_once / P.tiles_r; P.step_r = at_once % P.tiles_r;
-  const unsigned grid = (unsigned)(at_once * PAIR * P.split);
-  return launched("launch of the linear-layer kernel", launch(kernel, grid, (unsigned)(PAIR * P.split), kTcThreads, smem, st, ma, mb, P));
 }
 
 // Runs a product: operands that cannot be read in place are packed into the workspace first.
@@ -246,8 +81,8 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
   P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
   const TcShape shape = choose_shape(ops, q, PARTS, KIND == kWeightGrad, KIND != kForward);
   P.split = shape.split;
-  P.tiles_r = (int)((q.R + shape.bn - 1) / shape.bn);
-  const long long tiles = (long long)P.tiles_r * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
+  P.tiles_fast = (int)((q.R + shape.bn - 1) / shape.bn);
+  const long long tiles = (long long)P.tiles_fast * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
   if (tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles");
   P.tiles = (int)tiles;
   CUtensorMap ma{}, mb{};
@@ -313,8 +148,8 @@ gbmuf_status check_backward_weight(const gbmuf_ops* ops, const gbmuf_linear_back
 
 Product forward_product(const gbmuf_linear_forward_args* a) {
   Product q{};
-  q.a = {a->w, a->n_out, a->n_in, a->ld_w, true};
-  q.b = {a->x, a->rows, a->n_in, a->ld_x, true};
+  q.a = {a->w, a->n_out, a->n_in, a->ld_w, true, false, 0};
+  q.b = {a->x, a->rows, a->n_in, a->ld_x, true, false, 0};
   q.R = a->rows; q.C = a->n_out; q.K = a->n_in; q.dtype = a->dtype;
   q.E.bias = a->bias; q.E.residual = a->residual; q.E.ld_residual = a->ld_residual;
   q.E.out0 = a->y; q.E.ld_out0 = a->ld_y; q.E.out1 = a->z; q.E.ld_out1 = a->ld_z; q.E.act = a->activation;
@@ -354,8 +189,8 @@ template <typename T> gbmuf_status forward_rows(const gbmuf_ops* ops, const gbmu
 
 Product input_grad_product(const gbmuf_linear_backward_input_args* a) {
   Product q{};
-  q.a = {a->w, a->n_out, a->n_in, a->ld_w, false};
-  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, true};
+  q.a = {a->w, a->n_out, a->n_in, a->ld_w, false, false, 0};
+  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, true, false, 0};
   q.R = a->rows; q.C = a->n_in; q.K = a->n_out; q.dtype = a->dtype;
   q.E.residual = a->residual; q.E.ld_residual = a->ld_residual; q.E.z_in = a->z_prev; q.E.ld_z_in = a->ld_z_prev;
   q.E.out0 = a->dx; q.E.ld_out0 = a->ld_dx; q.E.out1 = a->dz_prev; q.E.ld_out1 = a->ld_dz_prev;
@@ -365,10 +200,21 @@ Product input_grad_product(const gbmuf_linear_backward_input_args* a) {
 
 Product weight_grad_product(const gbmuf_linear_backward_weight_args* a) {
   Product q{};
-  q.a = {a->x, a->rows, a->n_in, a->ld_x, false};
-  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, false};
+  q.a = {a->x, a->rows, a->n_in, a->ld_x, false, false, 0};
+  q.b = {a->dz, a->rows, a->n_out, a->ld_dz, false, false, 0};
   q.R = a->dw ? a->n_out : 0; q.C = a->n_in; q.K = a->rows; q.dtype = a->dtype;
   q.E.out0 = a->dw; q.E.ld_out0 = a->ld_dw; q.E.accumulate = a->accumulate;
+  return q;
+}
+
+// The operands' sides of a ready product: see ready_product.h.
+Product of_ready(const gbmuf_ready_product& r) {
+  Product q{};
+  q.a = {r.a, r.a_outer, r.a_inner, r.a_ld, false, true, 0};
+  q.b = {r.b, r.b_outer, r.b_inner, r.b_ld, !r.weight_grad, true, 0};
+  q.R = r.rows; q.C = r.cols; q.K = r.terms; q.dtype = r.dtype;
+  q.E.residual = r.residual; q.E.ld_residual = r.ld_residual; q.E.out0 = r.out; q.E.ld_out0 = r.ld_out;
+  q.E.out1 = r.rounded; q.E.ld_out1 = r.ld_rounded; q.E.accumulate = r.accumulate;
   return q;
 }
 
@@ -387,22 +233,6 @@ cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t 
 }
 
 constexpr long long kLossCacheBytes = 64ll << 20;   // of the 126 MB: the gradient passes through as well
-
-// How many clusters of 1, 2, 4 and 8 blocks of a kernel the GPU holds at once.
-template <typename K> cudaError_t count_clusters(K kernel, int threads, uint32_t smem, int blocks, int (&clusters)[4]) {
-  cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1u << i; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(blocks >> i << i)); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
-    cfg.attrs = &attr; cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&clusters[i], kernel, &cfg);
-    if (clusters[i] < 1) clusters[i] = 1;
-  }
-  return e;
-}
 
 // Short rows: a warp each.  Longer ones: a cluster of CTAs each, of more CTAs where there are too few
 // rows to fill the GPU, or where the slices that are fetched twice would not fit the L2 cache.
@@ -441,6 +271,18 @@ gbmuf_status read_status(int device, int32_t* word, void* stream, int32_t* out) 
 }
 
 }  // namespace
+
+gbmuf_status gbmuf_run_ready_product(const gbmuf_ops* ops, const gbmuf_ready_product& r, void* stream) {
+  const Product q = of_ready(r);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (r.weight_grad) {
+    DISPATCH_DTYPE(r.dtype, T, DISPATCH_DTYPE(r.out_dtype, TO,
+        return (run_product<kWeightGrad, TO, TO, (sizeof(T) == 4 ? 3 : 1)>(ops, q, nullptr, 0, st))));
+  }
+  if (r.dtype == GBMUF_F32) return run_product<kInputGrad, float, float, 3>(ops, q, nullptr, 0, st);
+  if (r.out_dtype == GBMUF_BF16) return run_product<kInputGrad, __nv_bfloat16, __nv_bfloat16, 1>(ops, q, nullptr, 0, st);
+  return run_product<kInputGrad, __nv_bfloat16, float, 1>(ops, q, nullptr, 0, st);
+}
 
 extern "C" {
 
