@@ -477,6 +477,61 @@ gbmuf_status gbmuf_linear_cross_entropy_workspace(gbmuf_ops* ops, const gbmuf_li
                                                   int64_t* bytes);
 gbmuf_status gbmuf_linear_cross_entropy(gbmuf_ops* ops, const gbmuf_linear_cross_entropy_args* a, void* stream);
 
+/* The k largest logits of each row, largest first, with their indices and the row's log-sum-exp: a teacher's
+ * side of distillation, or the words that may come next.  Among equal logits the lower index comes first
+ * (-0 and 0 are equal), NaN counts as larger than any number.
+ * logits [rows][vocab]; values [rows][k] of the same dtype, index [rows][k] int64; lse: device fp32 [rows] or
+ * NULL, log sum_v exp(logits_v / temperature) (NaN where a logit is NaN or +inf).  1 <= k <= 256, k <= vocab;
+ * 1/1024 <= temperature <= 1024.  One pass over the logits. */
+typedef struct {
+  int64_t rows, vocab;
+  const void* logits;
+  void* values;
+  int64_t* index;
+  float* lse;
+  int64_t ld_logits, ld_values, ld_index;
+  int32_t dtype, k;
+  float temperature;
+  int32_t reserved;
+} gbmuf_top_logits_args;
+gbmuf_status gbmuf_top_logits(gbmuf_ops* ops, const gbmuf_top_logits_args* a, void* stream);
+
+/* Distillation: the loss of a student's logits x against the k largest logits of a teacher, and its gradient.
+ * With T = temperature, p = softmax(x / T), and for row i the teacher's logits t_j at words v_j:
+ *   q_j = exp(t_j / T - A), A = teacher_lse_i, or log sum_j exp(t_j / T) if teacher_lse is NULL
+ *   soft = T^2 (sum_j q_j (log q_j - log p_vj) + q_r (log q_r - log P_r))
+ *   hard = log sum_v exp(x_v) - x_target
+ *   loss_i = s_i ((1 - hard_weight) soft + hard_weight hard),  s_i = scale * row_weight_i
+ * and dlogits its gradient.  With teacher_lse (the teacher's own log-sum-exp over its vocabulary at the same
+ * temperature, as gbmuf_top_logits gives it) the words outside the list are one more class, with q_r =
+ * max(0, 1 - sum_j q_j) and P_r the sum of their p; without it, or where no word is outside, q_r = 0.
+ * logits, dlogits [rows][vocab] of dtype (dlogits may be NULL, or the logits themselves with the same ld);
+ * teacher_logits [rows][k] of teacher_dtype, teacher_index [rows][k] int64, 1 <= k <= 256; teacher_lse,
+ * row_weight, loss, lse (log sum exp(x / T)): device fp32 [rows] or NULL; targets: device int64 [rows], may be
+ * NULL with hard_weight 0.  0 <= hard_weight <= 1.
+ * An entry whose index is -1 or whose logit is -inf is not there (shorter lists); a word that comes twice
+ * has the sum of both q.  A row whose target is ignore_index, or whose s_i is 0, has loss 0 and a zero
+ * gradient.  A list without entries has soft 0.  A student's logit of -inf at a word with q > 0 gives
+ * loss +inf; a row of nothing but -inf loss +inf, lse -inf and a zero gradient; NaN or +inf in a row (or a
+ * NaN of the teacher's) gives NaN.  Any other index outside 0 .. vocab-1, a target among them, gives loss
+ * NaN, a zero gradient and GBMUF_ERR_INVALID_ARG in the status word.  Sums are fp32 or wider; the
+ * probabilities of the list's words and of the rest are summed apart, so that neither takes the other's
+ * digits.  1/1024 <= temperature <= 1024. */
+typedef struct {
+  int64_t rows, vocab;
+  const void *logits, *teacher_logits;
+  const int64_t* teacher_index;
+  const float* teacher_lse;
+  const int64_t* targets;
+  const float* row_weight;
+  float *loss, *lse;
+  void* dlogits;
+  int64_t ld_logits, ld_teacher, ld_index, ld_dlogits, ignore_index;
+  int32_t dtype, teacher_dtype, k;
+  float temperature, hard_weight, scale;
+} gbmuf_distillation_args;
+gbmuf_status gbmuf_distillation(gbmuf_ops* ops, const gbmuf_distillation_args* a, void* stream);
+
 /* The norm of all gradients of a group (a worker), over any number of tensors, and clipping.
  * A tensor is [rows][cols] with row stride ld_grad, fp32 or bf16; out (or NULL: it only counts in
  * the norm) has row stride ld_out and is fp32 or of the gradient's own type, and may be the

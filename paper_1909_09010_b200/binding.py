@@ -33,7 +33,7 @@ EXPORTS = ["gbmuf_create", "gbmuf_set_partition", "gbmuf_init", "gbmuf_local_per
            "gbmuf_linear_backward_input_workspace", "gbmuf_linear_backward_input",
            "gbmuf_linear_backward_weight_workspace", "gbmuf_linear_backward_weight",
            "gbmuf_activation_backward", "gbmuf_cross_entropy", "gbmuf_linear_cross_entropy_workspace",
-           "gbmuf_linear_cross_entropy", "gbmuf_clip_create",
+           "gbmuf_linear_cross_entropy", "gbmuf_top_logits", "gbmuf_distillation", "gbmuf_clip_create",
            "gbmuf_clip_set_tensors", "gbmuf_clip_norms", "gbmuf_clip_scale", "gbmuf_clip_device_status",
            "gbmuf_clip_selftest_wait_timeout", "gbmuf_clip_destroy"]
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
@@ -93,6 +93,19 @@ class LinearCrossEntropyArgs(ctypes.Structure):
     _fields_ = _fields("l rows n_in vocab, p x w bias targets row_weight loss lse dx dw dbias, "
                        "l ld_x ld_w ld_dx ld_dw ignore_index piece, i dtype grad_dtype accumulate, f scale, "
                        "p workspace, l workspace_bytes")
+
+
+class TopLogitsArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_top_logits_args``."""
+    _fields_ = _fields("l rows vocab, p logits values index lse, l ld_logits ld_values ld_index, i dtype k, "
+                       "f temperature, i reserved")
+
+
+class DistillationArgs(ctypes.Structure):
+    """Mirror of ``gbmuf_distillation_args``."""
+    _fields_ = _fields("l rows vocab, p logits teacher_logits teacher_index teacher_lse targets row_weight loss lse "
+                       "dlogits, l ld_logits ld_teacher ld_index ld_dlogits ignore_index, i dtype teacher_dtype k, "
+                       "f temperature hard_weight scale")
 
 
 class GradTensor(ctypes.Structure):
@@ -157,6 +170,8 @@ def lib() -> ctypes.CDLL:
     L.gbmuf_cross_entropy.argtypes = [vp, vp, vp]
     L.gbmuf_linear_cross_entropy_workspace.argtypes = [vp, vp, vp]
     L.gbmuf_linear_cross_entropy.argtypes = [vp, vp, vp]
+    L.gbmuf_top_logits.argtypes = [vp, vp, vp]
+    L.gbmuf_distillation.argtypes = [vp, vp, vp]
     L.gbmuf_clip_create.argtypes = [i32, i32, i64, vp, ctypes.POINTER(vp)]
     L.gbmuf_clip_set_tensors.argtypes = [vp, i64, vp]
     L.gbmuf_clip_norms.argtypes = [vp, vp, vp]
@@ -450,6 +465,8 @@ _pack_backward_input = _packer(LinearBackwardInputArgs)
 _pack_backward_weight = _packer(LinearBackwardWeightArgs)
 _pack_cross_entropy = _packer(CrossEntropyArgs)
 _pack_linear_cross_entropy = _packer(LinearCrossEntropyArgs)
+_pack_top_logits = _packer(TopLogitsArgs)
+_pack_distillation = _packer(DistillationArgs)
 
 
 def _dtype_code(t) -> int:
@@ -765,6 +782,65 @@ class LocalOps(_OnDevice):
             args = _pack_linear_cross_entropy(*fields, work.data_ptr(), need.value)
         self._check(self._L.gbmuf_linear_cross_entropy(self._h, args, self._raw_stream(dev)))
         return (loss, lse, *results)
+
+    def top_logits(self, logits, k, temperature=1.0, want_lse=True, values_out=None, index_out=None, lse_out=None,
+                   stream=None):
+        """``gbmuf_top_logits``: (values, index, lse) of the k largest logits of each row, largest first, lower
+        indices first among equal ones; (values, index) without ``want_lse``.  index is int64, lse (float32) the
+        log-sum-exp of the row over the temperature."""
+        if stream is not None:
+            return self._on_stream(stream, (values_out, index_out, lse_out), self.top_logits, logits, k, temperature,
+                                   want_lse, values_out, index_out, lse_out)
+        torch = self._torch
+        shape = _two_dims("logits", logits)
+        rows, vocab = shape
+        dtype, dev = logits.dtype, self.device
+        code = _dtype_code(logits)
+        pl, ll = _matrix("logits", logits, shape, dtype, dev)
+        if not 1 <= k <= 256:
+            raise ValueError("k must be 1 .. 256")
+        values, pv, lv = _result("values_out", values_out, logits, (rows, k), dtype, dev)
+        index, pi, li = _result("index_out", index_out, logits, (rows, k), torch.int64, dev)
+        lse = lse_out
+        if lse is None and want_lse:
+            lse = logits.new_empty((rows,), dtype=torch.float32)
+        args = _pack_top_logits(rows, vocab, pl, pv, pi, _vector("lse_out", lse, rows, torch.float32, dev), ll, lv, li, code,
+                                k, temperature, 0)
+        self._check(self._L.gbmuf_top_logits(self._h, args, self._raw_stream(dev)))
+        return (values, index) if lse is None else (values, index, lse)
+
+    def distillation(self, logits, teacher_logits, teacher_index, teacher_lse=None, temperature=1.0, targets=None,
+                     hard_weight=0.0, ignore_index=-100, row_weight=None, scale=1.0, want_grad=True, dlogits_out=None,
+                     stream=None):
+        """``gbmuf_distillation``: (loss, lse, dlogits), or (loss, lse) without ``want_grad``: the loss of a
+        student's logits against a teacher's largest ones (as :meth:`top_logits` gives them), mixed with the
+        cross-entropy of ``targets`` by ``hard_weight``.  ``dlogits_out`` may be the logits."""
+        if stream is not None:
+            return self._on_stream(stream, (dlogits_out,), self.distillation, logits, teacher_logits, teacher_index,
+                                   teacher_lse, temperature, targets, hard_weight, ignore_index, row_weight, scale,
+                                   want_grad, dlogits_out)
+        torch = self._torch
+        shape = _two_dims("logits", logits)
+        rows, vocab = shape
+        k = _two_dims("teacher_logits", teacher_logits)[1]
+        dtype, dev = logits.dtype, self.device
+        code = _dtype_code(logits)
+        pl, ll = _matrix("logits", logits, shape, dtype, dev)
+        teacher_code = _dtype_code(teacher_logits)
+        px, lx = _matrix("teacher_logits", teacher_logits, (rows, k), teacher_logits.dtype, dev)
+        pi, li = _matrix("teacher_index", teacher_index, (rows, k), torch.int64, dev)
+        pe = _vector("teacher_lse", teacher_lse, rows, torch.float32, dev)
+        pt = _vector("targets", targets, rows, torch.int64, dev)
+        pw = _vector("row_weight", row_weight, rows, torch.float32, dev)
+        d, pd, ldd = None, 0, 0
+        if want_grad or dlogits_out is not None:
+            d, pd, ldd = _result("dlogits_out", dlogits_out, logits, shape, dtype, dev)
+        loss = logits.new_empty((rows,), dtype=torch.float32)
+        lse = logits.new_empty((rows,), dtype=torch.float32)
+        args = _pack_distillation(rows, vocab, pl, px, pi, pe, pt, pw, loss.data_ptr(), lse.data_ptr(), pd, ll, lx, li,
+                                  ldd, ignore_index, code, teacher_code, k, temperature, hard_weight, scale)
+        self._check(self._L.gbmuf_distillation(self._h, args, self._raw_stream(dev)))
+        return (loss, lse) if d is None else (loss, lse, d)
 
     def device_status(self, stream=None) -> int:
         """Waits for the stream; reads and clears the status word."""

@@ -7,7 +7,7 @@ import subprocess
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-SRCS = [os.path.join(CSRC, f) for f in ("gbmuf.cu", "local_ops.cu", "linear_loss.cu")]   # they include csrc/*.cuh
+SRCS = [os.path.join(CSRC, f) for f in ("gbmuf.cu", "local_ops.cu", "linear_loss.cu", "vocab_ops.cu")]   # they include csrc/*.cuh
 HDR = os.path.join(ROOT, "include", "gbmuf.h")
 LIB = os.path.join(PKG, "libgbmuf.so")
 

@@ -74,33 +74,6 @@ __global__ void __launch_bounds__(128) cross_entropy_warp_kernel(const LossParam
 // their slots, then over the others, last to first, which the producer has fetched again -- from the
 // L2 cache: what was read last is needed first, and the host splits rows so that all slices in flight
 // fit it.  Two CTAs per SM: one sums while the other one writes or waits.
-constexpr int kLossWorkers = 256;
-constexpr int kLossWarps = kLossWorkers / 32;
-constexpr int kLossThreads = kLossWorkers + 32;
-constexpr int kLossPieces = 4;                              // per thread and chunk
-constexpr int kLossChunk = 16 * kLossPieces * kLossWorkers; // 16 KB
-constexpr int kLossRing = 6;
-constexpr int kLossKept = 5;
-constexpr int kLossBlocksPerSm = 2;
-constexpr uint32_t kLossHead = 512;
-constexpr uint32_t kLossSmem = kLossHead + kLossRing * kLossChunk;
-
-struct RowSpan {
-  int a0;                    // elements before the first whole piece
-  int pieces;                // whole pieces of the row
-  int p0, n;                 // this CTA's pieces
-};
-__device__ __forceinline__ void loss_workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kLossWorkers) : "memory"); }
-template <typename T> __device__ __forceinline__ RowSpan row_span(const LossParams& P, long long row, int rank) {
-  constexpr int E = 16 / (int)sizeof(T);
-  RowSpan r;
-  const int past = (int)((uintptr_t)(static_cast<const T*>(P.logits) + row * P.ld) % 16 / sizeof(T));
-  r.a0 = past ? E - past : 0;                              // vocab > E
-  r.pieces = ((int)P.vocab - r.a0) / E;
-  r.p0 = (int)((unsigned)r.pieces * (unsigned)rank / (unsigned)P.split);       // pieces * 8 < 2^32
-  r.n = (int)((unsigned)r.pieces * (unsigned)(rank + 1) / (unsigned)P.split) - r.p0;
-  return r;
-}
 // What a thread needs of a row besides the ring, asked for a row ahead.  The elements before and after
 // the whole pieces, at most 7 each, belong to one thread of rank 0 each.
 template <typename T> struct RowAhead {
@@ -121,24 +94,6 @@ template <typename T> struct RowAhead {
     own = to_f32((static_cast<const T*>(P.logits) + row * P.ld)[e]);
   }
 };
-// Maximum of a piece's values (NaN does not count) and its values.
-__device__ __forceinline__ float piece_max(uint4 u, const float (&)[4]) {
-  return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
-}
-__device__ __forceinline__ float piece_max(uint4 u, const float (&)[8]) {
-  auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
-  const __nv_bfloat162 m = __hmax2(__hmax2(h(u.x), h(u.y)), __hmax2(h(u.z), h(u.w)));
-  return fmaxf(__low2float(m), __high2float(m));
-}
-__device__ __forceinline__ void piece_values(uint4 u, float (&v)[4]) {
-  v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
-}
-__device__ __forceinline__ void piece_values(uint4 u, float (&v)[8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads, kLossBlocksPerSm) cross_entropy_ring_kernel(const LossParams P) {
   constexpr bool FAST = sizeof(T) == 2;

@@ -121,17 +121,6 @@ __device__ __forceinline__ uint32_t in_leader(uint32_t addr) {
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_sync() {
-  cluster_arrive();
-  cluster_wait();
-}
-__device__ __forceinline__ void st_remote(uint32_t addr, uint32_t rank, float v) {
-  asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.f32 [r], %2;\n\t}" ::"r"(addr),
-               "r"(rank), "f"(v)
-               : "memory");
-}
 // N accumulator columns of this warp's 32 lanes.
 template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[N]) {
   static_assert(N == 8 || N == 16, "");

@@ -9,6 +9,7 @@
 //   linear_rows.cuh      the layer for a few rows, on the fp32 units
 //   column_sum.cuh       column sums (bias gradients), gradient of an activation by itself
 //   softmax_math.cuh     exponentials of logits, a row's loss
+//   row_pieces.cuh       long rows by 16-byte pieces
 //   cross_entropy.cuh    cross-entropy over a vocabulary with its gradient
 //   grad_clip.cuh        norms over many tensors and the clipped copies
 
@@ -38,6 +39,7 @@
 #include "linear_tc.cuh"
 #include "linear_rows.cuh"
 #include "column_sum.cuh"
+#include "row_pieces.cuh"
 #include "cross_entropy.cuh"
 #include "grad_clip.cuh"
 #include "linear_tc_host.h"
@@ -305,11 +307,12 @@ gbmuf_status gbmuf_ops_create(int32_t device, gbmuf_ops** out) {
     if (e == cudaSuccess) e = cudaMalloc(&ops->d_status, 256);
     if (e == cudaSuccess) e = cudaMemset(ops->d_status, 0, 256);
     if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);          // other streams do not wait for the default one
-    if (e != cudaSuccess) {
+    gbmuf_status rc = e == cudaSuccess ? gbmuf_setup_vocab_ops(ops) : cuda_refuse("set-up of the local-step operators", e);
+    if (rc != GBMUF_OK) {
       cudaGetLastError();
       cudaFree(ops->d_status);
       delete ops;
-      return cuda_refuse("set-up of the local-step operators", e);
+      return rc;
     }
     *out = ops;
     return GBMUF_OK;

@@ -64,6 +64,18 @@ __device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void* src, ui
       : "memory");
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  cluster_arrive();
+  cluster_wait();
+}
+__device__ __forceinline__ void st_remote(uint32_t addr, uint32_t rank, float v) {
+  asm volatile("{\n\t.reg .b32 r;\n\tmapa.shared::cluster.u32 r, %0, %1;\n\tst.shared::cluster.f32 [r], %2;\n\t}" ::"r"(addr),
+               "r"(rank), "f"(v)
+               : "memory");
+}
+
 // mbar_wait_bounded with the first try in line.
 __device__ __noinline__ bool wait_slowly(uint32_t bar, uint32_t parity, int32_t* status) {
   return mbar_wait_bounded(bar, parity, status);

@@ -68,6 +68,37 @@ __device__ __forceinline__ void report_target(const LossParams& P, long long t, 
   if (!target_ignored(P, t, w) && !target_inside(P, t)) atomicExch(P.status, (int32_t)GBMUF_ERR_INVALID_ARG);
 }
 
+// exp((x - m) / T), as Shift: log2 e / T = hi + lo; below `least` (x - m) the result is 0 in fp32.
+struct Temperature {
+  float hi, lo, least;
+  double inverse;            // 1 / T
+};
+template <bool FAST> struct TemperedShift {
+  float m, hi, lo, least;
+  __device__ __forceinline__ void at(const Temperature& t) { hi = t.hi; lo = t.lo; least = t.least; }
+  __device__ __forceinline__ void set(float top) { m = top == -INFINITY ? 0.0f : top; }
+  __device__ __forceinline__ Two operator()(float x0, float x1) const {
+    Two t = two(x0, x1) + two(-m, -m);
+    float y0, y1;
+    if (FAST) {
+      apart(t * two(hi, hi), y0, y1);
+      return two(exp2_unit(y0), exp2_unit(y1));
+    }
+    apart(t, y0, y1);
+    t = two(max_nan(y0, least), max_nan(y1, least));
+    const Two y = t * two(hi, hi);
+    const Two f = fma_two(t, two(lo, lo), fma_two(t, two(hi, hi), y * two(-1.0f, -1.0f)));
+    apart(y, y0, y1);
+    const Two r = two(exp2_unit(y0), exp2_unit(y1));
+    return fma_two(r, f * two(0.693147181f, 0.693147181f), r);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    float a, b;
+    apart((*this)(x, x), a, b);
+    return a;
+  }
+};
+
 }  // namespace
 
 #endif  // GBMUF_CSRC_SOFTMAX_MATH_CUH

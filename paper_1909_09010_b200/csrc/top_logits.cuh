@@ -1,0 +1,472 @@
+// The largest logits of each row, with their indices and the row's log-sum-exp.
+// Part of libgbmuf (CUDA, sm_100a); included by vocab_ops.cu.
+#ifndef GBMUF_CSRC_TOP_LOGITS_CUH
+#define GBMUF_CSRC_TOP_LOGITS_CUH
+
+namespace {
+
+// One pass over the row.  A logit and its index make one whole number (key) that is larger where the logit
+// is, and among equal logits where the index is smaller; keys are all different, so "the k largest" has one
+// answer.  A block keeps the k largest keys so far, and a threshold that no key below it can be among the k
+// largest.  Keys at or above it are appended to a buffer; once that has grown, its keys are ranked by
+// counting, the k largest stay, and the threshold is the last of them.  Most pieces of a row are passed
+// over after one comparison of their maximum.
+//
+// The first threshold of a row: of 256 threads' largest keys in the first chunk the k-th largest.  It is at
+// most the k-th largest key of all, and at most k threads have keys above it.  That also bounds what a
+// piece per thread can append (k times its elements), which is how a chunk is taken that overflows the
+// buffer (a row that rises, or holds few different values): piece by piece, with a new threshold each.
+struct TopParams {
+  const void* logits;
+  void* values;
+  long long* index;
+  float* lse;
+  long long rows, vocab, ld, ld_values, ld_index;
+  int k, split;
+  Temperature temperature;
+  int32_t* status;
+};
+constexpr int kTopMost = 256;                  // k
+constexpr int kTopBuffer = kTopMost * 10;      // keys: k kept ones and k pieces of 8, and room
+constexpr int kTopShort = 2048;                // vocabulary of the kernel without a ring
+typedef unsigned long long Key;
+
+__device__ __forceinline__ Key top_key(float x, int index) {
+  const uint32_t b = __float_as_uint(x + 0.0f);                     // -0 counts as 0
+  const uint32_t o = x == x ? b ^ ((uint32_t)((int)b >> 31) | 0x80000000u) : 0xffffffffu;
+  return (Key)o << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ float key_value(Key k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);   // all ones: a NaN
+}
+__device__ __forceinline__ int key_index(Key k) { return (int)~(uint32_t)k; }
+// Maximum of a piece's values, NaN if one of them is.
+__device__ __forceinline__ float piece_max_nan(uint4 u, const float (&)[4]) {
+  return max_nan(max_nan(__uint_as_float(u.x), __uint_as_float(u.y)), max_nan(__uint_as_float(u.z), __uint_as_float(u.w)));
+}
+__device__ __forceinline__ float piece_max_nan(uint4 u, const float (&)[8]) {
+  auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h(u.x), h(u.y)), __hmax2_nan(h(u.z), h(u.w)));
+  return max_nan(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ bool any_worker(bool mine) {
+  uint32_t any;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(any)
+               : "r"((uint32_t)mine), "n"(kLossWorkers)
+               : "memory");
+  return any != 0;
+}
+
+struct TopShared {
+  Key buffer[kTopBuffer];
+  Key threshold;
+  int count;
+  int pad;
+  float2 stat[kLossWarps];
+  float2 told[8];
+};
+
+// What the 256 workers of a block keep of a row.  All of them call all functions.
+struct TopState {
+  TopShared& S;
+  int k, thread;
+  Key threshold;             // keys at or above it are wanted; the same in all threads
+  float least;               // its logit
+
+  __device__ __forceinline__ void start() {
+    set(0);
+    if (thread == 0) S.count = 0;
+    loss_workers_sync();
+  }
+  __device__ __forceinline__ void set(Key t) {
+    threshold = t;
+    least = t == 0 ? -INFINITY : key_value(t);
+  }
+  __device__ __forceinline__ bool wanted(float top) const { return !(top < least); }
+  // true where the buffer has got long
+  __device__ __forceinline__ bool append(Key key) {
+    const int at = atomicAdd(&S.count, 1);
+    if (at < kTopBuffer) S.buffer[at] = key;
+    return at >= k + max(k / 2, 32);
+  }
+  // A threshold from the threads' largest wanted keys (0: none).  The buffer past `used` is free.
+  __device__ __forceinline__ void raise(Key mine, int used) {
+    Key* const all = S.buffer + (used + 1) / 2 * 2;
+    all[thread] = mine;
+    if (thread == 0) S.threshold = threshold;
+    loss_workers_sync();
+    if (mine != 0) {
+      int above = 0;
+#pragma unroll 8
+      for (int i = 0; i < kLossWorkers; i += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(all + i);
+        above += (o.x > mine) + (o.y > mine);
+      }
+      if (above == k - 1) S.threshold = mine;
+    }
+    loss_workers_sync();
+    set(S.threshold);
+    loss_workers_sync();
+  }
+  // Sorts the buffer, keeps its k largest keys.  Returns how many keys there had been.
+  __device__ __forceinline__ int compact() {
+    loss_workers_sync();
+    const int found = S.count, n = min(found, kTopBuffer);
+    constexpr int MOST = kTopBuffer / kLossWorkers;
+    if (thread == 0 && (n & 1)) S.buffer[n] = 0;           // pairs are read; the buffer's size is even
+    loss_workers_sync();
+    Key mine[MOST];
+    int rank[MOST];
+#pragma unroll
+    for (int q = 0; q < MOST; ++q) {
+      rank[q] = k;
+      if (q * kLossWorkers >= n) continue;                 // the same for all threads
+      const int i = q * kLossWorkers + thread;
+      mine[q] = i < n ? S.buffer[i] : 0;
+      int above = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; j += 2) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(S.buffer + j);
+        above += (o.x > mine[q]) + (o.y > mine[q]);
+      }
+      if (i < n) rank[q] = above;
+    }
+    loss_workers_sync();
+#pragma unroll
+    for (int q = 0; q < MOST; ++q)
+      if (rank[q] < k) S.buffer[rank[q]] = mine[q];
+    if (thread == 0) S.count = min(n, k);
+    loss_workers_sync();
+    if (n >= k) {
+      const Key last = S.buffer[k - 1];
+      set(last + (last != ~(Key)0));                       // itself is there already
+    }
+    return found;
+  }
+  // Whether a key is among the `n` sorted ones at the buffer's start.
+  __device__ __forceinline__ bool kept(Key key, int n) const {
+    int low = 0, high = n;
+    while (low < high) {
+      const int mid = (low + high) / 2;
+      if (S.buffer[mid] > key) low = mid + 1; else high = mid;
+    }
+    return low < n && S.buffer[low] == key;
+  }
+};
+
+// Maxima and sums of the warps, the block: every thread ends with the row's.
+template <bool FAST>
+__device__ __forceinline__ float2 join_workers(const Temperature& t, float m, float s, float2* stat, int lane, int warp) {
+  TemperedShift<FAST> e;
+  e.at(t);
+  float top = m;
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  e.set(top);
+  if (top != -INFINITY && m != -INFINITY) s *= e(m);
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+  if (lane == 0) stat[warp] = make_float2(top, s);
+  loss_workers_sync();
+  const float2 o = stat[lane & 7];
+  top = o.x;
+  for (int d = 4; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  e.set(top);
+  s = o.x == -INFINITY ? o.y : o.y * e(o.x);
+  for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+  loss_workers_sync();                                     // stat may be written again
+  return make_float2(top, s);
+}
+__device__ __forceinline__ float tempered_lse(const Temperature& t, float m, float s) {
+  if (m == -INFINITY && s == 0.0f) return -INFINITY;
+  return (float)((double)m * t.inverse + (double)logf(s));
+}
+template <typename T> __device__ __forceinline__ void top_write(const TopParams& P, long long row, int at, Key key) {
+  const int i = key_index(key);
+  static_cast<T*>(P.values)[row * P.ld_values + at] = (static_cast<const T*>(P.logits) + row * P.ld)[i];
+  P.index[row * P.ld_index + at] = i;
+}
+
+// ---- short rows: a block per row, up to eight logits per thread
+template <typename T>
+__global__ void __launch_bounds__(kLossWorkers) top_short_kernel(const TopParams P) {
+  constexpr bool FAST = sizeof(T) == 2;
+  constexpr int N = kTopShort / kLossWorkers;
+  __shared__ __align__(16) TopShared S;
+  grid_launch_dependents();
+  grid_dependency_wait();
+  const int thread = threadIdx.x, lane = thread & 31, warp = thread >> 5, V = (int)P.vocab;
+  for (long long row = blockIdx.x; row < P.rows; row += gridDim.x) {
+    const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
+    float v[N];
+    Key largest = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = thread + i * kLossWorkers;
+      v[i] = c < V ? to_f32(x[c]) : -INFINITY;
+      if (c < V) largest = max(largest, top_key(v[i], c));
+    }
+    TopState top{S, P.k, thread};
+    top.start();
+    top.raise(largest, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = thread + i * kLossWorkers;
+      const Key key = top_key(v[i], c);
+      if (c < V && key >= top.threshold) top.append(key);
+    }
+    top.compact();
+    if (thread < P.k) top_write<T>(P, row, thread, S.buffer[thread]);
+    if (P.lse) {
+      TemperedShift<FAST> e;
+      e.at(P.temperature);
+      float m = v[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+      m = m == m ? m : -INFINITY;
+      e.set(m);
+      Two s = two(0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < N; i += 2) s = s + e(v[i], v[i + 1]);
+      float a, b;
+      apart(s, a, b);
+      const float2 r = join_workers<FAST>(P.temperature, m, a + b, S.stat, lane, warp);
+      if (thread == 0) P.lse[row] = tempered_lse(P.temperature, r.x, r.y);
+    }
+    loss_workers_sync();                                   // the buffer may be written again
+  }
+}
+
+// ---- longer rows: chunks of a row through a ring of slots, which a producer warp fills.  Few rows: a cluster
+// of `split` blocks shares one row, each keeps the k largest of its slice, and rank 0 joins the lists (one
+// row per cluster).
+constexpr int kTopRing = 4;
+constexpr int kTopBlocksPerSm = 2;
+constexpr uint32_t kTopHead = (256u + (uint32_t)sizeof(TopShared) + 127u) / 128u * 128u;
+constexpr uint32_t kTopSmem = kTopHead + kTopRing * kLossChunk;
+
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel(const TopParams P) {
+  constexpr bool FAST = sizeof(T) == 2;
+  constexpr int E = 16 / (int)sizeof(T);
+  extern __shared__ __align__(128) unsigned char smem[];
+  const uint32_t bars = smem_u32(smem), ring = bars + kTopHead;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 64u + 8u * s; };
+  TopShared& S = *reinterpret_cast<TopShared*>(smem + 256);
+  const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;
+  const long long first = blockIdx.x / (unsigned)P.split, step = gridDim.x / (unsigned)P.split;
+  const int thread = threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (thread == 0) {
+    for (int s = 0; s < kTopRing; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), kLossWarps); }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  if (P.split > 1) cluster_sync();                         // every block has started before a peer writes to it
+  grid_launch_dependents();
+  grid_dependency_wait();
+  int slot = 0;
+  uint32_t phase = 0;
+  auto advance = [&] { if (++slot == kTopRing) { slot = 0; phase ^= 1; } };
+  if (thread >= kLossWorkers) {
+    // ------------------------------------------------------------------ producer
+    if (lane == 0) {
+      int filled = 0;
+      bool ok = true;
+      for (long long row = first; row < P.rows && ok; row += step) {
+        const RowSpan r = row_span<T>(P, row, rank);
+        const char* const src = reinterpret_cast<const char*>(static_cast<const T*>(P.logits) + row * P.ld + r.a0) + 16ll * r.p0;
+        const int chunks = (int)((16ll * r.n + kLossChunk - 1) / kLossChunk);
+        for (int c = 0; c < chunks; ++c) {
+          if (filled == kTopRing) ok = mbar_wait_bounded(empty(slot), phase ^ 1, P.status);
+          else ++filled;
+          if (!ok) break;
+          const long long left = 16ll * r.n - (long long)c * kLossChunk;
+          const uint32_t bytes = left < kLossChunk ? (uint32_t)left : (uint32_t)kLossChunk;
+          mbar_arrive_expect_tx(full(slot), bytes);
+          bulk_load_row(ring + slot * kLossChunk, src + (long long)c * kLossChunk, bytes, full(slot));
+          advance();
+        }
+      }
+      if (!ok)                                             // copies requested into this block's memory land first
+        for (int j = 0; j < kTopRing; ++j) { mbar_wait_bounded(full(slot), phase ^ 1, P.status); advance(); }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ 8 worker warps
+    bool ok = true;
+    for (long long row = first; row < P.rows; row += step) {
+      const RowSpan r = row_span<T>(P, row, rank);
+      const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
+      const int chunks = (r.n + kLossPieces * kLossWorkers - 1) / (kLossPieces * kLossWorkers);
+      // the elements before and after the whole pieces: one thread of rank 0 each
+      float own = -INFINITY;
+      int own_at = -1;
+      if (rank == 0 && thread < 2 * E) {
+        const int at = thread < r.a0 ? thread : r.pieces * E + thread;
+        if (at < (int)P.vocab) { own_at = at; own = to_f32(x[at]); }
+      }
+      TopState top{S, P.k, thread};
+      top.start();
+      TemperedShift<FAST> e;
+      e.at(P.temperature);
+      float m = own == own ? own : -INFINITY;
+      e.set(m);
+      Two s01 = two(own_at >= 0 && own != -INFINITY ? 1.0f + (own - own) : 0.0f, 0.0f), s23 = two(0.0f, 0.0f);
+      for (int c = 0; c < (chunks > 0 ? chunks : 1); ++c) {
+        const int left = c < chunks ? r.n - c * kLossPieces * kLossWorkers - thread : 0;
+        uint4 u[kLossPieces];
+        float tops[kLossPieces], v[E];
+        const int c0 = r.a0 + (r.p0 + c * kLossPieces * kLossWorkers + thread) * E;
+        auto there = [&](int h) { return h * kLossWorkers < left && ok; };
+        if (c < chunks) {
+          ok = ok && mbar_wait_bounded(full(slot), phase, P.status);
+          const uint4* const p = reinterpret_cast<const uint4*>(smem + kTopHead + slot * kLossChunk) + thread;
+#pragma unroll
+          for (int h = 0; h < kLossPieces; ++h) u[h] = p[h * kLossWorkers < left ? h * kLossWorkers : 0];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(empty(slot));
+          advance();
+        }
+#pragma unroll
+        for (int h = 0; h < kLossPieces; ++h) tops[h] = there(h) ? piece_max_nan(u[h], v) : -INFINITY;
+        auto largest_of = [&](uint4 piece, int h) {        // largest wanted key of a piece
+          Key k = 0;
+          piece_values(piece, v);
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const Key key = top_key(v[i], c0 + h * kLossWorkers * E + i);
+            if (key >= top.threshold) k = max(k, key);
+          }
+          return k;
+        };
+        if (c == 0) {
+          Key largest = own_at >= 0 ? top_key(own, own_at) : 0;
+#pragma unroll
+          for (int h = 0; h < kLossPieces; ++h)
+            if (there(h)) largest = max(largest, largest_of(u[h], h));
+          top.raise(largest, 0);
+        }
+        bool lengthy = c == 0;
+        if (c == 0 && own_at >= 0 && top_key(own, own_at) >= top.threshold) top.append(top_key(own, own_at));
+#pragma unroll
+        for (int h = 0; h < kLossPieces; ++h)
+          if (there(h) && top.wanted(tops[h])) {
+            piece_values(u[h], v);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              const Key key = top_key(v[i], c0 + h * kLossWorkers * E + i);
+              if (key >= top.threshold) lengthy |= top.append(key);
+            }
+          }
+        if (any_worker(lengthy)) {
+          if (top.compact() > kTopBuffer) {
+            // what did not fit: piece by piece; keys that are there already are passed over
+#pragma unroll 1
+            for (int h = -1; h < kLossPieces; ++h) {
+              uint4 piece = u[0];
+#pragma unroll
+              for (int j = 1; j < kLossPieces; ++j) piece = h == j ? u[j] : piece;
+              const int have = S.count;
+              Key mine[E], largest = 0;
+              piece_values(piece, v);
+#pragma unroll
+              for (int i = 0; i < E; ++i) {
+                const bool is = h >= 0 ? there(h) : i == 0 && c == 0 && own_at >= 0;
+                mine[i] = !is ? 0 : h >= 0 ? top_key(v[i], c0 + h * kLossWorkers * E + i) : top_key(own, own_at);
+                if (mine[i] < top.threshold || (mine[i] != 0 && top.kept(mine[i], have))) mine[i] = 0;
+                largest = max(largest, mine[i]);
+              }
+              loss_workers_sync();                         // the count has been read
+              top.raise(largest, have);
+#pragma unroll
+              for (int i = 0; i < E; ++i)
+                if (mine[i] != 0 && mine[i] >= top.threshold) top.append(mine[i]);
+              top.compact();
+            }
+          }
+        }
+        if (P.lse && left > 0 && ok) {
+          float highest = piece_max(u[0], v);
+#pragma unroll
+          for (int h = 1; h < kLossPieces; ++h) highest = fmaxf(highest, piece_max(u[h], v));
+          if (highest > m) {
+            const float before = m;
+            m = highest;
+            e.set(m);
+            if (before != -INFINITY) {
+              const float f = e(before);
+              s01 = s01 * two(f, f);
+              s23 = s23 * two(f, f);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < kLossPieces; ++h)
+            if (h * kLossWorkers < left) {
+              piece_values(u[h], v);
+#pragma unroll
+              for (int i = 0; i < E; i += 4) {
+                s01 = s01 + e(v[i], v[i + 1]);
+                s23 = s23 + e(v[i + 2], v[i + 3]);
+              }
+            }
+        }
+      }
+      top.compact();
+      float2 stat = make_float2(0.0f, 0.0f);
+      if (P.lse) {
+        float a, b;
+        apart(s01 + s23, a, b);
+        stat = join_workers<FAST>(P.temperature, m, a + b, S.stat, lane, warp);
+      }
+      if (P.split == 1) {
+        if (thread < P.k) top_write<T>(P, row, thread, S.buffer[thread]);
+        if (P.lse && thread == 0) P.lse[row] = tempered_lse(P.temperature, stat.x, stat.y);
+        loss_workers_sync();                               // the buffer may be written again
+      } else {
+        // this block's list, 0 where it has fewer than k keys, for rank 0
+        const int n = S.count;
+        const Key key = thread < n && thread < P.k ? S.buffer[thread] : 0;
+        cluster_sync();                                    // nobody uses rank 0's buffer any more
+        uint32_t list, told;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(list) : "r"(smem_u32(&S.buffer[rank * kTopMost + thread])));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(told) : "r"(smem_u32(&S.told[rank])));
+        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(list), "l"(key) : "memory");
+        if (thread == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(told), "f"(stat.x), "f"(stat.y) : "memory");
+        cluster_sync();
+        if (rank == 0) {
+          for (int q = 0; q < P.split; ++q) {
+            const Key k = S.buffer[q * kTopMost + thread];
+            if (k == 0) continue;
+            int above = thread;
+            for (int o = 0; o < P.split; ++o) {
+              if (o == q) continue;
+              int low = 0, high = P.k;                     // sorted, zeros last
+              while (low < high) {
+                const int mid = (low + high) / 2;
+                if (S.buffer[o * kTopMost + mid] > k) low = mid + 1; else high = mid;
+              }
+              above += low;
+            }
+            if (above < P.k) top_write<T>(P, row, above, k);
+          }
+          if (P.lse && thread == 0) {
+            float hi = -INFINITY, sum = 0.0f;
+            for (int o = 0; o < P.split; ++o) hi = fmaxf(hi, S.told[o].x);
+            e.set(hi);
+            for (int o = 0; o < P.split; ++o) sum += S.told[o].x == -INFINITY ? S.told[o].y : S.told[o].y * e(S.told[o].x);
+            P.lse[row] = tempered_lse(P.temperature, hi, sum);
+          }
+        }
+      }
+    }
+  }
+  if (P.split > 1 && thread >= kLossWorkers) {             // the producer's part in the two exchanges above
+    cluster_sync();
+    cluster_sync();
+  }
+}
+
+}  // namespace
+
+#endif  // GBMUF_CSRC_TOP_LOGITS_CUH
