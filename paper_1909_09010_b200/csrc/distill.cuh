@@ -44,7 +44,8 @@ struct RowList {
   short next[kListMost];     // of the chain, -1: end
   int head[kListHeads];
   // sums: q (log q - (x - m) / T); q; and of the student's exponentials, at T and at 1, relative to m
-  float gap, q_sum, m, s, s1, q_rest, target_logit, weight;
+  double gap;
+  float q_sum, m, s, s1, q_rest, target_logit, weight;
   int target;                // -1: none
   bool outside, ignored;
 };
@@ -94,14 +95,14 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
 #pragma unroll
     for (int i = 0; i < kListLanes; ++i)
       if (word[i] >= 0) s += expf((float)(a[i] - (double)largest));
-    A = (double)largest + (double)logf(warp_sum(s));
+    A = (double)largest + log_of(warp_sum(s));
   }
-  float q[kListLanes], xs[kListLanes], log_q[kListLanes], m = -INFINITY;
+  float q[kListLanes], xs[kListLanes], m = -INFINITY;
   double q_sum = 0.0;
 #pragma unroll
   for (int i = 0; i < kListLanes; ++i) {
-    log_q[i] = (float)(a[i] - A);
-    q[i] = word[i] >= 0 ? expf(log_q[i]) : 0.0f;
+    a[i] -= A;                                             // log q
+    q[i] = word[i] >= 0 ? expf((float)a[i]) : 0.0f;
     xs[i] = word[i] >= 0 ? to_f32(x[word[i]]) : -INFINITY;
     q_sum += (double)q[i];
     m = fmaxf(m, xs[i]);
@@ -147,13 +148,14 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   e.at(P.temperature);
   e.set(m);
   e1.set(m);
-  float s = 0.0f, s1 = 0.0f, gap = 0.0f;
+  float s = 0.0f, s1 = 0.0f;
+  double gap = 0.0;
   int words = 0;
 #pragma unroll
   for (int i = 0; i < kListLanes; ++i) {
     const int j = lane + 32 * i;
     if (word[i] >= 0) {
-      if (q[i] != 0.0f) gap += q[i] * (log_q[i] - (float)((double)(xs[i] - e.m) * P.temperature.inverse));
+      if (q[i] != 0.0f) gap += (double)q[i] * (a[i] - (double)(xs[i] - e.m) * P.temperature.inverse);
       if (first[i]) {
         s += e(xs[i]);
         s1 += e1(xs[i]);
@@ -166,7 +168,7 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   }
   s = warp_sum(s);
   s1 = warp_sum(s1);
-  gap = warp_sum(gap);
+  for (int d = 16; d > 0; d >>= 1) gap += __shfl_xor_sync(~0u, gap, d);
   words = __reduce_add_sync(~0u, words);
   outside = __any_sync(~0u, outside);
   if (lane == 0) {
@@ -207,22 +209,24 @@ __device__ __forceinline__ DistillRow distill_row(const DistillParams& P, const 
   e1.set(top);
   const float fr = m == -INFINITY ? 1.0f : e(m), fs = L.m == -INFINITY ? 1.0f : e(L.m);
   const float fr1 = m == -INFINITY ? 1.0f : e1(m), fs1 = L.m == -INFINITY ? 1.0f : e1(L.m);
-  const float z = r * fr + L.s * fs, z1 = one ? z : r1 * fr1 + L.s1 * fs1, log_z = logf(z);
+  const float z = r * fr + L.s * fs, z1 = one ? z : r1 * fr1 + L.s1 * fs1;
   const float w = L.weight, h = P.hard, q_rest = L.q_rest, mass = L.q_sum + q_rest;
-  o.lse = empty ? -INFINITY : (float)((double)e.m * P.temperature.inverse + (double)log_z);
-  o.zero = L.ignored || L.outside || empty;
-  // sum q (log q - log p): log p = (x - m_s) / T + (m_s - top) / T - log z
-  const float shift_s = L.m == -INFINITY ? 0.0f : (float)((double)(L.m - top) * P.temperature.inverse);
-  const float shift_r = m == -INFINITY ? 0.0f : (float)((double)(m - top) * P.temperature.inverse);
-  float soft = L.q_sum == 0.0f ? 0.0f : L.gap - L.q_sum * (shift_s - log_z);
-  if (q_rest != 0.0f) soft += q_rest * (logf(q_rest) - (logf(r) + shift_r - log_z));
-  const float hard = (top - L.target_logit) + logf(z1);
-  float loss = 0.0f;
-  if (h != 1.0f) loss += (1.0f - h) * (P.T * P.T) * soft;
-  if (h != 0.0f) loss += h * hard;
-  o.loss = L.ignored ? 0.0f : L.outside ? NAN : empty ? INFINITY : w * loss;
-  const float ws = w * (1.0f - h) * P.T, wh = w * h;
   const float share = r * fr / z;                          // P_r
+  const double log_z = log_of(z);
+  o.lse = empty ? -INFINITY : (float)((double)e.m * P.temperature.inverse + log_z);
+  o.zero = L.ignored || L.outside || empty;
+  // sum q (log q - log p): log p = (x - m_s) / T + (m_s - top) / T - log z.  In 64 bits: log z may be many times
+  // the loss.
+  const double shift_s = L.m == -INFINITY ? 0.0 : (double)(L.m - top) * P.temperature.inverse;
+  double soft = L.q_sum == 0.0f ? 0.0 : L.gap - (double)L.q_sum * (shift_s - log_z);
+  if (q_rest != 0.0f)
+    soft += (double)q_rest * (share > 1e-30f ? (double)logf(q_rest / share)
+                                             : (double)logf(q_rest) - (log_of(r) + (m == -INFINITY ? 0.0 : (double)(m - top) * P.temperature.inverse) - log_z));
+  double loss = 0.0;
+  if (h != 1.0f) loss += (1.0 - (double)h) * (double)(P.T * P.T) * soft;
+  if (h != 0.0f) loss += (double)h * ((double)(top - L.target_logit) + (one ? log_z : log_of(z1)));
+  o.loss = L.ignored ? 0.0f : L.outside ? NAN : empty ? INFINITY : (float)((double)w * loss);
+  const float ws = w * (1.0f - h) * P.T, wh = w * h;
   o.k = r == 0.0f ? 0.0f : ws * (mass * share - q_rest) / r;
   o.k1 = h == 0.0f || (one ? r : r1) == 0.0f ? 0.0f : wh * fr1 / z1;
   o.per = ws * mass / z;

@@ -152,12 +152,14 @@ struct Epilogue {
   int act, accumulate;
   int pairs;           // bf16: every matrix above may be accessed two columns at a time
   // of the loss alone
-  const void* loss_rows;     // kLossStats: int64 targets; kLossGrad: LossRow
+  const void* loss_rows;     // kLossStats: int64 targets; kLossGrad: RowPair
+  const int* loss_targets;   // kLossGrad
+  const float* loss_weights; // kLossGrad
   float* target_logit;       // kLossStats
   void* partial;             // kLossStats: float2 [slots][ld_partial]; kLossGrad: float [strips][ld_partial] or NULL
   long long ld_partial;
   long long part;            // kLossGrad, fp32: elements from one bf16 part of the output to the next
-  int first_word, words;     // kLossGrad: of the vocabulary's piece
+  int first_word, words;     // of the vocabulary's piece
 };
 
 // N rows of a warp's 32 neighbouring columns: lane l holds column c (= c of lane 0 + l) of rows

@@ -66,9 +66,10 @@ int rows_at_once(int tiles, int fit) {
 struct Plan {
   int parts;                                      // bf16 parts of an operand
   bool grad, x_ready, w_ready;                    // ready: read in place
-  long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, rows_padded, strips, slot_rows;
+  bool bias_once;
+  long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
-  long long x_off, w_off, row_off, target_off, slot_off, d_off, partial_off, acc_off, bytes;
+  long long x_off, w_off, target_off, slot_off, pair_off, word_off, weight_off, d_off, partial_off, acc_off, bytes;
 };
 
 Operand operand_x(const Args* a) { return {a->x, a->rows, a->n_in, a->ld_x, true, false, 0}; }
@@ -87,18 +88,37 @@ int stats_slots(const gbmuf_ops* ops, const TcShape& s, int tiles_c, long long w
   return (int)std::min<long long>(ops->num_sms / s.pair / tiles_c, (words + s.bn - 1) / s.bn) * (kTcFinishers / 4);
 }
 
+// The time of a piece by the model of the launch shapes, and a little for its launches.
+double piece_time(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
+  double ns = choose_shape(ops, logits_product(p, a, false, a->rows, words), p.parts, false, false, false).ns + 5000.0;
+  if (a->dw) ns += ready_shape(ops, a->dtype, true, words, a->n_in, a->rows).ns;
+  if (a->dx) ns += ready_shape(ops, a->dtype, false, a->rows, a->n_in, words).ns;
+  return ns;
+}
+// Words of a piece: what fits kPieceBytes, or a little less where that leaves fewer CTAs without a tile.
+long long choose_piece(const gbmuf_ops* ops, const Plan& p, const Args* a) {
+  const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * a->rows) / 256 * 256);
+  if (a->vocab <= most) return a->vocab;
+  const long long least = (a->vocab + most - 1) / most;
+  long long best = most;
+  double best_t = 1e300;
+  for (long long n = least; n <= least + least / 2 + 2; ++n) {
+    const long long piece = round_up((a->vocab + n - 1) / n, 256);
+    if (piece < kPieceLeast && n > least) break;
+    const long long whole = a->vocab / piece, rest = a->vocab % piece;
+    const double t = whole * piece_time(ops, p, a, piece) + (rest ? piece_time(ops, p, a, rest) : 0.0);
+    if (t < best_t) { best_t = t; best = piece; }
+  }
+  return best;
+}
+
 Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   Plan p{};
   p.parts = a->dtype == GBMUF_F32 ? 3 : 1;
   p.grad = a->dx || a->dw || a->dbias;
-  const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * std::max<long long>(a->rows, 1)) / 256 * 256);
   p.x_ready = in_place(operand_x(a), a->dtype);
   p.w_ready = in_place(operand_w(a, 0, a->vocab), a->dtype);
-  p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : a->vocab;
-  if (!a->piece && (p.grad || !p.w_ready) && a->vocab > most) {
-    const long long n = (a->vocab + most - 1) / most;
-    p.piece = round_up((a->vocab + n - 1) / n, 256);
-  }
+  p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : p.grad || !p.w_ready ? choose_piece(ops, p, a) : a->vocab;
   p.pieces = (a->vocab + p.piece - 1) / p.piece;
   p.ld_x = p.x_ready && a->rows > 1 ? a->ld_x : round_up(a->n_in, 8);      // the stride of a single row says nothing
   p.ld_w = p.w_ready && a->vocab > 1 ? a->ld_w : round_up(a->n_in, 8);
@@ -112,7 +132,6 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
   p.x_off = take(p.x_ready ? 0 : packed_bytes(operand_x(a), a->dtype));
   p.w_off = take(p.w_ready ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype));
-  p.row_off = take(p.rows_padded * (long long)sizeof(LossRow));
   p.target_off = take(a->rows * 4);
   long long slots = 0;                            // of the widest launch
   for (long long r = 0; r < a->rows;) {
@@ -123,9 +142,17 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   }
   p.slot_off = take(slots * 8);
   if (p.grad) {
+    p.pair_off = take(p.rows_padded / 2 * (long long)sizeof(RowPair));
+    p.word_off = take(p.rows_padded * 4);
+    p.weight_off = take(p.rows_padded * 4);
     p.d_off = take(a->rows * p.ld_d * 2 * p.parts);
-    p.strips = (a->rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
-    p.partial_off = take(a->dbias ? p.strips * p.ld_d * 4 : 0);
+    if (a->dbias) {
+      // the strips' sums of all words, added up once at the end, unless that takes too much room
+      p.strips = (a->rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
+      p.bias_once = p.strips * a->vocab * 4 <= kPieceBytes;
+      p.ld_partial = p.bias_once ? a->vocab : p.piece;
+      p.partial_off = take(p.strips * p.ld_partial * 4);
+    }
     p.acc_off = take(a->dx && p.pieces > 1 && a->dtype == GBMUF_BF16 ? a->rows * p.ld_acc * 4 : 0);
   }
   p.bytes = at;
@@ -155,6 +182,34 @@ gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* d
   if (j.blocks == 0) return GBMUF_OK;
   return launched("launch of the operand-packing kernel",
                   launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)j.blocks, 1, 256, 0, st, j, PackJob{}));
+}
+
+// A few fp32 rows without gradients: the fp32 units read the weights once, where the tensor cores would need
+// them packed as three bf16 parts first (8 x 512 -> 267,735 words: 431 us).  Their logits are few: they are
+// kept, in the workspace.
+gbmuf_linear_forward_args few_rows_args(const Args* a) {
+  gbmuf_linear_forward_args f{};
+  f.rows = a->rows; f.n_in = a->n_in; f.n_out = a->vocab; f.x = a->x; f.w = a->w; f.bias = a->bias;
+  f.y = a->workspace ? a->workspace : reinterpret_cast<void*>(256);
+  f.ld_x = a->ld_x; f.ld_w = a->ld_w; f.ld_y = a->vocab; f.dtype = a->dtype;
+  return f;
+}
+bool is_few_rows(gbmuf_ops* ops, const Args* a) {
+  if (a->dtype != GBMUF_F32 || a->rows > 16 || a->dx || a->dw || a->dbias) return false;
+  const gbmuf_linear_forward_args f = few_rows_args(a);
+  int64_t bytes = 0;
+  return gbmuf_linear_forward_workspace(ops, &f, &bytes) == GBMUF_OK && bytes == 0;
+}
+gbmuf_status run_few_rows(gbmuf_ops* ops, const Args* a, void* stream) {
+  const int64_t need = a->rows * a->vocab * 4;
+  if (need > a->workspace_bytes || !a->workspace || (uintptr_t)a->workspace % 256 != 0)
+    return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
+  const gbmuf_linear_forward_args f = few_rows_args(a);
+  if (gbmuf_status rc = gbmuf_linear_forward(ops, &f, stream)) return rc;
+  gbmuf_cross_entropy_args c{};
+  c.rows = a->rows; c.vocab = a->vocab; c.logits = a->workspace; c.targets = a->targets; c.row_weight = a->row_weight;
+  c.loss = a->loss; c.lse = a->lse; c.ld_logits = a->vocab; c.ignore_index = a->ignore_index; c.dtype = a->dtype; c.scale = a->scale;
+  return gbmuf_cross_entropy(ops, &c, stream);
 }
 
 template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cudaStream_t st) {
@@ -224,7 +279,11 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     J.L.rows = n; J.L.vocab = V; J.L.ignore_index = a->ignore_index; J.L.scale = a->scale; J.L.status = ops->d_status;
     J.slots = reinterpret_cast<const float2*>(ws + p.slot_off);
     J.target_logit = reinterpret_cast<const float*>(ws + p.target_off) + r0;
-    J.out = p.grad ? reinterpret_cast<LossRow*>(ws + p.row_off) + r0 : nullptr;
+    if (p.grad) {                                          // r0 is a multiple of 128
+      J.pairs = reinterpret_cast<RowPair*>(ws + p.pair_off) + r0 / 2;
+      J.targets = reinterpret_cast<int*>(ws + p.word_off) + r0;
+      J.weights = reinterpret_cast<float*>(ws + p.weight_off) + r0;
+    }
     J.ld = ld; J.count = slots;
     J.rows_padded = r0 + n == N ? p.rows_padded - r0 : n;
     const cudaError_t e = launch(loss_join_kernel, (unsigned)((J.rows_padded + 31) / 32), 1, 32 * kJoinShares, 0, st, J);
@@ -242,18 +301,21 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     // an even number of columns, so that bf16 goes out two at a time: the last one may lie beyond the piece
     TcParams P = tc_params(p.tc, N, round_up(words, 2), false);
     P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
-    P.E.loss_rows = ws + p.row_off;
-    P.E.partial = a->dbias ? ws + p.partial_off : nullptr;
-    P.E.ld_partial = p.ld_d;
+    P.E.loss_rows = ws + p.pair_off;
+    P.E.loss_targets = reinterpret_cast<const int*>(ws + p.word_off);
+    P.E.loss_weights = reinterpret_cast<const float*>(ws + p.weight_off);
+    P.E.partial = a->dbias ? reinterpret_cast<float*>(ws + p.partial_off) + (p.bias_once ? v0 : 0) : nullptr;
+    P.E.ld_partial = p.ld_partial;
     P.E.first_word = (int)v0; P.E.words = (int)words;
     P.E.out0 = d; P.E.ld_out0 = p.ld_d; P.E.part = N * p.ld_d; P.E.pairs = 1;
     const int at_once = std::min(P.tiles, ops->num_sms / p.tc.pair);
     if (gbmuf_status rc = launch_logits<kLossGrad, T, PARTS>(ops, p.tc, P, at_once, w, x, a->dtype, st)) return rc;
-    if (a->dbias) {
+    if (a->dbias && (!p.bias_once || last)) {
+      const long long first = p.bias_once ? 0 : v0, n = v0 + words - first;
       cudaError_t e = cudaSuccess;
-      DISPATCH_DTYPE(a->grad_dtype, TO, e = launch(loss_bias_kernel<TO>, (unsigned)((words + 255) / 256), 1, 256, 0, st,
-                                                   reinterpret_cast<const float*>(ws + p.partial_off), p.ld_d, (int)p.strips, words,
-                                                   static_cast<TO*>(a->dbias) + v0, (int)a->accumulate));
+      DISPATCH_DTYPE(a->grad_dtype, TO, e = launch(loss_bias_kernel<TO>, (unsigned)((n + 255) / 256), 1, 256, 0, st,
+                                                   reinterpret_cast<const float*>(ws + p.partial_off), p.ld_partial, (int)p.strips, n,
+                                                   static_cast<TO*>(a->dbias) + first, (int)a->accumulate));
       if (e != cudaSuccess) return cuda_refuse("launch of the loss's bias-gradient kernel", e);
     }
     if (H == 0) continue;
@@ -295,7 +357,7 @@ gbmuf_status gbmuf_linear_cross_entropy_workspace(gbmuf_ops* ops, const gbmuf_li
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check(ops, a)) return st;
-    *bytes = a->rows == 0 ? 0 : make_plan(ops, a).bytes;
+    *bytes = a->rows == 0 ? 0 : is_few_rows(ops, a) ? a->rows * a->vocab * 4 : make_plan(ops, a).bytes;
     return GBMUF_OK;
   });
 }
@@ -313,6 +375,7 @@ gbmuf_status gbmuf_linear_cross_entropy(gbmuf_ops* ops, const gbmuf_linear_cross
     }
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
+    if (is_few_rows(ops, a)) return run_few_rows(ops, a, stream);
     DISPATCH_DTYPE(a->dtype, T, return run<T>(ops, a, (cudaStream_t)stream));
   });
 }

@@ -13,13 +13,12 @@ namespace {
 // fp32 as its three parts.  bf16: that rounding is off by at most 2^-9 of an element, and the products'
 // sums of many such elements by less.
 
-// kLossGrad: what it needs of a row.
-struct __align__(16) LossRow {
-  float m, k, w;             // maximum; weight / sum; weight
-  int target;                // -1: no word of the vocabulary; -2: the row's gradient is zero
-};
-constexpr int kLossRowPad = 256;   // rows of a tile, at most: there are as many LossRow as rows of all tiles
+// What kLossGrad needs of two rows of the batch, as two packed operands: minus their maxima, and weight / sum.  Next to it stand per row the target (-1: no word of the vocabulary; -2: the row's
+// gradient is zero) and the weight.
+struct __align__(16) RowPair { float m[2], k[2]; };
+constexpr int kLossRowPad = 256;   // rows of a tile, at most: the arrays cover all tiles
 
+// Measured (2,048 x 1,024 x 14,080 bf16): see the figures at the kernel.
 template <typename T, bool PROMOTE> struct RowStats {
   static constexpr bool FAST = sizeof(T) == 2;
   float m = -INFINITY;
@@ -38,21 +37,33 @@ template <typename T, bool PROMOTE> struct RowStats {
     e.set(m);
     there = c < rows;
     const long long t = there ? static_cast<const long long*>(E.loss_rows)[c] : -1;
-    target = t >= 0 && t <= 0x7fffffff ? (int)t : -1;
+    target = t >= 0 && t <= 0x7fffffff ? (int)t - E.first_word : -1;
   }
   // N words from r on
   template <int N> __device__ __forceinline__ void add(const Epilogue& E, float (&v)[N], int r, int words) {
-    if (E.bias) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += r + i < words ? to_f32(static_cast<const T*>(E.bias)[r + i]) : 0.0f;
-    }
-    if (r + N > words) {
+    if (r + N > words) {                                   // the vocabulary's end
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (r + i >= words) v[i] = -INFINITY;
+        v[i] = r + i >= words ? -INFINITY : E.bias ? v[i] + to_f32(static_cast<const T*>(E.bias)[r + i]) : v[i];
+    } else if (E.bias) {
+      const T* const bias = static_cast<const T*>(E.bias) + r;
+      if (FAST && (uintptr_t)bias % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+          const uint4 u = *reinterpret_cast<const uint4*>(bias + i);
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            apart(two(v[i + 2 * j], v[i + 2 * j + 1]) + two(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)),
+                  v[i + 2 * j], v[i + 2 * j + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += to_f32(bias[i]);
+      }
     }
-    const int at_target = target - E.first_word - r;
-    if ((unsigned)at_target < (unsigned)N) {
+    const int at_target = target - r;
+    if ((unsigned)at_target < (unsigned)N && target >= 0) {
       float x = v[0];
 #pragma unroll
       for (int i = 1; i < N; ++i) x = at_target == i ? v[i] : x;
@@ -88,23 +99,40 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
   template <bool WHOLE>
   __device__ __forceinline__ void finish_(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
     constexpr bool FAST = sizeof(T) == 2;
-    const LossRow* const rows = static_cast<const LossRow*>(E.loss_rows) + r;
-    const int word = c + E.first_word;
+    const ulonglong2* const rows = static_cast<const ulonglong2*>(E.loss_rows) + r / 2;
+    const int t = lane < N ? E.loss_targets[r + lane] : -1;
     Two sum = two(0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
-      const LossRow a = rows[i], b = rows[i + 1];
-      const Two z = two(v[i], v[i + 1]) + two(bias, bias);
-      apart(exp_of<FAST>(z + two(-a.m, -b.m)) * two(a.k, b.k), v[i], v[i + 1]);
-      if (word == a.target) v[i] -= a.w;
-      if (word == b.target) v[i + 1] -= b.w;
-      if (a.target == -2) v[i] = 0.0f;
-      if (b.target == -2) v[i + 1] = 0.0f;
-      sum = sum + two(v[i], v[i + 1]);
+      const ulonglong2 pair = rows[i / 2];
+      const Two z = two(v[i], v[i + 1]) + two(bias, bias), m{pair.x}, k{pair.y};
+      const Two d = exp_of<FAST>(z + m) * k;
+      sum = sum + d;
+      apart(d, v[i], v[i + 1]);
     }
     float s0, s1;
     apart(sum, s0, s1);
     column = s0 + s1;
+    // rows whose target is among the warp's words: few
+    const unsigned hit = __ballot_sync(~0u, (unsigned)(t - E.first_word - (c - lane)) < 32u && t >= 0);
+    if (hit) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (hit >> i & 1) {
+          const float w = __shfl_sync(~0u, t, i) == c + E.first_word ? E.loss_weights[r + i] : 0.0f;
+          v[i] -= w;
+          column -= w;
+        }
+    }
+    // rows without a gradient have k = 0: only what is not finite is left to be cleared
+    if (!(fabsf(column) <= 3.4e38f)) {
+      column = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (E.loss_targets[r + i] == -2) v[i] = 0.0f;
+        column += v[i];
+      }
+    }
     if constexpr (FAST) {
       store_strip<T, WHOLE>(v, E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);
     } else {
@@ -134,7 +162,9 @@ struct JoinParams {
   LossParams L;
   const float2* slots;
   const float* target_logit;
-  LossRow* out;              // or NULL
+  RowPair* pairs;            // or NULL
+  int* targets;
+  float* weights;
   long long ld, rows_padded;
   int count;
 };
@@ -157,7 +187,8 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
   part[share][lane] = make_float2(m, s);
   __syncthreads();
   if (share != 0 || row >= P.rows_padded) return;
-  LossRow out{0.0f, 0.0f, 0.0f, -2};
+  float offset = 0.0f, k = 0.0f, weight = 0.0f;
+  int target = -2;
   if (row < P.L.rows) {
     for (int i = 1; i < kJoinShares; ++i) join_stats(m, s, part[i][lane]);
     const long long t = P.L.targets[row];
@@ -167,9 +198,18 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
     report_target(P.L, t, w);
     if (P.L.loss) P.L.loss[row] = o.loss;
     if (P.L.lse) P.L.lse[row] = o.lse;
-    if (!o.zero) out = LossRow{m == -INFINITY ? 0.0f : m, w / s, w, (int)t};
+    if (!o.zero) {
+      offset = m == -INFINITY ? 0.0f : -m;
+      k = w / s;
+      weight = w;
+      target = (int)t;
+    }
   }
-  if (P.out) P.out[row] = out;
+  if (!P.pairs) return;
+  P.pairs[row / 2].m[row & 1] = offset;
+  P.pairs[row / 2].k[row & 1] = k;
+  P.targets[row] = target;
+  P.weights[row] = weight;
 }
 
 // dbias of a piece: the strips' sums in their order.

@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
-  constexpr int N = NCOL < 16 ? NCOL : 16;        // of them at a time
+  constexpr int N = KIND == kLossGrad && PROMOTE ? 8 : NCOL < 16 ? NCOL : 16;        // of them at a time (16 would spill)
   extern __shared__ __align__(128) unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const uint32_t bars = smem_u32(smem), ring = bars + kTcHead;

@@ -75,9 +75,9 @@ int may_pair(const Product& q) {
 // by a model whose eight constants were fitted to 180 measured products of 12 to 100,000 rows, columns
 // and terms in both types (its choice was 0.8 % above the best one on average, 15 % at worst; no sum along
 // a vocabulary among them).  The 1.45 for pairs with a strided A says what was measured, not why.
-struct TcShape { int bn, split, pair; };
+struct TcShape { int bn, split, pair; double ns; };
 TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided, bool may_split = true) {
-  TcShape best{64, 1, 1};
+  TcShape best{64, 1, 1, 0.0};
   double best_t = 1e300;
   const long long ksteps = (q.K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
@@ -94,9 +94,18 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
         const double sums = 1000.0 + (double)((ksteps + split - 1) / split) * step, epilogue = 15.0 * bn / split;
         double t = split > 1 ? waves * (sums + 1100.0 + 19.0 * bn) : waves * std::max(sums, epilogue);
         t += epilogue + (pair == 2 ? 2000.0 : 0.0);
-        if (t < best_t) { best_t = t; best = {bn, split, pair}; }
+        if (t < best_t) { best_t = t; best = {bn, split, pair, t}; }
       }
   return best;
+}
+
+// The shape of a product of a piece of the vocabulary (ready_product.h), whose sums are 1,000 terms and more.  There
+// pairs pay with a strided first operand too (bf16, pieces of 14,336 words, 2,048 x 1,024: weight gradient 48.9 us
+// with pairs, 55.1 without; input gradient 48.1 and 57.3).
+TcShape ready_shape(const gbmuf_ops* ops, int32_t dtype, bool weight_grad, long long rows, long long cols, long long terms) {
+  Product q{};
+  q.R = rows; q.C = cols; q.K = terms; q.dtype = dtype;
+  return choose_shape(ops, q, dtype == GBMUF_F32 ? 3 : 1, weight_grad, false);
 }
 
 // at_once: tiles that are worked on side by side.

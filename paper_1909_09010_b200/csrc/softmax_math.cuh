@@ -68,6 +68,13 @@ __device__ __forceinline__ void report_target(const LossParams& P, long long t, 
   if (!target_ignored(P, t, w) && !target_inside(P, t)) atomicExch(P.status, (int32_t)GBMUF_ERR_INVALID_ARG);
 }
 
+// log z to 2^-24 or so whatever its size: the exponent's part in 64 bits, beside the logarithm of 0.7 .. 1.4.
+__device__ __forceinline__ double log_of(float z) {
+  if (!(z > 1e-37f && z < 3.4e38f)) return (double)logf(z);
+  const uint32_t b = __float_as_uint(z), shifted = b - 0x3f350000u;           // sqrt 1/2
+  const int e = (int)shifted >> 23;
+  return (double)e * 0.69314718055994531 + (double)logf(__uint_as_float(b - ((uint32_t)e << 23)));
+}
 // exp((x - m) / T), as Shift: log2 e / T = hi + lo; below `least` (x - m) the result is 0 in fp32.
 struct Temperature {
   float hi, lo, least;

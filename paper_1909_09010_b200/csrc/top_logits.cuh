@@ -179,7 +179,7 @@ __device__ __forceinline__ float2 join_workers(const Temperature& t, float m, fl
 }
 __device__ __forceinline__ float tempered_lse(const Temperature& t, float m, float s) {
   if (m == -INFINITY && s == 0.0f) return -INFINITY;
-  return (float)((double)m * t.inverse + (double)logf(s));
+  return (float)((double)m * t.inverse + log_of(s));
 }
 template <typename T> __device__ __forceinline__ void top_write(const TopParams& P, long long row, int at, Key key) {
   const int i = key_index(key);
