@@ -7,15 +7,16 @@ namespace {
 
 // One pass over the row.  A logit and its index make one whole number (key) that is larger where the logit
 // is, and among equal logits where the index is smaller; keys are all different, so "the k largest" has one
-// answer.  A block keeps the k largest keys so far, and a threshold that no key below it can be among the k
-// largest.  Keys at or above it are appended to a buffer; once that has grown, its keys are ranked by
-// counting, the k largest stay, and the threshold is the last of them.  Most pieces of a row are passed
-// over after one comparison of their maximum.
+// answer.  The pass keeps only the maximum of each group of 32 or more logits (what a thread sees of a chunk or
+// a few).  The k-th largest maximum is a bound that at least k logits reach, and only the groups whose
+// maximum reaches it, k of them but for equal ones, hold any of the k largest: they are read again (a few
+// KB), and what reaches the bound is ranked.  Both selections go the same way: 256 threads' largest keys
+// give a first bound (their k-th largest), what reaches it is put in a buffer, the buffer's k largest are
+// kept and sorted.
 //
-// The first threshold of a row: of 256 threads' largest keys in the first chunk the k-th largest.  It is at
-// most the k-th largest key of all, and at most k threads have keys above it.  That also bounds what a
-// piece per thread can append (k times its elements), which is how a chunk is taken that overflows the
-// buffer (a row that rises, or holds few different values): piece by piece, with a new threshold each.
+// Rows with so many equal or so unevenly placed logits that lists or buffer overflow are gone through once
+// more, chunk by chunk, with a bound that rises: at most k threads have keys above the k-th largest of the
+// threads' largest keys, so piece by piece (a thread's 16 bytes) the buffer cannot overflow.
 struct TopParams {
   const void* logits;
   void* values;
@@ -28,6 +29,8 @@ struct TopParams {
 };
 constexpr int kTopMost = 256;                  // k
 constexpr int kTopBuffer = kTopMost * 10;      // keys: k kept ones and k pieces of 8, and room
+constexpr int kTopGroupBytes = 16384;          // maxima of groups
+constexpr int kTopHot = 1024;                  // groups that are read again
 constexpr int kTopShort = 2048;                // vocabulary of the kernel without a ring
 typedef unsigned long long Key;
 
@@ -61,9 +64,11 @@ __device__ __forceinline__ bool any_worker(bool mine) {
 
 struct TopShared {
   Key buffer[kTopBuffer];
+  unsigned char groups[kTopGroupBytes];
+  unsigned short hot[kTopHot];
+  int counts[64];
   Key threshold;
-  int count;
-  int pad;
+  int count, hot_count;
   float2 stat[kLossWarps];
   float2 told[8];
 };
@@ -111,22 +116,49 @@ struct TopState {
     loss_workers_sync();
   }
   // Sorts the buffer, keeps its k largest keys.  Returns how many keys there had been.
-  __device__ __forceinline__ int compact() {
+  __device__ __noinline__ int compact() {
     loss_workers_sync();
-    const int found = S.count, n = min(found, kTopBuffer);
+    const int found = S.count;
+    int n = min(found, kTopBuffer);
     constexpr int MOST = kTopBuffer / kLossWorkers;
+    if (n > 2 * kLossWorkers && n > k) {
+      // Many: the k-th largest bit by bit, from how many keys reach a number; then those that reach it.
+      Key mine[MOST], bound = 0;
+#pragma unroll
+      for (int q = 0; q < MOST; ++q) mine[q] = q * kLossWorkers + thread < n ? S.buffer[q * kLossWorkers + thread] : 0;
+      if (thread < 64) S.counts[thread] = 0;
+      loss_workers_sync();
+      if (thread == 0) S.count = 0;                        // everybody has read it
+      for (int bit = 63; bit >= 0; --bit) {
+        const Key next = bound | (Key)1 << bit;
+        int reach = 0;
+#pragma unroll
+        for (int q = 0; q < MOST; ++q) reach += mine[q] >= next;
+        reach = __reduce_add_sync(~0u, reach);
+        if ((thread & 31) == 0) atomicAdd(&S.counts[bit], reach);
+        loss_workers_sync();
+        reach = S.counts[bit];
+        if (reach >= k) bound = next;
+        if (reach == k) break;
+      }
+#pragma unroll
+      for (int q = 0; q < MOST; ++q)
+        if (mine[q] != 0 && mine[q] >= bound) S.buffer[atomicAdd(&S.count, 1)] = mine[q];
+      loss_workers_sync();
+      n = S.count;                                         // k: keys are all different
+    }
     if (thread == 0 && (n & 1)) S.buffer[n] = 0;           // pairs are read; the buffer's size is even
     loss_workers_sync();
-    Key mine[MOST];
-    int rank[MOST];
+    Key mine[2];
+    int rank[2];
 #pragma unroll
-    for (int q = 0; q < MOST; ++q) {
+    for (int q = 0; q < 2; ++q) {
       rank[q] = k;
       if (q * kLossWorkers >= n) continue;                 // the same for all threads
       const int i = q * kLossWorkers + thread;
       mine[q] = i < n ? S.buffer[i] : 0;
       int above = 0;
-#pragma unroll 4
+#pragma unroll 8
       for (int j = 0; j < n; j += 2) {
         const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(S.buffer + j);
         above += (o.x > mine[q]) + (o.y > mine[q]);
@@ -135,7 +167,7 @@ struct TopState {
     }
     loss_workers_sync();
 #pragma unroll
-    for (int q = 0; q < MOST; ++q)
+    for (int q = 0; q < 2; ++q)
       if (rank[q] < k) S.buffer[rank[q]] = mine[q];
     if (thread == 0) S.count = min(n, k);
     loss_workers_sync();
@@ -245,10 +277,69 @@ constexpr int kTopBlocksPerSm = 2;
 constexpr uint32_t kTopHead = (256u + (uint32_t)sizeof(TopShared) + 127u) / 128u * 128u;
 constexpr uint32_t kTopSmem = kTopHead + kTopRing * kLossChunk;
 
+// A slice of a row, chunk by chunk, with a rising bound; `at_least`: a bound to begin with.
+template <typename T>
+__device__ __noinline__ void top_scan(TopState& top, const T* x, const RowSpan r, int chunks, float own, int own_at, Key at_least) {
+  constexpr int E = 16 / (int)sizeof(T);
+  TopShared& S = top.S;
+  const int thread = top.thread;
+  top.start();
+  top.set(at_least);
+  for (int c = 0; c < (chunks > 0 ? chunks : 1); ++c) {
+    const int left = c < chunks ? r.n - c * kLossPieces * kLossWorkers - thread : 0;
+    const int c0 = r.a0 + (r.p0 + c * kLossPieces * kLossWorkers + thread) * E;
+    float v[E];
+    // a thread's keys of one piece; h = -1: the element that it holds outside the whole pieces
+    auto keys_of = [&](int h, Key (&mine)[E]) {
+      const bool there = h >= 0 ? h * kLossWorkers < left : c == 0 && own_at >= 0;
+      uint4 piece = make_uint4(0, 0, 0, 0);
+      if (there && h >= 0) piece = *reinterpret_cast<const uint4*>(x + c0 + h * kLossWorkers * E);
+      piece_values(piece, v);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        mine[i] = !there ? 0 : h >= 0 ? top_key(v[i], c0 + h * kLossWorkers * E + i) : i == 0 ? top_key(own, own_at) : 0;
+        if (mine[i] < top.threshold) mine[i] = 0;
+      }
+    };
+    bool lengthy = false;
+#pragma unroll 1
+    for (int h = -1; h < kLossPieces; ++h) {
+      Key mine[E];
+      keys_of(h, mine);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (mine[i] != 0) lengthy |= top.append(mine[i]);
+    }
+    if (!any_worker(lengthy)) continue;
+    if (top.compact() <= kTopBuffer) continue;
+    // what did not fit: piece by piece; keys that are there already are passed over
+#pragma unroll 1
+    for (int h = -1; h < kLossPieces; ++h) {
+      const int have = S.count;
+      Key mine[E], largest = 0;
+      keys_of(h, mine);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        if (mine[i] != 0 && top.kept(mine[i], have)) mine[i] = 0;
+        largest = max(largest, mine[i]);
+      }
+      loss_workers_sync();                                 // the count has been read
+      top.raise(largest, have);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (mine[i] != 0 && mine[i] >= top.threshold) top.append(mine[i]);
+      top.compact();
+    }
+  }
+  top.compact();
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel(const TopParams P) {
   constexpr bool FAST = sizeof(T) == 2;
   constexpr int E = 16 / (int)sizeof(T);
+  typedef std::conditional_t<FAST, unsigned short, unsigned> Order;    // a maximum, as a whole number in its order
+  constexpr int GROUPS = kTopGroupBytes / (int)sizeof(Order) / kLossWorkers;       // per thread
   extern __shared__ __align__(128) unsigned char smem[];
   const uint32_t bars = smem_u32(smem), ring = bars + kTopHead;
   auto full = [&](int s) { return bars + 8u * s; };
@@ -295,10 +386,12 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
   } else {
     // ------------------------------------------------------------------ 8 worker warps
     bool ok = true;
+    Order* const groups = reinterpret_cast<Order*>(S.groups);
     for (long long row = first; row < P.rows; row += step) {
       const RowSpan r = row_span<T>(P, row, rank);
       const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
       const int chunks = (r.n + kLossPieces * kLossWorkers - 1) / (kLossPieces * kLossWorkers);
+      const int run = (chunks + GROUPS - 1) / GROUPS;      // chunks of a group
       // the elements before and after the whole pieces: one thread of rank 0 each
       float own = -INFINITY;
       int own_at = -1;
@@ -306,113 +399,124 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
         const int at = thread < r.a0 ? thread : r.pieces * E + thread;
         if (at < (int)P.vocab) { own_at = at; own = to_f32(x[at]); }
       }
-      TopState top{S, P.k, thread};
-      top.start();
       TemperedShift<FAST> e;
       e.at(P.temperature);
       float m = own == own ? own : -INFINITY;
       e.set(m);
       Two s01 = two(own_at >= 0 && own != -INFINITY ? 1.0f + (own - own) : 0.0f, 0.0f), s23 = two(0.0f, 0.0f);
-      for (int c = 0; c < (chunks > 0 ? chunks : 1); ++c) {
-        const int left = c < chunks ? r.n - c * kLossPieces * kLossWorkers - thread : 0;
+      Key largest = 0;                                     // of this thread's groups
+      float group = -INFINITY;
+      int in_run = 0, mine = 0;                            // chunks of the group so far, groups so far
+      for (int c = 0; c < chunks; ++c) {
+        ok = ok && mbar_wait_bounded(full(slot), phase, P.status);
+        const int left = r.n - c * kLossPieces * kLossWorkers - thread;
+        const uint4* const p = reinterpret_cast<const uint4*>(smem + kTopHead + slot * kLossChunk) + thread;
         uint4 u[kLossPieces];
-        float tops[kLossPieces], v[E];
-        const int c0 = r.a0 + (r.p0 + c * kLossPieces * kLossWorkers + thread) * E;
-        auto there = [&](int h) { return h * kLossWorkers < left && ok; };
-        if (c < chunks) {
-          ok = ok && mbar_wait_bounded(full(slot), phase, P.status);
-          const uint4* const p = reinterpret_cast<const uint4*>(smem + kTopHead + slot * kLossChunk) + thread;
+        float v[E];
+        const bool whole = (kLossPieces - 1) * kLossWorkers < left;
 #pragma unroll
-          for (int h = 0; h < kLossPieces; ++h) u[h] = p[h * kLossWorkers < left ? h * kLossWorkers : 0];
-          __syncwarp();
-          if (lane == 0) mbar_arrive(empty(slot));
-          advance();
-        }
+        for (int h = 0; h < kLossPieces; ++h) u[h] = p[h * kLossWorkers < left ? h * kLossWorkers : 0];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(slot));
+        advance();
+        if (left > 0 && ok) {
+          float top = piece_max_nan(u[0], v);              // what is missing counts as the first piece again
 #pragma unroll
-        for (int h = 0; h < kLossPieces; ++h) tops[h] = there(h) ? piece_max_nan(u[h], v) : -INFINITY;
-        auto largest_of = [&](uint4 piece, int h) {        // largest wanted key of a piece
-          Key k = 0;
-          piece_values(piece, v);
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            const Key key = top_key(v[i], c0 + h * kLossWorkers * E + i);
-            if (key >= top.threshold) k = max(k, key);
-          }
-          return k;
-        };
-        if (c == 0) {
-          Key largest = own_at >= 0 ? top_key(own, own_at) : 0;
-#pragma unroll
-          for (int h = 0; h < kLossPieces; ++h)
-            if (there(h)) largest = max(largest, largest_of(u[h], h));
-          top.raise(largest, 0);
-        }
-        bool lengthy = c == 0;
-        if (c == 0 && own_at >= 0 && top_key(own, own_at) >= top.threshold) top.append(top_key(own, own_at));
-#pragma unroll
-        for (int h = 0; h < kLossPieces; ++h)
-          if (there(h) && top.wanted(tops[h])) {
-            piece_values(u[h], v);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-              const Key key = top_key(v[i], c0 + h * kLossWorkers * E + i);
-              if (key >= top.threshold) lengthy |= top.append(key);
-            }
-          }
-        if (any_worker(lengthy)) {
-          if (top.compact() > kTopBuffer) {
-            // what did not fit: piece by piece; keys that are there already are passed over
-#pragma unroll 1
-            for (int h = -1; h < kLossPieces; ++h) {
-              uint4 piece = u[0];
-#pragma unroll
-              for (int j = 1; j < kLossPieces; ++j) piece = h == j ? u[j] : piece;
-              const int have = S.count;
-              Key mine[E], largest = 0;
-              piece_values(piece, v);
-#pragma unroll
-              for (int i = 0; i < E; ++i) {
-                const bool is = h >= 0 ? there(h) : i == 0 && c == 0 && own_at >= 0;
-                mine[i] = !is ? 0 : h >= 0 ? top_key(v[i], c0 + h * kLossWorkers * E + i) : top_key(own, own_at);
-                if (mine[i] < top.threshold || (mine[i] != 0 && top.kept(mine[i], have))) mine[i] = 0;
-                largest = max(largest, mine[i]);
+          for (int h = 1; h < kLossPieces; ++h) top = max_nan(top, piece_max_nan(u[h], v));
+          group = max_nan(group, top);
+          if (P.lse) {
+            if (top > m || top != top) {
+              const float before = m;
+              if (top != top) s01 = s01 + two(top, top);   // a NaN among them: the sum is one
+              else m = top;
+              e.set(m);
+              if (before != -INFINITY) {
+                const float f = e(before);
+                s01 = s01 * two(f, f);
+                s23 = s23 * two(f, f);
               }
-              loss_workers_sync();                         // the count has been read
-              top.raise(largest, have);
-#pragma unroll
-              for (int i = 0; i < E; ++i)
-                if (mine[i] != 0 && mine[i] >= top.threshold) top.append(mine[i]);
-              top.compact();
             }
-          }
-        }
-        if (P.lse && left > 0 && ok) {
-          float highest = piece_max(u[0], v);
-#pragma unroll
-          for (int h = 1; h < kLossPieces; ++h) highest = fmaxf(highest, piece_max(u[h], v));
-          if (highest > m) {
-            const float before = m;
-            m = highest;
-            e.set(m);
-            if (before != -INFINITY) {
-              const float f = e(before);
-              s01 = s01 * two(f, f);
-              s23 = s23 * two(f, f);
-            }
-          }
-#pragma unroll
-          for (int h = 0; h < kLossPieces; ++h)
-            if (h * kLossWorkers < left) {
-              piece_values(u[h], v);
+            auto add = [&](uint4 piece) {
+              piece_values(piece, v);
 #pragma unroll
               for (int i = 0; i < E; i += 4) {
                 s01 = s01 + e(v[i], v[i + 1]);
                 s23 = s23 + e(v[i + 2], v[i + 3]);
               }
+            };
+            if (whole) {
+#pragma unroll
+              for (int h = 0; h < kLossPieces; ++h) add(u[h]);
+            } else {
+#pragma unroll
+              for (int h = 0; h < kLossPieces; ++h)
+                if (h * kLossWorkers < left) add(u[h]);
             }
+          }
+        }
+        if (++in_run == run || c == chunks - 1) {
+          // a group's key: its maximum, and its number where an index would be
+          const bool any = r.n - (c + 1 - in_run) * kLossPieces * kLossWorkers - thread > 0;
+          const Key key = top_key(group, mine * kLossWorkers + thread);
+          groups[mine * kLossWorkers + thread] = any ? (Order)((key >> 32) >> (FAST ? 16 : 0)) : (Order)0;
+          if (any) largest = max(largest, key);
+          group = -INFINITY;
+          in_run = 0;
+          ++mine;
         }
       }
-      top.compact();
+      TopState top{S, P.k, thread};
+      auto group_key = [&](int g) {
+        const Order o = groups[g * kLossWorkers + thread];
+        return o == 0 ? (Key)0 : (Key)((uint32_t)o << (FAST ? 16 : 0)) << 32 | (uint32_t)~(g * kLossWorkers + thread);
+      };
+      // (bf16: the lower half of a key's order is left out on both sides)
+      if (FAST) largest &= ~((Key)0xffff << 32);
+      if (thread == 0) S.hot_count = 0;
+      top.start();
+      top.raise(largest, 0);
+      if (largest >= top.threshold && largest != 0)
+        for (int g = 0; g < mine; ++g) {
+          const Key key = group_key(g);
+          if (key != 0 && key >= top.threshold) top.append(key);
+        }
+      const bool crowded = top.compact() > kTopBuffer;
+      const bool few = S.count < P.k;                      // fewer groups than k: everything is read again
+      const Key bound = few || crowded ? 0 : S.buffer[P.k - 1] & ~(Key)0xffffffffu;
+      bool again = crowded;
+      loss_workers_sync();                                 // buffer and count have been read
+      if (!again) {
+        top.start();
+        top.set(bound);
+        for (int g = 0; g < mine; ++g) {
+          const Key key = group_key(g);
+          if (key == 0 || key < bound) continue;
+          const int at = atomicAdd(&S.hot_count, 1);
+          if (at < kTopHot) S.hot[at] = (unsigned short)(g * kLossWorkers + thread);
+        }
+        if (own_at >= 0 && top_key(own, own_at) >= bound) top.append(top_key(own, own_at));
+        loss_workers_sync();
+        const int hot = S.hot_count;
+        again = hot > kTopHot;
+        if (!again) {
+          // a warp per group: lanes over its pieces' elements, one chunk of the run at a time
+          constexpr int LANES = E * kLossPieces, AT_ONCE = 32 / LANES;
+          const int part = lane / LANES, h = lane % LANES / E, i = lane % E;
+#pragma unroll 4
+          for (int j = warp * AT_ONCE + part; j < hot; j += kLossWarps * AT_ONCE) {
+            const int id = S.hot[j], g = id / kLossWorkers, t = id % kLossWorkers;
+            for (int c = g * run; c < min((g + 1) * run, chunks); ++c) {
+              const int piece = (c * kLossPieces + h) * kLossWorkers + t;
+              if (piece >= r.n) continue;
+              const int at = r.a0 + (r.p0 + piece) * E + i;
+              const Key key = top_key(to_f32(x[at]), at);
+              if (key >= bound) top.append(key);
+            }
+          }
+          again = top.compact() > kTopBuffer;
+        }
+      }
+      if (again) top_scan<T>(top, x, r, chunks, own, own_at, bound);
       float2 stat = make_float2(0.0f, 0.0f);
       if (P.lse) {
         float a, b;
