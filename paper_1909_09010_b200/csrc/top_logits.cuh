@@ -29,7 +29,7 @@ struct TopParams {
 };
 constexpr int kTopMost = 256;                  // k
 constexpr int kTopBuffer = kTopMost * 10;      // keys: k kept ones and k pieces of 8, and room
-constexpr int kTopGroupBytes = 16384;          // maxima of groups
+constexpr int kTopGroupBytes = 20480;          // maxima of groups: 40 chunks of bf16 are a group each
 constexpr int kTopHot = 1024;                  // groups that are read again
 constexpr int kTopShort = 2048;                // vocabulary of the kernel without a ring
 typedef unsigned long long Key;
@@ -62,15 +62,25 @@ __device__ __forceinline__ bool any_worker(bool mine) {
   return any != 0;
 }
 
+__device__ __forceinline__ int count_workers(bool mine) {
+  int n;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.popc.u32 %0, 1, %2, p;\n\t}"
+               : "=r"(n)
+               : "r"((uint32_t)mine), "n"(kLossWorkers)
+               : "memory");
+  return n;
+}
+
 struct TopShared {
   Key buffer[kTopBuffer];
   unsigned char groups[kTopGroupBytes];
   unsigned short hot[kTopHot];
   int counts[64];
   Key threshold;
+  uint32_t bounds[8];          // of the ranks
   int count, hot_count;
   float2 stat[kLossWarps];
-  float2 told[8];
+  float4 told[8];
 };
 
 // What the 256 workers of a block keep of a row.  All of them call all functions.
@@ -114,6 +124,19 @@ struct TopState {
     loss_workers_sync();
     set(S.threshold);
     loss_workers_sync();
+  }
+  // A number that at least k (and not many more) of the threads' numbers reach, or 0 where fewer than k are not 0: bit
+  // by bit, from how many threads reach a number.
+  // Where few threads reach it, an eighth too many is near enough.
+  __device__ __forceinline__ uint32_t bound_of(uint32_t mine, int last_bit) {
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= last_bit; --bit) {
+      const uint32_t next = bound | 1u << bit;
+      const int reach = count_workers(mine >= next);
+      if (reach >= k) bound = next;
+      if (reach >= k && reach <= k + k / 8 && k <= kLossWorkers / 2) break;
+    }
+    return bound;
   }
   // Sorts the buffer, keeps its k largest keys.  Returns how many keys there had been.
   __device__ __noinline__ int compact() {
@@ -215,7 +238,9 @@ __device__ __forceinline__ float tempered_lse(const Temperature& t, float m, flo
 }
 template <typename T> __device__ __forceinline__ void top_write(const TopParams& P, long long row, int at, Key key) {
   const int i = key_index(key);
-  static_cast<T*>(P.values)[row * P.ld_values + at] = (static_cast<const T*>(P.logits) + row * P.ld)[i];
+  const float v = key_value(key);                          // which zero and which NaN it is stands in the row
+  static_cast<T*>(P.values)[row * P.ld_values + at] =
+      v != 0.0f && v == v ? from_f32<T>(v) : (static_cast<const T*>(P.logits) + row * P.ld)[i];
   P.index[row * P.ld_index + at] = i;
 }
 
@@ -404,7 +429,7 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
       float m = own == own ? own : -INFINITY;
       e.set(m);
       Two s01 = two(own_at >= 0 && own != -INFINITY ? 1.0f + (own - own) : 0.0f, 0.0f), s23 = two(0.0f, 0.0f);
-      Key largest = 0;                                     // of this thread's groups
+      uint32_t largest = 0;                                // order of this thread's largest maximum
       float group = -INFINITY;
       int in_run = 0, mine = 0;                            // chunks of the group so far, groups so far
       for (int c = 0; c < chunks; ++c) {
@@ -455,66 +480,85 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
           }
         }
         if (++in_run == run || c == chunks - 1) {
-          // a group's key: its maximum, and its number where an index would be
           const bool any = r.n - (c + 1 - in_run) * kLossPieces * kLossWorkers - thread > 0;
-          const Key key = top_key(group, mine * kLossWorkers + thread);
-          groups[mine * kLossWorkers + thread] = any ? (Order)((key >> 32) >> (FAST ? 16 : 0)) : (Order)0;
-          if (any) largest = max(largest, key);
+          const uint32_t order = any ? (uint32_t)(top_key(group, 0) >> 32) >> (FAST ? 16 : 0) : 0u;
+          groups[mine * kLossWorkers + thread] = (Order)order;
+          largest = max(largest, order << (FAST ? 16 : 0));
           group = -INFINITY;
           in_run = 0;
           ++mine;
         }
       }
       TopState top{S, P.k, thread};
-      auto group_key = [&](int g) {
-        const Order o = groups[g * kLossWorkers + thread];
-        return o == 0 ? (Key)0 : (Key)((uint32_t)o << (FAST ? 16 : 0)) << 32 | (uint32_t)~(g * kLossWorkers + thread);
-      };
-      // (bf16: the lower half of a key's order is left out on both sides)
-      if (FAST) largest &= ~((Key)0xffff << 32);
+      auto group_order = [&](int g) { return (uint32_t)groups[g * kLossWorkers + thread] << (FAST ? 16 : 0); };
+      // (bf16: the lower half of an order is left out on both sides)
       if (thread == 0) S.hot_count = 0;
       top.start();
-      top.raise(largest, 0);
-      if (largest >= top.threshold && largest != 0)
-        for (int g = 0; g < mine; ++g) {
-          const Key key = group_key(g);
-          if (key != 0 && key >= top.threshold) top.append(key);
+      uint32_t least = top.bound_of(largest, FAST ? 16 : 0);
+      if (P.split > 1) {                                   // the best of all ranks' bounds
+        if (thread < P.split) {
+          uint32_t there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(&S.bounds[rank])), "r"(thread));
+          asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(there), "r"(least) : "memory");
         }
-      const bool crowded = top.compact() > kTopBuffer;
-      const bool few = S.count < P.k;                      // fewer groups than k: everything is read again
-      const Key bound = few || crowded ? 0 : S.buffer[P.k - 1] & ~(Key)0xffffffffu;
-      bool again = crowded;
-      loss_workers_sync();                                 // buffer and count have been read
-      if (!again) {
-        top.start();
-        top.set(bound);
-        for (int g = 0; g < mine; ++g) {
-          const Key key = group_key(g);
-          if (key == 0 || key < bound) continue;
-          const int at = atomicAdd(&S.hot_count, 1);
-          if (at < kTopHot) S.hot[at] = (unsigned short)(g * kLossWorkers + thread);
-        }
-        if (own_at >= 0 && top_key(own, own_at) >= bound) top.append(top_key(own, own_at));
+        cluster_sync();
+        for (int o = 0; o < P.split; ++o) least = max(least, S.bounds[o]);
+      }
+      auto list_groups = [&] {
+        if (largest >= least)
+          for (int g = 0; g < mine; ++g) {
+            const uint32_t o = group_order(g);
+            if (o == 0 || o < least) continue;
+            const int at = atomicAdd(&S.hot_count, 1);
+            if (at < kTopHot) S.hot[at] = (unsigned short)(g * kLossWorkers + thread);
+          }
         loss_workers_sync();
-        const int hot = S.hot_count;
-        again = hot > kTopHot;
-        if (!again) {
-          // a warp per group: lanes over its pieces' elements, one chunk of the run at a time
-          constexpr int LANES = E * kLossPieces, AT_ONCE = 32 / LANES;
-          const int part = lane / LANES, h = lane % LANES / E, i = lane % E;
-#pragma unroll 4
-          for (int j = warp * AT_ONCE + part; j < hot; j += kLossWarps * AT_ONCE) {
-            const int id = S.hot[j], g = id / kLossWorkers, t = id % kLossWorkers;
-            for (int c = g * run; c < min((g + 1) * run, chunks); ++c) {
-              const int piece = (c * kLossPieces + h) * kLossWorkers + t;
-              if (piece >= r.n) continue;
-              const int at = r.a0 + (r.p0 + piece) * E + i;
-              const Key key = top_key(to_f32(x[at]), at);
+        return S.hot_count;
+      };
+      int hot = list_groups();
+      if (hot > 2 * P.k + 64) {
+        // k near the number of threads, or many equal maxima: the k-th largest of all groups' maxima
+        loss_workers_sync();
+        if (thread == 0) S.hot_count = 0;
+        for (int g = 0; g < mine; ++g) {
+          const uint32_t o = group_order(g);
+          if (o != 0 && o >= least) top.append((Key)o << 32 | (uint32_t)~(g * kLossWorkers + thread));
+        }
+        if (top.compact() <= kTopBuffer && S.count >= P.k) least = (uint32_t)(S.buffer[P.k - 1] >> 32);
+        loss_workers_sync();                               // buffer and count have been read
+        if (thread == 0) S.count = 0;
+        hot = list_groups();
+      }
+      const Key bound = (Key)least << 32;
+      top.set(bound);
+      if (own_at >= 0 && top_key(own, own_at) >= bound) top.append(top_key(own, own_at));
+      bool again = hot > kTopHot;
+      if (!again) {
+        // a warp takes the pieces of several groups at a time, a lane an element of a piece of one chunk of the run
+        constexpr int LANES = E * kLossPieces, AT_ONCE = 32 / LANES, BATCH = 8;
+        const int part = lane / LANES, h = lane % LANES / E, i = lane % E, items = hot * run;
+        for (int j0 = warp * AT_ONCE + part; j0 - part < items; j0 += kLossWarps * AT_ONCE * BATCH) {
+          int at[BATCH];
+          T y[BATCH];
+#pragma unroll
+          for (int b = 0; b < BATCH; ++b) {
+            const int j = j0 + b * kLossWarps * AT_ONCE;
+            at[b] = -1;
+            if (j >= items) continue;
+            const int id = S.hot[run == 1 ? j : j / run], c = id / kLossWorkers * run + (run == 1 ? 0 : j % run);
+            const int piece = (c * kLossPieces + h) * kLossWorkers + id % kLossWorkers;
+            if (c >= chunks || piece >= r.n) continue;
+            at[b] = r.a0 + (r.p0 + piece) * E + i;
+            y[b] = x[at[b]];
+          }
+#pragma unroll
+          for (int b = 0; b < BATCH; ++b)
+            if (at[b] >= 0) {
+              const Key key = top_key(to_f32(y[b]), at[b]);
               if (key >= bound) top.append(key);
             }
-          }
-          again = top.compact() > kTopBuffer;
         }
+        again = top.compact() > kTopBuffer;
       }
       if (again) top_scan<T>(top, x, r, chunks, own, own_at, bound);
       float2 stat = make_float2(0.0f, 0.0f);
@@ -528,32 +572,36 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
         if (P.lse && thread == 0) P.lse[row] = tempered_lse(P.temperature, stat.x, stat.y);
         loss_workers_sync();                               // the buffer may be written again
       } else {
-        // this block's list, 0 where it has fewer than k keys, for rank 0
-        const int n = S.count;
-        const Key key = thread < n && thread < P.k ? S.buffer[thread] : 0;
+        // this block's list for rank 0
+        const int n = min(S.count, P.k);
+        const Key key = thread < n ? S.buffer[thread] : 0;
         cluster_sync();                                    // nobody uses rank 0's buffer any more
         uint32_t list, told;
         asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(list) : "r"(smem_u32(&S.buffer[rank * kTopMost + thread])));
         asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(told) : "r"(smem_u32(&S.told[rank])));
-        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(list), "l"(key) : "memory");
-        if (thread == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(told), "f"(stat.x), "f"(stat.y) : "memory");
+        if (thread < n) asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(list), "l"(key) : "memory");
+        if (thread == 0)
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %3};" ::"r"(told), "f"(stat.x), "f"(stat.y), "f"(__int_as_float(n))
+                       : "memory");
         cluster_sync();
         if (rank == 0) {
-          for (int q = 0; q < P.split; ++q) {
-            const Key k = S.buffer[q * kTopMost + thread];
-            if (k == 0) continue;
-            int above = thread;
-            for (int o = 0; o < P.split; ++o) {
-              if (o == q) continue;
-              int low = 0, high = P.k;                     // sorted, zeros last
-              while (low < high) {
-                const int mid = (low + high) / 2;
-                if (S.buffer[o * kTopMost + mid] > k) low = mid + 1; else high = mid;
-              }
-              above += low;
-            }
-            if (above < P.k) top_write<T>(P, row, above, k);
+          // the lists behind one another, and the k largest of them
+          Key keys[8];
+          int place[8], total = 0;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int n_q = q < P.split ? __float_as_int(S.told[q].z) : 0;
+            keys[q] = thread < n_q ? S.buffer[q * kTopMost + thread] : 0;
+            place[q] = total + thread;
+            total += n_q;
           }
+          loss_workers_sync();
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (keys[q] != 0) S.buffer[place[q]] = keys[q];
+          if (thread == 0) S.count = total;
+          top.compact();
+          if (thread < P.k) top_write<T>(P, row, thread, S.buffer[thread]);
           if (P.lse && thread == 0) {
             float hi = -INFINITY, sum = 0.0f;
             for (int o = 0; o < P.split; ++o) hi = fmaxf(hi, S.told[o].x);
@@ -565,7 +613,8 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
       }
     }
   }
-  if (P.split > 1 && thread >= kLossWorkers) {             // the producer's part in the two exchanges above
+  if (P.split > 1 && thread >= kLossWorkers) {             // the producer's part in the exchanges above
+    cluster_sync();
     cluster_sync();
     cluster_sync();
   }
