@@ -132,16 +132,14 @@ template <bool FAST, int N> __device__ __forceinline__ void slope_all(float (&v)
   }
 }
 
-enum LinearKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kLossStats = 3, kLossGrad = 4 };
+enum LinearKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kLossStats = 3, kLossGrad = 4, kLossWeight = 5, kLossTerm = 6 };
 
 // What happens to a finished sum `acc` of row r, column c of the result.  T: the type of all
 // operands but the weight gradient, which is TO.
 //   forward      z = acc + bias[c]; out1 <- z; out0 <- act(z) + residual
 //   input grad   d = acc + residual; out0 <- d; out1 <- d * act'(z_in)
-//                T bf16, TO fp32: one term of a sum of products, whose last one is rounded: residual and
-//                out0 are fp32, out1 <- d in bf16
-//   weight grad  out0 <- acc (+ out0)
-//   loss stats, loss grad: linear_loss.cuh
+//   weight grad  out0 <- acc (+ out0); loss weight: the same, of other operands
+//   loss stats, loss grad, loss term: linear_loss.cuh
 struct Epilogue {
   const void* bias;
   const void* residual;
@@ -158,7 +156,7 @@ struct Epilogue {
   float* target_logit;       // kLossStats
   void* partial;             // kLossStats: float2 [slots][ld_partial]; kLossGrad: float [strips][ld_partial] or NULL
   long long ld_partial;
-  long long part;            // kLossGrad, fp32: elements from one bf16 part of the output to the next
+  long long part;            // kLossGrad, fp32: elements from one bf16 part of out0 to the next; kLossTerm: from one slice's
   int first_word, words;     // of the vocabulary's piece
 };
 
@@ -233,14 +231,12 @@ __device__ __forceinline__ void store_strip(const float (&v)[N], void* base, lon
 
 // The epilogue of N rows.  ask() requests what the epilogue reads, early; finish() takes the sums.
 template <int KIND, typename T, typename TO, int N> struct Finisher {
-  static constexpr bool TERM = KIND == kInputGrad && sizeof(TO) > sizeof(T);
-  Strip<std::conditional_t<TERM, TO, T>, N> first;   // residual (or dw)
-  Strip<T, N> second;                                 // z_in
+  Strip<T, N> first, second;          // residual (or dw), z_in
 
   template <bool WHOLE>
   __device__ __forceinline__ void ask_(const Epilogue& E, int r, int c, int R, int C, int lane) {
-    if (KIND != kWeightGrad && E.residual) first.template load<WHOLE>(E.residual, E.ld_residual, r, c, R, C, E.pairs, lane);
-    if (KIND == kInputGrad && !TERM && E.out1) second.template load<WHOLE>(E.z_in, E.ld_z_in, r, c, R, C, E.pairs, lane);
+    if ((KIND == kForward || KIND == kInputGrad) && E.residual) first.template load<WHOLE>(E.residual, E.ld_residual, r, c, R, C, E.pairs, lane);
+    if (KIND == kInputGrad && E.out1) second.template load<WHOLE>(E.z_in, E.ld_z_in, r, c, R, C, E.pairs, lane);
   }
   template <bool WHOLE>
   __device__ __forceinline__ void finish_(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
@@ -263,10 +259,8 @@ template <int KIND, typename T, typename TO, int N> struct Finisher {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += x[i];
       }
-      if (E.out0) store_strip<std::conditional_t<TERM, TO, T>, WHOLE>(v, E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);
-      if (TERM) {
-        if (E.out1) store_strip<T, WHOLE>(v, E.out1, E.ld_out1, r, c, R, C, E.pairs, lane);
-      } else if (E.out1) {
+      if (E.out0) store_strip<T, WHOLE>(v, E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);
+      if (E.out1) {
         second.unpack(x, E.pairs, lane);
         slope_all<FAST>(v, x, E.act);
         store_strip<T, WHOLE>(v, E.out1, E.ld_out1, r, c, R, C, E.pairs, lane);

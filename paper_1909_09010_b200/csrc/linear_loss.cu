@@ -22,7 +22,6 @@
 #include "linear_loss.cuh"
 #include "linear_tc.cuh"
 #include "linear_tc_host.h"
-#include "ready_product.h"
 
 namespace {
 
@@ -63,12 +62,33 @@ int rows_at_once(int tiles, int fit) {
   while (fit / t * t * 10 < fit * 9) --t;
   return t;
 }
+// The sum over a piece's words (dx): tiles as any product's, and the words cut into slices where tiles are few.
+// Times per step as in choose_shape.
+struct TermShape { int bn, pair, slices; double ns; };
+TermShape choose_term(const gbmuf_ops* ops, long long rows, long long cols, long long words, int parts) {
+  TermShape best{64, 1, 1, 1e300};
+  const long long ksteps = (words + 63) / 64;
+  for (int pair = 1; pair <= 2; ++pair)
+    for (int bn = pair == 2 ? 128 : 64; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2) {
+      const long long tiles = ((cols + 128 * pair - 1) / (128 * pair)) * ((rows + bn - 1) / bn), fit = ops->num_sms / pair;
+      const double step = std::max(100.0, parts * tc_stage_bytes(bn, pair) / 126.0);
+      for (int w = 1; w <= 3; ++w) {                       // as many as fill w waves
+        const long long n = std::max<long long>(1, std::min(ksteps / 4, w * fit / tiles));
+        const long long waves = (tiles * n + fit - 1) / fit;
+        const double t = waves * (1000.0 + (double)((ksteps + n - 1) / n) * step) + 15.0 * bn + 4.0 * n * rows * cols / 4000.0;
+        if (t < best.ns) best = {bn, pair, (int)n, t};
+      }
+    }
+  return best;
+}
+
 struct Plan {
   int parts;                                      // bf16 parts of an operand
   bool grad, x_ready, w_ready;                    // ready: read in place
   bool bias_once;
   long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
+  TermShape term;
   long long x_off, w_off, target_off, slot_off, pair_off, word_off, weight_off, d_off, partial_off, acc_off, bytes;
 };
 
@@ -88,11 +108,18 @@ int stats_slots(const gbmuf_ops* ops, const TcShape& s, int tiles_c, long long w
   return (int)std::min<long long>(ops->num_sms / s.pair / tiles_c, (words + s.bn - 1) / s.bn) * (kTcFinishers / 4);
 }
 
+// The product of a piece's gradient with x.  Pairs pay here with a strided operand too (bf16, 14,336 words, 2,048 x
+// 1,024: 48.9 us with pairs, 55.1 without).
+TcShape weight_shape(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
+  Product q{};
+  q.R = words; q.C = a->n_in; q.K = a->rows; q.dtype = a->dtype;
+  return choose_shape(ops, q, p.parts, false, false, false);
+}
 // The time of a piece by the model of the launch shapes, and a little for its launches.
 double piece_time(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
   double ns = choose_shape(ops, logits_product(p, a, false, a->rows, words), p.parts, false, false, false).ns + 5000.0;
-  if (a->dw) ns += ready_shape(ops, a->dtype, true, words, a->n_in, a->rows).ns;
-  if (a->dx) ns += ready_shape(ops, a->dtype, false, a->rows, a->n_in, words).ns;
+  if (a->dw) ns += weight_shape(ops, p, a, words).ns;
+  if (a->dx) ns += choose_term(ops, a->rows, a->n_in, words, p.parts).ns;
   return ns;
 }
 // Words of a piece: what fits kPieceBytes, or a little less where that leaves fewer CTAs without a tile.
@@ -122,7 +149,7 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   p.pieces = (a->vocab + p.piece - 1) / p.piece;
   p.ld_x = p.x_ready && a->rows > 1 ? a->ld_x : round_up(a->n_in, 8);      // the stride of a single row says nothing
   p.ld_w = p.w_ready && a->vocab > 1 ? a->ld_w : round_up(a->n_in, 8);
-  p.ld_d = round_up(p.piece, 8);
+  p.ld_d = round_up(a->rows, 64);                 // whole strips of rows are stored
   p.ld_acc = round_up(a->n_in, 4);
   p.rows_padded = round_up(a->rows, kLossRowPad);
   const long long together = p.w_ready ? a->vocab : p.piece;
@@ -145,7 +172,7 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
     p.pair_off = take(p.rows_padded / 2 * (long long)sizeof(RowPair));
     p.word_off = take(p.rows_padded * 4);
     p.weight_off = take(p.rows_padded * 4);
-    p.d_off = take(a->rows * p.ld_d * 2 * p.parts);
+    p.d_off = take(p.piece * p.ld_d * 2 * p.parts);
     if (a->dbias) {
       // the strips' sums of all words, added up once at the end, unless that takes too much room
       p.strips = (a->rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
@@ -153,7 +180,10 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
       p.ld_partial = p.bias_once ? a->vocab : p.piece;
       p.partial_off = take(p.strips * p.ld_partial * 4);
     }
-    p.acc_off = take(a->dx && p.pieces > 1 && a->dtype == GBMUF_BF16 ? a->rows * p.ld_acc * 4 : 0);
+    if (a->dx) {
+      p.term = choose_term(ops, a->rows, a->n_in, p.piece, p.parts);
+      p.acc_off = take(p.term.slices * a->rows * p.ld_acc * 4);
+    }
   }
   p.bytes = at;
   return p;
@@ -175,6 +205,24 @@ gbmuf_status launch_logits(const gbmuf_ops* ops, const TcShape& s, TcParams& P, 
     if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 1>(ops, P, at_once, ma, mb, st);
   return s.bn == 64 ? launch_tc_at<KIND, T, T, PARTS, 64, 1>(ops, P, at_once, ma, mb, st)
                     : launch_tc_at<KIND, T, T, PARTS, 128, 1>(ops, P, at_once, ma, mb, st);
+}
+
+// The two products with the gradient of a piece's logits.
+template <int KIND, typename T, typename TO, int PARTS>
+gbmuf_status launch_loss_product(const gbmuf_ops* ops, int bn, int pair, TcParams& P, int at_once, const Operand& a, const Operand& b,
+                                 int32_t dtype, cudaStream_t st) {
+  CUtensorMap ma{}, mb{};
+  if (gbmuf_status rc = operand_map(a, dtype, nullptr, 64, &ma)) return rc;
+  if (gbmuf_status rc = operand_map(b, dtype, nullptr, b.k_inner ? bn / pair : 64, &mb)) return rc;
+  if (pair == 2)
+    return bn == 128 ? launch_tc_at<KIND, T, TO, PARTS, 128, 2>(ops, P, at_once, ma, mb, st)
+                     : launch_tc_at<KIND, T, TO, PARTS, 256, 2>(ops, P, at_once, ma, mb, st);
+  if constexpr (KIND == kLossWeight)
+    if (bn == 32) return launch_tc_at<KIND, T, TO, PARTS, 32, 1>(ops, P, at_once, ma, mb, st);
+  if constexpr (PARTS == 1)
+    if (bn == 256) return launch_tc_at<KIND, T, TO, PARTS, 256, 1>(ops, P, at_once, ma, mb, st);
+  return bn == 64 ? launch_tc_at<KIND, T, TO, PARTS, 64, 1>(ops, P, at_once, ma, mb, st)
+                  : launch_tc_at<KIND, T, TO, PARTS, 128, 1>(ops, P, at_once, ma, mb, st);
 }
 
 gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, cudaStream_t st) {
@@ -298,8 +346,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     Operand w;
     if (gbmuf_status rc = weights(v0, words, w)) return rc;
     void* const d = ws + p.d_off;
-    // an even number of columns, so that bf16 goes out two at a time: the last one may lie beyond the piece
-    TcParams P = tc_params(p.tc, N, round_up(words, 2), false);
+    TcParams P = tc_params(p.tc, N, words, false);
     P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
     P.E.loss_rows = ws + p.pair_off;
     P.E.loss_targets = reinterpret_cast<const int*>(ws + p.word_off);
@@ -307,7 +354,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     P.E.partial = a->dbias ? reinterpret_cast<float*>(ws + p.partial_off) + (p.bias_once ? v0 : 0) : nullptr;
     P.E.ld_partial = p.ld_partial;
     P.E.first_word = (int)v0; P.E.words = (int)words;
-    P.E.out0 = d; P.E.ld_out0 = p.ld_d; P.E.part = N * p.ld_d; P.E.pairs = 1;
+    P.E.out0 = d; P.E.ld_out0 = p.ld_d; P.E.part = words * p.ld_d;
     const int at_once = std::min(P.tiles, ops->num_sms / p.tc.pair);
     if (gbmuf_status rc = launch_logits<kLossGrad, T, PARTS>(ops, p.tc, P, at_once, w, x, a->dtype, st)) return rc;
     if (a->dbias && (!p.bias_once || last)) {
@@ -319,31 +366,41 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       if (e != cudaSuccess) return cuda_refuse("launch of the loss's bias-gradient kernel", e);
     }
     if (H == 0) continue;
-    gbmuf_ready_product r{};
-    r.dtype = a->dtype;
-    r.b = d; r.b_outer = N; r.b_inner = words; r.b_ld = p.ld_d;
+    // dw = d^T x: columns along the lanes, d's rows next to one another
+    Operand xw = x, dw_b{d, words, N, p.ld_d, true, true, 0}, dx_b{d, words, N, p.ld_d, false, true, 0};
+    xw.k_inner = false;
     if (a->dw) {
-      r.weight_grad = true; r.out_dtype = a->grad_dtype; r.accumulate = a->accumulate;
-      r.a = x.p; r.a_outer = N; r.a_inner = H; r.a_ld = x.ld;
-      r.rows = words; r.cols = H; r.terms = N;
-      r.out = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); r.ld_out = a->ld_dw;
-      if (gbmuf_status rc = gbmuf_run_ready_product(ops, r, st)) return rc;
+      const TcShape shape = weight_shape(ops, p, a, words);
+      TcParams W = tc_params(shape, words, H, false);
+      W.ksteps = (int)((N + kTcK - 1) / kTcK);
+      W.E.out0 = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); W.E.ld_out0 = a->ld_dw;
+      W.E.accumulate = a->accumulate;
+      W.E.pairs = a->grad_dtype == GBMUF_BF16 && (uintptr_t)W.E.out0 % 4 == 0 && H % 2 == 0 && (words == 1 || a->ld_dw % 2 == 0);
+      gbmuf_status rc = GBMUF_OK;
+      DISPATCH_DTYPE(a->grad_dtype, TO, (rc = launch_loss_product<kLossWeight, TO, TO, PARTS>(
+          ops, shape.bn, shape.pair, W, std::min(W.tiles, ops->num_sms / shape.pair), xw, dw_b, a->dtype, st)));
+      if (rc != GBMUF_OK) return rc;
     }
     if (a->dx) {
-      r.weight_grad = false; r.accumulate = 0;
-      r.a = w.p; r.a_outer = words; r.a_inner = H; r.a_ld = w.ld;
-      r.rows = N; r.cols = H; r.terms = words;
-      if (PARTS == 1 && p.pieces > 1) {
-        r.out_dtype = GBMUF_F32;
-        r.residual = i > 0 ? ws + p.acc_off : nullptr; r.ld_residual = p.ld_acc;
-        r.out = last ? nullptr : ws + p.acc_off; r.ld_out = p.ld_acc;
-        r.rounded = last ? a->dx : nullptr; r.ld_rounded = a->ld_dx;
-      } else {
-        r.out_dtype = a->dtype;
-        r.residual = i > 0 ? a->dx : nullptr; r.ld_residual = a->ld_dx;
-        r.out = a->dx; r.ld_out = a->ld_dx; r.rounded = nullptr;
+      // dx += d w, in fp32
+      Operand wk = w;
+      wk.k_inner = false;
+      TcShape shape{p.term.bn, 1, p.term.pair, 0.0};
+      TcParams D = tc_params(shape, N, H, false);
+      D.ksteps = (int)((words + kTcK - 1) / kTcK);
+      D.slices = p.term.slices;
+      D.tiles_c = D.tiles / D.tiles_fast;
+      D.tiles *= D.slices;
+      D.E.out0 = ws + p.acc_off; D.E.ld_out0 = p.ld_acc; D.E.part = N * p.ld_acc; D.E.accumulate = i > 0;
+      if (gbmuf_status rc = launch_loss_product<kLossTerm, T, float, PARTS>(ops, shape.bn, shape.pair, D, std::min(D.tiles, ops->num_sms / shape.pair),
+                                                                            wk, dx_b, a->dtype, st))
+        return rc;
+      if (last) {
+        const cudaError_t e = launch(loss_dx_kernel<T>, (unsigned)std::min<long long>(N, ops->num_sms * 8), 1, 256, 0, st,
+                                     reinterpret_cast<const float*>(ws + p.acc_off), p.ld_acc, N * p.ld_acc, p.term.slices,
+                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H);
+        if (e != cudaSuccess) return cuda_refuse("launch of the loss's input-gradient kernel", e);
       }
-      if (gbmuf_status rc = gbmuf_run_ready_product(ops, r, st)) return rc;
     }
   }
   return GBMUF_OK;

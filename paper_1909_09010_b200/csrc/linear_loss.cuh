@@ -92,12 +92,29 @@ template <typename T, bool PROMOTE> struct RowStats {
   }
 };
 
+// 8 bf16 a register quad; a strip's rows follow one another in memory.
+template <int N> __device__ __forceinline__ void store_rows(__nv_bfloat16* to, const float (&v)[N]) {
+  uint32_t u[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) u[i] = pair_bf16(two(v[2 * i], v[2 * i + 1]));
+#pragma unroll
+  for (int i = 0; i < N / 2; i += 8) {
+    if constexpr (N >= 16)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 2 * i), "r"(u[i]), "r"(u[i + 1]), "r"(u[i + 2]),
+                   "r"(u[i + 3]), "r"(u[i + 4]), "r"(u[i + 5]), "r"(u[i + 6]), "r"(u[i + 7])
+                   : "memory");
+    else
+      *reinterpret_cast<uint4*>(to) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+}
+
+// d is stored with the rows of the batch along memory ([words][rows]): a lane holds a word and stores a strip of
+// its rows in one piece.
 template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
   float column;              // sum over the strip's rows
 
   __device__ __forceinline__ void ask(const Epilogue&, int, int, int, int, int) {}
-  template <bool WHOLE>
-  __device__ __forceinline__ void finish_(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
+  __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int, int lane, float bias, float (&v)[N]) {
     constexpr bool FAST = sizeof(T) == 2;
     const ulonglong2* const rows = static_cast<const ulonglong2*>(E.loss_rows) + r / 2;
     const int t = lane < N ? E.loss_targets[r + lane] : -1;
@@ -133,10 +150,11 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
         column += v[i];
       }
     }
+    if (c >= E.words || r >= R) return;                    // a strip that holds a row at all is stored whole
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(E.out0) + (long long)c * E.ld_out0 + r;
     if constexpr (FAST) {
-      store_strip<T, WHOLE>(v, E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);
+      store_rows(out, v);
     } else {
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(E.out0);
       float part[N];
 #pragma unroll
       for (int q = 0; q < 3; ++q, out += E.part) {
@@ -145,15 +163,50 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
           part[i] = __bfloat162float(__float2bfloat16_rn(v[i]));
           v[i] -= part[i];
         }
-        store_strip<__nv_bfloat16, WHOLE>(part, out, E.ld_out0, r, c, R, C, E.pairs, lane);
+        store_rows(out, part);
       }
     }
   }
-  __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int C, int lane, float bias, float (&v)[N]) {
-    if (r + N <= R && c - lane + 32 <= C) finish_<true>(E, r, c, R, C, lane, bias, v);
-    else finish_<false>(E, r, c, R, C, lane, bias, v);
+};
+
+// A term of dx: the sum over one piece's words, or over one of `slices` parts of them (each sums into an array of its
+// own, so that a result of few tiles keeps all SMs busy; the arrays are added up at the end).  bf16 operands:
+// within a piece the sum stays in the accumulator, a few thousand words at most.
+template <typename T, typename TO, int N> struct Finisher<kLossTerm, T, TO, N> {
+  Strip<TO, N> old;
+  int slice;
+
+  __device__ __forceinline__ TO* base(const Epilogue& E) const { return static_cast<TO*>(E.out0) + slice * E.part; }
+  __device__ __forceinline__ void ask(const Epilogue& E, int r, int c, int R, int C, int lane) {
+    if (!E.accumulate) return;
+    if (r + N <= R && c - lane + 32 <= C) old.template load<true>(base(E), E.ld_out0, r, c, R, C, false, lane);
+    else old.template load<false>(base(E), E.ld_out0, r, c, R, C, false, lane);
+  }
+  __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int C, int lane, float, float (&v)[N]) {
+    if (E.accumulate) {
+      float x[N];
+      old.unpack(x, false, lane);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += x[i];
+    }
+    if (r + N <= R && c - lane + 32 <= C) store_strip<TO, true>(v, base(E), E.ld_out0, r, c, R, C, false, lane);
+    else store_strip<TO, false>(v, base(E), E.ld_out0, r, c, R, C, false, lane);
   }
 };
+template <typename T>
+__global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long long ld, long long slice, int slices, T* dx, long long ld_dx,
+                                                      long long rows, int cols) {
+  grid_launch_dependents();
+  grid_dependency_wait();
+  for (long long row = blockIdx.x; row < rows; row += gridDim.x)
+    for (int c = threadIdx.x; c < cols; c += 256) {
+      const float* p = terms + row * ld + c;
+      float s = *p;
+#pragma unroll 4
+      for (int i = 1; i < slices; ++i) s += p[i * slice];
+      dx[row * ld_dx + c] = from_f32<T>(s);
+    }
+}
 
 // Joins the statistics of a row's slots, in their order: loss, lse, and what kLossGrad needs (rows past the
 // last get a zero gradient).  32 rows by 16 shares of the slots per block.

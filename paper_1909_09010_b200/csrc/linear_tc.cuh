@@ -42,6 +42,8 @@ struct TcParams {
   int tiles_fast, tiles; // row tiles (kLossStats: column tiles), which run fastest; all tiles
   int tile_step, step_slow, step_fast;   // from a CTA's tile to its next: tiles, and as tiles of either kind
   int split;             // CTAs of a cluster that share a tile's steps (1: none)
+  int tiles_c;           // kLossTerm: column tiles; the tiles of a slice of the steps follow those of the one before
+  int slices;
   int stages;
 };
 
@@ -123,8 +125,17 @@ __device__ __forceinline__ void arrive_remote(uint32_t bar) {
 }
 // N accumulator columns of this warp's 32 lanes.
 template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[N]) {
-  static_assert(N == 8 || N == 16, "");
+  static_assert(N == 8 || N == 16 || N == 32, "");
   uint32_t u[N];
+  if constexpr (N == 32)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+          "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]),
+          "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]),
+          "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+        : "r"(addr));
   if constexpr (N == 16)
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -151,12 +162,14 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
-  constexpr bool A_K = KIND != kInputGrad && KIND != kWeightGrad, B_K = KIND != kWeightGrad, PROMOTE = sizeof(TO) == 4;
+  constexpr bool A_K = KIND == kForward || KIND == kLossStats || KIND == kLossGrad, B_K = KIND != kWeightGrad && KIND != kLossTerm;
+  constexpr bool PROMOTE = sizeof(TO) == 4 && !(KIND == kLossTerm && PARTS == 1);
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
-  constexpr int N = KIND == kLossGrad && PROMOTE ? 8 : NCOL < 16 ? NCOL : 16;        // of them at a time (16 would spill)
+  constexpr int MOST = (KIND == kLossStats || KIND == kLossGrad) && !PROMOTE ? 32 : KIND == kLossGrad ? 8 : 16;
+  constexpr int N = NCOL < MOST ? NCOL : MOST;    // of them at a time
   extern __shared__ __align__(128) unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
   const uint32_t bars = smem_u32(smem), ring = bars + kTcHead;
@@ -202,10 +215,25 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int side = PAIR == 2 ? (int)(blockIdx.x & 1) : 0;                        // of the pair that shares the tile
   const int step0 = P.split > 1 ? (int)((unsigned)P.ksteps * (unsigned)rank / (unsigned)P.split) : 0;
   const int step1 = P.split > 1 ? (int)((unsigned)P.ksteps * (unsigned)(rank + 1) / (unsigned)P.split) : P.ksteps;
-  const int iters = step1 - step0;
-  // without PROMOTE a tile is one chunk
-  const int chunk = PROMOTE ? (PARTS == 1 ? 4 : 1) : (iters > 0 ? iters : 1);
-  const int chunks = iters == 0 ? 0 : (iters + chunk - 1) / chunk;
+  // what of a tile there is to do: its column tile, its steps, and these in chunks (without PROMOTE a tile is one)
+  struct Share {
+    int c, slice, step0, iters, chunks;
+  };
+  constexpr int chunk = PROMOTE ? (PARTS == 1 ? 4 : 1) : 0x7fffffff;
+  auto chunks_of = [](int iters) { return PROMOTE ? (iters + chunk - 1) / chunk : iters > 0 ? 1 : 0; };
+  const Share whole{0, 0, step0, step1 - step0, chunks_of(step1 - step0)};
+  auto share = [&](int c) {
+    Share s = whole;
+    s.c = c;
+    if (KIND == kLossTerm) {
+      s.slice = c / P.tiles_c;
+      s.c = c - s.slice * P.tiles_c;
+      s.step0 = (int)((long long)P.ksteps * s.slice / P.slices);
+      s.iters = (int)((long long)P.ksteps * (s.slice + 1) / P.slices) - s.step0;
+      s.chunks = chunks_of(s.iters);
+    }
+    return s;
+  };
   const int first_tile = P.split > 1 ? (int)(blockIdx.x / (unsigned)P.split) : (int)(blockIdx.x / PAIR);
   struct Walk {                                                    // tile number, column tile, row tile
     int tile, c, r;
@@ -236,9 +264,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     uint32_t ph = 0;
     bool ok = true;
     for (Walk w = first(); w.tile < P.tiles; next(w)) {
-      const int c0 = w.c * TILE_C + side * 128, r0 = w.r * BN + side * OWN_R;
-      for (int it = 0; it < iters; ++it) {
-        const int k0 = (step0 + it) * kTcK;
+      const Share mine = share(w.c);
+      const int c0 = mine.c * TILE_C + side * 128, r0 = w.r * BN + side * OWN_R;
+      for (int it = 0; it < mine.iters; ++it) {
+        const int k0 = (mine.step0 + it) * kTcK;
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) {                          // parts in the order of their use: hi, lo, mid
           const int part = q == 0 ? 0 : 3 - q;
@@ -280,6 +309,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     };
     for (int tile = first_tile; tile < P.tiles; tile += P.tile_step) {
       int in_chunk = 0;
+      const int iters = KIND == kLossTerm ? share(tile / P.tiles_fast).iters : whole.iters;
       for (int it = 0; it < iters; ++it) {
         const uint32_t d = tmem + (uint32_t)(n & 1) * ACC;
         const bool last = in_chunk + 1 == chunk || it == iters - 1;
@@ -345,6 +375,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       int n = 0;
       bool ok = true;
       RowStats<T, PROMOTE> S;
+      const int chunks = whole.chunks;
       for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
         S.open(P.E, w.c * TILE_C + side * 128 + quad * 32 + lane, P.C, w.r * (kTcFinishers / 4) + part);
         const int r0 = w.r * BN + part * NCOL;
@@ -404,7 +435,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     int n = 0;
     bool ok = true;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
-      const int c = w.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL;
+      const Share mine = share(w.c);
+      const int c = mine.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL, chunks = mine.chunks;
       const T bias = bias_of(c);
       float column = 0.0f;                                         // kLossGrad: of the gradients of column c
       if (PROMOTE) {
@@ -431,6 +463,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
         for (int j = 0; j < NCOL; j += N) {
           Finisher<KIND, T, TO, N> F;
+          if constexpr (KIND == kLossTerm) F.slice = mine.slice;
           float v[N];
 #pragma unroll
           for (int i = 0; i < N; ++i) v[i] = acc[j + i];
@@ -441,6 +474,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       } else {
         // what the epilogue reads is requested one strip ahead, the first one during the sums
         Finisher<KIND, T, TO, N> F;
+        if constexpr (KIND == kLossTerm) F.slice = mine.slice;
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
           ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
@@ -468,7 +502,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         static_cast<float*>(P.E.partial)[(w.r * (kTcFinishers / 4) + part) * P.E.ld_partial + c] = column;
     }
   }
-  if constexpr (KIND != kLossStats && KIND != kLossGrad && PAIR == 1) if (P.split > 1) {
+  if constexpr (KIND < kLossStats && PAIR == 1) if (P.split > 1) {
+    const int chunks = whole.chunks;
     // The cluster's CTAs hold partial sums of one tile.  CTA j finishes accumulator columns
     // [j, j + 1) BN / split: everybody writes its sums of those columns into CTA j's shared memory
     // (the operand ring, idle by then) and CTA j adds them in the order of the ranks.

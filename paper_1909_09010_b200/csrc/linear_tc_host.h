@@ -99,15 +99,6 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
   return best;
 }
 
-// The shape of a product of a piece of the vocabulary (ready_product.h), whose sums are 1,000 terms and more.  There
-// pairs pay with a strided first operand too (bf16, pieces of 14,336 words, 2,048 x 1,024: weight gradient 48.9 us
-// with pairs, 55.1 without; input gradient 48.1 and 57.3).
-TcShape ready_shape(const gbmuf_ops* ops, int32_t dtype, bool weight_grad, long long rows, long long cols, long long terms) {
-  Product q{};
-  q.R = rows; q.C = cols; q.K = terms; q.dtype = dtype;
-  return choose_shape(ops, q, dtype == GBMUF_F32 ? 3 : 1, weight_grad, false);
-}
-
 // at_once: tiles that are worked on side by side.
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 gbmuf_status launch_tc_at(const gbmuf_ops* ops, TcParams& P, int at_once, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {

@@ -43,7 +43,6 @@
 #include "cross_entropy.cuh"
 #include "grad_clip.cuh"
 #include "linear_tc_host.h"
-#include "ready_product.h"
 
 struct gbmuf_clip {
   int device = 0, groups = 0, num_sms = 0;
@@ -73,8 +72,7 @@ gbmuf_status check_sizes(const gbmuf_ops* ops, int64_t rows, int64_t n_in, int64
 
 // Runs a product: operands that cannot be read in place are packed into the workspace first.
 template <int KIND, typename T, typename TO, int PARTS>
-gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64_t workspace_bytes, cudaStream_t st,
-                         const TcShape* given = nullptr) {
+gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64_t workspace_bytes, cudaStream_t st) {
   const long long need = product_workspace(q);
   if (need > workspace_bytes || (need > 0 && (!workspace || (uintptr_t)workspace % 256 != 0)))
     return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
@@ -82,7 +80,7 @@ gbmuf_status run_product(const gbmuf_ops* ops, Product q, void* workspace, int64
   TcParams P{};
   P.E = q.E; P.status = ops->d_status; P.R = (int)q.R; P.C = (int)q.C;
   P.ksteps = (int)((q.K + kTcK - 1) / kTcK);
-  const TcShape shape = given ? *given : choose_shape(ops, q, PARTS, KIND == kWeightGrad, KIND != kForward);
+  const TcShape shape = choose_shape(ops, q, PARTS, KIND == kWeightGrad, KIND != kForward);
   P.split = shape.split;
   P.tiles_fast = (int)((q.R + shape.bn - 1) / shape.bn);
   const long long tiles = (long long)P.tiles_fast * ((q.C + 128 * shape.pair - 1) / (128 * shape.pair));
@@ -210,17 +208,6 @@ Product weight_grad_product(const gbmuf_linear_backward_weight_args* a) {
   return q;
 }
 
-// The operands' sides of a ready product: see ready_product.h.
-Product of_ready(const gbmuf_ready_product& r) {
-  Product q{};
-  q.a = {r.a, r.a_outer, r.a_inner, r.a_ld, false, true, 0};
-  q.b = {r.b, r.b_outer, r.b_inner, r.b_ld, !r.weight_grad, true, 0};
-  q.R = r.rows; q.C = r.cols; q.K = r.terms; q.dtype = r.dtype;
-  q.E.residual = r.residual; q.E.ld_residual = r.ld_residual; q.E.out0 = r.out; q.E.ld_out0 = r.ld_out;
-  q.E.out1 = r.rounded; q.E.ld_out1 = r.ld_rounded; q.E.accumulate = r.accumulate;
-  return q;
-}
-
 template <typename T, typename TO>
 cudaError_t column_sum(const gbmuf_linear_backward_weight_args* a, cudaStream_t st) {
   const bool vec = (uintptr_t)a->dz % 16 == 0 && a->n_out % (16 / sizeof(T)) == 0 &&
@@ -274,19 +261,6 @@ gbmuf_status read_status(int device, int32_t* word, void* stream, int32_t* out) 
 }
 
 }  // namespace
-
-gbmuf_status gbmuf_run_ready_product(const gbmuf_ops* ops, const gbmuf_ready_product& r, void* stream) {
-  const Product q = of_ready(r);
-  cudaStream_t st = (cudaStream_t)stream;
-  const TcShape shape = ready_shape(ops, r.dtype, r.weight_grad, r.rows, r.cols, r.terms);
-  if (r.weight_grad) {
-    DISPATCH_DTYPE(r.dtype, T, DISPATCH_DTYPE(r.out_dtype, TO,
-        return (run_product<kWeightGrad, TO, TO, (sizeof(T) == 4 ? 3 : 1)>(ops, q, nullptr, 0, st, &shape))));
-  }
-  if (r.dtype == GBMUF_F32) return run_product<kInputGrad, float, float, 3>(ops, q, nullptr, 0, st, &shape);
-  if (r.out_dtype == GBMUF_BF16) return run_product<kInputGrad, __nv_bfloat16, __nv_bfloat16, 1>(ops, q, nullptr, 0, st, &shape);
-  return run_product<kInputGrad, __nv_bfloat16, float, 1>(ops, q, nullptr, 0, st, &shape);
-}
 
 extern "C" {
 
