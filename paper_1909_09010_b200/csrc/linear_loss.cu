@@ -189,22 +189,35 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   return p;
 }
 
+// Tensor map of a piece's gradient [words][rows], for stores of 32 rows by 32 words.
+gbmuf_status gradient_map(const TcParams& P, CUtensorMap* map) {
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return refuse(GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
+  const cuuint64_t dim[2] = {(cuuint64_t)P.R, (cuuint64_t)P.E.words}, stride[1] = {(cuuint64_t)P.E.ld_out0 * 2};
+  const cuuint32_t box[2] = {32, 32}, one[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P.E.out0, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return refuse(GBMUF_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
+  return GBMUF_OK;
+}
 template <int KIND, typename T, int PARTS>
 gbmuf_status launch_logits(const gbmuf_ops* ops, const TcShape& s, TcParams& P, int at_once, const Operand& a, const Operand& b,
                            int32_t dtype, cudaStream_t st) {
-  CUtensorMap ma{}, mb{};
+  CUtensorMap ma{}, mb{}, out{};
+  if (KIND == kLossGrad && PARTS == 1)
+    if (gbmuf_status rc = gradient_map(P, &out)) return rc;
   if (P.ksteps > 0) {
     if (gbmuf_status rc = operand_map(a, dtype, nullptr, 128, &ma)) return rc;
     if (gbmuf_status rc = operand_map(b, dtype, nullptr, s.bn / s.pair, &mb)) return rc;
   }
   if (s.pair == 2)
-    return s.bn == 128 ? launch_tc_at<KIND, T, T, PARTS, 128, 2>(ops, P, at_once, ma, mb, st)
-                       : launch_tc_at<KIND, T, T, PARTS, 256, 2>(ops, P, at_once, ma, mb, st);
-  if (s.bn == 32) return launch_tc_at<KIND, T, T, PARTS, 32, 1>(ops, P, at_once, ma, mb, st);
+    return s.bn == 128 ? launch_tc_at<KIND, T, T, PARTS, 128, 2>(ops, P, at_once, ma, mb, st, out)
+                       : launch_tc_at<KIND, T, T, PARTS, 256, 2>(ops, P, at_once, ma, mb, st, out);
+  if (s.bn == 32) return launch_tc_at<KIND, T, T, PARTS, 32, 1>(ops, P, at_once, ma, mb, st, out);
   if constexpr (PARTS == 1)
-    if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 1>(ops, P, at_once, ma, mb, st);
-  return s.bn == 64 ? launch_tc_at<KIND, T, T, PARTS, 64, 1>(ops, P, at_once, ma, mb, st)
-                    : launch_tc_at<KIND, T, T, PARTS, 128, 1>(ops, P, at_once, ma, mb, st);
+    if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 1>(ops, P, at_once, ma, mb, st, out);
+  return s.bn == 64 ? launch_tc_at<KIND, T, T, PARTS, 64, 1>(ops, P, at_once, ma, mb, st, out)
+                    : launch_tc_at<KIND, T, T, PARTS, 128, 1>(ops, P, at_once, ma, mb, st, out);
 }
 
 // The two products with the gradient of a piece's logits.

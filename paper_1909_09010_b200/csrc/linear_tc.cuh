@@ -51,6 +51,8 @@ struct TcParams {
 // of B's.  A stage of the ring holds 64 k of one part of both.
 __host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
+// Behind the ring: where the finishing warps lay results out for the copy engine (linear_loss.cuh), 4 KB each.
+template <int KIND, int PARTS, int BN> constexpr uint32_t kTcOut = KIND == kLossGrad && PARTS == 1 && BN >= 128 ? 4096u * kTcFinishers : 0u;
 __host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
   return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
 }
@@ -161,7 +163,8 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 // (2/3) k / 16 x 2^-23 of the result, 1.3e-3 at k = 267,735, about what the rounding to bf16 costs.
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
-    linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TcParams P) {
+    linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                     const TcParams P) {
   constexpr bool A_K = KIND == kForward || KIND == kLossStats || KIND == kLossGrad, B_K = KIND != kWeightGrad && KIND != kLossTerm;
   constexpr bool PROMOTE = sizeof(TO) == 4 && !(KIND == kLossTerm && PARTS == 1);
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
@@ -434,6 +437,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (KIND != kLossStats && warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
+    const uint32_t out_base = ring + (uint32_t)S * STAGE + 4096u * (uint32_t)(warp - 4);
+    uint32_t out_half = 0;                                         // of the two, in turn
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const Share mine = share(w.c);
       const int c = mine.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL, chunks = mine.chunks;
@@ -475,6 +480,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         // what the epilogue reads is requested one strip ahead, the first one during the sums
         Finisher<KIND, T, TO, N> F;
         if constexpr (KIND == kLossTerm) F.slice = mine.slice;
+        if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_base + out_half; }
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
           ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
@@ -488,6 +494,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
           Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
+          if constexpr (kTcOut<KIND, PARTS, BN> > 0) out_half ^= 2048u, F.room = out_base + out_half;
           now.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
           if constexpr (KIND == kLossGrad) column += now.column;
         }
@@ -501,6 +508,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (KIND == kLossGrad && P.E.partial && c < P.E.words)
         static_cast<float*>(P.E.partial)[(w.r * (kTcFinishers / 4) + part) * P.E.ld_partial + c] = column;
     }
+    if (kTcOut<KIND, PARTS, BN> > 0 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   if constexpr (KIND < kLossStats && PAIR == 1) if (P.split > 1) {
     const int chunks = whole.chunks;

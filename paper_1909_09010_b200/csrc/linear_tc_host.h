@@ -101,10 +101,12 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
 
 // at_once: tiles that are worked on side by side.
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
-gbmuf_status launch_tc_at(const gbmuf_ops* ops, TcParams& P, int at_once, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
+gbmuf_status launch_tc_at(const gbmuf_ops* ops, TcParams& P, int at_once, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st,
+                          const CUtensorMap& out = CUtensorMap{}) {
   const auto kernel = linear_tc_kernel<KIND, T, TO, PARTS, BN, PAIR>;
-  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)kTcHead) / (int)tc_stage_bytes(BN, PAIR));
-  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages);
+  constexpr uint32_t OUT = kTcOut<KIND, PARTS, BN>;
+  P.stages = std::min<int>(kTcMaxStages, (ops->max_smem - 1024 - (int)(kTcHead + OUT)) / (int)tc_stage_bytes(BN, PAIR));
+  const uint32_t smem = tc_smem_bytes(BN, PAIR, P.stages) + OUT;
   static std::atomic<uint64_t> ready{0};                  // devices on which the limit has been raised
   const uint64_t bit = 1ull << (ops->device & 63);
   if (!(ready.load() & bit)) {
@@ -114,7 +116,7 @@ gbmuf_status launch_tc_at(const gbmuf_ops* ops, TcParams& P, int at_once, const 
   }
   P.tile_step = at_once; P.step_slow = at_once / P.tiles_fast; P.step_fast = at_once % P.tiles_fast;
   const unsigned grid = (unsigned)(at_once * PAIR * P.split);
-  return launched("launch of the linear-layer kernel", launch(kernel, grid, (unsigned)(PAIR * P.split), kTcThreads, smem, st, ma, mb, P));
+  return launched("launch of the linear-layer kernel", launch(kernel, grid, (unsigned)(PAIR * P.split), kTcThreads, smem, st, ma, mb, out, P));
 }
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
 gbmuf_status launch_tc(const gbmuf_ops* ops, TcParams& P, const CUtensorMap& ma, const CUtensorMap& mb, cudaStream_t st) {
