@@ -21,15 +21,17 @@
 #include "softmax_math.cuh"
 #include "linear_loss.cuh"
 #include "linear_tc.cuh"
+#include "linear_rows.cuh"
 #include "linear_tc_host.h"
 
 namespace {
 
 typedef gbmuf_linear_cross_entropy_args Args;
 
-// The gradient of a piece's logits is written once and read twice, by the two products; it should still
-// be in the L2 cache then (126 MB, next to the piece's weights and their gradient).
-constexpr long long kPieceBytes = 64ll << 20;
+// The gradient of a piece's logits is written once and read twice, by the two products.  Smaller pieces would stay
+// in the L2 cache, but every piece costs three launches and their last waves (2,048 x 1,024 x 100,000: pieces of 9,472
+// words 1,543 us, 18,944 1,494, 56,832 1,533; 1,024 x 512 x 267,735: 9,472 1,454, 28,416 1,286, 56,832 1,254).
+constexpr long long kPieceBytes = 128ll << 20;
 constexpr long long kPieceLeast = 2048;           // words: fewer leave the products too short
 
 gbmuf_status check(const gbmuf_ops* ops, const Args* a) {
@@ -85,7 +87,8 @@ TermShape choose_term(const gbmuf_ops* ops, long long rows, long long cols, long
 struct Plan {
   int parts;                                      // bf16 parts of an operand
   bool grad, x_ready, w_ready;                    // ready: read in place
-  bool bias_once;
+  bool bias_once, few;                            // few: the statistics of a few rows, on the fp32 units
+  int few_blocks;
   long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
   TermShape term;
@@ -143,9 +146,13 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   Plan p{};
   p.parts = a->dtype == GBMUF_F32 ? 3 : 1;
   p.grad = a->dx || a->dw || a->dbias;
+  // as the linear layer's rule for a few rows
+  const int64_t most = a->dtype == GBMUF_F32 ? 16 : 8, rounded = a->rows <= 1 ? 1 : a->rows <= 2 ? 2 : a->rows <= 4 ? 4 : a->rows <= 8 ? 8 : 16;
+  p.few = a->rows <= most && rounded * ((a->n_in + 7) / 8 * 8) * (int64_t)size_of(a->dtype) <= kRowsMostBytes;
   p.x_ready = in_place(operand_x(a), a->dtype);
   p.w_ready = in_place(operand_w(a, 0, a->vocab), a->dtype);
-  p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : p.grad || !p.w_ready ? choose_piece(ops, p, a) : a->vocab;
+  const bool products = p.grad || !p.few;         // operands of the tensor cores are needed
+  p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : p.grad || (!p.w_ready && products) ? choose_piece(ops, p, a) : a->vocab;
   p.pieces = (a->vocab + p.piece - 1) / p.piece;
   p.ld_x = p.x_ready && a->rows > 1 ? a->ld_x : round_up(a->n_in, 8);      // the stride of a single row says nothing
   p.ld_w = p.w_ready && a->vocab > 1 ? a->ld_w : round_up(a->n_in, 8);
@@ -157,11 +164,13 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   p.tc = choose_shape(ops, logits_product(p, a, false, a->rows, p.piece), p.parts, false, false, false);
   long long at = 0;
   auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
-  p.x_off = take(p.x_ready ? 0 : packed_bytes(operand_x(a), a->dtype));
-  p.w_off = take(p.w_ready ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype));
+  p.x_off = take(p.x_ready || !products ? 0 : packed_bytes(operand_x(a), a->dtype));
+  p.w_off = take(p.w_ready || !products ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype));
   p.target_off = take(a->rows * 4);
-  long long slots = 0;                            // of the widest launch
-  for (long long r = 0; r < a->rows;) {
+  const int per_block = (rounded >= 16 ? 2 : 4) * kRowsThreads / 32;
+  p.few_blocks = (int)std::min<long long>((a->vocab + per_block - 1) / per_block, ops->num_sms * 2);
+  long long slots = p.few ? p.few_blocks * a->rows : 0;               // of the widest launch
+  for (long long r = 0; r < a->rows && !p.few;) {
     const int t = stats_rows(ops, p.stats, a->rows - r);
     const long long n = std::min<long long>(a->rows - r, 128ll * p.stats.pair * t);
     slots = std::max(slots, n * stats_slots(ops, p.stats, t, together) * (p.w_ready ? 1 : p.pieces));
@@ -189,14 +198,16 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   return p;
 }
 
-// Tensor map of a piece's gradient [words][rows], for stores of 32 rows by 32 words.
-gbmuf_status gradient_map(const TcParams& P, CUtensorMap* map) {
+// Tensor map of a piece's gradient [words][rows], for stores of 32 rows by 32 words, or of its three parts, for stores of
+// 16 rows by 32 words of each.
+gbmuf_status gradient_map(const TcParams& P, int parts, CUtensorMap* map) {
   const EncodeTiledFn encode = encode_tiled_fn();
   if (!encode) return refuse(GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-  const cuuint64_t dim[2] = {(cuuint64_t)P.R, (cuuint64_t)P.E.words}, stride[1] = {(cuuint64_t)P.E.ld_out0 * 2};
-  const cuuint32_t box[2] = {32, 32}, one[2] = {1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, P.E.out0, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t dim[3] = {(cuuint64_t)P.R, (cuuint64_t)P.E.words, 3}, stride[2] = {(cuuint64_t)P.E.ld_out0 * 2, (cuuint64_t)P.E.part * 2};
+  const cuuint32_t box[3] = {parts == 1 ? 32u : 16u, 32, 3}, one[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, parts == 1 ? 2 : 3, P.E.out0, dim, stride, box, one,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, parts == 1 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return refuse(GBMUF_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
   return GBMUF_OK;
 }
@@ -204,8 +215,8 @@ template <int KIND, typename T, int PARTS>
 gbmuf_status launch_logits(const gbmuf_ops* ops, const TcShape& s, TcParams& P, int at_once, const Operand& a, const Operand& b,
                            int32_t dtype, cudaStream_t st) {
   CUtensorMap ma{}, mb{}, out{};
-  if (KIND == kLossGrad && PARTS == 1)
-    if (gbmuf_status rc = gradient_map(P, &out)) return rc;
+  if (KIND == kLossGrad)
+    if (gbmuf_status rc = gradient_map(P, PARTS, &out)) return rc;
   if (P.ksteps > 0) {
     if (gbmuf_status rc = operand_map(a, dtype, nullptr, 128, &ma)) return rc;
     if (gbmuf_status rc = operand_map(b, dtype, nullptr, s.bn / s.pair, &mb)) return rc;
@@ -245,32 +256,26 @@ gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* d
                   launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)j.blocks, 1, 256, 0, st, j, PackJob{}));
 }
 
-// A few fp32 rows without gradients: the fp32 units read the weights once, where the tensor cores would need
-// them packed as three bf16 parts first (8 x 512 -> 267,735 words: 431 us).  Their logits are few: they are
-// kept, in the workspace.
-gbmuf_linear_forward_args few_rows_args(const Args* a) {
-  gbmuf_linear_forward_args f{};
-  f.rows = a->rows; f.n_in = a->n_in; f.n_out = a->vocab; f.x = a->x; f.w = a->w; f.bias = a->bias;
-  f.y = a->workspace ? a->workspace : reinterpret_cast<void*>(256);
-  f.ld_x = a->ld_x; f.ld_w = a->ld_w; f.ld_y = a->vocab; f.dtype = a->dtype;
-  return f;
+// A few rows: one read of the weights on the fp32 units, as in the linear layer.
+template <typename T, int ROWS> cudaError_t launch_rows_loss(const RowsParams& P, bool vec, unsigned grid, cudaStream_t st) {
+  const uint32_t smem = (uint32_t)(ROWS * ((P.K + 7) / 8 * 8) * (int)sizeof(T));
+  const auto kernel = vec ? linear_rows_kernel<T, ROWS, true, true> : linear_rows_kernel<T, ROWS, false, true>;
+  if (smem > 48 * 1024 - 4096) {                  // 4 KB: what it has besides
+    const cudaError_t e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsMostBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(kernel, grid, 1, kRowsThreads, smem, st, P);
 }
-bool is_few_rows(gbmuf_ops* ops, const Args* a) {
-  if (a->dtype != GBMUF_F32 || a->rows > 16 || a->dx || a->dw || a->dbias) return false;
-  const gbmuf_linear_forward_args f = few_rows_args(a);
-  int64_t bytes = 0;
-  return gbmuf_linear_forward_workspace(ops, &f, &bytes) == GBMUF_OK && bytes == 0;
-}
-gbmuf_status run_few_rows(gbmuf_ops* ops, const Args* a, void* stream) {
-  const int64_t need = a->rows * a->vocab * 4;
-  if (need > a->workspace_bytes || !a->workspace || (uintptr_t)a->workspace % 256 != 0)
-    return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(need) + " bytes");
-  const gbmuf_linear_forward_args f = few_rows_args(a);
-  if (gbmuf_status rc = gbmuf_linear_forward(ops, &f, stream)) return rc;
-  gbmuf_cross_entropy_args c{};
-  c.rows = a->rows; c.vocab = a->vocab; c.logits = a->workspace; c.targets = a->targets; c.row_weight = a->row_weight;
-  c.loss = a->loss; c.lse = a->lse; c.ld_logits = a->vocab; c.ignore_index = a->ignore_index; c.dtype = a->dtype; c.scale = a->scale;
-  return gbmuf_cross_entropy(ops, &c, stream);
+template <typename T> cudaError_t rows_loss(const Args* a, RowsParams& P, unsigned grid, cudaStream_t st) {
+  P.x = a->x; P.w = a->w; P.ld_x = a->ld_x; P.ld_w = a->ld_w;
+  P.R = (int)a->rows; P.C = (int)a->vocab; P.K = (int)a->n_in;
+  const bool vec = (uintptr_t)a->w % 16 == 0 && (a->vocab == 1 || a->ld_w * (int64_t)sizeof(T) % 16 == 0);
+  if (a->rows <= 1) return launch_rows_loss<T, 1>(P, vec, grid, st);
+  if (a->rows <= 2) return launch_rows_loss<T, 2>(P, vec, grid, st);
+  if (a->rows <= 4) return launch_rows_loss<T, 4>(P, vec, grid, st);
+  if (a->rows <= 8 || sizeof(T) == 2) return launch_rows_loss<T, 8>(P, vec, grid, st);
+  if constexpr (sizeof(T) == 4) return launch_rows_loss<T, 16>(P, vec, grid, st);
+  return cudaErrorInvalidValue;
 }
 
 template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cudaStream_t st) {
@@ -281,17 +286,20 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
   char* const ws = static_cast<char*>(a->workspace);
   const long long N = a->rows, V = a->vocab, H = a->n_in, size = (long long)sizeof(T);
   Operand x = operand_x(a);
-  if (!p.x_ready) {
+  if (!p.x_ready && (p.grad || !p.few)) {
     if (gbmuf_status rc = pack(ops, x, a->dtype, ws + p.x_off, st)) return rc;
     x.p = ws + p.x_off;
   }
   x.ld = p.ld_x;
   x.ready = true;
   x.part = N * x.ld;
+  long long packed = -1;                          // the piece that lies packed
   auto weights = [&](long long v0, long long words, Operand& w) -> gbmuf_status {
     w = operand_w(a, v0, words);
     if (!p.w_ready) {
-      if (gbmuf_status rc = pack(ops, w, a->dtype, ws + p.w_off, st)) return rc;
+      if (packed != v0)
+        if (gbmuf_status rc = pack(ops, w, a->dtype, ws + p.w_off, st)) return rc;
+      packed = v0;
       w.p = ws + p.w_off;
     }
     w.ld = p.ld_w;
@@ -312,11 +320,20 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
   if (most_tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles of logits");
   // ---- statistics: every CTA keeps to one row tile, so its threads keep a row's running maximum and sum
   for (long long r0 = 0; r0 < N;) {
-    const int t = stats_rows(ops, s, N - r0);
-    const long long n = std::min<long long>(N - r0, 128ll * s.pair * t), ld = n;
+    const int t = p.few ? 1 : stats_rows(ops, s, N - r0);
+    const long long n = p.few ? N : std::min<long long>(N - r0, 128ll * s.pair * t), ld = n;
     const long long step = p.w_ready ? V : p.piece;
     int slots = 0;
-    for (long long v0 = 0; v0 < V; v0 += step) {
+    if (p.few) {
+      RowsParams P{};
+      P.E.bias = a->bias; P.E.loss_rows = a->targets;
+      P.E.target_logit = reinterpret_cast<float*>(ws + p.target_off);
+      P.E.partial = ws + p.slot_off; P.E.ld_partial = ld;
+      slots = p.few_blocks;
+      const cudaError_t e = rows_loss<T>(a, P, (unsigned)slots, st);
+      if (e != cudaSuccess) return cuda_refuse("launch of the few-rows loss kernel", e);
+    }
+    for (long long v0 = 0; v0 < V && !p.few; v0 += step) {
       const long long words = std::min(step, V - v0);
       Operand w;
       if (gbmuf_status rc = weights(v0, words, w)) return rc;
@@ -340,7 +357,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     J.L.rows = n; J.L.vocab = V; J.L.ignore_index = a->ignore_index; J.L.scale = a->scale; J.L.status = ops->d_status;
     J.slots = reinterpret_cast<const float2*>(ws + p.slot_off);
     J.target_logit = reinterpret_cast<const float*>(ws + p.target_off) + r0;
-    if (p.grad) {                                          // r0 is a multiple of 128
+    if (p.grad) {                                // r0 is a multiple of 128
       J.pairs = reinterpret_cast<RowPair*>(ws + p.pair_off) + r0 / 2;
       J.targets = reinterpret_cast<int*>(ws + p.word_off) + r0;
       J.weights = reinterpret_cast<float*>(ws + p.weight_off) + r0;
@@ -427,7 +444,7 @@ gbmuf_status gbmuf_linear_cross_entropy_workspace(gbmuf_ops* ops, const gbmuf_li
   return guarded([&]() -> gbmuf_status {
     if (!bytes) return invalid("bytes is NULL");
     if (gbmuf_status st = check(ops, a)) return st;
-    *bytes = a->rows == 0 ? 0 : is_few_rows(ops, a) ? a->rows * a->vocab * 4 : make_plan(ops, a).bytes;
+    *bytes = a->rows == 0 ? 0 : make_plan(ops, a).bytes;
     return GBMUF_OK;
   });
 }
@@ -445,7 +462,6 @@ gbmuf_status gbmuf_linear_cross_entropy(gbmuf_ops* ops, const gbmuf_linear_cross
     }
     DeviceGuard guard(ops->device);
     if (!guard.ok) return refuse(GBMUF_ERR_CUDA, "cudaSetDevice failed");
-    if (is_few_rows(ops, a)) return run_few_rows(ops, a, stream);
     DISPATCH_DTYPE(a->dtype, T, return run<T>(ops, a, (cudaStream_t)stream));
   });
 }

@@ -114,8 +114,10 @@ template <int N> __device__ __forceinline__ void store_rows(__nv_bfloat16* to, c
 // us, without any stores 19.8).  The 64-byte swizzle keeps a warp's 16-byte stores off the same banks.
 template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
   float column;              // sum over the strip's rows
-  const CUtensorMap* map;    // N 32: of d, boxes of 32 rows x 32 words
-  uint32_t room;             // 2 KB of shared memory; what went out of it two strips ago has been read
+  // bf16, N 32: tensor map of d, boxes of 32 rows x 32 words; 2 KB of shared memory, what went out of it two strips ago
+  // has been read.  fp32, N 16: boxes of 16 rows x 32 words x 3 parts; 3 KB, the strip before has been read.
+  const CUtensorMap* map;
+  uint32_t room;
 
   __device__ __forceinline__ void ask(const Epilogue&, int, int, int, int, int) {}
   __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int, int lane, float bias, float (&v)[N]) {
@@ -175,6 +177,37 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
       if (lane == 0) {
         asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(r),
                      "r"(c), "r"(room)
+                     : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+      return;
+    }
+    if constexpr (!FAST && N == 16) {
+      if (r >= R || c - lane >= E.words) return;
+      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      __syncwarp();
+      Two rest[N / 2];
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) rest[i] = two(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        uint32_t u[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          u[i] = pair_bf16(rest[i]);
+          if (q < 2) rest[i] = rest[i] - pair_f32(u[i]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(room + 1024u * q + 32u * lane + 16u * (h ^ (lane >> 2 & 1))), "r"(u[4 * h]),
+                       "r"(u[4 * h + 1]), "r"(u[4 * h + 2]), "r"(u[4 * h + 3])
+                       : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
+                     "r"(r), "r"(c), "r"(0), "r"(room)
                      : "memory");
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
       }
@@ -264,9 +297,16 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
   const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
   const long long row = (long long)blockIdx.x * 32 + lane;
   float m = -INFINITY, s = 0.0f;
-  if (row < P.L.rows)
-#pragma unroll 4
-    for (int i = share; i < P.count; i += kJoinShares) join_stats(m, s, P.slots[i * P.ld + row]);
+  if (row < P.L.rows) {
+    // the maximum first: neither loop's loads and exponentials wait for one another
+#pragma unroll 8
+    for (int i = share; i < P.count; i += kJoinShares) m = fmaxf(m, P.slots[i * P.ld + row].x);
+#pragma unroll 8
+    for (int i = share; i < P.count; i += kJoinShares) {
+      const float2 o = P.slots[i * P.ld + row];
+      s += o.x == -INFINITY ? o.y : o.y * expf(o.x - m);
+    }
+  }
   part[share][lane] = make_float2(m, s);
   __syncthreads();
   if (share != 0 || row >= P.rows_padded) return;

@@ -36,7 +36,9 @@ __device__ __forceinline__ void rows_step(float (&acc)[NF * ROWS], const T (&u)[
   }
 }
 
-template <typename T, int ROWS, bool VEC>
+// LOSS: the layer is a softmax layer; its logits are not stored, a block leaves each row's maximum, the sum of the
+// exponentials relative to it, and the target's logit (linear_loss.cuh joins the blocks).
+template <typename T, int ROWS, bool VEC, bool LOSS = false>
 __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const RowsParams P) {
   constexpr int NF = ROWS >= 16 ? 2 : 4, NA = NF * ROWS, V = VEC ? 16 / (int)sizeof(T) : 1;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -50,6 +52,7 @@ __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const Rows
   }
   __syncthreads();
   const int lane = threadIdx.x & 31, warps = gridDim.x * (kRowsThreads / 32);
+  float m = -INFINITY, s = 0.0f;                 // LOSS: of this lane's row and words
   for (int c0 = (blockIdx.x * (kRowsThreads / 32) + (threadIdx.x >> 5)) * NF; c0 < P.C; c0 += warps * NF) {
     float acc[NA] = {};
     const T* w[NF];
@@ -109,7 +112,38 @@ __global__ void __launch_bounds__(kRowsThreads, 2) linear_rows_kernel(const Rows
     }
     constexpr int SPARE = NA >= 32 ? 0 : 32 / NA - 1;      // lanes that hold the same sum
     const int c = c0 + index / ROWS, r = index % ROWS;
-    if ((lane & SPARE) == 0 && c < P.C && r < P.R) finish_element<T>(P.E, r, c, acc[0]);
+    if constexpr (!LOSS) {
+      if ((lane & SPARE) == 0 && c < P.C && r < P.R) finish_element<T>(P.E, r, c, acc[0]);
+    } else if (c < P.C && r < P.R) {
+      const float z = P.E.bias ? acc[0] + to_f32(static_cast<const T*>(P.E.bias)[c]) : acc[0];
+      if ((lane & SPARE) == 0 && static_cast<const long long*>(P.E.loss_rows)[r] == c) P.E.target_logit[r] = z;
+      const float top = fmaxf(m, z);
+      if (top == -INFINITY) s += z == z ? 0.0f : z;        // nothing but -inf and NaN
+      else s = (m == -INFINITY ? s : s * expf(m - top)) + expf(z - top);
+      m = top;
+    }
+  }
+  if constexpr (LOSS) {
+    // lanes that differ in the bits of the exchanges' first log2(NF) steps hold other words of the same row
+    int index = 0;
+#pragma unroll
+    for (int d = 16, n = NA / 2; n >= 1 && d > 0; d >>= 1, n >>= 1)
+      if (lane & d) index += n;
+#pragma unroll
+    for (int d = 16, f = NF / 2; f >= 1; d >>= 1, f >>= 1) {
+      const float m2 = __shfl_xor_sync(~0u, m, d), s2 = __shfl_xor_sync(~0u, s, d);
+      join_stats(m, s, make_float2(m2, s2));
+    }
+    __shared__ float2 stat[kRowsThreads / 32][ROWS];
+    if (index < ROWS && (lane & (NA >= 32 ? 0 : 32 / NA - 1)) == 0) stat[threadIdx.x >> 5][index] = make_float2(m, s);
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r < ROWS && r < P.R) {
+      m = -INFINITY;
+      s = 0.0f;
+      for (int w = 0; w < kRowsThreads / 32; ++w) join_stats(m, s, stat[w][r]);
+      static_cast<float2*>(P.E.partial)[(long long)blockIdx.x * P.E.ld_partial + r] = make_float2(m, s);
+    }
   }
 }
 

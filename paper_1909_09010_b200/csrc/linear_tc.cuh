@@ -52,7 +52,9 @@ struct TcParams {
 __host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
 // Behind the ring: where the finishing warps lay results out for the copy engine (linear_loss.cuh), 4 KB each.
-template <int KIND, int PARTS, int BN> constexpr uint32_t kTcOut = KIND == kLossGrad && PARTS == 1 && BN >= 128 ? 4096u * kTcFinishers : 0u;
+// (Tiles too narrow for strips of that many rows store by themselves.)
+template <int KIND, int PARTS, int BN> constexpr uint32_t kTcOut =
+    KIND != kLossGrad ? 0u : PARTS == 1 ? (BN >= 128 ? 4096u * kTcFinishers : 0u) : BN >= 64 ? 3072u * kTcFinishers : 0u;
 __host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
   return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
 }
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
-  constexpr int MOST = (KIND == kLossStats || KIND == kLossGrad) && !PROMOTE ? 32 : KIND == kLossGrad ? 8 : 16;
+  constexpr int MOST = (KIND == kLossStats || KIND == kLossGrad) && !PROMOTE ? 32 : 16;
   constexpr int N = NCOL < MOST ? NCOL : MOST;    // of them at a time
   extern __shared__ __align__(128) unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
@@ -437,7 +439,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (KIND != kLossStats && warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
-    const uint32_t out_base = ring + (uint32_t)S * STAGE + 4096u * (uint32_t)(warp - 4);
+    const uint32_t out_base = ring + (uint32_t)S * STAGE + kTcOut<KIND, PARTS, BN> / kTcFinishers * (uint32_t)(warp - 4);
     uint32_t out_half = 0;                                         // of the two, in turn
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const Share mine = share(w.c);
@@ -469,6 +471,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int j = 0; j < NCOL; j += N) {
           Finisher<KIND, T, TO, N> F;
           if constexpr (KIND == kLossTerm) F.slice = mine.slice;
+          if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_base; }
           float v[N];
 #pragma unroll
           for (int i = 0; i < N; ++i) v[i] = acc[j + i];
