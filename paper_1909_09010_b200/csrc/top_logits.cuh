@@ -177,11 +177,11 @@ struct TopState {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       rank[q] = k;
-      if (q * kLossWorkers >= n) continue;                 // the same for all threads
+      if (q * kLossWorkers + (thread & ~31) >= n) continue;    // the same for a warp
       const int i = q * kLossWorkers + thread;
       mine[q] = i < n ? S.buffer[i] : 0;
       int above = 0;
-#pragma unroll 8
+#pragma unroll 4
       for (int j = 0; j < n; j += 2) {
         const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(S.buffer + j);
         above += (o.x > mine[q]) + (o.y > mine[q]);
@@ -505,13 +505,18 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
         for (int o = 0; o < P.split; ++o) least = max(least, S.bounds[o]);
       }
       auto list_groups = [&] {
-        if (largest >= least)
-          for (int g = 0; g < mine; ++g) {
-            const uint32_t o = group_order(g);
-            if (o == 0 || o < least) continue;
-            const int at = atomicAdd(&S.hot_count, 1);
-            if (at < kTopHot) S.hot[at] = (unsigned short)(g * kLossWorkers + thread);
-          }
+        if (largest >= least) {
+          unsigned long long wanted = 0;
+          for (int g0 = 0; g0 < mine; g0 += 8)
+#pragma unroll
+            for (int g = g0; g < g0 + 8; ++g) {
+              const uint32_t o = g < mine ? group_order(g) : 0u;
+              if (o != 0 && o >= least) wanted |= 1ull << g;
+            }
+          int at = wanted ? atomicAdd(&S.hot_count, __popcll(wanted)) : 0;
+          for (; wanted; wanted &= wanted - 1, ++at)
+            if (at < kTopHot) S.hot[at] = (unsigned short)((__ffsll(wanted) - 1) * kLossWorkers + thread);
+        }
         loss_workers_sync();
         return S.hot_count;
       };
@@ -535,7 +540,7 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
       bool again = hot > kTopHot;
       if (!again) {
         // a warp takes the pieces of several groups at a time, a lane an element of a piece of one chunk of the run
-        constexpr int LANES = E * kLossPieces, AT_ONCE = 32 / LANES, BATCH = 8;
+        constexpr int LANES = E * kLossPieces, AT_ONCE = 32 / LANES, BATCH = 12;
         const int part = lane / LANES, h = lane % LANES / E, i = lane % E, items = hot * run;
         for (int j0 = warp * AT_ONCE + part; j0 - part < items; j0 += kLossWarps * AT_ONCE * BATCH) {
           int at[BATCH];
@@ -551,12 +556,20 @@ __global__ void __launch_bounds__(kLossThreads, kTopBlocksPerSm) top_ring_kernel
             at[b] = r.a0 + (r.p0 + piece) * E + i;
             y[b] = x[at[b]];
           }
+          // one place in the buffer for all that a lane has found
+          unsigned found = 0;
 #pragma unroll
           for (int b = 0; b < BATCH; ++b)
-            if (at[b] >= 0) {
-              const Key key = top_key(to_f32(y[b]), at[b]);
-              if (key >= bound) top.append(key);
-            }
+            if (at[b] >= 0 && top_key(to_f32(y[b]), at[b]) >= bound) found |= 1u << b;
+          if (found) {
+            int to = atomicAdd(&S.count, __popc(found));
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+              if (found >> b & 1) {
+                if (to < kTopBuffer) S.buffer[to] = top_key(to_f32(y[b]), at[b]);
+                ++to;
+              }
+          }
         }
         again = top.compact() > kTopBuffer;
       }

@@ -68,7 +68,9 @@ template <typename T> cudaError_t launch_distill(const gbmuf_ops* ops, DistillPa
   P.split = 1 << log;
   const bool both = P.hard != 0.0f && P.T != 1.0f;
   const int clusters = (int)std::min<long long>(P.rows, ops->distill_clusters[sizeof(T) == 2][both][log]);
-  return launch(both ? distill_ring_kernel<T, true> : distill_ring_kernel<T, false>, (unsigned)(clusters * P.split), (unsigned)P.split,
+  const auto kernel = !both ? distill_ring_kernel<T, 0> : P.T == 2.0f ? distill_ring_kernel<T, 2> : P.T == 3.0f ? distill_ring_kernel<T, 3>
+                    : P.T == 4.0f ? distill_ring_kernel<T, 4> : distill_ring_kernel<T, 1>;
+  return launch(kernel, (unsigned)(clusters * P.split), (unsigned)P.split,
                 kDistillThreads, kDistillSmem, st, P);
 }
 
@@ -96,10 +98,15 @@ const char* check_index(const void* p, int64_t rows, int64_t k, int64_t ld) {
 gbmuf_status gbmuf_setup_vocab_ops(gbmuf_ops* ops) {
   const int blocks = ops->num_sms * kLossBlocksPerSm;
   int unused[4];
-  cudaError_t e = count_clusters(distill_ring_kernel<float, false>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][0]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<float, true>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][1]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, false>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][0]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, true>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][1]);
+  cudaError_t e = count_clusters(distill_ring_kernel<float, 0>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][0]);
+  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<float, 1>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][1]);
+  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, 0>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][0]);
+  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, 1>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][1]);
+  const void* const powers[] = {(const void*)distill_ring_kernel<float, 2>,         (const void*)distill_ring_kernel<float, 3>,
+                                (const void*)distill_ring_kernel<float, 4>,         (const void*)distill_ring_kernel<__nv_bfloat16, 2>,
+                                (const void*)distill_ring_kernel<__nv_bfloat16, 3>, (const void*)distill_ring_kernel<__nv_bfloat16, 4>};
+  for (const void* k : powers)                    // their threads and shared memory are those of mode 1
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDistillSmem);
   if (e == cudaSuccess) e = count_clusters(top_ring_kernel<float>, kLossThreads, kTopSmem, blocks, unused);
   if (e == cudaSuccess) e = count_clusters(top_ring_kernel<__nv_bfloat16>, kLossThreads, kTopSmem, blocks, unused);
   return launched("set-up of the vocabulary operators", e);
