@@ -34,7 +34,6 @@ struct DistillParams {
   int32_t* status;
 };
 constexpr int kListMost = 256;                 // entries
-constexpr int kListLanes = kListMost / 32;     // of them per lane
 constexpr int kListHeads = kLossWorkers;
 
 struct RowList {
@@ -47,7 +46,7 @@ struct RowList {
   double gap;
   float q_sum, m, s, s1, q_rest, target_logit, weight;
   int target;                // -1: none
-  bool outside, ignored;
+  bool outside, ignored, target_listed;
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -59,51 +58,85 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
-// Fills a row's list; all lanes of one warp.  owner(word): the worker thread whose pieces hold a word.
-template <typename T, typename Owner>
-__device__ __forceinline__ void prepare_list(const DistillParams& P, long long row, RowList& L, int lane, Owner owner) {
-  constexpr bool FAST = false;
-  const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
-  const long long* const index = P.index + row * P.ld_index;
-  for (int i = lane; i < kListHeads; i += 32) L.head[i] = -1;
-  long long word[kListLanes];
-  double a[kListLanes];
-  float largest = -INFINITY;
-  bool outside = false;
+// What a lane needs of a row's list from memory (LANES entries of it): asked for two rows ahead, the student's
+// logits at its words one row ahead.
+template <typename T, int LANES> struct ListAhead {
+  float t[LANES], x[LANES];
+  long long word[LANES], target;
+  float weight, lse, target_logit;
+
+  __device__ __forceinline__ bool inside(const DistillParams& P, long long v) const { return v >= 0 && v < P.vocab; }
+  __device__ __forceinline__ void ask(const DistillParams& P, long long row, int lane) {
+    if (row >= P.rows) return;
 #pragma unroll
-  for (int i = 0; i < kListLanes; ++i) {
-    const int j = lane + 32 * i;
+    for (int i = 0; i < LANES; ++i) {
+      const int j = lane + 32 * i;
+      t[i] = -INFINITY;
+      word[i] = -1;
+      if (j >= P.k) continue;
+      t[i] = P.teacher_bf16 ? to_f32(static_cast<const __nv_bfloat16*>(P.teacher)[row * P.ld_teacher + j])
+                            : static_cast<const float*>(P.teacher)[row * P.ld_teacher + j];
+      word[i] = P.index[row * P.ld_index + j];
+    }
+    target = P.targets ? P.targets[row] : -1;
+    weight = P.row_weight ? P.row_weight[row] : 1.0f;
+    lse = P.teacher_lse ? P.teacher_lse[row] : 0.0f;
+  }
+  __device__ __forceinline__ void ask_student(const DistillParams& P, long long row) {
+    if (row >= P.rows) return;
+    const T* const student = static_cast<const T*>(P.logits) + row * P.ld;
+#pragma unroll
+    for (int i = 0; i < LANES; ++i) x[i] = inside(P, word[i]) ? to_f32(student[word[i]]) : -INFINITY;
+    target_logit = inside(P, target) ? to_f32(student[target]) : 0.0f;
+  }
+};
+
+// Fills a row's list from what has been asked for; all lanes of one warp.  owner(word): the worker thread whose pieces
+// hold a word.
+template <typename T, int LANES, typename Owner>
+__device__ __forceinline__ void prepare_list(const DistillParams& P, RowList& L, int lane, Owner owner, const ListAhead<T, LANES>& from) {
+  constexpr bool FAST = false;
+  for (int i = lane; i < kListHeads; i += 32) L.head[i] = -1;
+  long long word[LANES];
+  double a[LANES];
+  float xs[LANES], largest = -INFINITY;
+  bool outside = false, target_listed = false;
+#pragma unroll
+  for (int i = 0; i < LANES; ++i) {
+    const float t = from.t[i];
+    const long long v = from.word[i];
     word[i] = -1;
     a[i] = -INFINITY;
-    if (j >= P.k) continue;
-    const float t = P.teacher_bf16 ? to_f32(static_cast<const __nv_bfloat16*>(P.teacher)[row * P.ld_teacher + j])
-                                   : static_cast<const float*>(P.teacher)[row * P.ld_teacher + j];
-    const long long v = index[j];
+    xs[i] = -INFINITY;
     if (v == -1 || t == -INFINITY) continue;               // no entry
     if (v < 0 || v >= P.vocab) { outside = true; continue; }
     word[i] = v;
+    target_listed |= v == from.target;
+    xs[i] = from.x[i];
     a[i] = (double)t * P.temperature.inverse;
     largest = fmaxf(largest, (float)a[i]);
   }
+  const long long target = from.target;
+  const bool inside = from.inside(P, target);
+  const float w = P.scale * from.weight, target_logit = from.target_logit, teacher_lse = from.lse;
   // log of the probabilities' common divisor
   double A;
   if (P.teacher_lse) {
-    A = (double)P.teacher_lse[row];
+    A = (double)teacher_lse;
   } else {
     largest = warp_max(largest);
     float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kListLanes; ++i)
+    for (int i = 0; i < LANES; ++i)
       if (word[i] >= 0) s += expf((float)(a[i] - (double)largest));
     A = (double)largest + log_of(warp_sum(s));
   }
-  float q[kListLanes], xs[kListLanes], m = -INFINITY;
+  float q[LANES], m = -INFINITY;
   double q_sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < kListLanes; ++i) {
+  for (int i = 0; i < LANES; ++i) {
     a[i] -= A;                                             // log q
     q[i] = word[i] >= 0 ? expf((float)a[i]) : 0.0f;
-    xs[i] = word[i] >= 0 ? to_f32(x[word[i]]) : -INFINITY;
     q_sum += (double)q[i];
     m = fmaxf(m, xs[i]);
   }
@@ -111,7 +144,7 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   m = warp_max(m);
   __syncwarp();                                            // heads are clear
 #pragma unroll
-  for (int i = 0; i < kListLanes; ++i) {
+  for (int i = 0; i < LANES; ++i) {
     const int j = lane + 32 * i;
     if (j >= P.k) continue;
     L.word[j] = (int)word[i];
@@ -121,10 +154,10 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   }
   __syncwarp();
   // entries of the same word: the first one stands for all, with the sum of their q in the list's order
-  bool first[kListLanes];
-  float total[kListLanes];
+  bool first[LANES];
+  float total[LANES];
 #pragma unroll
-  for (int i = 0; i < kListLanes; ++i) {
+  for (int i = 0; i < LANES; ++i) {
     const int j = lane + 32 * i;
     first[i] = word[i] >= 0;
     total[i] = q[i];
@@ -152,7 +185,7 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   double gap = 0.0;
   int words = 0;
 #pragma unroll
-  for (int i = 0; i < kListLanes; ++i) {
+  for (int i = 0; i < LANES; ++i) {
     const int j = lane + 32 * i;
     if (word[i] >= 0) {
       if (q[i] != 0.0f) gap += (double)q[i] * (a[i] - (double)(xs[i] - e.m) * P.temperature.inverse);
@@ -171,32 +204,31 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, long long r
   for (int d = 16; d > 0; d >>= 1) gap += __shfl_xor_sync(~0u, gap, d);
   words = __reduce_add_sync(~0u, words);
   outside = __any_sync(~0u, outside);
+  target_listed = __any_sync(~0u, target_listed);
   if (lane == 0) {
-    const float w = P.scale * (P.row_weight ? P.row_weight[row] : 1.0f);
-    const long long t = P.targets ? P.targets[row] : -1;
-    const bool ignored = w == 0.0f || (P.targets && t == P.ignore_index);
-    const bool inside = t >= 0 && t < P.vocab;
+    const bool ignored = w == 0.0f || (P.targets && target == P.ignore_index);
     if (P.targets && !inside) outside = true;
     L.gap = gap; L.m = m; L.s = s; L.s1 = s1;
     L.q_sum = (float)q_sum;
     const double rest = 1.0 - q_sum;
     L.q_rest = P.teacher_lse && words < P.vocab ? (rest < 0.0 ? 0.0f : (float)rest) : 0.0f;
-    L.target = inside ? (int)t : -1;
-    L.target_logit = inside ? to_f32(x[t]) : 0.0f;
+    L.target = inside ? (int)target : -1;
+    L.target_logit = target_logit;
     L.weight = w;
     L.outside = outside && !ignored;
     L.ignored = ignored;
+    L.target_listed = target_listed;
   }
   __syncwarp();
 }
 
 // What a row's statistics and its list say.  (m, r, r1): maximum of the rest, its sums at T and at 1.
 struct DistillRow {
-  float lse, loss;
-  bool zero;
-  float k, k1;               // the gradient of a word of the rest is k exp((x - m_r) / T) + k1 exp(x - m_r)
+  bool empty, zero;          // nothing but -inf; no gradient
+  float k, k1;               // the gradient of a word of the rest is k exp((x - m) / T) + k1 exp(x - m)
   float top, per, per1;      // of a word of the list: per exp((x - top) / T) + per1 exp(x - top) - soft Q - hard [target]
   float soft, hard;
+  float z, z1, share;        // sums of all words relative to top; P_r
 };
 __device__ __forceinline__ DistillRow distill_row(const DistillParams& P, const RowList& L, float m, float r, float r1) {
   DistillRow o;
@@ -204,39 +236,49 @@ __device__ __forceinline__ DistillRow distill_row(const DistillParams& P, const 
   Shift<false> e1;
   e.at(P.temperature);
   const float top = fmaxf(m, L.m);
-  const bool empty = top == -INFINITY && r + L.s == 0.0f, one = P.T == 1.0f;
+  const bool one = P.T == 1.0f;
   e.set(top);
   e1.set(top);
   const float fr = m == -INFINITY ? 1.0f : e(m), fs = L.m == -INFINITY ? 1.0f : e(L.m);
   const float fr1 = m == -INFINITY ? 1.0f : e1(m), fs1 = L.m == -INFINITY ? 1.0f : e1(L.m);
-  const float z = r * fr + L.s * fs, z1 = one ? z : r1 * fr1 + L.s1 * fs1;
-  const float w = L.weight, h = P.hard, q_rest = L.q_rest, mass = L.q_sum + q_rest;
-  const float share = r * fr / z;                          // P_r
-  const double log_z = log_of(z);
-  o.lse = empty ? -INFINITY : (float)((double)e.m * P.temperature.inverse + log_z);
-  o.zero = L.ignored || L.outside || empty;
-  // sum q (log q - log p): log p = (x - m_s) / T + (m_s - top) / T - log z.  In 64 bits: log z may be many times
-  // the loss.
-  const double shift_s = L.m == -INFINITY ? 0.0 : (double)(L.m - top) * P.temperature.inverse;
-  double soft = L.q_sum == 0.0f ? 0.0 : L.gap - (double)L.q_sum * (shift_s - log_z);
-  if (q_rest != 0.0f)
-    soft += (double)q_rest * (share > 1e-30f ? (double)logf(q_rest / share)
-                                             : (double)logf(q_rest) - (log_of(r) + (m == -INFINITY ? 0.0 : (double)(m - top) * P.temperature.inverse) - log_z));
-  double loss = 0.0;
-  if (h != 1.0f) loss += (1.0 - (double)h) * (double)(P.T * P.T) * soft;
-  if (h != 0.0f) loss += (double)h * ((double)(top - L.target_logit) + (one ? log_z : log_of(z1)));
-  o.loss = L.ignored ? 0.0f : L.outside ? NAN : empty ? INFINITY : (float)((double)w * loss);
-  const float ws = w * (1.0f - h) * P.T, wh = w * h;
-  o.k = r == 0.0f ? 0.0f : ws * (mass * share - q_rest) / r;
-  o.k1 = h == 0.0f || (one ? r : r1) == 0.0f ? 0.0f : wh * fr1 / z1;
-  o.per = ws * mass / z;
-  o.per1 = wh / z1;
+  o.empty = top == -INFINITY && r + L.s == 0.0f;
+  o.zero = L.ignored || L.outside || o.empty;
+  o.z = r * fr + L.s * fs;
+  o.z1 = one ? o.z : r1 * fr1 + L.s1 * fs1;
+  o.share = r * fr / o.z;
+  const float h = P.hard, mass = L.q_sum + L.q_rest, ws = L.weight * (1.0f - h) * P.T, wh = L.weight * h;
+  o.k = r == 0.0f ? 0.0f : ws * (mass * o.share - L.q_rest) / r;
+  o.k1 = h == 0.0f || (one ? r : r1) == 0.0f ? 0.0f : wh * fr1 / o.z1;
+  o.per = ws * mass / o.z;
+  o.per1 = h == 0.0f ? 0.0f : wh / o.z1;
   if (one) { o.k += o.k1; o.per += o.per1; o.k1 = o.per1 = 0.0f; }
-  if (h == 0.0f) o.per1 = 0.0f;
   o.top = e.m;
   o.soft = ws;
   o.hard = wh;
   return o;
+}
+// (lse, loss).  In 64 bits past the sums: log z may be many times the loss.
+__device__ __noinline__ float2 distill_loss(const DistillParams& P, const RowList& L, const DistillRow o, float m, float r) {
+  const bool empty = o.empty, one = P.T == 1.0f;
+  const double inverse = P.temperature.inverse, log_z = log_of(o.z);
+  const float lse = empty ? -INFINITY : (float)((double)o.top * inverse + log_z);
+  // sum q (log q - log p): log p = (x - m_s) / T + (m_s - top) / T - log z
+  const double shift_s = L.m == -INFINITY ? 0.0 : (double)(L.m - o.top) * inverse;
+  double soft = L.q_sum == 0.0f ? 0.0 : L.gap - (double)L.q_sum * (shift_s - log_z);
+  if (L.q_rest != 0.0f)
+    soft += (double)L.q_rest * (o.share > 1e-30f ? (double)logf(L.q_rest / o.share)
+                                                 : (double)logf(L.q_rest) - (log_of(r) + (m == -INFINITY ? 0.0 : (double)(m - o.top) * inverse) - log_z));
+  double loss = 0.0;
+  if (P.hard != 1.0f) loss += (1.0 - (double)P.hard) * (double)(P.T * P.T) * soft;
+  if (P.hard != 0.0f) loss += (double)P.hard * ((double)(o.top - L.target_logit) + (one ? log_z : log_of(o.z1)));
+  return make_float2(lse, L.ignored ? 0.0f : L.outside ? NAN : empty ? INFINITY : (float)((double)L.weight * loss));
+}
+struct DistillEnd { DistillRow o; float m, r; };           // what the loss needs besides the list
+__device__ __forceinline__ void store_loss(const DistillParams& P, const RowList& L, const DistillRow& o, float m, float r, long long row) {
+  if (L.outside) atomicExch(P.status, (int32_t)GBMUF_ERR_INVALID_ARG);
+  const float2 v = distill_loss(P, L, o, m, r);
+  if (P.lse) P.lse[row] = v.x;
+  if (P.loss) P.loss[row] = v.y;
 }
 __device__ __forceinline__ float listed_gradient(const DistillParams& P, const DistillRow& o, float x, float q, bool is_target) {
   TemperedShift<false> e;
@@ -249,7 +291,7 @@ __device__ __forceinline__ float listed_gradient(const DistillParams& P, const D
 }
 
 // ---- short rows: one warp per row, up to 32 * REGS logits in its registers
-template <typename T, int REGS>
+template <typename T, int REGS, int LANES>
 __global__ void __launch_bounds__(128) distill_warp_kernel(const DistillParams P) {
   constexpr bool FAST = sizeof(T) == 2;
   __shared__ RowList lists[4];
@@ -263,10 +305,13 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const DistillParams P
   const T* const x = static_cast<const T*>(P.logits) + row * P.ld;
   const int V = (int)P.vocab;
   float v[REGS];
+  ListAhead<T, LANES> ahead;
+  ahead.ask(P, row, lane);
 #pragma unroll
   for (int i = 0; i < REGS; ++i) v[i] = lane + 32 * i < V ? to_f32(x[lane + 32 * i]) : -INFINITY;
   for (int i = lane; i < REGS; i += 32) listed[warp][i] = 0;
-  prepare_list<T>(P, row, L, lane, [](int word) { return word % kListHeads; });
+  ahead.ask_student(P, row);
+  prepare_list(P, L, lane, [](int word) { return word % kListHeads; }, ahead);
   for (int j = lane; j < P.k; j += 32)
     if (L.word[j] >= 0) atomicOr(&listed[warp][L.word[j] >> 5], 1u << (L.word[j] & 31));
   __syncwarp();
@@ -293,12 +338,10 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const DistillParams P
   r = warp_sum(r);
   r1 = warp_sum(r1);
   const DistillRow o = distill_row(P, L, m, r, r1);
-  if (lane == 0) {
-    if (L.outside) atomicExch(P.status, (int32_t)GBMUF_ERR_INVALID_ARG);
-    if (P.loss) P.loss[row] = o.loss;
-    if (P.lse) P.lse[row] = o.lse;
+  if (!P.dlogits) {
+    if (lane == 0) store_loss(P, L, o, m, r, row);
+    return;
   }
-  if (!P.dlogits) return;
   T* const d = static_cast<T*>(P.dlogits) + row * P.ld_d;
 #pragma unroll
   for (int i = 0; i < REGS; ++i) {
@@ -312,12 +355,14 @@ __global__ void __launch_bounds__(128) distill_warp_kernel(const DistillParams P
   if (!o.zero)
     for (int j = lane; j < P.k; j += 32)
       if (L.word[j] >= 0) d[L.word[j]] = from_f32<T>(listed_gradient(P, o, L.x[j], L.q[j], L.word[j] == L.target));
+  if (lane == 0) store_loss(P, L, o, m, r, row);
 }
 
 // ---- longer rows: as the cross-entropy's (a cluster per row, chunks through a ring of slots, the last ones kept
 // and the others fetched again for the gradient), with the list's warp beside the producer.
 constexpr int kDistillThreads = kLossWorkers + 64;
-constexpr uint32_t kDistillLists = 576;
+constexpr uint32_t kDistillLists = 768;
+static_assert(576 + 2 * sizeof(DistillEnd) <= kDistillLists, "");
 constexpr uint32_t kDistillHead = (kDistillLists + 2u * (uint32_t)sizeof(RowList) + 127u) / 128u * 128u;
 constexpr uint32_t kDistillSmem = kDistillHead + kLossRing * kLossChunk;
 
@@ -335,7 +380,7 @@ template <typename T> __device__ __forceinline__ void take_out(uint4& u, int at)
 // MODE 0: one exponential per logit.  Else the hard targets' softmax is another one (T is not 1): 1, with exponentials of
 // its own; 2, 3 and 4, where that is T: exp(x) = exp(x / T)^T, two multiplications at most (each 2^-24) in place of
 // an exponential (1,003 x 33,278 fp32 at T = 3: see the figures above).
-template <typename T, int MODE>
+template <typename T, int MODE, int LANES>
 __global__ void __launch_bounds__(kDistillThreads, kLossBlocksPerSm) distill_ring_kernel(const DistillParams P) {
   constexpr bool FAST = sizeof(T) == 2, TWO = MODE != 0;
   constexpr int E = 16 / (int)sizeof(T);
@@ -349,6 +394,7 @@ __global__ void __launch_bounds__(kDistillThreads, kLossBlocksPerSm) distill_rin
   auto list_empty = [&](int b) { return bars + 160u + 8u * b; };
   float4* const told = reinterpret_cast<float4*>(smem + 192);          // [2][8]: statistics of the ranks
   float4* const warp_stat = reinterpret_cast<float4*>(smem + 448);     // [8]
+  DistillEnd* const outcome = reinterpret_cast<DistillEnd*>(smem + 576);       // [2]
   RowList* const lists = reinterpret_cast<RowList*>(smem + kDistillLists);
   const int rank = P.split > 1 ? (int)(blockIdx.x % (unsigned)P.split) : 0;
   const long long first = blockIdx.x / (unsigned)P.split, step = gridDim.x / (unsigned)P.split;
@@ -400,18 +446,57 @@ __global__ void __launch_bounds__(kDistillThreads, kLossBlocksPerSm) distill_rin
     }
     __syncwarp();
   } else if (warp > kLossWarps) {
-    // ------------------------------------------------------------------ lists
+    // ------------------------------------------------------------------ lists; what is left to do of rows behind the workers
     int turn = 0;
     bool ok = true;
-    for (long long row = first; row < P.rows && ok; row += step, ++turn) {
-      const int b = turn & 1;
-      if (turn >= 2) ok = mbar_wait_bounded(list_empty(b), (turn >> 1 & 1) ^ 1, P.status);
+    ListAhead<T, LANES> now, ahead;
+    now.ask(P, first, lane);
+    now.ask_student(P, first);
+    ahead.ask(P, first + step, lane);
+    // The row of turn t, once the workers have stored its gradient and left its list: the list's words and the
+    // target are stored once more, and the loss is formed (its 64-bit logarithms would hold the workers up).
+    auto finish = [&](long long row, int t) {
+      ok = ok && mbar_wait_bounded(list_empty(t & 1), t >> 1 & 1, P.status);
       ok = __all_sync(~0u, ok);
+      if (!ok) return;
+      const RowList& L = lists[t & 1];
+      const DistillEnd& end = outcome[t & 1];
+      if (P.dlogits && !end.o.zero) {
+        const RowSpan r = row_span<T>(P, row, rank);
+        T* const d = static_cast<T*>(P.dlogits) + row * P.ld_d;
+        const int slice = r.a0 + r.p0 * E, length = r.n * E;
+        auto mine = [&](int word) {
+          const bool edge = word < r.a0 || word >= r.a0 + r.pieces * E;
+          return edge ? rank == 0 : word >= slice && word - slice < length;
+        };
+        for (int j = lane; j < P.k; j += 32)
+          if (L.word[j] >= 0 && mine(L.word[j]))
+            d[L.word[j]] = from_f32<T>(listed_gradient(P, end.o, L.x[j], L.q[j], L.word[j] == L.target));
+        if (lane == 0 && end.o.hard != 0.0f && L.target >= 0 && !L.target_listed && mine(L.target)) {
+          TemperedShift<FAST> e;
+          Shift<FAST> e1;
+          e.at(P.temperature);
+          e.set(end.m);
+          e1.set(end.m);
+          const float x = L.target_logit;
+          d[L.target] = from_f32<T>((TWO ? e(x) * end.o.k + e1(x) * end.o.k1 : e(x) * end.o.k) - end.o.hard);
+        }
+      }
+      if (lane == 0 && rank == 0) store_loss(P, L, end.o, end.m, end.r, row);
+      __syncwarp();
+    };
+    for (long long row = first; row < P.rows; row += step, ++turn) {
+      const int b = turn & 1;
+      if (turn >= 2) finish(row - 2 * step, turn - 2);
       if (!ok) break;
       const RowSpan r = row_span<T>(P, row, rank);
-      prepare_list<T>(P, row, lists[b], lane, [&](int word) { return owner_of(r, word); });
+      ahead.ask_student(P, row + step);
+      prepare_list(P, lists[b], lane, [&](int word) { return owner_of(r, word); }, now);
       if (lane == 0) mbar_arrive(list_full(b));
+      now = ahead;
+      ahead.ask(P, row + 2 * step, lane);
     }
+    for (int t = turn > 2 ? turn - 2 : 0; t < turn && ok; ++t) finish(first + t * step, t);
   } else {
     // ------------------------------------------------------------------ 8 worker warps
     bool ok = true;
@@ -572,11 +657,6 @@ __global__ void __launch_bounds__(kDistillThreads, kLossBlocksPerSm) distill_rin
         st = join((lane & 7) < P.split ? told[b * 8 + (lane & 7)] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f), 8);
       }
       const DistillRow o = distill_row(P, L, st.x, st.y, st.z);
-      if (thread == 0 && rank == 0 && ok) {
-        if (L.outside) atomicExch(P.status, (int32_t)GBMUF_ERR_INVALID_ARG);
-        if (P.loss) P.loss[row] = o.loss;
-        if (P.lse) P.lse[row] = o.lse;
-      }
       if (P.dlogits) {
         e.set(st.x);
         e1.set(st.x);
@@ -630,19 +710,10 @@ __global__ void __launch_bounds__(kDistillThreads, kLossBlocksPerSm) distill_rin
           if (kept) { if (++kept_slot == kLossRing) kept_slot = 0; }
           else advance();
         }
-        // the target and the list's words: the thread that has stored an element stores it once more
-        auto mine = [&](int word) {
-          return word == own_at || (word >= slice && word - slice < length && owner_of(r, word) == thread);
-        };
-        if (!o.zero && ok) {
-          if (o.hard != 0.0f && L.target >= 0 && mine(L.target)) d[L.target] = from_f32<T>(rest_gradient(L.target_logit) - o.hard);
-          for (int j = L.head[thread]; j >= 0; j = L.next[j])
-            if (L.word[j] >= 0 && mine(L.word[j]))
-              d[L.word[j]] = from_f32<T>(listed_gradient(P, o, L.x[j], L.q[j], L.word[j] == L.target));
-        }
       }
+      if (thread == 0) outcome[b] = DistillEnd{o, st.x, st.y};
       __syncwarp();
-      if (lane == 0) mbar_arrive(list_empty(b));
+      if (lane == 0) mbar_arrive(list_empty(b));           // and the row's stores are done
       loss_workers_sync();                                 // warp_stat may be written again
     }
   }

@@ -22,7 +22,7 @@ struct gbmuf_ops {
   int32_t* d_status = nullptr;
   int tc_clusters[4] = {};       // clusters of 1, 2, 4, 8 CTAs of the linear-layer kernel that fit at once
   int loss_clusters[2][4] = {};  // clusters of 1, 2, 4, 8 CTAs of the cross-entropy kernel (fp32, bf16) that fit at once
-  int distill_clusters[2][2][4] = {};   // the same of the distillation kernel, with one and two exponentials per logit
+  int distill_clusters[4] = {};         // the same of the distillation kernel
 };
 // What gbmuf_ops_create does for the kernels of vocab_ops.cu.
 __attribute__((visibility("hidden"))) gbmuf_status gbmuf_setup_vocab_ops(gbmuf_ops* ops);

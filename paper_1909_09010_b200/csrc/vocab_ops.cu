@@ -56,9 +56,12 @@ template <typename T> cudaError_t launch_top(const gbmuf_ops* ops, TopParams& P,
 
 constexpr long long kDistillCacheBytes = 64ll << 20;      // of the 126 MB of L2: the gradient passes through as well
 
-template <typename T> cudaError_t launch_distill(const gbmuf_ops* ops, DistillParams& P, cudaStream_t st) {
+constexpr int kFewLanes = 2;                    // lists of up to 64 entries: two per lane
+
+template <typename T, int LANES> cudaError_t launch_distill(const gbmuf_ops* ops, DistillParams& P, cudaStream_t st) {
   if (P.vocab <= 2048) {
-    const auto kernel = P.vocab <= 256 ? distill_warp_kernel<T, 8> : P.vocab <= 1024 ? distill_warp_kernel<T, 32> : distill_warp_kernel<T, 64>;
+    const auto kernel = P.vocab <= 256 ? distill_warp_kernel<T, 8, LANES> : P.vocab <= 1024 ? distill_warp_kernel<T, 32, LANES>
+                                                                                             : distill_warp_kernel<T, 64, LANES>;
     return launch(kernel, (unsigned)((P.rows + 3) / 4), 1, 128, 0, st, P);
   }
   const long long bytes = P.vocab * (long long)sizeof(T), ctas = (long long)ops->num_sms * kLossBlocksPerSm;
@@ -66,12 +69,11 @@ template <typename T> cudaError_t launch_distill(const gbmuf_ops* ops, DistillPa
   // the slices that are fetched twice should fit the L2 cache
   while (log < 3 && (bytes - ((long long)kLossKept * kLossChunk << log)) * (ctas >> log) >= kDistillCacheBytes) ++log;
   P.split = 1 << log;
-  const bool both = P.hard != 0.0f && P.T != 1.0f;
-  const int clusters = (int)std::min<long long>(P.rows, ops->distill_clusters[sizeof(T) == 2][both][log]);
-  const auto kernel = !both ? distill_ring_kernel<T, 0> : P.T == 2.0f ? distill_ring_kernel<T, 2> : P.T == 3.0f ? distill_ring_kernel<T, 3>
-                    : P.T == 4.0f ? distill_ring_kernel<T, 4> : distill_ring_kernel<T, 1>;
-  return launch(kernel, (unsigned)(clusters * P.split), (unsigned)P.split,
-                kDistillThreads, kDistillSmem, st, P);
+  const int clusters = (int)std::min<long long>(P.rows, ops->distill_clusters[log]);
+  const auto kernel = P.hard == 0.0f || P.T == 1.0f ? distill_ring_kernel<T, 0, LANES>
+                    : P.T == 2.0f ? distill_ring_kernel<T, 2, LANES> : P.T == 3.0f ? distill_ring_kernel<T, 3, LANES>
+                    : P.T == 4.0f ? distill_ring_kernel<T, 4, LANES> : distill_ring_kernel<T, 1, LANES>;
+  return launch(kernel, (unsigned)(clusters * P.split), (unsigned)P.split, kDistillThreads, kDistillSmem, st, P);
 }
 
 gbmuf_status check_rows(const gbmuf_ops* ops, int64_t rows, int64_t vocab, int32_t dtype, int32_t k) {
@@ -95,18 +97,29 @@ const char* check_index(const void* p, int64_t rows, int64_t k, int64_t ld) {
 
 }  // namespace
 
+namespace {
+
+template <typename T, int LANES> cudaError_t raise_limits() {
+  const void* const kernels[] = {(const void*)distill_ring_kernel<T, 0, LANES>, (const void*)distill_ring_kernel<T, 1, LANES>,
+                                 (const void*)distill_ring_kernel<T, 2, LANES>, (const void*)distill_ring_kernel<T, 3, LANES>,
+                                 (const void*)distill_ring_kernel<T, 4, LANES>};
+  cudaError_t e = cudaSuccess;
+  for (const void* k : kernels)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDistillSmem);
+  return e;
+}
+
+}  // namespace
+
 gbmuf_status gbmuf_setup_vocab_ops(gbmuf_ops* ops) {
   const int blocks = ops->num_sms * kLossBlocksPerSm;
   int unused[4];
-  cudaError_t e = count_clusters(distill_ring_kernel<float, 0>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][0]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<float, 1>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[0][1]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, 0>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][0]);
-  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<__nv_bfloat16, 1>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters[1][1]);
-  const void* const powers[] = {(const void*)distill_ring_kernel<float, 2>,         (const void*)distill_ring_kernel<float, 3>,
-                                (const void*)distill_ring_kernel<float, 4>,         (const void*)distill_ring_kernel<__nv_bfloat16, 2>,
-                                (const void*)distill_ring_kernel<__nv_bfloat16, 3>, (const void*)distill_ring_kernel<__nv_bfloat16, 4>};
-  for (const void* k : powers)                    // their threads and shared memory are those of mode 1
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDistillSmem);
+  cudaError_t e = raise_limits<float, kFewLanes>();
+  if (e == cudaSuccess) e = raise_limits<float, kListMost / 32>();
+  if (e == cudaSuccess) e = raise_limits<__nv_bfloat16, kFewLanes>();
+  if (e == cudaSuccess) e = raise_limits<__nv_bfloat16, kListMost / 32>();
+  // all of them have the same threads, shared memory and launch bounds
+  if (e == cudaSuccess) e = count_clusters(distill_ring_kernel<float, 1, kListMost / 32>, kDistillThreads, kDistillSmem, blocks, ops->distill_clusters);
   if (e == cudaSuccess) e = count_clusters(top_ring_kernel<float>, kLossThreads, kTopSmem, blocks, unused);
   if (e == cudaSuccess) e = count_clusters(top_ring_kernel<__nv_bfloat16>, kLossThreads, kTopSmem, blocks, unused);
   return launched("set-up of the vocabulary operators", e);
@@ -167,7 +180,8 @@ gbmuf_status gbmuf_distillation(gbmuf_ops* ops, const gbmuf_distillation_args* a
     P.k = a->k; P.split = 1; P.teacher_bf16 = a->teacher_dtype == GBMUF_BF16;
     P.T = a->temperature; P.hard = a->hard_weight; P.scale = a->scale; P.status = ops->d_status;
     cudaError_t e = cudaSuccess;
-    DISPATCH_DTYPE(a->dtype, T, e = launch_distill<T>(ops, P, (cudaStream_t)stream));
+    DISPATCH_DTYPE(a->dtype, T, e = a->k <= 32 * kFewLanes ? launch_distill<T, kFewLanes>(ops, P, (cudaStream_t)stream)
+                                                        : launch_distill<T, kListMost / 32>(ops, P, (cudaStream_t)stream));
     return launched("launch of the distillation kernel", e);
   });
 }
