@@ -3,11 +3,11 @@ own text, a gossip-BMUF round every H steps, the average at the end.
 
 Everything between the tokens and the new parameters runs through the library: the linear layers and
 their gradients (``linear_forward``, ``linear_backward_input``, ``linear_backward_weight``), the loss
-(``cross_entropy``), the gradient norm of each worker and clipping (``GradClip``), the Adagrad step
+(``cross_entropy``, or ``linear_cross_entropy`` for the softmax layer and the loss in one), the gradient norm of each worker and clipping (``GradClip``), the Adagrad step
 and the synchronisation round.  Weights are views into the workers' rows of theta and gradients are
 written straight into the rows of the optimiser's gradient buffer.
 
-    python examples/local_step_lm.py [--steps 200] [--workers 4] [--dtype bf16]
+    python examples/local_step_lm.py [--steps 200] [--workers 4] [--dtype bf16] [--no-scores]
 """
 from __future__ import annotations
 
@@ -52,17 +52,22 @@ class Model:
         return flat.to(dtype).to(device)
 
 
-def loss_and_gradients(ops, model, p, grad, words, targets):
+def loss_and_gradients(ops, model, p, grad, words, targets, keep_scores=True):
     """Forward and backward pass of one worker: fills the views ``grad`` (float32), returns the losses
-    of the batch's words (their mean is the objective)."""
+    of the batch's words (their mean is the objective).  Without ``keep_scores`` the softmax layer and
+    its loss are one call, and the scores of the vocabulary are never in memory."""
     n = words.shape[0]
     x = p["embedding"][words].reshape(n, 2 * model.width)
     h, z = ops.linear_forward(x, p["w1"], bias=p["b1"], activation="gelu", keep_z=True)
     y = ops.linear_forward(h, p["w2"], bias=p["b2"], residual=x)
-    scores = ops.linear_forward(y, p["ws"], bias=p["bs"])
-    loss, _, dscores = ops.cross_entropy(scores, targets, scale=1.0 / n, dlogits_out=scores)
-    ops.linear_backward_weight(dscores, y, dw_out=grad["ws"], dbias_out=grad["bs"])
-    dy = ops.linear_backward_input(dscores, p["ws"])
+    if keep_scores:
+        scores = ops.linear_forward(y, p["ws"], bias=p["bs"])
+        loss, _, dscores = ops.cross_entropy(scores, targets, scale=1.0 / n, dlogits_out=scores)
+        ops.linear_backward_weight(dscores, y, dw_out=grad["ws"], dbias_out=grad["bs"])
+        dy = ops.linear_backward_input(dscores, p["ws"])
+    else:
+        loss, _, dy, _, _ = ops.linear_cross_entropy(y, p["ws"], targets, bias=p["bs"], scale=1.0 / n,
+                                                     dw_out=grad["ws"], dbias_out=grad["bs"])
     ops.linear_backward_weight(dy, h, dw_out=grad["w2"], dbias_out=grad["b2"])
     dz = ops.linear_backward_input(dy, p["w2"], z_prev=z, activation="gelu")
     ops.linear_backward_weight(dz, x, dw_out=grad["w1"], dbias_out=grad["b1"])
@@ -81,7 +86,7 @@ def text(g, vocab, n, device):
 
 
 def train(steps=200, workers=4, vocab=64, width=48, hidden=256, batch=512, period=4, lr=0.1, clip=1.0,
-          dtype="f32", seed=0):
+          dtype="f32", seed=0, keep_scores=True):
     """Returns the mean loss of all workers at every step, and the averaged model."""
     device = torch.device("cuda", torch.cuda.current_device())
     kind = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
@@ -102,7 +107,7 @@ def train(steps=200, workers=4, vocab=64, width=48, hidden=256, batch=512, perio
         g.manual_seed(1000 * seed + k)
     history = []
     for t in range(1, steps + 1):
-        losses = [loss_and_gradients(ops, model, params[k], grads[k], *text(streams[k], vocab, batch, device))
+        losses = [loss_and_gradients(ops, model, params[k], grads[k], *text(streams[k], vocab, batch, device), keep_scores)
                   for k in range(workers)]
         clipping.clip(clip)
         ctx.local_adagrad(grad, accum, lr, eps=1e-8)
@@ -124,8 +129,9 @@ def main():
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--workers", type=int, default=4)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
+    ap.add_argument("--no-scores", action="store_true", help="never keep the vocabulary's scores in memory")
     a = ap.parse_args()
-    history, _ = train(steps=a.steps, workers=a.workers, dtype=a.dtype)
+    history, _ = train(steps=a.steps, workers=a.workers, dtype=a.dtype, keep_scores=not a.no_scores)
     for t in sorted({0, *range(9, len(history), max(1, len(history) // 10)), len(history) - 1}):
         print(f"step {t + 1:5d}  loss {history[t]:.4f}")
 

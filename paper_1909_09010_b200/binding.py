@@ -570,6 +570,8 @@ class LocalOps(_OnDevice):
     handed in that were last used on another stream are the caller's to guard, and a result has to
     be waited for before another stream reads it, as for any torch operation."""
 
+    _loss_bytes = {}                                             # workspace sizes of linear_cross_entropy
+
     def __init__(self, device=0):
         self._open(device)
         self._check(self._L.gbmuf_ops_create(device, ctypes.byref(self._h)))
@@ -775,12 +777,21 @@ class LocalOps(_OnDevice):
         lse = x.new_empty((rows,), dtype=torch.float32)
         fields = (rows, n_in, vocab, px, pw, pb, pt, pr, loss.data_ptr(), lse.data_ptr(), pdx, pdw, pdb, lx, lw, ldx,
                   ldw, ignore_index, piece, code, grad_code, 1 if accumulate else 0, scale)
-        args, need = _pack_linear_cross_entropy(*fields, 0, 0), ctypes.c_int64()
-        self._check(self._L.gbmuf_linear_cross_entropy_workspace(self._h, args, ctypes.byref(need)))
-        if need.value:
-            work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
-            args = _pack_linear_cross_entropy(*fields, work.data_ptr(), need.value)
-        self._check(self._L.gbmuf_linear_cross_entropy(self._h, args, self._raw_stream(dev)))
+        # the bytes follow from sizes, types, alignment and which results there are
+        key = (dev, rows, n_in, vocab, code, px & 15, pw & 15, lx, lw, piece, pdx != 0, pdw != 0, pdb != 0)
+        need = self._loss_bytes.get(key)
+        if need is None:
+            answer = ctypes.c_int64()
+            self._check(self._L.gbmuf_linear_cross_entropy_workspace(
+                self._h, _pack_linear_cross_entropy(*fields, 0, 0), ctypes.byref(answer)))
+            if len(self._loss_bytes) >= 256:
+                self._loss_bytes.clear()
+            need = self._loss_bytes[key] = answer.value
+        work = torch.empty(need, dtype=torch.uint8, device=x.device)
+        args = _pack_linear_cross_entropy(*fields, work.data_ptr() if need else 0, need)
+        st = self._L.gbmuf_linear_cross_entropy(self._h, args, self._raw_stream(dev))
+        if st != GBMUF_OK:
+            self._check(st)
         return (loss, lse, *results)
 
     def top_logits(self, logits, k, temperature=1.0, want_lse=True, values_out=None, index_out=None, lse_out=None,

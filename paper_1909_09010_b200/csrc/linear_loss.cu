@@ -56,33 +56,45 @@ gbmuf_status check(const gbmuf_ops* ops, const Args* a) {
   return GBMUF_OK;
 }
 
-// Logits of `words` words for `rows` rows, statistics: launch shape, tiles side by side, slots per row.
-struct StatsShape { TcShape tc; int at_once, slots; };
 // Row tiles whose CTAs fill at least nine tenths of the GPU when each keeps to one row tile.
 int rows_at_once(int tiles, int fit) {
   int t = std::min(tiles, fit);
   while (fit / t * t * 10 < fit * 9) --t;
   return t;
 }
-// The sum over a piece's words (dx): tiles as any product's, and the words cut into slices where tiles are few.
-// Times per step as in choose_shape.
-struct TermShape { int bn, pair, slices; double ns; };
-TermShape choose_term(const gbmuf_ops* ops, long long rows, long long cols, long long words, int parts) {
-  TermShape best{64, 1, 1, 1e300};
-  const long long ksteps = (words + 63) / 64;
+// ---- launch shapes.  Time of 64 terms of a tile of 128 pair x bn: what its operands take to arrive (98 bytes a
+// nanosecond and CTA of a pair, 110 of a single one) or its products to be formed (386 ns for 256 columns at the
+// rate of a library product; six products of fp32 parts), whichever is longer.  Measured with bf16, 2,048 x 1,024 x
+// 14,336: pairs of 256 400 ns, of 128 250, single CTAs of 256 460, of 128 290; fp32 pairs of 256 2,290.
+double step_time(int parts, int bn, int pair) {
+  return std::max(parts * (double)tc_stage_bytes(bn, pair) / (pair == 2 ? 98.0 : 110.0), (parts == 3 ? 6 : 1) * 386.0 * bn / 256.0);
+}
+struct Shape { int bn, pair, slices; double ns; };
+enum Purpose { kStatistics, kGradient, kWeight, kTerm };
+// The shape with the least time: rows R and columns C of the result, K terms.  fp32 sums leave the accumulator as they
+// go, so there the epilogue (15 ns a column) does not overlap the next tile's sums.  kStatistics: whole rounds of the
+// column tiles only.  kTerm: the terms are cut into slices where tiles are few, as many as fill one to three waves.
+Shape choose(const gbmuf_ops* ops, Purpose why, long long R, long long C, long long K, int parts) {
+  Shape best{64, 1, 1, 1e300};
+  const long long steps = (K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
-    for (int bn = pair == 2 ? 128 : 64; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2) {
-      const long long tiles = ((cols + 128 * pair - 1) / (128 * pair)) * ((rows + bn - 1) / bn), fit = ops->num_sms / pair;
-      const double step = std::max(100.0, parts * tc_stage_bytes(bn, pair) / 126.0);
-      for (int w = 1; w <= 3; ++w) {                       // as many as fill w waves
-        const long long n = std::max<long long>(1, std::min(ksteps / 4, w * fit / tiles));
-        const long long waves = (tiles * n + fit - 1) / fit;
-        const double t = waves * (1000.0 + (double)((ksteps + n - 1) / n) * step) + 15.0 * bn + 4.0 * n * rows * cols / 4000.0;
+    for (int bn = pair == 2 ? 128 : why == kTerm ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2) {
+      const long long across = (C + 128 * pair - 1) / (128 * pair), tiles = std::max<long long>(1, across * ((R + bn - 1) / bn));
+      long long fit = ops->num_sms / pair;
+      if (why == kStatistics) { const long long t = rows_at_once((int)std::min<long long>(std::max<long long>(across, 1), 1 << 20), (int)fit); fit = fit / t * t; }
+      const double step = step_time(parts, bn, pair), epilogue = 15.0 * bn;
+      for (int w = 1; w <= (why == kTerm ? 3 : 1); ++w) {
+        const long long n = why == kTerm ? std::max<long long>(1, std::min(steps / 4, w * fit / tiles)) : 1;
+        const double sums = (double)((steps + n - 1) / n) * step;
+        const double tile = parts == 3 ? 1000.0 + sums + epilogue : 1000.0 + std::max(sums, epilogue);
+        double t = ((tiles * n + fit - 1) / fit) * tile + (parts == 3 ? 0.0 : epilogue) + 0.001 * (n - 1) * R * C;
+        if (pair == 2) t = (parts == 1 ? 0.95 : 1.0) * t + 2000.0;           // a third less through L2: power for the products
         if (t < best.ns) best = {bn, pair, (int)n, t};
       }
     }
   return best;
 }
+TcShape tc_shape(const Shape& s) { return {s.bn, 1, s.pair}; }
 
 struct Plan {
   int parts;                                      // bf16 parts of an operand
@@ -91,18 +103,13 @@ struct Plan {
   int few_blocks;
   long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
-  TermShape term;
+  Shape term;
   long long x_off, w_off, target_off, slot_off, pair_off, word_off, weight_off, d_off, partial_off, acc_off, bytes;
 };
 
 Operand operand_x(const Args* a) { return {a->x, a->rows, a->n_in, a->ld_x, true, false, 0}; }
 Operand operand_w(const Args* a, long long v0, long long words) {
   return {static_cast<const char*>(a->w) + v0 * a->ld_w * (long long)size_of(a->dtype), words, a->n_in, a->ld_w, true, false, 0};
-}
-Product logits_product(const Plan& p, const Args* a, bool stats, long long rows, long long words) {
-  Product q{};
-  q.R = stats ? words : rows; q.C = stats ? rows : words; q.K = a->n_in; q.dtype = a->dtype;
-  return q;
 }
 int row_tiles(const TcShape& s, long long rows) { return (int)((rows + 128 * s.pair - 1) / (128 * s.pair)); }
 // Row tiles of the next launch of the statistics, with `left` rows to do.
@@ -111,18 +118,11 @@ int stats_slots(const gbmuf_ops* ops, const TcShape& s, int tiles_c, long long w
   return (int)std::min<long long>(ops->num_sms / s.pair / tiles_c, (words + s.bn - 1) / s.bn) * (kTcFinishers / 4);
 }
 
-// The product of a piece's gradient with x.  Pairs pay here with a strided operand too (bf16, 14,336 words, 2,048 x
-// 1,024: 48.9 us with pairs, 55.1 without).
-TcShape weight_shape(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
-  Product q{};
-  q.R = words; q.C = a->n_in; q.K = a->rows; q.dtype = a->dtype;
-  return choose_shape(ops, q, p.parts, false, false, false);
-}
-// The time of a piece by the model of the launch shapes, and a little for its launches.
+// The time of a piece by that model, and a little for its launches.
 double piece_time(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
-  double ns = choose_shape(ops, logits_product(p, a, false, a->rows, words), p.parts, false, false, false).ns + 5000.0;
-  if (a->dw) ns += weight_shape(ops, p, a, words).ns;
-  if (a->dx) ns += choose_term(ops, a->rows, a->n_in, words, p.parts).ns;
+  double ns = choose(ops, kGradient, a->rows, words, a->n_in, p.parts).ns + 5000.0;
+  if (a->dw) ns += choose(ops, kWeight, words, a->n_in, a->rows, p.parts).ns;
+  if (a->dx) ns += choose(ops, kTerm, a->rows, a->n_in, words, p.parts).ns;
   return ns;
 }
 // Words of a piece: what fits kPieceBytes, or a little less where that leaves fewer CTAs without a tile.
@@ -160,8 +160,8 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   p.ld_acc = round_up(a->n_in, 4);
   p.rows_padded = round_up(a->rows, kLossRowPad);
   const long long together = p.w_ready ? a->vocab : p.piece;
-  p.stats = choose_shape(ops, logits_product(p, a, true, a->rows, together), p.parts, false, false, false);
-  p.tc = choose_shape(ops, logits_product(p, a, false, a->rows, p.piece), p.parts, false, false, false);
+  p.stats = tc_shape(choose(ops, kStatistics, together, a->rows, a->n_in, p.parts));
+  p.tc = tc_shape(choose(ops, kGradient, a->rows, p.piece, a->n_in, p.parts));
   long long at = 0;
   auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
   p.x_off = take(p.x_ready || !products ? 0 : packed_bytes(operand_x(a), a->dtype));
@@ -190,7 +190,7 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
       p.partial_off = take(p.strips * p.ld_partial * 4);
     }
     if (a->dx) {
-      p.term = choose_term(ops, a->rows, a->n_in, p.piece, p.parts);
+      p.term = choose(ops, kTerm, a->rows, a->n_in, p.piece, p.parts);
       p.acc_off = take(p.term.slices * a->rows * p.ld_acc * 4);
     }
   }
@@ -400,7 +400,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     Operand xw = x, dw_b{d, words, N, p.ld_d, true, true, 0}, dx_b{d, words, N, p.ld_d, false, true, 0};
     xw.k_inner = false;
     if (a->dw) {
-      const TcShape shape = weight_shape(ops, p, a, words);
+      const TcShape shape = tc_shape(choose(ops, kWeight, words, a->n_in, a->rows, p.parts));
       TcParams W = tc_params(shape, words, H, false);
       W.ksteps = (int)((N + kTcK - 1) / kTcK);
       W.E.out0 = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); W.E.ld_out0 = a->ld_dw;
@@ -415,7 +415,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       // dx += d w, in fp32
       Operand wk = w;
       wk.k_inner = false;
-      TcShape shape{p.term.bn, 1, p.term.pair, 0.0};
+      TcShape shape{p.term.bn, 1, p.term.pair};
       TcParams D = tc_params(shape, N, H, false);
       D.ksteps = (int)((words + kTcK - 1) / kTcK);
       D.slices = p.term.slices;

@@ -75,14 +75,14 @@ int may_pair(const Product& q) {
 // by a model whose eight constants were fitted to 180 measured products of 12 to 100,000 rows, columns
 // and terms in both types (its choice was 0.8 % above the best one on average, 15 % at worst; no sum along
 // a vocabulary among them).  The 1.45 for pairs with a strided A says what was measured, not why.
-struct TcShape { int bn, split, pair; double ns; };
-TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided, bool may_split = true) {
-  TcShape best{64, 1, 1, 0.0};
+struct TcShape { int bn, split, pair; };
+TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool rows_64, bool a_strided) {
+  TcShape best{64, 1, 1};
   double best_t = 1e300;
   const long long ksteps = (q.K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
     for (int bn = pair == 2 ? 128 : rows_64 ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2)
-      for (int log = 0; log <= (pair == 2 || !may_split ? 0 : 3); ++log) {
+      for (int log = 0; log <= (pair == 2 ? 0 : 3); ++log) {
         const int split = 1 << log;
         const long long tiles = ((q.C + 128 * pair - 1) / (128 * pair)) * ((q.R + bn - 1) / bn);
         const long long fit = ops->tc_clusters[pair == 2 ? 1 : log];
@@ -94,7 +94,7 @@ TcShape choose_shape(const gbmuf_ops* ops, const Product& q, int parts, bool row
         const double sums = 1000.0 + (double)((ksteps + split - 1) / split) * step, epilogue = 15.0 * bn / split;
         double t = split > 1 ? waves * (sums + 1100.0 + 19.0 * bn) : waves * std::max(sums, epilogue);
         t += epilogue + (pair == 2 ? 2000.0 : 0.0);
-        if (t < best_t) { best_t = t; best = {bn, split, pair, t}; }
+        if (t < best_t) { best_t = t; best = {bn, split, pair}; }
       }
   return best;
 }
