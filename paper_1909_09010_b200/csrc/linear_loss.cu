@@ -72,7 +72,7 @@ double step_time(int parts, int bn, int pair) {
 struct Shape { int bn, pair, slices; double ns; };
 enum Purpose { kStatistics, kGradient, kWeight, kTerm };
 // The shape with the least time: rows R and columns C of the result, K terms.  fp32 sums leave the accumulator as they
-// go, so there the epilogue (15 ns a column) does not overlap the next tile's sums.  kStatistics: whole rounds of the
+// go, so there the epilogue (15 ns a column) does not overlap the next tile's sums where there are two accumulators.  kStatistics: whole rounds of the
 // column tiles only.  kTerm: the terms are cut into slices where tiles are few, as many as fill one to three waves.
 Shape choose(const gbmuf_ops* ops, Purpose why, long long R, long long C, long long K, int parts) {
   Shape best{64, 1, 1, 1e300};
@@ -86,8 +86,9 @@ Shape choose(const gbmuf_ops* ops, Purpose why, long long R, long long C, long l
       for (int w = 1; w <= (why == kTerm ? 3 : 1); ++w) {
         const long long n = why == kTerm ? std::max<long long>(1, std::min(steps / 4, w * fit / tiles)) : 1;
         const double sums = (double)((steps + n - 1) / n) * step;
-        const double tile = parts == 3 ? 1000.0 + sums + epilogue : 1000.0 + std::max(sums, epilogue);
-        double t = ((tiles * n + fit - 1) / fit) * tile + (parts == 3 ? 0.0 : epilogue) + 0.001 * (n - 1) * R * C;
+        const bool hidden = parts == 1 || bn <= 128;
+        const double tile = 1000.0 + (hidden ? std::max(sums, epilogue) : sums + epilogue);
+        double t = ((tiles * n + fit - 1) / fit) * tile + (hidden ? epilogue : 0.0) + 0.001 * (n - 1) * R * C;
         if (pair == 2) t = (parts == 1 ? 0.95 : 1.0) * t + 2000.0;           // a third less through L2: power for the products
         if (t < best.ns) best = {bn, pair, (int)n, t};
       }
@@ -125,14 +126,17 @@ double piece_time(const gbmuf_ops* ops, const Plan& p, const Args* a, long long 
   if (a->dx) ns += choose(ops, kTerm, a->rows, a->n_in, words, p.parts).ns;
   return ns;
 }
-// Words of a piece: what fits kPieceBytes, or a little less where that leaves fewer CTAs without a tile.
+// Words of a piece: what fits kPieceBytes (gradient and packed weights each), or a little less where that leaves fewer
+// CTAs without a tile.
 long long choose_piece(const gbmuf_ops* ops, const Plan& p, const Args* a) {
-  const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * a->rows) / 256 * 256);
+  long long wide = p.grad ? a->rows : 1;           // of what is in memory of a word: its gradient, its weights packed
+  if (!p.w_ready) wide = std::max(wide, round_up(a->n_in, 8));
+  const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * wide) / 256 * 256);
   if (a->vocab <= most) return a->vocab;
   const long long least = (a->vocab + most - 1) / most;
   long long best = most;
   double best_t = 1e300;
-  for (long long n = least; n <= least + least / 2 + 2; ++n) {
+  for (long long n = least; n <= least + std::min<long long>(least / 2 + 2, 16); ++n) {
     const long long piece = round_up((a->vocab + n - 1) / n, 256);
     if (piece < kPieceLeast && n > least) break;
     const long long whole = a->vocab / piece, rest = a->vocab % piece;

@@ -172,6 +172,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
+  // Accumulators in turn.  Where sums leave them as they go, the finishing warps' work at a tile's end holds the chunks
+  // up: narrow tiles have room for four (fp32 loss: see linear_loss.cuh).
+  constexpr int NACC = PROMOTE && KIND >= kLossStats && BN <= 128 ? 4 : 2, LOG_ACC = NACC / 2;
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int MOST = (KIND == kLossStats || KIND == kLossGrad) && !PROMOTE ? 32 : 16;
   constexpr int N = NCOL < MOST ? NCOL : MOST;    // of them at a time
@@ -181,7 +184,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 128u + 8u * s; };
   auto acc_full = [&](int b) { return bars + 256u + 8u * b; };
-  auto acc_empty = [&](int b) { return bars + 272u + 8u * b; };
+  auto acc_empty = [&](int b) { return bars + 288u + 8u * b; };
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + 320);
   const int warp = __shfl_sync(~0u, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
   const int S = P.stages;
@@ -192,7 +195,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), PAIR * kTcFinishers); }
+    for (int b = 0; b < NACC; ++b) { mbar_init(acc_full(b), 1); mbar_init(acc_empty(b), PAIR * kTcFinishers); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -200,10 +203,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   // its dependents start first thing) cannot be on this SM, whose registers or shared memory do not hold both.
   if (warp == 1) {
     if (PAIR == 1) {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)NACC * ACC) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     } else {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2u * ACC) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)NACC * ACC) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
   }
@@ -316,7 +319,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       int in_chunk = 0;
       const int iters = KIND == kLossTerm ? share(tile / P.tiles_fast).iters : whole.iters;
       for (int it = 0; it < iters; ++it) {
-        const uint32_t d = tmem + (uint32_t)(n & 1) * ACC;
+        const uint32_t d = tmem + (uint32_t)(n & (NACC - 1)) * ACC;
         const bool last = in_chunk + 1 == chunk || it == iters - 1;
         // with three parts: hi in stage s, lo in s1, mid in s2
         int s1 = s + 1, s2 = s + 2;
@@ -327,7 +330,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         }
         if (elect_one()) {
           if (in_chunk == 0) {
-            if (n >= 2) ok = ok && wait_phase(acc_empty(n & 1), ((n >> 1) & 1) ^ 1, P.status);
+            if (n >= NACC) ok = ok && wait_phase(acc_empty(n & (NACC - 1)), ((n >> LOG_ACC) & 1) ^ 1, P.status);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           }
           ok = ok && wait_phase(full(s), ph, P.status);
@@ -352,7 +355,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
           if (ok) {
             mma_commit<PAIR>(empty(s));
-            if (last) mma_commit<PAIR>(acc_full(n & 1));
+            if (last) mma_commit<PAIR>(acc_full(n & (NACC - 1)));
           }
         }
         ++in_chunk;
@@ -389,20 +392,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
           for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
           for (int ch = 0; ch < chunks; ++ch, ++n) {
-            ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+            ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
             ok = __all_sync(~0u, ok);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int j = 0; j < NCOL; j += N) {
               float v[N];
-              tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+              tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
 #pragma unroll
               for (int i = 0; i < N; ++i) acc[j + i] += v[i];
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            release(n & 1);
+            release(n & (NACC - 1));
           }
           if (!ok) break;
 #pragma unroll
@@ -414,7 +417,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           }
         } else {
           if (chunks > 0) {
-            ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+            ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
             ok = __all_sync(~0u, ok);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -422,13 +425,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll 1
           for (int j = 0; j < NCOL; j += N) {
             float v[N] = {};
-            if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+            if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
             S.add(P.E, v, r0 + j, P.R);
           }
           if (chunks > 0) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
-            release(n & 1);
+            release(n & (NACC - 1));
             ++n;
           }
         }
@@ -451,20 +454,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
         for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
         for (int ch = 0; ch < chunks; ++ch, ++n) {
-          ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+          ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
           ok = __all_sync(~0u, ok);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
           for (int j = 0; j < NCOL; j += N) {
             float v[N];
-            tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+            tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
 #pragma unroll
             for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          release(n & 1);
+          release(n & (NACC - 1));
         }
         if (!ok) break;
 #pragma unroll
@@ -486,7 +489,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_base + out_half; }
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
-          ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+          ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
           ok = __all_sync(~0u, ok);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -494,7 +497,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll 1
         for (int j = 0; j < NCOL; j += N) {
           float v[N] = {};
-          if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+          if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
           Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
           if constexpr (kTcOut<KIND, PARTS, BN> > 0) out_half ^= 2048u, F.room = out_base + out_half;
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          release(n & 1);
+          release(n & (NACC - 1));
           ++n;
         }
       }
@@ -526,20 +529,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
         for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
       for (int n = 0; n < chunks && ok; ++n) {
-        ok = mbar_wait_bounded(acc_full(n & 1), (n >> 1) & 1, P.status);
+        ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
         ok = __all_sync(~0u, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (PROMOTE && ok) {
 #pragma unroll
           for (int j = 0; j < NCOL; j += N) {
             float v[N];
-            tmem_ld<N>(my_tmem + (uint32_t)(n & 1) * ACC + j, v);
+            tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
 #pragma unroll
             for (int i = 0; i < N; ++i) acc[j + i] += v[i];
           }
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
-          release(n & 1);
+          release(n & (NACC - 1));
         }
       }
     }
@@ -583,8 +586,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (PAIR == 2) cluster_sync();                                   // nothing of this CTA is used any more
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (PAIR == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ACC) : "memory");
+    if (PAIR == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)NACC * ACC) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)NACC * ACC) : "memory");
   }
 }
 

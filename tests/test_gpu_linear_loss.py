@@ -155,6 +155,55 @@ def test_values_and_gradients(ops, dtype, rows, n_in, vocab):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,n_in,vocab", [(300, 40, 7), (70, 24, 1), (8, 520, 3001), (9, 64, 5000), (16, 72, 2500), (17, 72, 2500),
+                                             (4, 1000, 40_000), (2000, 24, 33), (33, 2056, 96)])
+def test_few_rows_few_words(ops, dtype, rows, n_in, vocab):
+    """On both sides of the rules for a few rows, and tiles wider than the vocabulary or the batch."""
+    x, w, t, b, rw = problem(gen(rows + vocab), rows, n_in, vocab, dtype)
+    R = reference(x, w, t, b, rw, 0.5)
+    for how in ("plain", "odd"):
+        got = ops.linear_cross_entropy(lay(x, how), lay(w, how), t, lay(b, how), row_weight=rw, scale=0.5)
+        check(got, R, dtype, dtype, how)
+        alone = ops.linear_cross_entropy(lay(x, how), lay(w, how), t, lay(b, how), row_weight=rw, scale=0.5, want_grad=False)
+        check(alone, R, dtype, dtype, how)
+    assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_masks_of_the_lowest_value(ops, dtype, rows):
+    """A bias of the type's lowest value: words that hardly occur, or a mask that leaves nothing (all words equal)."""
+    g = gen(rows)
+    n_in, vocab = 32, 700
+    x, w, t, b, rw = problem(g, rows, n_in, vocab, dtype)
+    lowest = torch.finfo(dtype).min
+    some = torch.where(torch.rand(vocab, device="cuda", generator=g) < 0.5, lowest, b.float()).to(dtype)
+    some[t[t != IGNORE]] = 0.0
+    for bias in (some, torch.full_like(b, lowest)):
+        z = x.double() @ w.double().t() + bias.double()
+        top = z.amax(1, keepdim=True)
+        if float(bias.max()) == lowest:
+            z = torch.zeros_like(z)                        # lowest plus anything of this size is lowest
+            top = torch.full_like(top, lowest)
+        else:
+            z, top = z - top, top
+        lse = torch.logsumexp(z, 1, keepdim=True)
+        valid = t != IGNORE
+        at = torch.where(valid, t, 0)[:, None]
+        s = torch.where(valid, rw.double(), 0.0)
+        loss = s * (lse - z.gather(1, at))[:, 0]
+        d = s[:, None] * (torch.exp(z - lse) - torch.zeros_like(z).scatter_(1, at, 1.0))
+        got = ops.linear_cross_entropy(x, w, t, bias, row_weight=rw, grad_dtype=F, piece=256)
+        # logits of a few units off by 1e-6, as their exponentials and sums
+        assert float((got[0].double() - loss).abs().max()) <= 1e-5 * (1 + float(loss.abs().max()))
+        assert float((got[1].double() - (top + lse)[:, 0]).abs().max()) <= 1e-5 * (1 + float((top + lse).abs().max()))
+        assert float((got[4].double() - d.sum(0)).abs().max()) <= 1e-5 * (1 + float(d.abs().sum(0).max()))
+        dw = d.t() @ x.double()
+        assert float((got[3].double() - dw).norm()) <= (2.0 ** -8 if dtype is BF else 2.0 ** -17) * float(dw.norm())
+    assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
 def test_accumulate_and_single_gradients(ops, dtype):
     g = gen(5)
     x, w, t, b, rw = problem(g, 150, 96, 777, dtype)
