@@ -62,27 +62,29 @@ int rows_at_once(int tiles, int fit) {
   while (fit / t * t * 10 < fit * 9) --t;
   return t;
 }
-// ---- launch shapes.  Time of 64 terms of a tile of 128 pair x bn: what its operands take to arrive (98 bytes a
+// ---- launch shapes.  Time of 64 terms of a tile of 128 pair x bn.  bf16: what its operands take to arrive (98 bytes a
 // nanosecond and CTA of a pair, 110 of a single one) or its products to be formed (386 ns for 256 columns at the
-// rate of a library product; six products of fp32 parts), whichever is longer.  Measured with bf16, 2,048 x 1,024 x
-// 14,336: pairs of 256 400 ns, of 128 250, single CTAs of 256 460, of 128 290; fp32 pairs of 256 2,290.
+// rate of a library product), whichever is longer; measured at 2,048 x 1,024 x 14,336: pairs of 256 400 ns, of 128
+// 250, single CTAs of 256 460, of 128 290.  fp32, six products: as measured at 2,048 x 512 x 20,000, bound by the
+// products for pairs of 256, by the shared memory that feeds them for the others.
 double step_time(int parts, int bn, int pair) {
-  return std::max(parts * (double)tc_stage_bytes(bn, pair) / (pair == 2 ? 98.0 : 110.0), (parts == 3 ? 6 : 1) * 386.0 * bn / 256.0);
+  if (parts == 3) return bn >= 256 ? 1800.0 : bn == 128 ? (pair == 2 ? 1100.0 : 1200.0) : bn == 64 ? 820.0 : 700.0;
+  return std::max((double)tc_stage_bytes(bn, pair) / (pair == 2 ? 98.0 : 110.0), 386.0 * bn / 256.0);
 }
 struct Shape { int bn, pair, slices; double ns; };
 enum Purpose { kStatistics, kGradient, kWeight, kTerm };
 // The shape with the least time: rows R and columns C of the result, K terms.  fp32 sums leave the accumulator as they
-// go, so there the epilogue (15 ns a column) does not overlap the next tile's sums where there are two accumulators.  kStatistics: whole rounds of the
+// go, so there the epilogue (15 ns a column; 45 of the gradient, with its three parts) does not overlap the next tile's sums where there are two accumulators.  kStatistics: whole rounds of the
 // column tiles only.  kTerm: the terms are cut into slices where tiles are few, as many as fill one to three waves.
 Shape choose(const gbmuf_ops* ops, Purpose why, long long R, long long C, long long K, int parts) {
   Shape best{64, 1, 1, 1e300};
   const long long steps = (K + 63) / 64;
   for (int pair = 1; pair <= 2; ++pair)
-    for (int bn = pair == 2 ? 128 : why == kTerm ? 64 : 32; bn <= (parts == 3 && pair == 1 ? 128 : 256); bn *= 2) {
+    for (int bn = pair == 2 ? 128 : why == kTerm ? 64 : 32; bn <= (parts == 3 && (pair == 1 || why == kGradient) ? 128 : 256); bn *= 2) {
       const long long across = (C + 128 * pair - 1) / (128 * pair), tiles = std::max<long long>(1, across * ((R + bn - 1) / bn));
       long long fit = ops->num_sms / pair;
       if (why == kStatistics) { const long long t = rows_at_once((int)std::min<long long>(std::max<long long>(across, 1), 1 << 20), (int)fit); fit = fit / t * t; }
-      const double step = step_time(parts, bn, pair), epilogue = 15.0 * bn;
+      const double step = step_time(parts, bn, pair), epilogue = (parts == 3 && why == kGradient ? 45.0 : 15.0) * bn;
       for (int w = 1; w <= (why == kTerm ? 3 : 1); ++w) {
         const long long n = why == kTerm ? std::max<long long>(1, std::min(steps / 4, w * fit / tiles)) : 1;
         const double sums = (double)((steps + n - 1) / n) * step;
@@ -202,16 +204,15 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   return p;
 }
 
-// Tensor map of a piece's gradient [words][rows], for stores of 32 rows by 32 words, or of its three parts, for stores of
-// 16 rows by 32 words of each.
+// Tensor map of a piece's gradient [parts][words][rows], for stores of 32 rows by 32 words.
 gbmuf_status gradient_map(const TcParams& P, int parts, CUtensorMap* map) {
   const EncodeTiledFn encode = encode_tiled_fn();
   if (!encode) return refuse(GBMUF_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-  const cuuint64_t dim[3] = {(cuuint64_t)P.R, (cuuint64_t)P.E.words, 3}, stride[2] = {(cuuint64_t)P.E.ld_out0 * 2, (cuuint64_t)P.E.part * 2};
-  const cuuint32_t box[3] = {parts == 1 ? 32u : 16u, 32, 3}, one[3] = {1, 1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, parts == 1 ? 2 : 3, P.E.out0, dim, stride, box, one,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, parts == 1 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
-                            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t dim[3] = {(cuuint64_t)P.R, (cuuint64_t)P.E.words, (cuuint64_t)parts};
+  const cuuint64_t stride[2] = {(cuuint64_t)P.E.ld_out0 * 2, (cuuint64_t)P.E.part * 2};
+  const cuuint32_t box[3] = {32, 32, 1}, one[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, P.E.out0, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return refuse(GBMUF_ERR_CUDA, "cuTensorMapEncodeTiled failed with code " + std::to_string((int)r));
   return GBMUF_OK;
 }
@@ -225,9 +226,11 @@ gbmuf_status launch_logits(const gbmuf_ops* ops, const TcShape& s, TcParams& P, 
     if (gbmuf_status rc = operand_map(a, dtype, nullptr, 128, &ma)) return rc;
     if (gbmuf_status rc = operand_map(b, dtype, nullptr, s.bn / s.pair, &mb)) return rc;
   }
-  if (s.pair == 2)
-    return s.bn == 128 ? launch_tc_at<KIND, T, T, PARTS, 128, 2>(ops, P, at_once, ma, mb, st, out)
-                       : launch_tc_at<KIND, T, T, PARTS, 256, 2>(ops, P, at_once, ma, mb, st, out);
+  if (s.pair == 2) {
+    if constexpr (KIND != kLossGrad || PARTS == 1)
+      if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 2>(ops, P, at_once, ma, mb, st, out);
+    return launch_tc_at<KIND, T, T, PARTS, 128, 2>(ops, P, at_once, ma, mb, st, out);
+  }
   if (s.bn == 32) return launch_tc_at<KIND, T, T, PARTS, 32, 1>(ops, P, at_once, ma, mb, st, out);
   if constexpr (PARTS == 1)
     if (s.bn == 256) return launch_tc_at<KIND, T, T, PARTS, 256, 1>(ops, P, at_once, ma, mb, st, out);

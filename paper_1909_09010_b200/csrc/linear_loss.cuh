@@ -112,15 +112,17 @@ template <int N> __device__ __forceinline__ void store_rows(__nv_bfloat16* to, c
 }
 
 // d is stored with the rows of the batch along memory ([words][rows]): a lane holds a word and has a strip of its
-// rows in one piece.  32 words of 32 rows (bf16) go through shared memory and leave by the copy engine: 32 stores to
-// 32 lines each would keep the load-store unit longer than the tile's product takes (1,024 x 512 x 18,944: 24.9
+// rows in one piece.  32 words of 32 rows (of each part) go through shared memory and leave by the copy engine: 32 stores
+// to 32 lines each would keep the load-store unit longer than the tile's product takes (1,024 x 512 x 18,944 bf16: 24.9
 // us, without any stores 19.8).  The 64-byte swizzle keeps a warp's 16-byte stores off the same banks.
 template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
   float column;              // sum over the strip's rows
-  // bf16, N 32: tensor map of d, boxes of 32 rows x 32 words; 2 KB of shared memory, what went out of it two strips ago
-  // has been read.  fp32, N 16: boxes of 16 rows x 32 words x 3 parts; 3 KB, the strip before has been read.
+  // N 32: tensor map of d's parts, boxes of 32 rows x 32 words of one.  bf16: the half of 4 KB of shared memory that comes
+  // next, and what turns it into the other one; what went out of a half two stores ago has been read.  fp32: 2 KB (and
+  // half 0), which the store before has left: three parts of both operands need the room for stages of the ring (1,003 x
+  // 515 x 10,007 on single CTAs: 85 -> 74 us).
   const CUtensorMap* map;
-  uint32_t room;
+  uint32_t room, half;
 
   __device__ __forceinline__ void ask(const Epilogue&, int, int, int, int, int) {}
   __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int, int lane, float bias, float (&v)[N]) {
@@ -159,60 +161,43 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
         column += v[i];
       }
     }
-    if constexpr (FAST && N == 32) {
-      if (r >= R || c - lane >= E.words) {                 // nothing of it exists; a group all the same, for the count of two
-        if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        return;
-      }
-      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-      __syncwarp();
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = pair_bf16(two(v[8 * q + 2 * i], v[8 * q + 2 * i + 1]));
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(room + 64u * lane + 16u * (q ^ (lane >> 1 & 3))), "r"(u[0]), "r"(u[1]),
-                     "r"(u[2]), "r"(u[3])
-                     : "memory");
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) {
-        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(r),
-                     "r"(c), "r"(room)
-                     : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-      }
-      return;
-    }
-    if constexpr (!FAST && N == 16) {
-      if (r >= R || c - lane >= E.words) return;
-      if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      __syncwarp();
+    if constexpr (N == 32) {
+      constexpr int PARTS = FAST ? 1 : 3;
+      const bool there = r < R && c - lane < E.words;
       Two rest[N / 2];
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) rest[i] = two(v[2 * i], v[2 * i + 1]);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        uint32_t u[N / 2];
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-          u[i] = pair_bf16(rest[i]);
-          if (q < 2) rest[i] = rest[i] - pair_f32(u[i]);
+      for (int q = 0; q < PARTS; ++q, room ^= half) {
+        if (!there) {                                      // a group all the same, for the count of two
+          if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          continue;
         }
+        if (lane == 0) {
+          if (FAST) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+          else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        }
+        __syncwarp();
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(room + 1024u * q + 32u * lane + 16u * (h ^ (lane >> 2 & 1))), "r"(u[4 * h]),
-                       "r"(u[4 * h + 1]), "r"(u[4 * h + 2]), "r"(u[4 * h + 3])
+        for (int p = 0; p < 4; ++p) {
+          uint32_t u[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            u[i] = pair_bf16(rest[4 * p + i]);
+            if (q + 1 < PARTS) rest[4 * p + i] = rest[4 * p + i] - pair_f32(u[i]);
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(room + 64u * lane + 16u * (p ^ (lane >> 1 & 3))), "r"(u[0]), "r"(u[1]),
+                       "r"(u[2]), "r"(u[3])
                        : "memory");
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) {
-        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
-                     "r"(r), "r"(c), "r"(0), "r"(room)
-                     : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
+                       "r"(r), "r"(c), "r"(q), "r"(room)
+                       : "memory");
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
       }
       return;
     }

@@ -51,10 +51,9 @@ struct TcParams {
 // of B's.  A stage of the ring holds 64 k of one part of both.
 __host__ __device__ constexpr uint32_t tc_stage_bytes(int bn, int pair) { return (128u + (uint32_t)(bn / pair)) * 128u; }
 constexpr uint32_t kTcHead = 1024;             // barriers and the tensor-memory address
-// Behind the ring: where the finishing warps lay results out for the copy engine (linear_loss.cuh), 4 KB each.
-// (Tiles too narrow for strips of that many rows store by themselves.)
-template <int KIND, int PARTS, int BN> constexpr uint32_t kTcOut =
-    KIND != kLossGrad ? 0u : PARTS == 1 ? (BN >= 128 ? 4096u * kTcFinishers : 0u) : BN >= 64 ? 3072u * kTcFinishers : 0u;
+// Behind the ring: where the finishing warps lay results out for the copy engine (linear_loss.cuh), 4 or 2 KB each.
+// (Tiles too narrow for strips of 32 rows store by themselves.)
+template <int KIND, int PARTS, int BN> constexpr uint32_t kTcOut = KIND == kLossGrad && BN >= 128 ? (PARTS == 1 ? 4096u : 2048u) * kTcFinishers : 0u;
 __host__ __device__ constexpr uint32_t tc_smem_bytes(int bn, int pair, int stages) {
   return 1024u + kTcHead + (uint32_t)stages * tc_stage_bytes(bn, pair);
 }
@@ -176,7 +175,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   // up: narrow tiles have room for four (fp32 loss: see linear_loss.cuh).
   constexpr int NACC = PROMOTE && KIND >= kLossStats && BN <= 128 ? 4 : 2, LOG_ACC = NACC / 2;
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
-  constexpr int MOST = (KIND == kLossStats || KIND == kLossGrad) && !PROMOTE ? 32 : 16;
+  constexpr int MOST = (KIND == kLossStats && !PROMOTE) || KIND == kLossGrad ? 32 : 16;
   constexpr int N = NCOL < MOST ? NCOL : MOST;    // of them at a time
   extern __shared__ __align__(128) unsigned char raw[];
   unsigned char* const smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
@@ -442,8 +441,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   if (KIND != kLossStats && warp >= 4 && P.split == 1) {
     int n = 0;
     bool ok = true;
+    // two halves in turn: from one address to the other and back
     const uint32_t out_base = ring + (uint32_t)S * STAGE + kTcOut<KIND, PARTS, BN> / kTcFinishers * (uint32_t)(warp - 4);
-    uint32_t out_half = 0;                                         // of the two, in turn
+    const uint32_t out_flip = PARTS == 1 ? out_base ^ (out_base + 2048u) : 0u;
+    uint32_t out_room = out_base;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const Share mine = share(w.c);
       const int c = mine.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL, chunks = mine.chunks;
@@ -474,19 +475,20 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int j = 0; j < NCOL; j += N) {
           Finisher<KIND, T, TO, N> F;
           if constexpr (KIND == kLossTerm) F.slice = mine.slice;
-          if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_base; }
+          if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_room; F.half = out_flip; }
           float v[N];
 #pragma unroll
           for (int i = 0; i < N; ++i) v[i] = acc[j + i];
           F.ask(P.E, r0 + j, c, P.R, P.C, lane);
           F.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
           if constexpr (KIND == kLossGrad) column += F.column;
+          if constexpr (kTcOut<KIND, PARTS, BN> > 0) out_room = F.room;
         }
       } else {
         // what the epilogue reads is requested one strip ahead, the first one during the sums
         Finisher<KIND, T, TO, N> F;
         if constexpr (KIND == kLossTerm) F.slice = mine.slice;
-        if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_base + out_half; }
+        if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_room; F.half = out_flip; }
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
           ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
@@ -500,9 +502,9 @@ __global__ void __launch_bounds__(kTcThreads, 1)
           if (chunks > 0) tmem_ld<N>(my_tmem + (uint32_t)(n & (NACC - 1)) * ACC + j, v);
           Finisher<KIND, T, TO, N> now = F;
           if (j + N < NCOL) F.ask(P.E, r0 + j + N, c, P.R, P.C, lane);
-          if constexpr (kTcOut<KIND, PARTS, BN> > 0) out_half ^= 2048u, F.room = out_base + out_half;
           now.finish(P.E, r0 + j, c, P.R, P.C, lane, to_f32(bias), v);
           if constexpr (KIND == kLossGrad) column += now.column;
+          if constexpr (kTcOut<KIND, PARTS, BN> > 0) out_room = F.room = now.room;
         }
         if (chunks > 0) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
