@@ -171,7 +171,7 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   long long at = 0;
   auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
   p.x_off = take(p.x_ready || !products ? 0 : packed_bytes(operand_x(a), a->dtype));
-  p.w_off = take(p.w_ready || !products ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype));
+  p.w_off = take(p.w_ready || !products ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype, true));
   p.target_off = take(a->rows * 4);
   const int per_block = (rounded >= 16 ? 2 : 4) * kRowsThreads / 32;
   p.few_blocks = (int)std::min<long long>((a->vocab + per_block - 1) / per_block, ops->num_sms * 2);
@@ -257,7 +257,7 @@ gbmuf_status launch_loss_product(const gbmuf_ops* ops, int bn, int pair, TcParam
 }
 
 gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, cudaStream_t st) {
-  const PackJob j = pack_job(ops, o, dtype, dst);
+  const PackJob j = pack_job(ops, o, dtype, dst, true);       // a piece of a single word might do in place, its matrix does not
   if (j.blocks == 0) return GBMUF_OK;
   return launched("launch of the operand-packing kernel",
                   launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)j.blocks, 1, 256, 0, st, j, PackJob{}));

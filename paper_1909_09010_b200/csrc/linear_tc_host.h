@@ -28,16 +28,17 @@ bool in_place(const Operand& o, int32_t dtype) {
   return o.ready || (dtype == GBMUF_BF16 && (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || (o.ld % 8 == 0 && o.ld < ((long long)1 << 38))));
 }
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
-long long packed_bytes(const Operand& o, int32_t dtype) {
-  return in_place(o, dtype) ? 0 : round_up((dtype == GBMUF_F32 ? 3 : 1) * o.outer * round_up(o.inner, 8) * 2, 256);
+long long packed_bytes(const Operand& o, int32_t dtype, bool always = false) {
+  return !always && in_place(o, dtype) ? 0 : round_up((dtype == GBMUF_F32 ? 3 : 1) * o.outer * round_up(o.inner, 8) * 2, 256);
 }
 long long product_workspace(const Product& q) {
   return q.K == 0 || q.R == 0 || q.C == 0 ? 0 : packed_bytes(q.a, q.dtype) + packed_bytes(q.b, q.dtype);
 }
 
-PackJob pack_job(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst) {
+// always: a part of a matrix that as a whole cannot be read in place.
+PackJob pack_job(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, bool always = false) {
   PackJob j{};
-  if (in_place(o, dtype)) return j;
+  if (!always && in_place(o, dtype)) return j;
   j.src = o.p; j.dst = static_cast<__nv_bfloat16*>(dst); j.ld = o.ld; j.outer = o.outer; j.inner = o.inner; j.ld_dst = round_up(o.inner, 8);
   j.vec = (uintptr_t)o.p % 16 == 0 && (o.outer <= 1 || o.ld * (long long)size_of(dtype) % 16 == 0);
   j.blocks = (int)std::min<long long>((o.outer * (j.ld_dst / 8) + 255) / 256, (long long)ops->num_sms * 16);

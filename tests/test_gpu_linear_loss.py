@@ -119,7 +119,7 @@ def check(got, R, dtype, grad_dtype, what, bias=True, before=None):
     inside(got[3], dw, ed_rounded.t() @ R["x"].abs() + (rows + 8) * 2.0 ** -23 * (d.abs().t() @ R["x"].abs()) + more,
            grad_dtype, what + " dw")
     if before is None:
-        close(got[3], dw, dtype, what + " dw")
+        close(got[3], dw, BF if BF in (dtype, grad_dtype) else F, what + " dw")
     if bias:
         db = d.sum(0) + b
         inside(got[4], db, ed.sum(0) + (rows + 8) * 2.0 ** -23 * d.abs().sum(0) + 2.0 ** -23 * db.abs(), grad_dtype,
@@ -166,6 +166,18 @@ def test_few_rows_few_words(ops, dtype, rows, n_in, vocab):
         check(got, R, dtype, dtype, how)
         alone = ops.linear_cross_entropy(lay(x, how), lay(w, how), t, lay(b, how), row_weight=rw, scale=0.5, want_grad=False)
         check(alone, R, dtype, dtype, how)
+    assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,n_in,vocab,piece", [(495, 170, 3, 1), (4, 3, 9, 2), (40, 7, 33, 16), (100, 8, 65, 64), (12, 40, 21, 5)])
+def test_pieces_of_a_single_word(ops, dtype, rows, n_in, vocab, piece):
+    """A piece of one word may be aligned where its matrix is not: it is packed like the others."""
+    x, w, t, b, rw = problem(gen(rows + vocab), rows, n_in, vocab, dtype)
+    R = reference(x, w, t, b, rw, 0.3)
+    for how in ("plain", "padded", "odd"):
+        got = ops.linear_cross_entropy(lay(x, how), lay(w, how), t, lay(b, how), row_weight=rw, scale=0.3, piece=piece)
+        check(got, R, dtype, dtype, how)
     assert ops.device_status() == 0
 
 
