@@ -447,3 +447,28 @@ def test_refusals(ops):
         assert L.gbmuf_linear_cross_entropy(ops._h, ctypes.byref(a), None) == binding.ERR_INVALID_ARG
         assert b"workspace" in L.gbmuf_last_error(None)
     assert ops.device_status() == 0
+
+
+def test_weights_past_two_to_the_31(ops):
+    """270,001 words of 8,000 bf16: the last words' gradients."""
+    g = gen(16)
+    rows, n_in, vocab = 40, 8000, 270_001
+    x = rnd(g, (rows, n_in), BF)
+    w = torch.empty((vocab, n_in), dtype=BF, device="cuda").normal_(0.0, 2.0 * n_in ** -0.5, generator=g)
+    t = torch.randint(vocab - 50, vocab, (rows,), device="cuda", generator=g)
+    loss, lse, dx, dw = ops.linear_cross_entropy(x, w, t, scale=1.0 / rows)
+    z = torch.cat([x.double() @ part.double().t() for part in w.split(30_000)], 1)
+    ref = torch.logsumexp(z, 1)
+    # z: an fp32 sum of 8,000 products, each step off by at most 2^-23 of a partial sum
+    ez = 8008 * 2.0 ** -23 * float((x.double().abs() @ w[-500:].double().abs().t()).max())
+    assert float((lse.double() - ref).abs().max()) <= ez + 1e-2
+    assert float((loss.double() * rows - (ref - z.gather(1, t[:, None])[:, 0])).abs().max()) <= 2 * ez + 1e-2
+    d = (torch.exp(z - ref[:, None]) - torch.zeros_like(z).scatter_(1, t[:, None], 1.0)) / rows
+    for words in (slice(0, 300), slice(vocab - 300, vocab)):
+        exact = d[:, words].t() @ x.double()
+        assert float((dw[words].double() - exact).norm()) <= 2.0 ** -7 * float(exact.norm())
+    exact = torch.zeros((rows, n_in), dtype=torch.float64, device="cuda")
+    for a in range(0, vocab, 30_000):
+        exact += d[:, a:a + 30_000] @ w[a:a + 30_000].double()
+    close(dx, exact, BF, "dx")
+    assert ops.device_status() == 0

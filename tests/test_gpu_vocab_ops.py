@@ -470,3 +470,60 @@ def test_distillation_refusals(ops):
     with pytest.raises(binding.GbmufError):
         ops.distillation(x, t[:, :0], ix[:, :0])
     assert ops.device_status() == 0
+
+
+def test_two_streams_at_once(ops):
+    """All three operators on two streams side by side, again and again, give the bits of one after another."""
+    g = gen(31)
+    jobs = []
+    for rows, vocab, dtype in ((300, 20_011, BF), (150, 9_001, F)):
+        x = rnd(g, (rows, vocab), dtype, 2.0)
+        t, ix, tlse = lists(g, x, 30, 2.0, dtype)
+        h, w, b = rnd(g, (rows, 72), dtype), rnd(g, (vocab, 72), dtype, 0.2), rnd(g, (vocab,), dtype)
+        targets = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+        jobs.append(lambda x=x, t=t, ix=ix, tlse=tlse, h=h, w=w, b=b, targets=targets: (
+            *ops.top_logits(x, 20), *ops.distillation(x, t, ix, teacher_lse=tlse, temperature=2.0, targets=targets, hard_weight=0.2),
+            *ops.linear_cross_entropy(h, w, targets, b, piece=4000)))
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    results = []
+    for _ in range(10):
+        for job, s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                results.append(job())
+    torch.cuda.synchronize()
+    for i, got in enumerate(results):
+        assert all(torch.equal(a, b) for a, b in zip(want[i % 2], got))
+    assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 2_000_003), (2, 700_001)])
+def test_very_long_rows(ops, rows, vocab):
+    """Rows of many chunks: groups of several chunks in the largest logits, every slice fetched twice in distillation."""
+    g = gen(vocab)
+    for dtype in (BF, F):
+        x = rnd(g, (rows, vocab), dtype, 2.0)
+        check_top(ops, x, 100)
+        t, ix, tlse = lists(g, x, 40, 2.0, dtype)
+        R = reference(x, t, ix, tlse, 2.0, None, 0.0, None, 1.0)
+        check(ops.distillation(x, t, ix, teacher_lse=tlse, temperature=2.0), R, dtype, vocab, "long")
+    many = rnd(g, (40, 400_003), F, 2.0)                   # a block to a row: more chunks than groups
+    check_top(ops, many.repeat(8, 1), 64)
+    assert ops.device_status() == 0
+
+
+def test_logits_past_two_to_the_31(ops):
+    """8,100 x 267,735 bf16 logits: the last rows, in place."""
+    g = gen(41)
+    rows, vocab, k = 8100, 267_735, 20
+    x = torch.empty((rows, vocab), dtype=BF, device="cuda").normal_(0.0, 2.0, generator=g)
+    last = x[-40:].clone()
+    values, index, lse = ops.top_logits(x, k, temperature=2.0)
+    want = largest(last, k)
+    assert torch.equal(index[-40:], want) and torch.equal(values[-40:], last.gather(1, want))
+    t = values.float() + 0.5
+    out = ops.distillation(x, t, index, temperature=2.0, dlogits_out=x)
+    R = reference(last, t[-40:], index[-40:], None, 2.0, None, 0.0, None, 1.0)
+    check([v[-40:] for v in out], R, BF, vocab, "last rows")
+    assert ops.device_status() == 0
