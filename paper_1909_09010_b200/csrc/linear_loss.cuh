@@ -22,7 +22,7 @@ constexpr int kLossRowPad = 256;   // rows of a tile, at most: the arrays cover 
 // Statistics of a row of the batch.  2,048 x 1,024 x 100,000 bf16: 263 us in short runs (1,595 TFLOP/s, tensor pipe 84 %
 // active), bound by the products; 1,024 x 512 x 267,735: 217 to 232 us (1,210 to 1,290 TFLOP/s): eight steps a tile, whose
 // epilogue takes as long.  Strips of 32 words: with 16 the loads' latencies and the tests cost 5 us more there.
-template <typename T, bool PROMOTE> struct RowStats {
+template <typename T> struct RowStats {
   static constexpr bool FAST = sizeof(T) == 2;
   float m = -INFINITY;
   Two s = two(0.0f, 0.0f);

@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (warp >= 4) {
       int n = 0;
       bool ok = true;
-      RowStats<T, PROMOTE> S;
+      RowStats<T> S;
       const int chunks = whole.chunks;
       for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
         S.open(P.E, w.c * TILE_C + side * 128 + quad * 32 + lane, P.C, w.r * (kTcFinishers / 4) + part);
