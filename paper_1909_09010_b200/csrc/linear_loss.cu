@@ -74,8 +74,9 @@ double step_time(int parts, int bn, int pair) {
 struct Shape { int bn, pair, slices; double ns; };
 enum Purpose { kStatistics, kGradient, kWeight, kTerm };
 // The shape with the least time: rows R and columns C of the result, K terms.  fp32 sums leave the accumulator as they
-// go, so there the epilogue (15 ns a column; 45 of the gradient, with its three parts) does not overlap the next tile's sums where there are two accumulators.  kStatistics: whole rounds of the
-// column tiles only.  kTerm: the terms are cut into slices where tiles are few, as many as fill one to three waves.
+// go, so there the epilogue (15 ns a column; 45 of the gradient, with its three parts) does not overlap the next tile's
+// sums where there are two accumulators.  kStatistics: whole rounds of the column tiles only.  kTerm: the terms are cut
+// into slices where tiles are few, as many as fill one to three waves.
 Shape choose(const gbmuf_ops* ops, Purpose why, long long R, long long C, long long K, int parts) {
   Shape best{64, 1, 1, 1e300};
   const long long steps = (K + 63) / 64;
