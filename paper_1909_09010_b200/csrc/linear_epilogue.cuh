@@ -138,7 +138,7 @@ enum LinearKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kLossStats = 3,
 // operands but the weight gradient, which is TO.
 //   forward      z = acc + bias[c]; out1 <- z; out0 <- act(z) + residual
 //   input grad   d = acc + residual; out0 <- d; out1 <- d * act'(z_in)
-//   weight grad  out0 <- acc (+ out0); loss weight: the same, of other operands
+//   weight grad  out0 <- acc (+ out0); loss weight: out0 <- scale acc (+ out0), of other operands
 //   loss stats, loss grad, loss term: linear_loss.cuh
 struct Epilogue {
   const void* bias;
@@ -158,6 +158,7 @@ struct Epilogue {
   long long ld_partial;
   long long part;            // kLossGrad, fp32: elements from one bf16 part of out0 to the next; kLossTerm: from one slice's
   int first_word, words;     // of the vocabulary's piece
+  float scale;               // kLossWeight: of the sums
 };
 
 // N rows of a warp's 32 neighbouring columns: lane l holds column c (= c of lane 0 + l) of rows
@@ -266,6 +267,10 @@ template <int KIND, typename T, typename TO, int N> struct Finisher {
         store_strip<T, WHOLE>(v, E.out1, E.ld_out1, r, c, R, C, E.pairs, lane);
       }
     } else {
+      if (KIND == kLossWeight) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= E.scale;
+      }
       if (E.accumulate) {
         Strip<TO, N> old;
         old.template load<WHOLE>(E.out0, E.ld_out0, r, c, R, C, E.pairs, lane);

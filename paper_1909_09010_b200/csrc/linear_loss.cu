@@ -400,7 +400,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       cudaError_t e = cudaSuccess;
       DISPATCH_DTYPE(a->grad_dtype, TO, e = launch(loss_bias_kernel<TO>, (unsigned)((n + 255) / 256), 1, 256, 0, st,
                                                    reinterpret_cast<const float*>(ws + p.partial_off), p.ld_partial, (int)p.strips, n,
-                                                   static_cast<TO*>(a->dbias) + first, (int)a->accumulate));
+                                                   static_cast<TO*>(a->dbias) + first, (int)a->accumulate, a->scale));
       if (e != cudaSuccess) return cuda_refuse("launch of the loss's bias-gradient kernel", e);
     }
     if (H == 0) continue;
@@ -413,6 +413,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       W.ksteps = (int)((N + kTcK - 1) / kTcK);
       W.E.out0 = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); W.E.ld_out0 = a->ld_dw;
       W.E.accumulate = a->accumulate;
+      W.E.scale = a->scale;
       W.E.pairs = a->grad_dtype == GBMUF_BF16 && (uintptr_t)W.E.out0 % 4 == 0 && H % 2 == 0 && (words == 1 || a->ld_dw % 2 == 0);
       gbmuf_status rc = GBMUF_OK;
       DISPATCH_DTYPE(a->grad_dtype, TO, (rc = launch_loss_product<kLossWeight, TO, TO, PARTS>(
@@ -436,7 +437,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       if (last) {
         const cudaError_t e = launch(loss_dx_kernel<T>, (unsigned)std::min<long long>(N, ops->num_sms * 8), 1, 256, 0, st,
                                      reinterpret_cast<const float*>(ws + p.acc_off), p.ld_acc, N * p.ld_acc, p.term.slices,
-                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H);
+                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H, a->scale);
         if (e != cudaSuccess) return cuda_refuse("launch of the loss's input-gradient kernel", e);
       }
     }

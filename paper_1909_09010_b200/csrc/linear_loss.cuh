@@ -10,8 +10,10 @@ namespace {
 // sum: rows of the batch lie along the lanes, words along the columns, so no two threads share a row's tile.
 // The second time (kLossGrad) words lie along the lanes and d = w (exp(z - m) / s - [target]) of a piece of
 // the vocabulary is stored, once, as the operand of the two products that follow: rounded to bf16, or for
-// fp32 as its three parts.  bf16: that rounding is off by at most 2^-9 of an element, and the products'
-// sums of many such elements by less.
+// fp32 as its three parts.  bf16: that rounding is off by at most 2^-8 of an element, and the products'
+// sums of many such elements by less.  w is the row's weight alone; the scale of all rows is a factor of the
+// finished fp32 sums: within d it would be rounded the same way in every row, so that 1 / 300 (say) would take
+// 0.2 % off every gradient, where a target's -1 is exact.
 
 // What kLossGrad needs of two rows of the batch, as two packed operands: minus their maxima, and weight / sum.
 // Next to it stand per row the target (-1: no word of the vocabulary; -2: the row's gradient is zero) and the
@@ -246,7 +248,7 @@ template <typename T, typename TO, int N> struct Finisher<kLossTerm, T, TO, N> {
 };
 template <typename T>
 __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long long ld, long long slice, int slices, T* dx, long long ld_dx,
-                                                      long long rows, int cols) {
+                                                      long long rows, int cols, float scale) {
   grid_launch_dependents();
   grid_dependency_wait();
   for (long long row = blockIdx.x; row < rows; row += gridDim.x)
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long l
       float s = *p;
 #pragma unroll 4
       for (int i = 1; i < slices; ++i) s += p[i * slice];
-      dx[row * ld_dx + c] = from_f32<T>(s);
+      dx[row * ld_dx + c] = from_f32<T>(s * scale);
     }
 }
 
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
   if (row < P.L.rows) {
     for (int i = 1; i < kJoinShares; ++i) join_stats(m, s, part[i][lane]);
     const long long t = P.L.targets[row];
-    const float w = P.L.scale * (P.L.row_weight ? P.L.row_weight[row] : 1.0f);
+    const float own = P.L.row_weight ? P.L.row_weight[row] : 1.0f, w = P.L.scale * own;
     const float x = target_inside(P.L, t) ? P.target_logit[row] : 0.0f;
     const RowOutcome o = row_outcome(P.L, m, s, x, t, w);
     report_target(P.L, t, w);
@@ -311,8 +313,8 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
     if (P.L.lse) P.L.lse[row] = o.lse;
     if (!o.zero) {
       offset = m == -INFINITY ? 0.0f : -m;
-      k = w / s;
-      weight = w;
+      k = own / s;
+      weight = own;
       target = (int)t;
     }
   }
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
 // dbias of a piece: the strips' sums in their order.
 template <typename TO>
 __global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, long long ld, int strips, long long words, TO* out,
-                                                        int accumulate) {
+                                                        int accumulate, float scale) {
   grid_launch_dependents();
   grid_dependency_wait();
   const long long c = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -334,6 +336,7 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, lo
   float t = 0.0f;
 #pragma unroll 8
   for (int i = 0; i < strips; ++i) t += partial[i * ld + c];
+  t *= scale;
   out[c] = from_f32<TO>(accumulate ? t + to_f32(out[c]) : t);
 }
 

@@ -472,3 +472,38 @@ def test_weights_past_two_to_the_31(ops):
         exact += d[:, a:a + 30_000] @ w[a:a + 30_000].double()
     close(dx, exact, BF, "dx")
     assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("rows,piece", [(3, 0), (300, 0), (142, 1500)])
+def test_the_scale_is_a_factor_of_finished_sums(ops, dtype, rows, piece):
+    """A mean's 1 / rows takes no digits from the gradients: they are those of scale 1, multiplied once."""
+    g = gen(91)
+    x, w, t, b, weight = problem(g, rows, 200, 4001, dtype, weighted=rows == 142)
+    scale = torch.tensor(1.0 / rows, dtype=F).item()
+    one, got = (ops.linear_cross_entropy(x, w, t, b, ignore_index=IGNORE, row_weight=weight, scale=s, grad_dtype=F,
+                                         piece=piece) for s in (1.0, scale))
+    for i, what in ((3, "dw"), (4, "dbias")) + (((2, "dx"),) if dtype is F else ()):
+        assert torch.equal(got[i], one[i] * scale), what
+    assert ops.device_status() == 0
+
+
+def test_a_mean_over_any_rows_is_as_exact_as_a_sum(ops):
+    """bf16, p small beside a target's 1: of d / scale a target's -1 + p, p < 2^-9, is rounded to -1 and so off by p, the
+    others by half a step.  1 / 300 rounded to bf16 is 2.1e-3 off; dw, projected on the exact one, must not be."""
+    g = gen(92)
+    rows, n_in, vocab = 300, 256, 20000
+    x, w, t, b, _ = problem(g, rows, n_in, vocab, BF, weighted=False, spread=0.25)
+    R = reference(x, w, t, b, None, 1.0 / rows)
+    got = ops.linear_cross_entropy(x, w, t, b, ignore_index=IGNORE, scale=1.0 / rows, grad_dtype=F)
+    p = torch.exp(R["z"] - R["lse"][:, None]) * (t != IGNORE)[:, None] / rows
+    valid = (t != IGNORE).nonzero()[:, 0]
+    off = HALF[BF] * p
+    off[valid, t[valid]] = p[valid, t[valid]]
+    assert float(off[valid, t[valid]].max()) * rows < 2.0 ** -9
+    exact = R["d"].t() @ R["x"]
+    bound = float(((off + R["ed"]).t() @ R["x"].abs()).norm() / exact.norm()) + rows * 2.0 ** -23
+    assert bound < 1e-3
+    mean = float((got[3].double() * exact).sum() / exact.square().sum())
+    assert abs(mean - 1) < bound, (mean, bound)
+    assert ops.device_status() == 0
