@@ -778,7 +778,7 @@ class LocalOps(_OnDevice):
         fields = (rows, n_in, vocab, px, pw, pb, pt, pr, loss.data_ptr(), lse.data_ptr(), pdx, pdw, pdb, lx, lw, ldx,
                   ldw, ignore_index, piece, code, grad_code, 1 if accumulate else 0, scale)
         # the bytes follow from sizes, types, alignment and which results there are
-        key = (dev, rows, n_in, vocab, code, px & 15, pw & 15, lx, lw, piece, pdx != 0, pdw != 0, pdb != 0)
+        key = (dev, rows, n_in, vocab, code, px & 15, pw & 15, lx, lw, piece, pdx != 0, pdw != 0, pdb != 0, pr != 0)
         need = self._loss_bytes.get(key)
         if need is None:
             answer = ctypes.c_int64()

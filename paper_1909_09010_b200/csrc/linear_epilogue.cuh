@@ -158,6 +158,7 @@ struct Epilogue {
   long long ld_partial;
   long long part;            // kLossGrad, fp32: elements from one bf16 part of out0 to the next; kLossTerm: from one slice's
   int first_word, words;     // of the vocabulary's piece
+  int rest_from;             // kLossGrad, bf16: rows from here on are the first ones again, of which the rounding's rest is stored
   float scale;               // kLossWeight: of the sums
 };
 

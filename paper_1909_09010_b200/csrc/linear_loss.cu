@@ -103,8 +103,9 @@ TcShape tc_shape(const Shape& s) { return {s.bn, 1, s.pair}; }
 struct Plan {
   int parts;                                      // bf16 parts of an operand
   bool grad, x_ready, w_ready;                    // ready: read in place
-  bool bias_once, few;                            // few: the statistics of a few rows, on the fp32 units
+  bool bias_once, few, twice;                     // few: the statistics of a few rows, on the fp32 units
   int few_blocks;
+  long long rows;                                 // of the gradients' products
   long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
   Shape term;
@@ -124,15 +125,15 @@ int stats_slots(const gbmuf_ops* ops, const TcShape& s, int tiles_c, long long w
 
 // The time of a piece by that model, and a little for its launches.
 double piece_time(const gbmuf_ops* ops, const Plan& p, const Args* a, long long words) {
-  double ns = choose(ops, kGradient, a->rows, words, a->n_in, p.parts).ns + 5000.0;
-  if (a->dw) ns += choose(ops, kWeight, words, a->n_in, a->rows, p.parts).ns;
-  if (a->dx) ns += choose(ops, kTerm, a->rows, a->n_in, words, p.parts).ns;
+  double ns = choose(ops, kGradient, p.rows, words, a->n_in, p.parts).ns + 5000.0;
+  if (a->dw) ns += choose(ops, kWeight, words, a->n_in, p.rows, p.parts).ns;
+  if (a->dx) ns += choose(ops, kTerm, p.rows, a->n_in, words, p.parts).ns;
   return ns;
 }
 // Words of a piece: what fits kPieceBytes (gradient and packed weights each), or a little less where that leaves fewer
 // CTAs without a tile.
 long long choose_piece(const gbmuf_ops* ops, const Plan& p, const Args* a) {
-  long long wide = p.grad ? a->rows : 1;           // of what is in memory of a word: its gradient, its weights packed
+  long long wide = p.grad ? p.rows : 1;           // of what is in memory of a word: its gradient, its weights packed
   if (!p.w_ready) wide = std::max(wide, round_up(a->n_in, 8));
   const long long most = std::max(kPieceLeast, kPieceBytes / (2 * p.parts * wide) / 256 * 256);
   if (a->vocab <= most) return a->vocab;
@@ -156,22 +157,24 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   // as the linear layer's rule for a few rows
   const int64_t most = a->dtype == GBMUF_F32 ? 16 : 8, rounded = a->rows <= 1 ? 1 : a->rows <= 2 ? 2 : a->rows <= 4 ? 4 : a->rows <= 8 ? 8 : 16;
   p.few = a->rows <= most && rounded * ((a->n_in + 7) / 8 * 8) * (int64_t)size_of(a->dtype) <= kRowsMostBytes;
-  p.x_ready = in_place(operand_x(a), a->dtype);
+  p.twice = p.grad && p.parts == 1 && a->row_weight && a->rows <= kLossTwice;
+  p.rows = p.twice ? 2 * a->rows : a->rows;
+  p.x_ready = !p.twice && in_place(operand_x(a), a->dtype);
   p.w_ready = in_place(operand_w(a, 0, a->vocab), a->dtype);
   const bool products = p.grad || !p.few;         // operands of the tensor cores are needed
   p.piece = a->piece ? std::min<long long>(a->piece, a->vocab) : p.grad || (!p.w_ready && products) ? choose_piece(ops, p, a) : a->vocab;
   p.pieces = (a->vocab + p.piece - 1) / p.piece;
   p.ld_x = p.x_ready && a->rows > 1 ? a->ld_x : round_up(a->n_in, 8);      // the stride of a single row says nothing
   p.ld_w = p.w_ready && a->vocab > 1 ? a->ld_w : round_up(a->n_in, 8);
-  p.ld_d = round_up(a->rows, 64);                 // whole strips of rows are stored
+  p.ld_d = round_up(p.rows, 64);                 // whole strips of rows are stored
   p.ld_acc = round_up(a->n_in, 4);
-  p.rows_padded = round_up(a->rows, kLossRowPad);
+  p.rows_padded = round_up(p.rows, kLossRowPad);
   const long long together = p.w_ready ? a->vocab : p.piece;
   p.stats = tc_shape(choose(ops, kStatistics, together, a->rows, a->n_in, p.parts));
-  p.tc = tc_shape(choose(ops, kGradient, a->rows, p.piece, a->n_in, p.parts));
+  p.tc = tc_shape(choose(ops, kGradient, p.rows, p.piece, a->n_in, p.parts));
   long long at = 0;
   auto take = [&](long long bytes) { const long long here = at; at += round_up(bytes, 256); return here; };
-  p.x_off = take(p.x_ready || !products ? 0 : packed_bytes(operand_x(a), a->dtype));
+  p.x_off = take(p.x_ready || !products ? 0 : packed_bytes(operand_x(a), a->dtype, true) * (p.twice ? 2 : 1));
   p.w_off = take(p.w_ready || !products ? 0 : packed_bytes(operand_w(a, 0, p.piece), a->dtype, true));
   p.target_off = take(a->rows * 4);
   const int per_block = (rounded >= 16 ? 2 : 4) * kRowsThreads / 32;
@@ -191,14 +194,14 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
     p.d_off = take(p.piece * p.ld_d * 2 * p.parts);
     if (a->dbias) {
       // the strips' sums of all words, added up once at the end, unless that takes too much room
-      p.strips = (a->rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
+      p.strips = (p.rows + p.tc.bn - 1) / p.tc.bn * (kTcFinishers / 4);
       p.bias_once = p.strips * a->vocab * 4 <= kPieceBytes;
       p.ld_partial = p.bias_once ? a->vocab : p.piece;
       p.partial_off = take(p.strips * p.ld_partial * 4);
     }
     if (a->dx) {
-      p.term = choose(ops, kTerm, a->rows, a->n_in, p.piece, p.parts);
-      p.acc_off = take(p.term.slices * a->rows * p.ld_acc * 4);
+      p.term = choose(ops, kTerm, p.rows, a->n_in, p.piece, p.parts);
+      p.acc_off = take(p.term.slices * p.rows * p.ld_acc * 4);
     }
   }
   p.bytes = at;
@@ -257,11 +260,17 @@ gbmuf_status launch_loss_product(const gbmuf_ops* ops, int bn, int pair, TcParam
                   : launch_tc_at<KIND, T, TO, PARTS, 128, 1>(ops, P, at_once, ma, mb, st);
 }
 
-gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, cudaStream_t st) {
+// twice: and once more behind it
+gbmuf_status pack(const gbmuf_ops* ops, const Operand& o, int32_t dtype, void* dst, bool twice, cudaStream_t st) {
   const PackJob j = pack_job(ops, o, dtype, dst, true);       // a piece of a single word might do in place, its matrix does not
   if (j.blocks == 0) return GBMUF_OK;
+  PackJob again{};
+  if (twice) {
+    again = j;
+    again.dst = j.dst + j.outer * j.ld_dst;
+  }
   return launched("launch of the operand-packing kernel",
-                  launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)j.blocks, 1, 256, 0, st, j, PackJob{}));
+                  launch(dtype == GBMUF_F32 ? pack_kernel<float> : pack_kernel<__nv_bfloat16>, (unsigned)(j.blocks + again.blocks), 1, 256, 0, st, j, again));
 }
 
 // A few rows: one read of the weights on the fp32 units, as in the linear layer.
@@ -292,10 +301,10 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
   if (p.bytes > a->workspace_bytes || !a->workspace || (uintptr_t)a->workspace % 256 != 0)
     return invalid("workspace must be 256-byte aligned device memory of at least " + std::to_string(p.bytes) + " bytes");
   char* const ws = static_cast<char*>(a->workspace);
-  const long long N = a->rows, V = a->vocab, H = a->n_in, size = (long long)sizeof(T);
+  const long long N = a->rows, G = p.rows, V = a->vocab, H = a->n_in, size = (long long)sizeof(T);
   Operand x = operand_x(a);
   if (!p.x_ready && (p.grad || !p.few)) {
-    if (gbmuf_status rc = pack(ops, x, a->dtype, ws + p.x_off, st)) return rc;
+    if (gbmuf_status rc = pack(ops, x, a->dtype, ws + p.x_off, p.twice, st)) return rc;
     x.p = ws + p.x_off;
   }
   x.ld = p.ld_x;
@@ -306,7 +315,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     w = operand_w(a, v0, words);
     if (!p.w_ready) {
       if (packed != v0)
-        if (gbmuf_status rc = pack(ops, w, a->dtype, ws + p.w_off, st)) return rc;
+        if (gbmuf_status rc = pack(ops, w, a->dtype, ws + p.w_off, false, st)) return rc;
       packed = v0;
       w.p = ws + p.w_off;
     }
@@ -324,7 +333,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     return P;
   };
   const TcShape& s = p.stats;
-  const long long most_tiles = std::max((V / s.bn + 1) * (N / 128 + 1), (V / 128 + 1) * (N / p.tc.bn + 1));
+  const long long most_tiles = std::max((V / s.bn + 1) * (N / 128 + 1), (V / 128 + 1) * (G / p.tc.bn + 1));
   if (most_tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles of logits");
   // ---- statistics: every CTA keeps to one row tile, so its threads keep a row's running maximum and sum
   for (long long r0 = 0; r0 < N;) {
@@ -370,7 +379,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       J.targets = reinterpret_cast<int*>(ws + p.word_off) + r0;
       J.weights = reinterpret_cast<float*>(ws + p.weight_off) + r0;
     }
-    J.ld = ld; J.count = slots;
+    J.ld = ld; J.count = slots; J.twice = p.twice;
     J.rows_padded = r0 + n == N ? p.rows_padded - r0 : n;
     const cudaError_t e = launch(loss_join_kernel, (unsigned)((J.rows_padded + 31) / 32), 1, 32 * kJoinShares, 0, st, J);
     if (e != cudaSuccess) return cuda_refuse("launch of the loss's join kernel", e);
@@ -378,13 +387,14 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
   }
   if (!p.grad) return GBMUF_OK;
   // ---- gradients, a piece of the vocabulary at a time
+  x.outer = G;
   for (long long i = 0, v0 = 0; v0 < V; ++i, v0 += p.piece) {
     const long long words = std::min(p.piece, V - v0);
     const bool last = v0 + words == V;
     Operand w;
     if (gbmuf_status rc = weights(v0, words, w)) return rc;
     void* const d = ws + p.d_off;
-    TcParams P = tc_params(p.tc, N, words, false);
+    TcParams P = tc_params(p.tc, G, words, false);
     P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
     P.E.loss_rows = ws + p.pair_off;
     P.E.loss_targets = reinterpret_cast<const int*>(ws + p.word_off);
@@ -392,6 +402,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     P.E.partial = a->dbias ? reinterpret_cast<float*>(ws + p.partial_off) + (p.bias_once ? v0 : 0) : nullptr;
     P.E.ld_partial = p.ld_partial;
     P.E.first_word = (int)v0; P.E.words = (int)words;
+    P.E.rest_from = p.twice ? (int)N : 0x7fffffff;
     P.E.out0 = d; P.E.ld_out0 = p.ld_d; P.E.part = words * p.ld_d;
     const int at_once = std::min(P.tiles, ops->num_sms / p.tc.pair);
     if (gbmuf_status rc = launch_logits<kLossGrad, T, PARTS>(ops, p.tc, P, at_once, w, x, a->dtype, st)) return rc;
@@ -405,12 +416,12 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     }
     if (H == 0) continue;
     // dw = d^T x: columns along the lanes, d's rows next to one another
-    Operand xw = x, dw_b{d, words, N, p.ld_d, true, true, 0}, dx_b{d, words, N, p.ld_d, false, true, 0};
+    Operand xw = x, dw_b{d, words, G, p.ld_d, true, true, 0}, dx_b{d, words, G, p.ld_d, false, true, 0};
     xw.k_inner = false;
     if (a->dw) {
-      const TcShape shape = tc_shape(choose(ops, kWeight, words, a->n_in, a->rows, p.parts));
+      const TcShape shape = tc_shape(choose(ops, kWeight, words, a->n_in, G, p.parts));
       TcParams W = tc_params(shape, words, H, false);
-      W.ksteps = (int)((N + kTcK - 1) / kTcK);
+      W.ksteps = (int)((G + kTcK - 1) / kTcK);
       W.E.out0 = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); W.E.ld_out0 = a->ld_dw;
       W.E.accumulate = a->accumulate;
       W.E.scale = a->scale;
@@ -425,19 +436,19 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       Operand wk = w;
       wk.k_inner = false;
       TcShape shape{p.term.bn, 1, p.term.pair};
-      TcParams D = tc_params(shape, N, H, false);
+      TcParams D = tc_params(shape, G, H, false);
       D.ksteps = (int)((words + kTcK - 1) / kTcK);
       D.slices = p.term.slices;
       D.tiles_c = D.tiles / D.tiles_fast;
       D.tiles *= D.slices;
-      D.E.out0 = ws + p.acc_off; D.E.ld_out0 = p.ld_acc; D.E.part = N * p.ld_acc; D.E.accumulate = i > 0;
+      D.E.out0 = ws + p.acc_off; D.E.ld_out0 = p.ld_acc; D.E.part = G * p.ld_acc; D.E.accumulate = i > 0;
       if (gbmuf_status rc = launch_loss_product<kLossTerm, T, float, PARTS>(ops, shape.bn, shape.pair, D, std::min(D.tiles, ops->num_sms / shape.pair),
                                                                             wk, dx_b, a->dtype, st))
         return rc;
       if (last) {
         const cudaError_t e = launch(loss_dx_kernel<T>, (unsigned)std::min<long long>(N, ops->num_sms * 8), 1, 256, 0, st,
-                                     reinterpret_cast<const float*>(ws + p.acc_off), p.ld_acc, N * p.ld_acc, p.term.slices,
-                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H, a->scale);
+                                     reinterpret_cast<const float*>(ws + p.acc_off), p.ld_acc, G * p.ld_acc, p.term.slices,
+                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H, a->scale, p.twice);
         if (e != cudaSuccess) return cuda_refuse("launch of the loss's input-gradient kernel", e);
       }
     }

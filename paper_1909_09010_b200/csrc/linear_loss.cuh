@@ -13,13 +13,16 @@ namespace {
 // fp32 as its three parts.  bf16: that rounding is off by at most 2^-8 of an element, and the products'
 // sums of many such elements by less.  w is the row's weight alone; the scale of all rows is a factor of the
 // finished fp32 sums: within d it would be rounded the same way in every row, so that 1 / 300 (say) would take
-// 0.2 % off every gradient, where a target's -1 is exact.
+// 0.2 % off every gradient, where a target's -1 is exact.  Weights of the rows are rounded as they come, by 2^-9 or
+// so, and over many rows on average; up to kLossTwice weighted rows, which fill half a step of the sums and half a
+// tile at most, come a second time instead, with what the rounding left: 16 bits of d (32 x 512 x 10,000: 47 -> 56 us).
 
 // What kLossGrad needs of two rows of the batch, as two packed operands: minus their maxima, and weight / sum.
 // Next to it stand per row the target (-1: no word of the vocabulary; -2: the row's gradient is zero) and the
 // weight.
 struct __align__(16) RowPair { float m[2], k[2]; };
 constexpr int kLossRowPad = 256;   // rows of a tile, at most: the arrays cover all tiles
+constexpr int kLossTwice = 32;
 
 // Statistics of a row of the batch.  2,048 x 1,024 x 100,000 bf16: 263 us in short runs (1,595 TFLOP/s, tensor pipe 84 %
 // active), bound by the products; 1,024 x 512 x 267,735: 217 to 232 us (1,210 to 1,290 TFLOP/s): eight steps a tile, whose
@@ -163,6 +166,14 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
         column += v[i];
       }
     }
+    if (FAST && r + N > E.rest_from) {
+      column = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (r + i < E.rest_from) column += v[i];
+        else v[i] -= __bfloat162float(__float2bfloat16_rn(v[i]));
+      }
+    }
     if constexpr (N == 32) {
       constexpr int PARTS = FAST ? 1 : 3;
       const bool there = r < R && c - lane < E.words;
@@ -248,7 +259,7 @@ template <typename T, typename TO, int N> struct Finisher<kLossTerm, T, TO, N> {
 };
 template <typename T>
 __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long long ld, long long slice, int slices, T* dx, long long ld_dx,
-                                                      long long rows, int cols, float scale) {
+                                                      long long rows, int cols, float scale, bool twice) {
   grid_launch_dependents();
   grid_dependency_wait();
   for (long long row = blockIdx.x; row < rows; row += gridDim.x)
@@ -257,6 +268,8 @@ __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long l
       float s = *p;
 #pragma unroll 4
       for (int i = 1; i < slices; ++i) s += p[i * slice];
+      if (twice)
+        for (int i = 0; i < slices; ++i) s += p[i * slice + rows * ld];
       dx[row * ld_dx + c] = from_f32<T>(s * scale);
     }
 }
@@ -272,7 +285,7 @@ struct JoinParams {
   int* targets;
   float* weights;
   long long ld, rows_padded;
-  int count;
+  int count, twice;          // twice: the gradients have the rows a second time
 };
 __device__ __forceinline__ void join_stats(float& m, float& s, float2 o) {
   const float top = fmaxf(m, o.x);
@@ -319,10 +332,14 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
     }
   }
   if (!P.pairs) return;
-  P.pairs[row / 2].m[row & 1] = offset;
-  P.pairs[row / 2].k[row & 1] = k;
-  P.targets[row] = target;
-  P.weights[row] = weight;
+  const bool again = P.twice && row < P.L.rows;
+  if (P.twice && !again && row < 2 * P.L.rows) return;     // its first time's thread has it
+  for (long long at = row; at <= row + (again ? P.L.rows : 0); at += P.L.rows) {
+    P.pairs[at / 2].m[at & 1] = offset;
+    P.pairs[at / 2].k[at & 1] = k;
+    P.targets[at] = target;
+    P.weights[at] = weight;
+  }
 }
 
 // dbias of a piece: the strips' sums in their order.

@@ -507,3 +507,23 @@ def test_a_mean_over_any_rows_is_as_exact_as_a_sum(ops):
     mean = float((got[3].double() * exact).sum() / exact.square().sum())
     assert abs(mean - 1) < bound, (mean, bound)
     assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("rows,n_in,vocab,piece", [(1, 64, 1000, 0), (1, 70, 4001, 1000), (2, 1024, 5003, 0), (5, 33, 20_000, 0),
+                                                  (9, 512, 3001, 0), (31, 515, 1027, 300), (32, 256, 40_001, 0)])
+def test_few_rows_have_two_parts(ops, rows, n_in, vocab, piece):
+    """bf16, up to 32 rows: d is taken as two bf16 parts, the second one of what the first one's rounding left, so it is
+    off by half a step of half a step; dw and dbias are asked for in fp32."""
+    g = gen(rows + n_in + vocab)
+    x, w, t, b, rw = problem(g, rows, n_in, vocab, BF)
+    R = reference(x, w, t, b, rw, 1.0 / rows)
+    d, ed = R["d"], R["ed"]
+    er = ed + HALF[BF] ** 2 * (d.abs() + ed)
+    for how in ("plain", "odd"):
+        got = ops.linear_cross_entropy(lay(x, how), lay(w, how), t, lay(b, how), ignore_index=IGNORE, row_weight=rw,
+                                       scale=1.0 / rows, grad_dtype=F, piece=piece)
+        inside(got[0], R["loss"], R["eloss"], F, "loss")
+        inside(got[2], d @ R["w"], er @ R["w"].abs() + (vocab + 8) * 2.0 ** -23 * (d.abs() @ R["w"].abs()), BF, "dx")
+        inside(got[3], d.t() @ R["x"], er.t() @ R["x"].abs() + (2 * rows + 8) * 2.0 ** -23 * (d.abs().t() @ R["x"].abs()), F, "dw")
+        inside(got[4], d.sum(0), ed.sum(0) + (rows + 8) * 2.0 ** -23 * d.abs().sum(0), F, "dbias")
+    assert ops.device_status() == 0
