@@ -138,7 +138,7 @@ enum LinearKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kLossStats = 3,
 // operands but the weight gradient, which is TO.
 //   forward      z = acc + bias[c]; out1 <- z; out0 <- act(z) + residual
 //   input grad   d = acc + residual; out0 <- d; out1 <- d * act'(z_in)
-//   weight grad  out0 <- acc (+ out0); loss weight: out0 <- scale acc (+ out0), of other operands
+//   weight grad  out0 <- acc (+ out0); loss weight: out0 <- factor scale acc (+ out0), of other operands
 //   loss stats, loss grad, loss term: linear_loss.cuh
 struct Epilogue {
   const void* bias;
@@ -152,14 +152,17 @@ struct Epilogue {
   // of the loss alone
   const void* loss_rows;     // kLossStats: int64 targets; kLossGrad: RowPair
   const int* loss_targets;   // kLossGrad
-  const float* loss_weights; // kLossGrad
+  const float* loss_weights; // kLossGrad; kLossStats: row weights, where weight_max is wanted
   float* target_logit;       // kLossStats
   void* partial;             // kLossStats: float2 [slots][ld_partial]; kLossGrad: float [strips][ld_partial] or NULL
   long long ld_partial;
   long long part;            // kLossGrad, fp32: elements from one bf16 part of out0 to the next; kLossTerm: from one slice's
   int first_word, words;     // of the vocabulary's piece
   int rest_from;             // kLossGrad, bf16: rows from here on are the first ones again, of which the rounding's rest is stored
-  float scale;               // kLossWeight: of the sums
+  float scale;               // kLossWeight: of the sums; kLossStats: of the weights
+  const float* factor;       // kLossWeight: of the sums too, in device memory, or NULL
+  float* weight_max;         // kLossStats: the largest weight of each 32 rows, or NULL
+  long long vocab, ignore_index;     // kLossStats, for weight_max
 };
 
 // N rows of a warp's 32 neighbouring columns: lane l holds column c (= c of lane 0 + l) of rows
@@ -234,6 +237,7 @@ __device__ __forceinline__ void store_strip(const float (&v)[N], void* base, lon
 // The epilogue of N rows.  ask() requests what the epilogue reads, early; finish() takes the sums.
 template <int KIND, typename T, typename TO, int N> struct Finisher {
   Strip<T, N> first, second;          // residual (or dw), z_in
+  float factor;                       // kLossWeight
 
   template <bool WHOLE>
   __device__ __forceinline__ void ask_(const Epilogue& E, int r, int c, int R, int C, int lane) {
@@ -270,7 +274,7 @@ template <int KIND, typename T, typename TO, int N> struct Finisher {
     } else {
       if (KIND == kLossWeight) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] *= E.scale;
+        for (int i = 0; i < N; ++i) v[i] = v[i] * factor * E.scale;
       }
       if (E.accumulate) {
         Strip<TO, N> old;

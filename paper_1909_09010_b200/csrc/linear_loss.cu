@@ -103,13 +103,13 @@ TcShape tc_shape(const Shape& s) { return {s.bn, 1, s.pair}; }
 struct Plan {
   int parts;                                      // bf16 parts of an operand
   bool grad, x_ready, w_ready;                    // ready: read in place
-  bool bias_once, few, twice;                     // few: the statistics of a few rows, on the fp32 units
+  bool bias_once, few, twice, relative;           // few: the statistics of a few rows, on the fp32 units; relative: weights over the largest one
   int few_blocks;
   long long rows;                                 // of the gradients' products
   long long piece, pieces, ld_x, ld_w, ld_d, ld_acc, ld_partial, rows_padded, strips;
   TcShape stats, tc;                              // of the two products that form the logits
   Shape term;
-  long long x_off, w_off, target_off, slot_off, pair_off, word_off, weight_off, d_off, partial_off, acc_off, bytes;
+  long long x_off, w_off, target_off, slot_off, max_off, pair_off, word_off, weight_off, d_off, partial_off, acc_off, bytes;
 };
 
 Operand operand_x(const Args* a) { return {a->x, a->rows, a->n_in, a->ld_x, true, false, 0}; }
@@ -159,6 +159,7 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   p.few = a->rows <= most && rounded * ((a->n_in + 7) / 8 * 8) * (int64_t)size_of(a->dtype) <= kRowsMostBytes;
   p.twice = p.grad && p.parts == 1 && a->row_weight && a->rows <= kLossTwice;
   p.rows = p.twice ? 2 * a->rows : a->rows;
+  p.relative = p.grad && p.parts == 1 && a->row_weight && !p.twice;      // more rows than `few` has
   p.x_ready = !p.twice && in_place(operand_x(a), a->dtype);
   p.w_ready = in_place(operand_w(a, 0, a->vocab), a->dtype);
   const bool products = p.grad || !p.few;         // operands of the tensor cores are needed
@@ -179,14 +180,15 @@ Plan make_plan(const gbmuf_ops* ops, const Args* a) {
   p.target_off = take(a->rows * 4);
   const int per_block = (rounded >= 16 ? 2 : 4) * kRowsThreads / 32;
   p.few_blocks = (int)std::min<long long>((a->vocab + per_block - 1) / per_block, ops->num_sms * 2);
-  long long slots = p.few ? p.few_blocks * a->rows : 0;               // of the widest launch
+  long long slots = p.few ? p.few_blocks * a->rows : 0;
   for (long long r = 0; r < a->rows && !p.few;) {
     const int t = stats_rows(ops, p.stats, a->rows - r);
     const long long n = std::min<long long>(a->rows - r, 128ll * p.stats.pair * t);
-    slots = std::max(slots, n * stats_slots(ops, p.stats, t, together) * (p.w_ready ? 1 : p.pieces));
+    slots += n * stats_slots(ops, p.stats, t, together) * (p.w_ready ? 1 : p.pieces);
     r += n;
   }
   p.slot_off = take(slots * 8);
+  if (p.relative) p.max_off = take(((a->rows + 31) / 32 + 1) * 4);      // the factor comes first
   if (p.grad) {
     p.pair_off = take(p.rows_padded / 2 * (long long)sizeof(RowPair));
     p.word_off = take(p.rows_padded * 4);
@@ -335,22 +337,30 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
   const TcShape& s = p.stats;
   const long long most_tiles = std::max((V / s.bn + 1) * (N / 128 + 1), (V / 128 + 1) * (G / p.tc.bn + 1));
   if (most_tiles > 0x3fffffff) return refuse(GBMUF_ERR_UNSUPPORTED, "more than 2^30 tiles of logits");
-  // ---- statistics: every CTA keeps to one row tile, so its threads keep a row's running maximum and sum
-  for (long long r0 = 0; r0 < N;) {
-    const int t = p.few ? 1 : stats_rows(ops, s, N - r0);
-    const long long n = p.few ? N : std::min<long long>(N - r0, 128ll * s.pair * t), ld = n;
-    const long long step = p.w_ready ? V : p.piece;
-    int slots = 0;
-    if (p.few) {
-      RowsParams P{};
-      P.E.bias = a->bias; P.E.loss_rows = a->targets;
-      P.E.target_logit = reinterpret_cast<float*>(ws + p.target_off);
-      P.E.partial = ws + p.slot_off; P.E.ld_partial = ld;
-      slots = p.few_blocks;
-      const cudaError_t e = rows_loss<T>(a, P, (unsigned)slots, st);
-      if (e != cudaSuccess) return cuda_refuse("launch of the few-rows loss kernel", e);
+  float* const factor = p.relative ? reinterpret_cast<float*>(ws + p.max_off) : nullptr;
+  // ---- statistics: every CTA keeps to one row tile, so its threads keep a row's running maximum and sum.  Rows in ranges
+  // that fill the GPU; do_ranges(f): f(first row, rows, row tiles, the range's slots)
+  const long long step = p.w_ready ? V : p.piece, steps = (V + step - 1) / step;
+  auto do_ranges = [&](auto f) -> gbmuf_status {
+    float2* slots = reinterpret_cast<float2*>(ws + p.slot_off);
+    for (long long r0 = 0; r0 < N;) {
+      const int t = p.few ? 1 : stats_rows(ops, s, N - r0);
+      const long long n = p.few ? N : std::min<long long>(N - r0, 128ll * s.pair * t);
+      if (gbmuf_status rc = f(r0, n, t, slots)) return rc;
+      if (!p.few) slots += n * stats_slots(ops, s, t, step) * steps;
+      r0 += n;
     }
-    for (long long v0 = 0; v0 < V && !p.few; v0 += step) {
+    return GBMUF_OK;
+  };
+  if (p.few) {
+    RowsParams P{};
+    P.E.bias = a->bias; P.E.loss_rows = a->targets;
+    P.E.target_logit = reinterpret_cast<float*>(ws + p.target_off);
+    P.E.partial = ws + p.slot_off; P.E.ld_partial = N;
+    const cudaError_t e = rows_loss<T>(a, P, (unsigned)p.few_blocks, st);
+    if (e != cudaSuccess) return cuda_refuse("launch of the few-rows loss kernel", e);
+  } else if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
+    for (long long v0 = 0; v0 < V; v0 += step) {
       const long long words = std::min(step, V - v0);
       Operand w;
       if (gbmuf_status rc = weights(v0, words, w)) return rc;
@@ -361,29 +371,40 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       P.E.bias = a->bias ? static_cast<const char*>(a->bias) + v0 * size : nullptr;
       P.E.loss_rows = a->targets + r0;
       P.E.target_logit = reinterpret_cast<float*>(ws + p.target_off) + r0;
-      P.E.partial = reinterpret_cast<float2*>(ws + p.slot_off) + slots * ld;
-      P.E.ld_partial = ld;
+      P.E.partial = slots + v0 / step * stats_slots(ops, s, t, step) * n;
+      P.E.ld_partial = n;
       P.E.first_word = (int)v0;
+      if (factor) {                              // r0 is a multiple of 128
+        P.E.weight_max = factor + 1 + r0 / 32;
+        P.E.loss_weights = a->row_weight + r0; P.E.scale = a->scale; P.E.vocab = V; P.E.ignore_index = a->ignore_index;
+      }
       const int here = stats_slots(ops, s, t, words);
       if (gbmuf_status rc = launch_logits<kLossStats, T, PARTS>(ops, s, P, here / (kTcFinishers / 4) * t, xr, w, a->dtype, st)) return rc;
-      slots += here;
     }
+    return GBMUF_OK;
+  })) {
+    return rc;
+  }
+  if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
     JoinParams J{};
     J.L.targets = a->targets + r0; J.L.row_weight = a->row_weight ? a->row_weight + r0 : nullptr;
     J.L.loss = a->loss ? a->loss + r0 : nullptr; J.L.lse = a->lse ? a->lse + r0 : nullptr;
     J.L.rows = n; J.L.vocab = V; J.L.ignore_index = a->ignore_index; J.L.scale = a->scale; J.L.status = ops->d_status;
-    J.slots = reinterpret_cast<const float2*>(ws + p.slot_off);
+    J.slots = slots;
     J.target_logit = reinterpret_cast<const float*>(ws + p.target_off) + r0;
-    if (p.grad) {                                // r0 is a multiple of 128
+    if (p.grad) {
       J.pairs = reinterpret_cast<RowPair*>(ws + p.pair_off) + r0 / 2;
       J.targets = reinterpret_cast<int*>(ws + p.word_off) + r0;
       J.weights = reinterpret_cast<float*>(ws + p.weight_off) + r0;
     }
-    J.ld = ld; J.count = slots; J.twice = p.twice;
+    if (factor) { J.weight_max = factor + 1; J.factor = factor; J.groups = (N + 31) / 32; }
+    J.ld = n; J.twice = p.twice;
+    J.count = p.few ? p.few_blocks : (int)((steps - 1) * stats_slots(ops, s, t, step)) + stats_slots(ops, s, t, V - (steps - 1) * step);
     J.rows_padded = r0 + n == N ? p.rows_padded - r0 : n;
     const cudaError_t e = launch(loss_join_kernel, (unsigned)((J.rows_padded + 31) / 32), 1, 32 * kJoinShares, 0, st, J);
-    if (e != cudaSuccess) return cuda_refuse("launch of the loss's join kernel", e);
-    r0 += n;
+    return e == cudaSuccess ? GBMUF_OK : cuda_refuse("launch of the loss's join kernel", e);
+  })) {
+    return rc;
   }
   if (!p.grad) return GBMUF_OK;
   // ---- gradients, a piece of the vocabulary at a time
@@ -411,7 +432,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       cudaError_t e = cudaSuccess;
       DISPATCH_DTYPE(a->grad_dtype, TO, e = launch(loss_bias_kernel<TO>, (unsigned)((n + 255) / 256), 1, 256, 0, st,
                                                    reinterpret_cast<const float*>(ws + p.partial_off), p.ld_partial, (int)p.strips, n,
-                                                   static_cast<TO*>(a->dbias) + first, (int)a->accumulate, a->scale));
+                                                   static_cast<TO*>(a->dbias) + first, (int)a->accumulate, a->scale, (const float*)factor));
       if (e != cudaSuccess) return cuda_refuse("launch of the loss's bias-gradient kernel", e);
     }
     if (H == 0) continue;
@@ -425,6 +446,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       W.E.out0 = static_cast<char*>(a->dw) + v0 * a->ld_dw * (long long)size_of(a->grad_dtype); W.E.ld_out0 = a->ld_dw;
       W.E.accumulate = a->accumulate;
       W.E.scale = a->scale;
+      W.E.factor = factor;
       W.E.pairs = a->grad_dtype == GBMUF_BF16 && (uintptr_t)W.E.out0 % 4 == 0 && H % 2 == 0 && (words == 1 || a->ld_dw % 2 == 0);
       gbmuf_status rc = GBMUF_OK;
       DISPATCH_DTYPE(a->grad_dtype, TO, (rc = launch_loss_product<kLossWeight, TO, TO, PARTS>(
@@ -448,7 +470,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       if (last) {
         const cudaError_t e = launch(loss_dx_kernel<T>, (unsigned)std::min<long long>(N, ops->num_sms * 8), 1, 256, 0, st,
                                      reinterpret_cast<const float*>(ws + p.acc_off), p.ld_acc, G * p.ld_acc, p.term.slices,
-                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H, a->scale, p.twice);
+                                     static_cast<T*>(a->dx), (long long)a->ld_dx, N, (int)H, a->scale, (const float*)factor, p.twice);
         if (e != cudaSuccess) return cuda_refuse("launch of the loss's input-gradient kernel", e);
       }
     }

@@ -11,11 +11,12 @@ namespace {
 // The second time (kLossGrad) words lie along the lanes and d = w (exp(z - m) / s - [target]) of a piece of
 // the vocabulary is stored, once, as the operand of the two products that follow: rounded to bf16, or for
 // fp32 as its three parts.  bf16: that rounding is off by at most 2^-8 of an element, and the products'
-// sums of many such elements by less.  w is the row's weight alone; the scale of all rows is a factor of the
-// finished fp32 sums: within d it would be rounded the same way in every row, so that 1 / 300 (say) would take
-// 0.2 % off every gradient, where a target's -1 is exact.  Weights of the rows are rounded as they come, by 2^-9 or
-// so, and over many rows on average; up to kLossTwice weighted rows, which fill half a step of the sums and half a
-// tile at most, come a second time instead, with what the rounding left: 16 bits of d (32 x 512 x 10,000: 47 -> 56 us).
+// sums of many such elements by less.  What all rows have in common is a factor of the finished fp32 sums, the scale
+// and the largest weight of a row that counts: within d it would be rounded the same way in every row, so that
+// 1 / 300 (say) would take 0.2 % off every gradient, where a target's -1 is exact.  So w is the row's weight over that
+// largest one: 1 where all are equal, or a mask.  Where they differ, each is rounded its own way, by 2^-8 at most, as
+// any other element of d; up to kLossTwice weighted rows, which fill half a step of the sums and half a
+// tile at most, come a second time, with what the rounding left: 16 bits of d (32 x 512 x 10,000: 47 -> 56 us).
 
 // What kLossGrad needs of two rows of the batch, as two packed operands: minus their maxima, and weight / sum.
 // Next to it stand per row the target (-1: no word of the vocabulary; -2: the row's gradient is zero) and the
@@ -46,6 +47,11 @@ template <typename T> struct RowStats {
     there = c < rows;
     const long long t = there ? static_cast<const long long*>(E.loss_rows)[c] : -1;
     target = t >= 0 && t <= 0x7fffffff ? (int)t - E.first_word : -1;
+    if (!E.weight_max || slot != 0) return;                // one warp for each 32 rows
+    const float w = there && t >= 0 && t < E.vocab && t != E.ignore_index ? fabsf(E.loss_weights[c]) : 0.0f;
+    float top = E.scale * w != 0.0f && w < INFINITY ? w : 0.0f;
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    if (there && (c & 31) == 0) E.weight_max[c >> 5] = top;
   }
   // N words from r on
   template <int N> __device__ __forceinline__ void add(const Epilogue& E, float (&v)[N], int r, int words) {
@@ -259,9 +265,10 @@ template <typename T, typename TO, int N> struct Finisher<kLossTerm, T, TO, N> {
 };
 template <typename T>
 __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long long ld, long long slice, int slices, T* dx, long long ld_dx,
-                                                      long long rows, int cols, float scale, bool twice) {
+                                                      long long rows, int cols, float scale, const float* factor, bool twice) {
   grid_launch_dependents();
   grid_dependency_wait();
+  const float f = factor ? *factor : 1.0f;
   for (long long row = blockIdx.x; row < rows; row += gridDim.x)
     for (int c = threadIdx.x; c < cols; c += 256) {
       const float* p = terms + row * ld + c;
@@ -270,7 +277,7 @@ __global__ void __launch_bounds__(256) loss_dx_kernel(const float* terms, long l
       for (int i = 1; i < slices; ++i) s += p[i * slice];
       if (twice)
         for (int i = 0; i < slices; ++i) s += p[i * slice + rows * ld];
-      dx[row * ld_dx + c] = from_f32<T>(s * scale);
+      dx[row * ld_dx + c] = from_f32<T>(s * f * scale);
     }
 }
 
@@ -284,7 +291,9 @@ struct JoinParams {
   RowPair* pairs;            // or NULL
   int* targets;
   float* weights;
-  long long ld, rows_padded;
+  const float* weight_max;   // or NULL: the largest weights of `groups` groups of rows, all of the batch
+  float* factor;             // the largest of them
+  long long ld, rows_padded, groups;
   int count, twice;          // twice: the gradients have the rows a second time
 };
 __device__ __forceinline__ void join_stats(float& m, float& s, float2 o) {
@@ -295,6 +304,7 @@ __device__ __forceinline__ void join_stats(float& m, float& s, float2 o) {
 }
 __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinParams P) {
   __shared__ float2 part[kJoinShares][32];
+  __shared__ float largest[kJoinShares];
   grid_launch_dependents();
   grid_dependency_wait();
   const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
@@ -311,7 +321,19 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
     }
   }
   part[share][lane] = make_float2(m, s);
+  float factor = 0.0f;
+  if (P.weight_max) {
+    for (long long i = threadIdx.x; i < P.groups; i += 32 * kJoinShares) factor = fmaxf(factor, P.weight_max[i]);
+    for (int d = 16; d > 0; d >>= 1) factor = fmaxf(factor, __shfl_xor_sync(~0u, factor, d));
+    if (lane == 0) largest[share] = factor;
+  }
   __syncthreads();
+  if (P.weight_max) {
+    factor = largest[lane % kJoinShares];
+    for (int d = kJoinShares / 2; d > 0; d >>= 1) factor = fmaxf(factor, __shfl_xor_sync(~0u, factor, d));
+  }
+  if (factor == 0.0f) factor = 1.0f;                       // no weights, or no row counts
+  if (P.weight_max && blockIdx.x == 0 && threadIdx.x == 0) *P.factor = factor;
   if (share != 0 || row >= P.rows_padded) return;
   float offset = 0.0f, k = 0.0f, weight = 0.0f;
   int target = -2;
@@ -326,8 +348,8 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
     if (P.L.lse) P.L.lse[row] = o.lse;
     if (!o.zero) {
       offset = m == -INFINITY ? 0.0f : -m;
-      k = own / s;
-      weight = own;
+      weight = own / factor;
+      k = weight / s;
       target = (int)t;
     }
   }
@@ -345,7 +367,7 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
 // dbias of a piece: the strips' sums in their order.
 template <typename TO>
 __global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, long long ld, int strips, long long words, TO* out,
-                                                        int accumulate, float scale) {
+                                                        int accumulate, float scale, const float* factor) {
   grid_launch_dependents();
   grid_dependency_wait();
   const long long c = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -353,7 +375,7 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, lo
   float t = 0.0f;
 #pragma unroll 8
   for (int i = 0; i < strips; ++i) t += partial[i * ld + c];
-  t *= scale;
+  t = t * (factor ? *factor : 1.0f) * scale;
   out[c] = from_f32<TO>(accumulate ? t + to_f32(out[c]) : t);
 }
 

@@ -445,6 +445,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const uint32_t out_base = ring + (uint32_t)S * STAGE + kTcOut<KIND, PARTS, BN> / kTcFinishers * (uint32_t)(warp - 4);
     const uint32_t out_flip = PARTS == 1 ? out_base ^ (out_base + 2048u) : 0u;
     uint32_t out_room = out_base;
+    const float factor = KIND == kLossWeight && P.E.factor ? *P.E.factor : 1.0f;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const Share mine = share(w.c);
       const int c = mine.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL, chunks = mine.chunks;
@@ -475,6 +476,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int j = 0; j < NCOL; j += N) {
           Finisher<KIND, T, TO, N> F;
           if constexpr (KIND == kLossTerm) F.slice = mine.slice;
+          if constexpr (KIND == kLossWeight) F.factor = factor;
           if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_room; F.half = out_flip; }
           float v[N];
 #pragma unroll
@@ -488,6 +490,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         // what the epilogue reads is requested one strip ahead, the first one during the sums
         Finisher<KIND, T, TO, N> F;
         if constexpr (KIND == kLossTerm) F.slice = mine.slice;
+        if constexpr (KIND == kLossWeight) F.factor = factor;
         if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_room; F.half = out_flip; }
         F.ask(P.E, r0, c, P.R, P.C, lane);
         if (chunks > 0) {
