@@ -240,25 +240,20 @@ template <typename T, typename TO, int N> struct Finisher<kLossGrad, T, TO, N> {
 };
 
 // A term of dx: the sum over one piece's words, or over one of `slices` parts of them (each sums into an array of its
-// own, so that a result of few tiles keeps all SMs busy; the arrays are added up at the end).  bf16 operands:
-// within a piece the sum stays in the accumulator, a few thousand words at most.
+// own, so that a result of few tiles keeps all SMs busy; the arrays are added up at the end).  What an array holds of
+// the pieces before is where the sums begin: its loads are under way while the first products are formed.
 template <typename T, typename TO, int N> struct Finisher<kLossTerm, T, TO, N> {
-  Strip<TO, N> old;
   int slice;
 
   __device__ __forceinline__ TO* base(const Epilogue& E) const { return static_cast<TO*>(E.out0) + slice * E.part; }
-  __device__ __forceinline__ void ask(const Epilogue& E, int r, int c, int R, int C, int lane) {
-    if (!E.accumulate) return;
+  __device__ __forceinline__ void begin(const Epilogue& E, int r, int c, int R, int C, int lane, float (&v)[N]) {
+    Strip<TO, N> old;
     if (r + N <= R && c - lane + 32 <= C) old.template load<true>(base(E), E.ld_out0, r, c, R, C, false, lane);
     else old.template load<false>(base(E), E.ld_out0, r, c, R, C, false, lane);
+    old.unpack(v, false, lane);
   }
+  __device__ __forceinline__ void ask(const Epilogue&, int, int, int, int, int) {}
   __device__ __forceinline__ void finish(const Epilogue& E, int r, int c, int R, int C, int lane, float, float (&v)[N]) {
-    if (E.accumulate) {
-      float x[N];
-      old.unpack(x, false, lane);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += x[i];
-    }
     if (r + N <= R && c - lane + 32 <= C) store_strip<TO, true>(v, base(E), E.ld_out0, r, c, R, C, false, lane);
     else store_strip<TO, false>(v, base(E), E.ld_out0, r, c, R, C, false, lane);
   }

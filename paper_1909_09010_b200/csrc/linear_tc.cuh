@@ -159,7 +159,8 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&
 
 // PROMOTE (results that stay fp32): the tensor cores' sum is moved into fp32 registers, and added there
 // with rounding to nearest, after every 16 (24) instructions: in the accumulator every addition cuts
-// towards zero, which over thousands of them would cost a few units of 2^-18.  Results that are rounded
+// towards zero, which over thousands of them would cost a few units of 2^-18.  (Terms of dx of bf16 operands, which are
+// rounded to bf16 once they are added up: every 128, at most 1.5e-5 of the result.)  Results that are rounded
 // to bf16 stay in the accumulator: k / 16 cuts of at most 2^-23 of a sum that grows like a random walk are
 // (2/3) k / 16 x 2^-23 of the result, 1.3e-3 at k = 267,735, about what the rounding to bf16 costs.
 template <int KIND, typename T, typename TO, int PARTS, int BN, int PAIR>
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     linear_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
                      const TcParams P) {
   constexpr bool A_K = KIND == kForward || KIND == kLossStats || KIND == kLossGrad, B_K = KIND != kWeightGrad && KIND != kLossTerm;
-  constexpr bool PROMOTE = sizeof(TO) == 4 && !(KIND == kLossTerm && PARTS == 1);
+  constexpr bool PROMOTE = sizeof(TO) == 4;
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   struct Share {
     int c, slice, step0, iters, chunks;
   };
-  constexpr int chunk = PROMOTE ? (PARTS == 1 ? 4 : 1) : 0x7fffffff;
+  constexpr int chunk = !PROMOTE ? 0x7fffffff : PARTS == 3 ? 1 : KIND == kLossTerm ? 32 : 4;
   auto chunks_of = [](int iters) { return PROMOTE ? (iters + chunk - 1) / chunk : iters > 0 ? 1 : 0; };
   const Share whole{0, 0, step0, step1 - step0, chunks_of(step1 - step0)};
   auto share = [&](int c) {
@@ -455,6 +456,18 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         float acc[NCOL];
 #pragma unroll
         for (int i = 0; i < NCOL; ++i) acc[i] = 0.0f;
+        if constexpr (KIND == kLossTerm)
+          if (P.E.accumulate) {
+#pragma unroll
+            for (int j = 0; j < NCOL; j += N) {
+              Finisher<KIND, T, TO, N> F;
+              F.slice = mine.slice;
+              float v[N];
+              F.begin(P.E, r0 + j, c, P.R, P.C, lane, v);
+#pragma unroll
+              for (int i = 0; i < N; ++i) acc[j + i] = v[i];
+            }
+          }
         for (int ch = 0; ch < chunks; ++ch, ++n) {
           ok = mbar_wait_bounded(acc_full(n & (NACC - 1)), (n >> LOG_ACC) & 1, P.status);
           ok = __all_sync(~0u, ok);
@@ -489,7 +502,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       } else {
         // what the epilogue reads is requested one strip ahead, the first one during the sums
         Finisher<KIND, T, TO, N> F;
-        if constexpr (KIND == kLossTerm) F.slice = mine.slice;
         if constexpr (KIND == kLossWeight) F.factor = factor;
         if constexpr (kTcOut<KIND, PARTS, BN> > 0) { F.map = &map_out; F.room = out_room; F.half = out_flip; }
         F.ask(P.E, r0, c, P.R, P.C, lane);

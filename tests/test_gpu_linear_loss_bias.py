@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_1909_09010_b200 import binding
-from test_gpu_linear_loss import BF, F, HALF, IGNORE, check, gen, lay, problem, reference, rnd
+from test_gpu_linear_loss import BF, F, HALF, IGNORE, check, gen, lay, problem, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -90,4 +90,31 @@ def test_weights_of_any_size(ops):
     # no row counts
     none = ops.linear_cross_entropy(x, w, torch.full_like(t, IGNORE), b, ignore_index=IGNORE, row_weight=weight)
     assert all(bool((a == 0).all()) for a in (none[0], *none[2:]))
+    assert ops.device_status() == 0
+
+
+def test_long_sums_over_the_vocabulary(ops):
+    """dx of bf16 operands, 120,011 words in a piece.  The tensor cores' accumulator cuts every addition towards zero, so a
+    sum that stayed in it would make each target's term smaller, by 2^-24 on average and 2^-23 at most every 16 words.
+    Sums leave it after 2,048 words."""
+    g = gen(120)
+    rows, n_in, vocab = 1024, 4096, 120_011
+    x, w, t, _, _ = problem(g, rows, n_in, vocab, BF, bias=False, weighted=False, spread=0.25)
+    w = w - w.float().mean(0).to(BF)
+    got = ops.linear_cross_entropy(x, w, t, None, ignore_index=IGNORE, piece=vocab)[2]
+    wd = w.double()
+    z = x.double() @ wd.t()
+    valid = t != IGNORE
+    at = torch.where(valid, t, 0)[:, None]
+    p = torch.softmax(z, 1) * valid[:, None]
+    p_target = p.gather(1, at)[:, 0]
+    assert float(p_target.max()) < 2.0 ** -9
+    d = p.scatter_add(1, at, -valid[:, None].double())
+    exact = d @ wd
+    total = float(exact.square().sum())
+    ed = p * ((n_in / 16 + 8) * 2.0 ** -23 * z.abs().max() + 2.0 ** -20)
+    bound = 128 * 2.0 ** -23 + off_along(p, p_target, at, ed, (exact @ wd.t()) / total)
+    bound += 8 * HALF[BF] * float(exact.pow(4).sum().sqrt()) / total
+    assert bound < 6e-5
+    assert abs(along(got, exact) - 1) < bound, (along(got, exact), bound)
     assert ops.device_status() == 0
