@@ -212,6 +212,7 @@ __device__ __forceinline__ void prepare_list(const DistillParams& P, RowList& L,
   if (lane == 0) {
     const bool ignored = w == 0.0f || (P.targets && target == P.ignore_index);
     if (P.targets && !inside) outside = true;
+    if (P.teacher_lse && teacher_lse != teacher_lse) q_sum = (double)teacher_lse;      // of a list without entries too
     L.gap = gap; L.m = m; L.s = s; L.s1 = s1;
     L.q_sum = (float)q_sum;
     const double rest = 1.0 - q_sum;
@@ -251,9 +252,9 @@ __device__ __forceinline__ DistillRow distill_row(const DistillParams& P, const 
   o.z1 = one ? o.z : r1 * fr1 + L.s1 * fs1;
   o.share = r * fr / o.z;
   const float h = P.hard, mass = L.q_sum + L.q_rest, ws = L.weight * (1.0f - h) * P.T, wh = L.weight * h;
-  o.k = r == 0.0f ? 0.0f : ws * (mass * o.share - L.q_rest) / r;
-  o.k1 = h == 0.0f || (one ? r : r1) == 0.0f ? 0.0f : wh * fr1 / o.z1;
   o.per = ws * mass / o.z;
+  o.k = r == 0.0f ? 0.0f * o.per : ws * (mass * o.share - L.q_rest) / r;      // NaN stays, where no word of the rest can occur
+  o.k1 = h == 0.0f || (one ? r : r1) == 0.0f ? 0.0f : wh * fr1 / o.z1;
   o.per1 = h == 0.0f ? 0.0f : wh / o.z1;
   if (one) { o.k += o.k1; o.per += o.per1; o.k1 = o.per1 = 0.0f; }
   o.top = e.m;
@@ -274,6 +275,7 @@ __device__ __noinline__ float2 distill_loss(const DistillParams& P, const RowLis
                                                  : (double)logf(L.q_rest) - (log_of(r) + (m == -INFINITY ? 0.0 : (double)(m - o.top) * inverse) - log_z));
   double loss = 0.0;
   if (P.hard != 1.0f) loss += (1.0 - (double)P.hard) * (double)(P.T * P.T) * soft;
+  if (!(o.z == o.z && L.q_sum == L.q_sum)) loss = (double)(o.z + L.q_sum);     // NaN, where its factor is 0 too
   if (P.hard != 0.0f) loss += (double)P.hard * ((double)(o.top - L.target_logit) + (one ? log_z : log_of(o.z1)));
   return make_float2(lse, L.ignored ? 0.0f : L.outside ? NAN : empty ? INFINITY : (float)((double)L.weight * loss));
 }
