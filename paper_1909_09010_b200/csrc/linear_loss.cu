@@ -359,11 +359,12 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
     P.E.partial = ws + p.slot_off; P.E.ld_partial = N;
     const cudaError_t e = rows_loss<T>(a, P, (unsigned)p.few_blocks, st);
     if (e != cudaSuccess) return cuda_refuse("launch of the few-rows loss kernel", e);
-  } else if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
-    for (long long v0 = 0; v0 < V; v0 += step) {
-      const long long words = std::min(step, V - v0);
-      Operand w;
-      if (gbmuf_status rc = weights(v0, words, w)) return rc;
+  }
+  for (long long v0 = 0; v0 < V && !p.few; v0 += step) {      // weights that have to be packed are packed once for all rows
+    const long long words = std::min(step, V - v0);
+    Operand w;
+    if (gbmuf_status rc = weights(v0, words, w)) return rc;
+    if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
       Operand xr = x;
       xr.p = static_cast<const char*>(x.p) + r0 * x.ld * 2;
       xr.outer = n;
@@ -379,11 +380,10 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
         P.E.loss_weights = a->row_weight + r0; P.E.scale = a->scale; P.E.vocab = V; P.E.ignore_index = a->ignore_index;
       }
       const int here = stats_slots(ops, s, t, words);
-      if (gbmuf_status rc = launch_logits<kLossStats, T, PARTS>(ops, s, P, here / (kTcFinishers / 4) * t, xr, w, a->dtype, st)) return rc;
+      return launch_logits<kLossStats, T, PARTS>(ops, s, P, here / (kTcFinishers / 4) * t, xr, w, a->dtype, st);
+    })) {
+      return rc;
     }
-    return GBMUF_OK;
-  })) {
-    return rc;
   }
   if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
     JoinParams J{};

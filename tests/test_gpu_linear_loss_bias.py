@@ -1,4 +1,4 @@
-"""Gradients of ``linear_cross_entropy`` that are not off to one side."""
+"""Gradients of ``linear_cross_entropy`` that are not off to one side; batches that take several launches of the statistics."""
 import pytest
 import torch
 
@@ -117,4 +117,17 @@ def test_long_sums_over_the_vocabulary(ops):
     bound += 8 * HALF[BF] * float(exact.pow(4).sum().sqrt()) / total
     assert bound < 6e-5
     assert abs(along(got, exact) - 1) < bound, (along(got, exact), bound)
+    assert ops.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype,rows,n_in,vocab,piece,how", [
+    (BF, 4000, 136, 3001, 1000, "odd"), (BF, 4001, 33, 2100, 300, "odd"), (F, 4000, 136, 2500, 700, "plain"), (F, 4100, 72, 2500, 0, "odd"),
+    (F, 20_000, 16, 300, 128, "plain"), (BF, 20_011, 16, 600, 256, "odd")])
+def test_several_launches_of_the_statistics(ops, dtype, rows, n_in, vocab, piece, how):
+    """Rows whose tiles do not fill the GPU evenly, with weights that are packed a piece at a time."""
+    x, w, t, b, rw = problem(gen(rows + vocab), rows, n_in, vocab, dtype)
+    R = reference(x, w, t, b, rw, 0.5)
+    args = (lay(x, how), lay(w, how), t, lay(b, how))
+    check(ops.linear_cross_entropy(*args, row_weight=rw, scale=0.5, piece=piece), R, dtype, dtype, how)
+    check(ops.linear_cross_entropy(*args, row_weight=rw, scale=0.5, piece=piece, want_grad=False), R, dtype, dtype, how + " values")
     assert ops.device_status() == 0
