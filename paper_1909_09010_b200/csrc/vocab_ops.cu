@@ -66,8 +66,8 @@ template <typename T, int LANES> cudaError_t launch_distill(const gbmuf_ops* ops
   }
   const long long bytes = P.vocab * (long long)sizeof(T), ctas = (long long)ops->num_sms * kLossBlocksPerSm;
   int log = split_few(ops, P.rows, bytes, kLossBlocksPerSm);
-  // the slices that are fetched twice should fit the L2 cache
-  while (log < 3 && (bytes - ((long long)kLossKept * kLossChunk << log)) * (ctas >> log) >= kDistillCacheBytes) ++log;
+  // the slices that are fetched twice, for the gradient, should fit the L2 cache
+  while (P.dlogits && log < 3 && (bytes - ((long long)kLossKept * kLossChunk << log)) * (ctas >> log) >= kDistillCacheBytes) ++log;
   P.split = 1 << log;
   const int clusters = (int)std::min<long long>(P.rows, ops->distill_clusters[log]);
   const auto kernel = P.hard == 0.0f || P.T == 1.0f ? distill_ring_kernel<T, 0, LANES>
