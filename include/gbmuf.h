@@ -457,7 +457,8 @@ gbmuf_status gbmuf_cross_entropy(gbmuf_ops* ops, const gbmuf_cross_entropy_args*
  * The logits are formed twice, for the statistics and for the gradients, and the second time a piece of the
  * vocabulary at a time: `piece` words, or 0 for a choice that keeps the gradient of a piece's logits (and the
  * weights of a piece, where they have to be packed) within 128 MB, 2,048 words at least.  Statistics, sums over
- * pieces and dbias's sums are fp32.  Logits are not rounded; of bf16 operands d / scale is rounded to bf16, each
+ * pieces and dbias's sums are fp32.  Logits are not rounded (of bf16 operands they are sums of the tensor cores, off by
+ * n_in / 16 times 2^-23 of their largest partial sum at most); of bf16 operands d / scale is rounded to bf16, each
  * element by 2^-8 at most, before it is multiplied with w and x (with row weights d / (scale W), W the largest
  * |row_weight_i| of a row that has a gradient, so that equal weights are exact; up to 32 such rows: d / scale as two bf16
  * parts), of fp32 operands it is taken as three bf16 parts; W and scale multiply the finished sums.  Row weights are

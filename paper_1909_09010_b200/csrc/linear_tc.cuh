@@ -172,8 +172,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   constexpr int TILE_C = 128 * PAIR, OWN_R = BN / PAIR;           // a tile's columns; rows of B that this CTA loads
   constexpr uint32_t STAGE = tc_stage_bytes(BN, PAIR), A_BYTES = 128 * 128;
   constexpr int ACC = BN;                      // tensor-memory columns of one accumulator
-  // Accumulators in turn.  Where sums leave them as they go, the finishing warps' work at a tile's end holds the chunks
-  // up: narrow tiles have room for four (fp32 loss: see linear_loss.cuh).
+  // Accumulators in turn.  Where sums leave them as they go, the finishing warps' work at a tile's end (exponentials and
+  // stores of the loss) holds the chunks up: narrow tiles have room for four.
   constexpr int NACC = PROMOTE && KIND >= kLossStats && BN <= 128 ? 4 : 2, LOG_ACC = NACC / 2;
   constexpr int NCOL = BN / (kTcFinishers / 4);   // accumulator columns per finishing warp
   constexpr int MOST = (KIND == kLossStats && !PROMOTE) || KIND == kLossGrad ? 32 : 16;

@@ -93,18 +93,13 @@ struct TopState {
   TopShared& S;
   int k, thread;
   Key threshold;             // keys at or above it are wanted; the same in all threads
-  float least;               // its logit
 
   __device__ __forceinline__ void start() {
     set(0);
     if (thread == 0) S.count = 0;
     loss_workers_sync();
   }
-  __device__ __forceinline__ void set(Key t) {
-    threshold = t;
-    least = t == 0 ? -INFINITY : key_value(t);
-  }
-  __device__ __forceinline__ bool wanted(float top) const { return !(top < least); }
+  __device__ __forceinline__ void set(Key t) { threshold = t; }
   // true where the buffer has got long
   __device__ __forceinline__ bool append(Key key) {
     const int at = atomicAdd(&S.count, 1);
