@@ -160,8 +160,8 @@ struct Epilogue {
   int first_word, words;     // of the vocabulary's piece
   int rest_from;             // kLossGrad, bf16: rows from here on are the first ones again, of which the rounding's rest is stored
   float scale;               // kLossWeight: of the sums; kLossStats: of the weights
-  const float* factor;       // kLossWeight: of the sums too, in device memory, or NULL
-  float* weight_max;         // kLossStats: the largest weight of each 32 rows, or NULL
+  const float* factor;       // kLossWeight, bf16 operands: of the sums too, in device memory, or NULL
+  float* weight_max;         // kLossStats, bf16: the largest weight of each 32 rows, or NULL
   long long vocab, ignore_index;     // kLossStats, for weight_max
 };
 

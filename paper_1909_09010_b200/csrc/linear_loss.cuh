@@ -47,7 +47,7 @@ template <typename T> struct RowStats {
     there = c < rows;
     const long long t = there ? static_cast<const long long*>(E.loss_rows)[c] : -1;
     target = t >= 0 && t <= 0x7fffffff ? (int)t - E.first_word : -1;
-    if (!E.weight_max || slot != 0) return;                // one warp for each 32 rows
+    if (!FAST || !E.weight_max || slot != 0) return;       // one warp for each 32 rows
     const float w = there && t >= 0 && t < E.vocab && t != E.ignore_index ? fabsf(E.loss_weights[c]) : 0.0f;
     float top = E.scale * w != 0.0f && w < INFINITY ? w : 0.0f;
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));

@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const uint32_t out_base = ring + (uint32_t)S * STAGE + kTcOut<KIND, PARTS, BN> / kTcFinishers * (uint32_t)(warp - 4);
     const uint32_t out_flip = PARTS == 1 ? out_base ^ (out_base + 2048u) : 0u;
     uint32_t out_room = out_base;
-    const float factor = KIND == kLossWeight && P.E.factor ? *P.E.factor : 1.0f;
+    const float factor = KIND == kLossWeight && PARTS == 1 && P.E.factor ? *P.E.factor : 1.0f;
     for (Walk w = first(); w.tile < P.tiles && ok; next(w)) {
       const Share mine = share(w.c);
       const int c = mine.c * TILE_C + side * 128 + quad * 32 + lane, r0 = w.r * BN + part * NCOL, chunks = mine.chunks;
