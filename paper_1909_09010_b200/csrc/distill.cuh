@@ -19,9 +19,10 @@ namespace {
 // through.  A thread looks at its next entry's place once per chunk.  The order within a chain depends on
 // timing, the results do not: a word's Q is summed in the list's order.
 //
-// Measured: 2,048 x 267,735 bf16, lists of 64: 455 us (4.8 TB/s of the bytes that have to move, 74 % of the copy rate; the
-// cross-entropy without lists 422), 480 to 510 with hard targets at T = 2 or 3, 680 at T = 1.5; 1,003 x 33,278 fp32 at
-// T = 3 with hard targets 76 us (the cross-entropy 58): issue slots 59 % busy with the exact exponentials.
+// Measured: 2,048 x 267,735 bf16, lists of 64: 452 to 504 us (4.4 to 4.9 TB/s of the bytes that have to move, 67 to 74 % of
+// the copy rate; the cross-entropy without lists 417 to 463), the loss alone 226 to 300; 480 to 510 with hard targets at
+// T = 2 or 3, 680 at T = 1.5; 1,003 x 33,278 fp32 at T = 3 with hard targets 76 us (the cross-entropy 58): issue slots
+// 58 % busy with the exact exponentials, whose latency 19 warps an SM do not cover.
 struct DistillParams {
   const void* logits;
   const void* teacher;

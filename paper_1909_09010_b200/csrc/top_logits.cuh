@@ -18,8 +18,8 @@ namespace {
 // more, chunk by chunk, with a bound that rises: at most k threads have keys above the k-th largest of the
 // threads' largest keys, so piece by piece (a thread's 16 bytes) the buffer cannot overflow.
 //
-// Measured: 2,048 x 267,735 bf16, k 64: 260 us (4.2 TB/s), of which the log-sum-exp costs 55 (exponentials keep their unit
-// 47 % busy) and the selection 28; k 1 without log-sum-exp 178 (6.2 TB/s, 94 % of the copy rate).  Bounds that rise as the
+// Measured: 2,048 x 267,735 bf16, k 64: 259 to 266 us (4.1 to 4.2 TB/s), of which the log-sum-exp costs 55 (exponentials keep
+// their unit 47 % busy) and the selection 28; k 1 without log-sum-exp 178 (6.2 TB/s, 94 % of the copy rate).  Bounds that rise as the
 // row goes by, with a look at every piece, took 741.  A row's selection is 9 us, most of it waiting for memory that the
 // other block of the SM keeps busy; three blocks per SM, with a ring of two slots, were no faster (279).
 struct TopParams {
