@@ -385,6 +385,12 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       return rc;
     }
   }
+  long long groups = (N + 31) / 32;
+  if (factor && groups > kLossMostGroups) {        // 2,000,000 x 16, 300 words: read by every join block 1,160 us, this 60
+    const cudaError_t e = launch(loss_max_kernel, 1, 1, 1024, 0, st, factor + 1, groups);
+    if (e != cudaSuccess) return cuda_refuse("launch of the loss's weight kernel", e);
+    groups = 1;
+  }
   if (gbmuf_status rc = do_ranges([&](long long r0, long long n, int t, float2* slots) -> gbmuf_status {
     JoinParams J{};
     J.L.targets = a->targets + r0; J.L.row_weight = a->row_weight ? a->row_weight + r0 : nullptr;
@@ -397,7 +403,7 @@ template <typename T> gbmuf_status run(const gbmuf_ops* ops, const Args* a, cuda
       J.targets = reinterpret_cast<int*>(ws + p.word_off) + r0;
       J.weights = reinterpret_cast<float*>(ws + p.weight_off) + r0;
     }
-    if (factor) { J.weight_max = factor + 1; J.factor = factor; J.groups = (N + 31) / 32; }
+    if (factor) { J.weight_max = factor + 1; J.factor = factor; J.groups = groups; }
     J.ld = n; J.twice = p.twice;
     J.count = p.few ? p.few_blocks : (int)((steps - 1) * stats_slots(ops, s, t, step)) + stats_slots(ops, s, t, V - (steps - 1) * step);
     J.rows_padded = r0 + n == N ? p.rows_padded - r0 : n;

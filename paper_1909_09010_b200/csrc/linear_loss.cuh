@@ -359,6 +359,24 @@ __global__ void __launch_bounds__(32 * kJoinShares) loss_join_kernel(const JoinP
   }
 }
 
+// The largest of the rows' weights, where every block of the join would read more than kLossMostGroups of them: into the first.
+constexpr long long kLossMostGroups = 4096;
+__global__ void __launch_bounds__(1024) loss_max_kernel(float* weight_max, long long groups) {
+  __shared__ float largest[32];
+  grid_launch_dependents();
+  grid_dependency_wait();
+  float top = 0.0f;
+#pragma unroll 8
+  for (long long i = threadIdx.x; i < groups; i += 1024) top = fmaxf(top, weight_max[i]);
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  if ((threadIdx.x & 31) == 0) largest[threadIdx.x >> 5] = top;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  top = largest[threadIdx.x];
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  if (threadIdx.x == 0) weight_max[0] = top;
+}
+
 // dbias of a piece: the strips' sums in their order.
 template <typename TO>
 __global__ void __launch_bounds__(256) loss_bias_kernel(const float* partial, long long ld, int strips, long long words, TO* out,

@@ -13,7 +13,7 @@ def ops():
     return binding.local_ops(0)
 
 
-@pytest.mark.parametrize("rows,n_in,vocab,piece", [(33, 64, 4001, 0), (300, 200, 4001, 1500), (513, 72, 10_000, 0)])
+@pytest.mark.parametrize("rows,n_in,vocab,piece", [(33, 64, 4001, 0), (300, 200, 4001, 1500), (513, 72, 10_000, 0), (140_001, 8, 100, 0)])
 @pytest.mark.parametrize("value", [1.0 / 300, 1.0 / 513, 0.7, 3e-30])
 def test_equal_weights_are_a_scale(ops, rows, n_in, vocab, piece, value):
     """The same call written twice: the same weight for all rows, or as their scale; a mask divided by its count, or rows
@@ -130,4 +130,30 @@ def test_several_launches_of_the_statistics(ops, dtype, rows, n_in, vocab, piece
     args = (lay(x, how), lay(w, how), t, lay(b, how))
     check(ops.linear_cross_entropy(*args, row_weight=rw, scale=0.5, piece=piece), R, dtype, dtype, how)
     check(ops.linear_cross_entropy(*args, row_weight=rw, scale=0.5, piece=piece, want_grad=False), R, dtype, dtype, how + " values")
+    assert ops.device_status() == 0
+
+
+def test_graphs_take_the_weights_they_find(ops):
+    """A captured step, replayed after its weights, targets and inputs have changed, on another stream too."""
+    g = gen(5)
+    x, w, t, b, rw = problem(g, 300, 72, 3001, BF)
+    call = lambda **kw: ops.linear_cross_entropy(x, w, t, b, row_weight=rw, scale=0.1, piece=1000, **kw)      # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for turn in range(4):
+        rw.copy_(torch.rand(300, device="cuda", generator=g) * 10.0 ** (3 * turn - 4))
+        t.copy_(torch.randint(0, 3001, (300,), device="cuda", generator=g))
+        x.copy_(x.flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [a.clone() for a in out]
+        assert all(torch.equal(a, c) for a, c in zip(got, call()))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        other = call(stream=side)
+        side.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, other))
+        check(got, reference(x, w, t, b, rw, 0.1), BF, BF, f"turn {turn}")
     assert ops.device_status() == 0
